@@ -371,6 +371,71 @@ int spkv_decode_step_predict(spkv_cache_t* cache, const void* hidden, const void
                              void* out, float* lse, float* util_logits, void* workspace,
                              size_t workspace_bytes, float sm_scale, void* stream);
 
+/* Queries, keys and values of a layer out of one projection's rows, in one pass: RMS norm of every
+ * head, rotation by positions (rotary embedding), and the dense layout that the cache's calls take.
+ * For a head x of head_dim elements with weight w and rotated pair i = (a, b) of elements:
+ *   n = x * w / sqrt(mean(x^2) + eps)
+ *   a' = a cos(phi_i) - b sin(phi_i),  b' = a sin(phi_i) + b cos(phi_i),  phi_i = positions[axis[i]][t] * inv_freq[i]
+ * in fp32, rounded once at the end; the angle exactly, modulo a turn, whatever the position.
+ * Positions on several axes (time, height, width of images and video) are the case n_axes > 1. */
+#define SPKV_BF16 0
+#define SPKV_FP32 1
+#define SPKV_MAX_ROPE_PAIRS 64
+#define SPKV_MAX_ROPE_AXES  4
+
+typedef struct spkv_rope {
+    int32_t head_dim;           /* 64 or 128                                                     */
+    int32_t rot_dim;            /* elements that are rotated, 0 .. head_dim, even; the others pass.
+                                   A multiple of 16 unless `adjacent`                            */
+    int32_t adjacent;           /* 0: pair i = elements (i, i + rot_dim / 2); 1: (2 i, 2 i + 1)  */
+    int32_t n_axes;             /* 1 .. SPKV_MAX_ROPE_AXES                                       */
+    const double*  inv_freq;    /* host [rot_dim / 2], radians per position, finite              */
+    const uint8_t* axis;        /* host [rot_dim / 2], axis that each pair turns with; NULL: 0   */
+} spkv_rope_t;
+
+/* Heads of consecutive tokens: element (token, head, d) at token * token_stride +
+ * head * head_stride + d (strides in elements, >= 0, whole multiples of 16 bytes; `data` 16-byte
+ * aligned): a slice of a projection's rows as well as a dense tensor. */
+typedef struct spkv_heads {
+    void*   data;               /* device */
+    int64_t token_stride, head_stride;
+} spkv_heads_t;
+
+/*   q, k        [n_tokens, n_q_heads / n_kv_heads, head_dim] of `dtype` (SPKV_BF16, SPKV_FP32)
+ *   v           the same as k, copied as it is, or NULL with v_out NULL
+ *   q_weight, k_weight  device fp32 [head_dim] or NULL (ones)
+ *   eps         >= 0; negative: no norm, the weights are not read
+ *   positions   device int32 [n_axes, n_tokens]
+ *   *_out       of the same type; may be the inputs themselves (same data and strides), else they
+ *               must not overlap them or one another
+ * Needs no workspace, allocates nothing, waits for nothing; one launch.  n_tokens may be 0.
+ * SPKV_E_INVAL for shapes, strides or pointers out of these rules, and where
+ * n_tokens * (n_q_heads + 2 n_kv_heads) passes 2^30. */
+int spkv_qk_norm_rope(const spkv_heads_t* q, const spkv_heads_t* k, const spkv_heads_t* v,
+                      const float* q_weight, const float* k_weight, float eps,
+                      const int32_t* positions, const spkv_rope_t* rope, int32_t dtype,
+                      int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                      const spkv_heads_t* q_out, const spkv_heads_t* k_out,
+                      const spkv_heads_t* v_out, void* stream);
+
+/* Gradients of the above: from dq, dk, dv (of its outputs) to dq_in, dk_in, dv_in (of its
+ * inputs) and, where not NULL, dq_weight / dk_weight (fp32 [head_dim], written, not added to).
+ *   q, k        the forward's inputs; not read (may be NULL) without a norm
+ *   workspace   device, 16-byte aligned, at least spkv_qk_norm_rope_backward_workspace_bytes
+ *               bytes; not used (may be NULL) if no weight gradient is asked for
+ * One launch, and a second small one for the weights' gradients, whose sums run in a fixed
+ * order: equal calls give equal bits.  Weight gradients without a norm are refused. */
+size_t spkv_qk_norm_rope_backward_workspace_bytes(int64_t n_tokens, int32_t n_q_heads,
+                                                  int32_t n_kv_heads, int32_t head_dim);
+int spkv_qk_norm_rope_backward(const spkv_heads_t* dq, const spkv_heads_t* dk, const spkv_heads_t* dv,
+                               const spkv_heads_t* q, const spkv_heads_t* k,
+                               const float* q_weight, const float* k_weight, float eps,
+                               const int32_t* positions, const spkv_rope_t* rope, int32_t dtype,
+                               int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                               const spkv_heads_t* dq_in, const spkv_heads_t* dk_in,
+                               const spkv_heads_t* dv_in, float* dq_weight, float* dk_weight,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
 /* Replaying captured steps.  spkv_append (one token per sequence), spkv_decode_attention and
  * spkv_decode_step enqueue kernels only -- no allocation, no copy, no synchronisation as long
  * as the capacity bound holds -- so a serving loop may capture them into a HIP graph (one

@@ -29,7 +29,11 @@ EXPORTED_SYMBOLS = [
     "spkv_soft_gated_workspace_bytes", "spkv_soft_gated_attention", "spkv_cache_release_sequence", "spkv_utility_logits", "spkv_cache_safe_steps", "spkv_cache_advance", "spkv_cache_stats", "spkv_cache_kept_positions",
     "spkv_cache_threshold_logit", "spkv_cache_set_tau", "spkv_cache_prune", "spkv_cache_set_option", "spkv_cache_read_kernel_timing",
     "spkv_debug_layout_offset", "spkv_debug_copy", "spkv_debug_read", "spkv_strerror",
+    "spkv_qk_norm_rope", "spkv_qk_norm_rope_backward", "spkv_qk_norm_rope_backward_workspace_bytes",
 ]
+
+BF16, FP32 = 0, 1
+_HEAD_TYPES = {torch.bfloat16: BF16, torch.float32: FP32}
 
 
 class SPKVConfig(C.Structure):
@@ -51,6 +55,15 @@ class SPKVStats(C.Structure):
 
     def as_dict(self):
         return {n: getattr(self, n) for n, _ in self._fields_}
+
+
+class SPKVRope(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("adjacent", C.c_int32),
+                ("n_axes", C.c_int32), ("inv_freq", C.c_void_p), ("axis", C.c_void_p)]
+
+
+class SPKVHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 class SPKVError(RuntimeError):
@@ -115,6 +128,14 @@ def load_library():
     lib.spkv_cache_release_sequence.argtypes = [vp, i32, vp]
     lib.spkv_utility_logits.restype = C.c_int
     lib.spkv_utility_logits.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp]
+    ph, pr = P(SPKVHeads), P(SPKVRope)
+    lib.spkv_qk_norm_rope.restype = C.c_int
+    lib.spkv_qk_norm_rope.argtypes = [ph, ph, ph, vp, vp, f32, vp, pr, i32, i64, i32, i32, ph, ph, ph, vp]
+    lib.spkv_qk_norm_rope_backward_workspace_bytes.restype = C.c_size_t
+    lib.spkv_qk_norm_rope_backward_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    lib.spkv_qk_norm_rope_backward.restype = C.c_int
+    lib.spkv_qk_norm_rope_backward.argtypes = [ph, ph, ph, ph, ph, vp, vp, f32, vp, pr, i32, i64, i32, i32,
+                                               ph, ph, ph, vp, vp, vp, C.c_size_t, vp]
     lib.spkv_cache_prune.restype = C.c_int
     lib.spkv_cache_prune.argtypes = [vp, vp]
     lib.spkv_cache_safe_steps.restype = C.c_int
@@ -226,6 +247,130 @@ def utility_logits(hidden, w1, b1, w2, b2, out=None, workspace=None):
                                               C.c_void_p(workspace.data_ptr()), n, d_model,
                                               d_hidden, n_heads, _stream()), "spkv_utility_logits")
     return out
+
+
+class Rope:
+    """Rotation of heads by positions (spkv_rope_t): which elements form pairs, how fast each pair turns
+    and with which axis of the positions.  Made once per model, host memory only.
+
+    rot_dim elements of a head are rotated (all by default).  Pair i turns by theta ** (-2 i / rot_dim), or
+    inv_freq[i], radians per position.  sections = pairs of every axis in order (time, height, width), or
+    axis[i] = the axis of each pair.  adjacent: pair i is elements (2 i, 2 i + 1) instead of
+    (i, i + rot_dim / 2)."""
+
+    def __init__(self, head_dim, rot_dim=None, theta=10000.0, sections=None, axis=None, adjacent=False,
+                 inv_freq=None):
+        self.head_dim = int(head_dim)
+        self.rot_dim = self.head_dim if rot_dim is None else int(rot_dim)
+        pairs = self.rot_dim // 2
+        if inv_freq is None:
+            inv_freq = [float(theta) ** (-2.0 * i / self.rot_dim) for i in range(pairs)]
+        inv_freq = [float(f) for f in inv_freq]
+        if sections is not None:
+            if axis is not None:
+                raise ValueError("rope: sections or axis, not both")
+            axis = [a for a, n in enumerate(sections) for _ in range(int(n))]
+            self.n_axes = len(sections)
+        else:
+            axis = [0] * pairs if axis is None else [int(a) for a in axis]
+            self.n_axes = max(axis, default=0) + 1
+        if len(inv_freq) != pairs or len(axis) != pairs or any(not 0 <= a < 256 for a in axis):
+            raise ValueError(f"rope: need a frequency and an axis for each of {pairs} pairs")
+        self.adjacent = bool(adjacent)
+        self._freq = (C.c_double * max(pairs, 1))(*inv_freq)
+        self._axis = (C.c_uint8 * max(pairs, 1))(*axis)
+        self.struct = SPKVRope(self.head_dim, self.rot_dim, int(self.adjacent), self.n_axes,
+                               C.addressof(self._freq), C.addressof(self._axis))
+
+
+def _heads(t, dtype, shape, name):
+    if not t.is_cuda or t.dtype != dtype or t.shape != shape or (t.stride(2) != 1 and shape[2] != 1):
+        raise ValueError(f"{name}: need a cuda {dtype} tensor of shape {tuple(shape)} with dense heads, "
+                         f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+    return SPKVHeads(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _rope_call(q, k, v, positions, rope, q_weight, k_weight, eps, names):
+    """What both directions check and pass: shapes, type, weights, norm, positions."""
+    if q.dim() != 3 or k.dim() != 3 or q.dtype not in _HEAD_TYPES:
+        raise ValueError(f"{names[0]}, {names[1]}: need bf16 or fp32 [tokens, heads, head_dim]")
+    n, hq, d = q.shape
+    if d != rope.head_dim:
+        raise ValueError(f"{names[0]}: heads of {d} elements, rope made for {rope.head_dim}")
+    hk = k.shape[1]
+    ins = [_heads(q, q.dtype, (n, hq, d), names[0]), _heads(k, q.dtype, (n, hk, d), names[1]),
+           None if v is None else _heads(v, q.dtype, (n, hk, d), names[2])]
+    shape = (n,) if rope.n_axes == 1 and positions.dim() == 1 else (rope.n_axes, n)
+    pp = _dev_ptr(positions, torch.int32, shape, "positions")
+    if eps is None:
+        if q_weight is not None or k_weight is not None:
+            raise ValueError("weights of the norm without eps")
+        return n, hq, hk, d, ins, pp, None, None, -1.0
+    if not eps >= 0.0:
+        raise ValueError("eps: need a value >= 0, or None for no norm")
+    qw = _dev_ptr(q_weight, torch.float32, (d,), "q_weight") if q_weight is not None else None
+    kw = _dev_ptr(k_weight, torch.float32, (d,), "k_weight") if k_weight is not None else None
+    return n, hq, hk, d, ins, pp, qw, kw, float(eps)
+
+
+def qk_norm_rope(q, k, positions, rope, q_weight=None, k_weight=None, eps=None, v=None, out=None):
+    """RMS norm of every head (eps None: no norm), rotation by positions, dense layout, in one launch
+    (spkv_qk_norm_rope).  q: bf16 or fp32 [tokens, H_q, D]; k, v: [tokens, H_kv, D], slices of a
+    projection's rows as they are; positions: int32 [tokens] or [axes, tokens].  out: tensors to write
+    (the inputs themselves may be passed).  Returns (q, k) or, with v, (q, k, v)."""
+    n, hq, hk, d, ins, pp, qw, kw, eps = _rope_call(q, k, v, positions, rope, q_weight, k_weight, eps, "qkv")
+    if out is None:
+        out = (torch.empty((n, hq, d), dtype=q.dtype, device=q.device),
+               torch.empty((n, hk, d), dtype=q.dtype, device=q.device),
+               None if v is None else torch.empty((n, hk, d), dtype=q.dtype, device=q.device))
+    elif v is None:
+        out = (out[0], out[1], None)
+    outs = [_heads(out[0], q.dtype, (n, hq, d), "out[0]"), _heads(out[1], q.dtype, (n, hk, d), "out[1]"),
+            None if v is None else _heads(out[2], q.dtype, (n, hk, d), "out[2]")]
+    _check(load_library().spkv_qk_norm_rope(*ins, qw, kw, eps, pp, rope.struct, _HEAD_TYPES[q.dtype], n, hq, hk, *outs,
+                                            _stream()), "spkv_qk_norm_rope")
+    return tuple(out[:2]) if v is None else tuple(out)
+
+
+def qk_norm_rope_backward(dq, dk, positions, rope, q=None, k=None, q_weight=None, k_weight=None, eps=None,
+                          dv=None, out=None, want_weights=None, workspace=None):
+    """Gradients of qk_norm_rope (spkv_qk_norm_rope_backward) from those of its outputs: dq, dk, dv.
+    q, k: the forward's inputs (only with a norm).  out: tensors for the inputs' gradients, for example
+    slices of one buffer for the projection's rows.  Returns (dq, dk), with dv (dq, dk, dv) -- or nothing
+    of these if `out` was given -- and then, with a norm and unless want_weights is False, the
+    fp32 gradients of both weights."""
+    n, hq, hk, d, ins, pp, qw, kw, eps = _rope_call(dq, dk, dv, positions, rope, q_weight, k_weight, eps,
+                                                    ("dq", "dk", "dv"))
+    given = out is not None
+    if not given:
+        out = (torch.empty((n, hq, d), dtype=dq.dtype, device=dq.device),
+               torch.empty((n, hk, d), dtype=dq.dtype, device=dq.device),
+               None if dv is None else torch.empty((n, hk, d), dtype=dq.dtype, device=dq.device))
+    outs = [_heads(out[0], dq.dtype, (n, hq, d), "out[0]"), _heads(out[1], dq.dtype, (n, hk, d), "out[1]"),
+            None if dv is None else _heads(out[2], dq.dtype, (n, hk, d), "out[2]")]
+    xs, weights = [None, None], ()
+    if eps >= 0.0:
+        if q is None or k is None:
+            raise ValueError("q, k: the forward's inputs are needed with a norm")
+        xs = [_heads(q, dq.dtype, (n, hq, d), "q"), _heads(k, dq.dtype, (n, hk, d), "k")]
+        if want_weights is None or want_weights:
+            weights = (torch.empty(d, dtype=torch.float32, device=dq.device),
+                       torch.empty(d, dtype=torch.float32, device=dq.device))
+    elif want_weights:
+        raise ValueError("want_weights: there are no weights without a norm")
+    lib = load_library()
+    if weights and workspace is None:
+        workspace = torch.empty(int(lib.spkv_qk_norm_rope_backward_workspace_bytes(n, hq, hk, d)),
+                                dtype=torch.uint8, device=dq.device)
+    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 device tensor")
+    _check(lib.spkv_qk_norm_rope_backward(*ins, *xs, qw, kw, eps, pp, rope.struct, _HEAD_TYPES[dq.dtype], n, hq, hk, *outs,
+                                          *([w.data_ptr() for w in weights] or [None, None]),
+                                          workspace.data_ptr() if workspace is not None else None,
+                                          workspace.numel() if workspace is not None else 0, _stream()),
+           "spkv_qk_norm_rope_backward")
+    first = () if given else tuple(out[:2]) if dv is None else tuple(out)
+    return first + weights
 
 
 def _check(code, where):

@@ -1631,6 +1631,127 @@ int spkv_utility_logits(const void* hidden, const void* w1, const float* b1, con
                : SPKV_E_HIP;
 }
 
+namespace {
+// A set of heads as the kernels take it; false if it is not one of `size`-byte elements.
+bool heads_ok(const spkv_heads_t* s, int64_t n_tokens, int n_heads, int head_dim, int size, bool written, SpkvRowSet* o) {
+    if (s == nullptr || s->data == nullptr || !aligned16(s->data)) return false;
+    const int64_t unit = 16 / size, limit = (int64_t)1 << 40;
+    // the stride of an axis of one is not looked at
+    const int64_t ts = n_tokens > 1 ? s->token_stride : 0, hs = n_heads > 1 ? s->head_stride : 0;
+    if (ts < 0 || hs < 0 || ts > limit || hs > limit || ts % unit != 0 || hs % unit != 0) return false;
+    if (written) {              // two rows must not share an element
+        const bool inner_heads = n_tokens <= 1 || (n_heads > 1 && hs <= ts);
+        const int64_t s0 = inner_heads ? hs : ts, n0 = inner_heads ? n_heads : n_tokens;
+        const int64_t s1 = inner_heads ? ts : hs, n1 = inner_heads ? n_tokens : n_heads;
+        if (n0 > 1 && s0 < head_dim) return false;
+        if (n1 > 1 && s1 < (n0 - 1) * s0 + head_dim) return false;
+    }
+    *o = SpkvRowSet{s->data, ts, hs};
+    return true;
+}
+
+bool rope_ok(const spkv_rope_t* r) {
+    if (r == nullptr || (r->head_dim != 64 && r->head_dim != 128)) return false;
+    if (r->rot_dim < 0 || r->rot_dim > r->head_dim || r->rot_dim % (r->adjacent != 0 ? 2 : 16) != 0) return false;
+    if (r->n_axes < 1 || r->n_axes > SPKV_MAX_ROPE_AXES) return false;
+    if (r->rot_dim > 0 && r->inv_freq == nullptr) return false;
+    for (int i = 0; i < r->rot_dim / 2; ++i) {
+        if (!std::isfinite(r->inv_freq[i])) return false;
+        if (r->axis != nullptr && r->axis[i] >= r->n_axes) return false;
+    }
+    return true;
+}
+
+// What both directions check.  `in` and `out` of the kernel's direction.
+bool rope_args(const spkv_heads_t* const (&in)[3], const spkv_heads_t* const (&out)[3], const float* q_weight,
+               const float* k_weight, float eps, const int32_t* positions, const spkv_rope_t* rope, int32_t dtype,
+               int64_t n_tokens, int32_t n_q, int32_t n_kv, SpkvRope* a) {
+    if (!rope_ok(rope) || (dtype != SPKV_BF16 && dtype != SPKV_FP32) || std::isnan(eps) || std::isinf(eps)) return false;
+    if (n_tokens < 0 || n_q < 1 || n_kv < 1 || n_q > 16384 || n_kv > 16384) return false;
+    if ((in[2] == nullptr) != (out[2] == nullptr)) return false;
+    const int n_heads = n_q + (in[2] != nullptr ? 2 : 1) * n_kv;
+    if (n_tokens > ((int64_t)1 << 30) / n_heads) return false;
+    if (n_tokens == 0) return true;
+    const int size = dtype == SPKV_FP32 ? 4 : 2;
+    for (int i = 0; i < (in[2] != nullptr ? 3 : 2); ++i)
+        if (!heads_ok(in[i], n_tokens, i == 0 ? n_q : n_kv, rope->head_dim, size, false, &a->in[i]) ||
+            !heads_ok(out[i], n_tokens, i == 0 ? n_q : n_kv, rope->head_dim, size, true, &a->out[i]))
+            return false;
+    if (rope->rot_dim > 0 && (positions == nullptr || (reinterpret_cast<uintptr_t>(positions) & 3u) != 0)) return false;
+    if ((q_weight != nullptr && !aligned16(q_weight)) || (k_weight != nullptr && !aligned16(k_weight))) return false;
+    a->q_weight = q_weight;
+    a->k_weight = k_weight;
+    a->positions = positions;
+    a->eps = eps;
+    a->n_tokens = (int32_t)n_tokens;
+    a->n_q = n_q;
+    a->n_kv = n_kv;
+    a->n_heads = n_heads;
+    a->n_rows = (int32_t)(n_tokens * n_heads);
+    a->rot_dim = rope->rot_dim;
+    return true;
+}
+}  // namespace
+
+int spkv_qk_norm_rope(const spkv_heads_t* q, const spkv_heads_t* k, const spkv_heads_t* v, const float* q_weight,
+                      const float* k_weight, float eps, const int32_t* positions, const spkv_rope_t* rope,
+                      int32_t dtype, int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                      const spkv_heads_t* q_out, const spkv_heads_t* k_out, const spkv_heads_t* v_out, void* stream) {
+    SpkvRope a = {};
+    if (!rope_args({q, k, v}, {q_out, k_out, v_out}, q_weight, k_weight, eps, positions, rope, dtype, n_tokens,
+                   n_q_heads, n_kv_heads, &a))
+        return SPKV_E_INVAL;
+    if (n_tokens == 0) return SPKV_OK;
+    return spkv_launch_rope(a, rope->inv_freq, rope->axis, rope->head_dim, dtype == SPKV_FP32, rope->adjacent != 0,
+                            eps >= 0.f, false, static_cast<hipStream_t>(stream)) == hipSuccess
+               ? SPKV_OK
+               : SPKV_E_HIP;
+}
+
+size_t spkv_qk_norm_rope_backward_workspace_bytes(int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                                                  int32_t head_dim) {
+    if (n_tokens < 0 || n_q_heads < 1 || n_kv_heads < 1 || (head_dim != 64 && head_dim != 128)) return 0;
+    return (size_t)kRopeGradBlocks * 2 * head_dim * sizeof(float);
+}
+
+int spkv_qk_norm_rope_backward(const spkv_heads_t* dq, const spkv_heads_t* dk, const spkv_heads_t* dv,
+                               const spkv_heads_t* q, const spkv_heads_t* k, const float* q_weight,
+                               const float* k_weight, float eps, const int32_t* positions, const spkv_rope_t* rope,
+                               int32_t dtype, int64_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                               const spkv_heads_t* dq_in, const spkv_heads_t* dk_in, const spkv_heads_t* dv_in,
+                               float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+    SpkvRope a = {};
+    if (!rope_args({dq, dk, dv}, {dq_in, dk_in, dv_in}, q_weight, k_weight, eps, positions, rope, dtype, n_tokens,
+                   n_q_heads, n_kv_heads, &a))
+        return SPKV_E_INVAL;
+    const bool norm = eps >= 0.f, weights = dq_weight != nullptr || dk_weight != nullptr;
+    if (weights && (!norm || workspace == nullptr || !aligned16(workspace))) return SPKV_E_INVAL;
+    if (!aligned16(dq_weight) || !aligned16(dk_weight)) return SPKV_E_INVAL;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (n_tokens == 0) {
+        for (float* w : {dq_weight, dk_weight})
+            if (w != nullptr && spkv_launch_fill_zero(w, (size_t)rope->head_dim * sizeof(float), s) != hipSuccess)
+                return SPKV_E_HIP;
+        return SPKV_OK;
+    }
+    const int size = dtype == SPKV_FP32 ? 4 : 2, D = rope->head_dim;
+    if (norm && (!heads_ok(q, n_tokens, n_q_heads, D, size, false, &a.x[0]) ||
+                 !heads_ok(k, n_tokens, n_kv_heads, D, size, false, &a.x[1])))
+        return SPKV_E_INVAL;
+    if (weights) {
+        const size_t need = (size_t)spkv_rope_backward_blocks(a.n_rows, a.n_heads, D) * 2 * D * sizeof(float);
+        if (workspace_bytes < need) return SPKV_E_INVAL;
+        a.partial = static_cast<float*>(workspace);
+        a.dq_weight = dq_weight;
+        a.dk_weight = dk_weight;
+    }
+    return spkv_launch_rope(a, rope->inv_freq, rope->axis, D, dtype == SPKV_FP32, rope->adjacent != 0, norm, true,
+                            s) == hipSuccess
+               ? SPKV_OK
+               : SPKV_E_HIP;
+}
+
 int spkv_debug_copy(void* dst, const void* src, size_t bytes, void* stream) {
     if (dst == nullptr || src == nullptr || (bytes & 15u) != 0 || !aligned16(dst) || !aligned16(src))
         return SPKV_E_INVAL;

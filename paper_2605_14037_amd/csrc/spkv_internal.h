@@ -220,3 +220,28 @@ hipError_t spkv_launch_release_sequence(const SpkvView& v, int b, hipStream_t s)
 // Drops every long-term entry whose stored logit fails the view's threshold (in place).
 hipError_t spkv_launch_prune(const SpkvView& v, hipStream_t s);
 hipError_t spkv_launch_gather_positions(const SpkvView& v, int pair, hipStream_t s);
+
+// Queries, keys and values out of a projection's rows (spkv_rope.hip).
+constexpr int kRopeThreads = 256;
+constexpr int kRopeBlocks = 2048, kRopeGradBlocks = 1024;     // workgroups wanted / most of the backward pass
+struct SpkvRowSet {
+    void* p;                            // element (token, head, d) at token * token_stride + head * head_stride + d
+    int64_t token_stride, head_stride;
+};
+struct SpkvRope {
+    SpkvRowSet in[3], x[3], out[3];     // queries, keys, values; x: the forward's inputs (backward; no values)
+    const float* q_weight;              // [D] or null
+    const float* k_weight;
+    const int32_t* positions;           // [axes][n_tokens]
+    float* partial;                     // backward: [blocks][2][D], or null: no gradients of the weights
+    float* dq_weight;
+    float* dk_weight;
+    float eps;
+    int32_t n_tokens, n_q, n_kv, n_heads;      // n_heads: rows of a token, values among them if there are any
+    int32_t n_rows;                     // n_tokens * n_heads
+    int32_t rot_dim;
+    int32_t tile_rows, n_tiles;
+};
+hipError_t spkv_launch_rope(const SpkvRope& a, const double* inv_freq, const uint8_t* axis, int head_dim, bool fp32,
+                            bool adjacent, bool norm, bool backward, hipStream_t s);
+int spkv_rope_backward_blocks(int64_t n_rows, int n_heads, int head_dim);
