@@ -325,6 +325,49 @@ int spkv_soft_gated_attention(const void* q, const void* k, const void* v, const
                               float* lse, float sm_scale, void* workspace, size_t workspace_bytes,
                               void* stream);
 
+/* Attention over shared prompts.  Sequences that begin with the same tokens (a system prompt, a
+ * document) need not hold them each: the prompt is fed once, into a sequence of a cache of its own
+ * (`prefix`: same heads, head_dim and window; its threshold decides over its pairs), and `cache` holds
+ * only what comes behind it.  A token at place i of a sequence that continues a prompt of P tokens stands
+ * at position P + i: besides its own sequence's keys it sees the prompt's key at position s if P + i - s <
+ * window, and else if that key's gate is on -- the keys it would see had the prompt been
+ * appended to its own sequence (Eq. 3-5).  (Keys are stored as they are given: rotary positions of
+ * the sequence's tokens start at P.)  One pass over a prompt's lists serves all rows that
+ * continue it.  The prompts' cache is only read, and may serve any number of caches; appending to it
+ * changes what is attended to from then on.
+ *
+ * spkv_prefix_attention joins the attention of a call's tokens over their own sequences, which
+ * any of the calls above has left, with that over their prompts:
+ *   prefix_of    host int32 [batch of cache]: the sequence of `prefix` that each sequence continues, -1: none
+ *   q            device bf16 [total, n_q_heads, head_dim], as passed to that call
+ *   cu_seqlens   host int32 [batch + 1] as passed to that call, or NULL: one token per sequence
+ *   appended     1: the call has appended the tokens (spkv_decode_step, _chunk, spkv_prefill_attention;
+ *                spkv_decode_attention after spkv_append); 0: it has not (spkv_score_chunk)
+ *   own_out, own_lse  device bf16 [total, n_q_heads, head_dim], fp32 [total, n_q_heads]: what it left;
+ *                a row without any key of its own: own_lse = -infinity
+ *   out, lse     the same for all keys; may be own_out, own_lse; lse may be NULL.  Rows without a prompt (or
+ *                with an empty one) are passed through; a row without any key at all gets zeros and -infinity
+ *   workspace    device, 256-byte aligned, spkv_prefix_workspace_bytes(prefix, total) bytes
+ *                are enough for any call of at most `total` rows (with less, down to one range per list, a
+ *                call is slower); contents disposable
+ * Two launches (three with cu_seqlens); waits once for the lengths after the prompt's append, as
+ * spkv_decode_attention does, and never in steady state.  May be captured: the place of a row is read on the
+ * device.  Copies of a sequence get results that agree to rounding.
+ * Errors: SPKV_E_INVAL for shapes that differ, indices out of range, bad pointers, a workspace without
+ * room for one range; SPKV_E_STATE if a sequence holds fewer tokens than the call has appended. */
+size_t spkv_prefix_workspace_bytes(const spkv_cache_t* prefix, int64_t max_total_rows);
+int spkv_prefix_attention(spkv_cache_t* prefix, const spkv_cache_t* cache, const int32_t* prefix_of,
+                          const void* q, const int32_t* cu_seqlens, int32_t appended,
+                          const void* own_out, const float* own_lse, void* out, float* lse,
+                          float sm_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* spkv_decode_attention over the sequences and the prompts that they continue: the newest appended
+ * token of every sequence.  q, out, lse, sm_scale as there; prefix_of, workspace as above.
+ * Errors as for both. */
+int spkv_decode_attention_shared(spkv_cache_t* cache, spkv_cache_t* prefix, const int32_t* prefix_of,
+                                 const void* q, void* out, float* lse, float sm_scale,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
 /* Forget sequence b (for example when its request has finished): its window and long-term
  * entries are dropped, its pages return to the pool for reuse by any sequence, and slot b
  * holds an empty sequence that can be appended to again.  (The paper's cache manager grows

@@ -8,7 +8,7 @@ library is an error (there is no fallback path).  Build it with
 from .binding import (  # noqa: F401
     SPKVCache, SPKVConfig, SPKVStats, SPKVError, load_library, library_path,
     required_bytes, strerror, layout_offset, debug_copy, debug_read, utility_logits, soft_gated_attention,
-    Rope, qk_norm_rope, qk_norm_rope_backward,
+    PrefixSharing, Rope, qk_norm_rope, qk_norm_rope_backward,
     EXPORTED_SYMBOLS,
     OPT_ITEM_TARGET, OPT_KERNEL_TIMING, OPT_SPLIT_ONLY, OPT_SINK_TOKENS, OPT_MERGE_WAVES, OPT_STEP_LAUNCHES,
 )

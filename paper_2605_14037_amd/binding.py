@@ -30,6 +30,7 @@ EXPORTED_SYMBOLS = [
     "spkv_cache_threshold_logit", "spkv_cache_set_tau", "spkv_cache_prune", "spkv_cache_set_option", "spkv_cache_read_kernel_timing",
     "spkv_debug_layout_offset", "spkv_debug_copy", "spkv_debug_read", "spkv_strerror",
     "spkv_qk_norm_rope", "spkv_qk_norm_rope_backward", "spkv_qk_norm_rope_backward_workspace_bytes",
+    "spkv_prefix_workspace_bytes", "spkv_prefix_attention", "spkv_decode_attention_shared",
 ]
 
 BF16, FP32 = 0, 1
@@ -128,6 +129,12 @@ def load_library():
     lib.spkv_cache_release_sequence.argtypes = [vp, i32, vp]
     lib.spkv_utility_logits.restype = C.c_int
     lib.spkv_utility_logits.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp]
+    lib.spkv_prefix_workspace_bytes.restype = C.c_size_t
+    lib.spkv_prefix_workspace_bytes.argtypes = [vp, i64]
+    lib.spkv_prefix_attention.restype = C.c_int
+    lib.spkv_prefix_attention.argtypes = [vp, vp, P(i32), vp, P(i32), i32, vp, vp, vp, vp, f32, vp, C.c_size_t, vp]
+    lib.spkv_decode_attention_shared.restype = C.c_int
+    lib.spkv_decode_attention_shared.argtypes = [vp, vp, P(i32), vp, vp, vp, f32, vp, C.c_size_t, vp]
     ph, pr = P(SPKVHeads), P(SPKVRope)
     lib.spkv_qk_norm_rope.restype = C.c_int
     lib.spkv_qk_norm_rope.argtypes = [ph, ph, ph, vp, vp, f32, vp, pr, i32, i64, i32, i32, ph, ph, ph, vp]
@@ -640,6 +647,59 @@ class SPKVCache:
                "spkv_prefill_attention")
         return (out, lse) if lse is not None else out
 
+    # ---- shared prompts
+    def _share_workspace(self, sharing, rows, workspace, device):
+        if sharing.batch != self.cfg.batch:
+            raise ValueError(f"sharing: made for {sharing.batch} sequences, the cache has {self.cfg.batch}")
+        if workspace is None:
+            workspace = torch.empty(sharing.workspace_bytes(rows), dtype=torch.uint8, device=device)
+        if workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous uint8 device tensor")
+        return workspace
+
+    def decode_attention_shared(self, sharing, q, out=None, lse=None, sm_scale=0.0, want_lse=False,
+                                workspace=None):
+        """decode_attention over the sequences and the prompts that they continue
+        (spkv_decode_attention_shared).  sharing: a PrefixSharing."""
+        cfg = self.cfg
+        shape = (cfg.batch, cfg.n_q_heads, cfg.head_dim)
+        qp = _dev_ptr(q, torch.bfloat16, shape, "q")
+        workspace = self._share_workspace(sharing, cfg.batch, workspace, q.device)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+        op = _dev_ptr(out, torch.bfloat16, shape, "out")
+        if lse is None and want_lse:
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
+        lp = _dev_ptr(lse, torch.float32, shape[:2], "lse") if lse is not None else None
+        _check(self.lib.spkv_decode_attention_shared(self.handle, sharing.prefix.handle, sharing.prefix_of, qp, op, lp,
+                                                     float(sm_scale), workspace.data_ptr(), workspace.numel(),
+                                                     _stream()), "spkv_decode_attention_shared")
+        return (out, lse) if lse is not None else out
+
+    def prefix_attention(self, sharing, q, cu_seqlens, own_out, own_lse, appended=True, out=None, lse=None,
+                         sm_scale=0.0, workspace=None):
+        """Join own_out, own_lse -- the attention of a call's tokens over their own sequences -- with that over
+        the prompts that these continue (spkv_prefix_attention).  cu_seqlens as in that call, None: one token
+        per sequence.  out, lse may be own_out, own_lse.  Returns (out, lse)."""
+        cfg = self.cfg
+        cu = cu_seqlens if cu_seqlens is None or isinstance(cu_seqlens, C.Array) else self.make_cu(cu_seqlens)
+        total = cfg.batch if cu is None else cu[cfg.batch]
+        shape = (total, cfg.n_q_heads, cfg.head_dim)
+        qp = _dev_ptr(q, torch.bfloat16, shape, "q")
+        ip = _dev_ptr(own_out, torch.bfloat16, shape, "own_out")
+        zp = _dev_ptr(own_lse, torch.float32, shape[:2], "own_lse")
+        workspace = self._share_workspace(sharing, max(total, 1), workspace, q.device)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+        if lse is None:
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
+        op = _dev_ptr(out, torch.bfloat16, shape, "out")
+        lp = _dev_ptr(lse, torch.float32, shape[:2], "lse")
+        _check(self.lib.spkv_prefix_attention(sharing.prefix.handle, self.handle, sharing.prefix_of, qp, cu, int(appended), ip, zp,
+                                              op, lp, float(sm_scale), workspace.data_ptr(), workspace.numel(),
+                                              _stream()), "spkv_prefix_attention")
+        return out, lse
+
     # ---- bookkeeping
     def reset(self):
         _check(self.lib.spkv_cache_reset(self.handle, _stream()), "spkv_cache_reset")
@@ -701,3 +761,19 @@ class SPKVCache:
         _check(self.lib.spkv_cache_read_kernel_timing(self.handle, buf, cap, C.byref(n)),
                "spkv_cache_read_kernel_timing")
         return list(buf[:n.value])
+
+
+class PrefixSharing:
+    """Which sequence of `prefix`, a cache that holds prompts, every sequence of another cache continues
+    (-1: none).  Host memory only; prefix_of may be changed in place (sharing[b] = p) as sequences come and go."""
+
+    def __init__(self, prefix, prefix_of):
+        self.prefix, self.batch = prefix, len(prefix_of)
+        self.prefix_of = (C.c_int32 * self.batch)(*[int(p) for p in prefix_of])
+
+    def __setitem__(self, b, p):
+        self.prefix_of[b] = int(p)
+
+    def workspace_bytes(self, rows):
+        """Bytes that serve any call of at most `rows` rows (spkv_prefix_workspace_bytes)."""
+        return int(self.prefix.lib.spkv_prefix_workspace_bytes(self.prefix.handle, int(rows)))

@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspkv.so")
 SOURCES = ["spkv_api.hip", "spkv_write.hip", "spkv_decode.hip", "spkv_decode_short.hip",
-           "spkv_prefill.hip", "spkv_predictor.hip", "spkv_rope.hip"]
+           "spkv_prefill.hip", "spkv_predictor.hip", "spkv_rope.hip", "spkv_prefix.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

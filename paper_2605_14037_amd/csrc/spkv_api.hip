@@ -1632,6 +1632,220 @@ int spkv_utility_logits(const void* hidden, const void* w1, const float* b1, con
 }
 
 namespace {
+// Shared prompts.  Workspace of a call of n rows: the tables of its rows, their own attention's lse where
+// the caller wants none, and the partial results of the ranges.
+struct ShareCarve {
+    size_t table, by_row, first_row, own_lse, part;
+};
+ShareCarve share_carve(int64_t rows, int n_q_heads) {
+    ShareCarve k;
+    k.table = 0;
+    k.by_row = align_up((size_t)rows * sizeof(int2));
+    k.first_row = k.by_row + align_up((size_t)rows * sizeof(int2));
+    k.own_lse = k.first_row + align_up((SPKV_MAX_BATCH + 1) * sizeof(int32_t));
+    k.part = k.own_lse + align_up((size_t)rows * n_q_heads * sizeof(float));
+    return k;
+}
+// Bytes that one range of every list needs for the partial results of `rows` rows.
+size_t share_slot_bytes(int64_t rows, int n_q_heads, int head_dim) {
+    return (size_t)rows * n_q_heads * (head_dim + 2) * sizeof(float);
+}
+constexpr size_t kSharePartBytes = (size_t)96 << 20;     // ranges are no more than fit, beyond the first
+constexpr int kShareMaxSlots = 255;
+
+// The prompts of a call that hold tokens and are continued by some row of it.  (No container: nothing here allocates.)
+struct SharePrompts {
+    int32_t n;
+    int32_t id[SPKV_MAX_BATCH], rows[SPKV_MAX_BATCH];
+    int16_t active[SPKV_MAX_BATCH];        // of every sequence; -1: none
+};
+void share_prompts(const spkv_cache* pc, int batch, const int32_t* prefix_of, const int32_t* cu, SharePrompts* s) {
+    int16_t at[SPKV_MAX_BATCH];
+    std::fill(at, at + SPKV_MAX_BATCH, (int16_t)-1);
+    s->n = 0;
+    for (int b = 0; b < batch; ++b) {
+        const int p = prefix_of[b];
+        s->active[b] = -1;
+        if (p < 0 || pc->T[p] == 0 || tokens_for(cu, b) == 0) continue;
+        if (at[p] < 0) {
+            at[p] = (int16_t)s->n;
+            s->id[s->n] = p;
+            s->rows[s->n++] = 0;
+        }
+        s->active[b] = at[p];
+        s->rows[at[p]] += tokens_for(cu, b);
+    }
+}
+
+// Ranges of the prompts' lists: about as many workgroups as the chip holds at once.
+constexpr int kShareMinUnit = 4;
+void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_bytes, int* waves, SpkvShareCut* cut) {
+    const int Hkv = c->cfg.n_kv_heads, G = c->carve.G, n = prompts.n;
+    int64_t most = 0, all_rows = 0;
+    for (int a = 0; a < n; ++a) {
+        most = std::max<int64_t>(most, prompts.rows[a]);
+        all_rows += prompts.rows[a];
+    }
+    *waves = spkv_prefix_waves((int)std::min<int64_t>(most * G, 1 << 20));
+    const int64_t width = 32 * *waves;
+    auto blocks = [&](int a) -> int64_t { return ((int64_t)prompts.rows[a] * G + width - 1) / width; };
+    auto half_pages = [&](int a, int h) -> int64_t {
+        const int p = prompts.id[a], held = std::min(c->T[p], c->cfg.window);
+        return ((int64_t)c->L_ub[p * Hkv + h] + kHalfTokens - 1) / kHalfTokens + (held + kHalfTokens - 1) / kHalfTokens;
+    };
+    int64_t work = 0, longest = 1, lists = 0;
+    for (int a = 0; a < n; ++a) {
+        lists += blocks(a) * Hkv;
+        for (int h = 0; h < Hkv; ++h) {
+            const int64_t x = half_pages(a, h);
+            work += x * blocks(a);
+            longest = std::max(longest, x);
+        }
+    }
+    const int cus = spkv_compute_units();
+    const int64_t target = (cus > 0 ? cus : 256) * (*waves == 8 ? 1 : 2);
+    int64_t unit = std::max<int64_t>(kShareMinUnit, (work + target - 1) / target);
+    for (int guard = 0; guard < 64; ++guard) {
+        int64_t total = 0;
+        for (int a = 0; a < n; ++a)
+            for (int h = 0; h < Hkv; ++h) total += (half_pages(a, h) + unit - 1) / unit * blocks(a);
+        if (total <= target || total <= lists) break;
+        unit += std::max<int64_t>(1, unit / 16);
+    }
+    const size_t slot = share_slot_bytes(all_rows, c->cfg.n_q_heads, c->cfg.head_dim);
+    const int64_t fit = (int64_t)std::min<size_t>(part_bytes / slot, kShareMaxSlots);
+    cut->unit = (int32_t)unit;
+    cut->slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(fit, ((longest + unit - 1) / unit) | 1));    // odd: see choose_split
+    cut->n_active = n;
+    cut->n_blocks = (int32_t)((most * G + width - 1) / width);
+    cut->n_cols = (int32_t)(all_rows * G);
+}
+
+// Both calls: everything but the sequences' own attention.  cu null: one token per sequence.
+int share_check(const spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, const int32_t* cu, bool appended) {
+    if (pc == nullptr || c == nullptr || prefix_of == nullptr) return SPKV_E_INVAL;
+    const spkv_config_t &x = pc->cfg, &y = c->cfg;
+    if (x.n_q_heads != y.n_q_heads || x.n_kv_heads != y.n_kv_heads || x.head_dim != y.head_dim || x.window != y.window)
+        return SPKV_E_INVAL;
+    if (cu != nullptr && cu[0] != 0) return SPKV_E_INVAL;
+    for (int b = 0; b < y.batch; ++b) {
+        if (prefix_of[b] < -1 || prefix_of[b] >= x.batch || (pc == c && prefix_of[b] == b)) return SPKV_E_INVAL;
+        if (cu != nullptr && cu[b + 1] < cu[b]) return SPKV_E_INVAL;
+    }
+    // (the partial results are addressed by row * heads in 32 bits)
+    if (cu != nullptr && (int64_t)cu[y.batch] * y.n_q_heads > (int64_t)1 << 30) return SPKV_E_INVAL;
+    for (int b = 0; b < y.batch; ++b)
+        if (appended && c->T[b] < tokens_for(cu, b)) return SPKV_E_STATE;
+    return SPKV_OK;
+}
+
+int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, const uint16_t* q, const int32_t* cu,
+                 bool appended, const uint16_t* own_out, const float* own_lse, uint16_t* out, float* lse, float sm_scale,
+                 char* ws, size_t ws_bytes, hipStream_t s) {
+    const int B = c->cfg.batch, Hq = c->cfg.n_q_heads;
+    const int64_t total = cu != nullptr ? cu[B] : B;
+    if (pc->bound_is_loose) {
+        try {
+            const int rc = exact_lengths(pc, s);
+            if (rc != SPKV_OK) return rc;
+        } catch (const std::bad_alloc&) {
+            return SPKV_E_NOMEM;
+        }
+    }
+    SharePrompts prompts;
+    share_prompts(pc, B, prefix_of, cu, &prompts);
+    const ShareCarve k = share_carve(total, Hq);
+    SpkvShareCut cut = {};
+    int waves = 1;
+    if (prompts.n > 0) {
+        share_cut(pc, prompts, ws_bytes - k.part, &waves, &cut);
+        cut.part = reinterpret_cast<float*>(ws + k.part);
+    } else {
+        cut.unit = cut.slots = cut.n_blocks = 1;
+    }
+    cut.n_out = total * Hq;
+    SpkvShareRows by_prompt = {};
+    SpkvShareMerge by_row = {};
+    SpkvShareActive act = {};
+    by_prompt.t_own = c->view.t_pair;
+    int at = 0;
+    for (int a = 0; a < prompts.n; ++a) {
+        by_prompt.prefix[a] = by_row.prefix[a] = (uint16_t)prompts.id[a];
+        by_prompt.first[a] = (uint16_t)at;
+        for (int b = 0; cu == nullptr && b < B; ++b)
+            if (prompts.active[b] == a) {
+                by_row.place[b] = (uint16_t)at;
+                by_prompt.seq[at++] = (uint16_t)b;
+            }
+    }
+    by_prompt.first[prompts.n] = (uint16_t)at;
+    for (int b = 0; b < B; ++b) act.active[b] = by_row.active[b] = prompts.active[b];
+    if (cu != nullptr) {
+        SpkvCu rows_of;
+        std::memcpy(rows_of.v, cu, (size_t)(B + 1) * 4);
+        int32_t* table = reinterpret_cast<int32_t*>(ws + k.table);
+        int32_t* back = reinterpret_cast<int32_t*>(ws + k.by_row);
+        int32_t* first = reinterpret_cast<int32_t*>(ws + k.first_row);
+        if (spkv_launch_prefix_rows(rows_of, act, c->view.t_pair, B, c->cfg.n_kv_heads, appended, cut.n_active, table, back,
+                                    first, s) != hipSuccess)
+            return SPKV_E_HIP;
+        by_prompt.table = reinterpret_cast<const int2*>(table);
+        by_prompt.first_row = first;
+        by_row.by_row = reinterpret_cast<const int2*>(back);
+    }
+    return spkv_launch_prefix(pc->view, q, sm_scale, waves, cut, by_prompt, by_row, own_out, own_lse, out, lse, s) == hipSuccess
+               ? SPKV_OK
+               : SPKV_E_HIP;
+}
+
+bool share_workspace_ok(const spkv_cache* c, int64_t rows, const void* ws, size_t bytes) {
+    if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & (kAlign - 1)) != 0) return false;
+    const size_t at = share_carve(rows, c->cfg.n_q_heads).part;
+    return bytes >= at && bytes - at >= share_slot_bytes(rows, c->cfg.n_q_heads, c->cfg.head_dim);
+}
+}  // namespace
+
+size_t spkv_prefix_workspace_bytes(const spkv_cache_t* c, int64_t rows) {
+    if (c == nullptr || rows <= 0 || rows * c->cfg.n_q_heads > (int64_t)1 << 30) return 0;
+    const size_t slot = share_slot_bytes(rows, c->cfg.n_q_heads, c->cfg.head_dim);
+    const size_t slots = std::max<size_t>(1, std::min<size_t>(kShareMaxSlots, kSharePartBytes / slot));
+    return share_carve(rows, c->cfg.n_q_heads).part + align_up(slots * slot);
+}
+
+int spkv_prefix_attention(spkv_cache_t* pc, const spkv_cache_t* c, const int32_t* prefix_of, const void* q,
+                          const int32_t* cu_seqlens, int32_t appended, const void* own_out, const float* own_lse,
+                          void* out, float* lse, float sm_scale, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = share_check(pc, c, prefix_of, cu_seqlens, appended != 0);
+    if (rc != SPKV_OK) return rc;
+    const int64_t total = cu_seqlens != nullptr ? cu_seqlens[c->cfg.batch] : c->cfg.batch;
+    if (total == 0) return SPKV_OK;
+    if (q == nullptr || own_out == nullptr || own_lse == nullptr || out == nullptr) return SPKV_E_INVAL;
+    if (!aligned16(q) || !aligned16(own_out) || !aligned16(own_lse) || !aligned16(out) || !aligned16(lse)) return SPKV_E_INVAL;
+    if (!share_workspace_ok(pc, total, workspace, workspace_bytes)) return SPKV_E_INVAL;
+    if (!(sm_scale > 0.f)) sm_scale = 1.0f / std::sqrt((float)c->cfg.head_dim);
+    return share_attend(pc, c, prefix_of, static_cast<const uint16_t*>(q), cu_seqlens, appended != 0,
+                        static_cast<const uint16_t*>(own_out), own_lse, static_cast<uint16_t*>(out), lse, sm_scale,
+                        static_cast<char*>(workspace), workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+int spkv_decode_attention_shared(spkv_cache_t* c, spkv_cache_t* pc, const int32_t* prefix_of, const void* q, void* out,
+                                 float* lse, float sm_scale, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = share_check(pc, c, prefix_of, nullptr, true);
+    if (rc != SPKV_OK) return rc;
+    const int B = c->cfg.batch;
+    if (q == nullptr || out == nullptr || !aligned16(q) || !aligned16(out) || !aligned16(lse)) return SPKV_E_INVAL;
+    if (!share_workspace_ok(pc, B, workspace, workspace_bytes)) return SPKV_E_INVAL;
+    if (!(sm_scale > 0.f)) sm_scale = 1.0f / std::sqrt((float)c->cfg.head_dim);
+    char* ws = static_cast<char*>(workspace);
+    float* own_lse = lse != nullptr ? lse : reinterpret_cast<float*>(ws + share_carve(B, c->cfg.n_q_heads).own_lse);
+    rc = spkv_decode_attention(c, q, out, own_lse, sm_scale, stream);
+    if (rc != SPKV_OK) return rc;
+    return share_attend(pc, c, prefix_of, static_cast<const uint16_t*>(q), nullptr, true, static_cast<const uint16_t*>(out),
+                        own_lse, static_cast<uint16_t*>(out), lse, sm_scale, ws, workspace_bytes,
+                        static_cast<hipStream_t>(stream));
+}
+
+namespace {
 // A set of heads as the kernels take it; false if it is not one of `size`-byte elements.
 bool heads_ok(const spkv_heads_t* s, int64_t n_tokens, int n_heads, int head_dim, int size, bool written, SpkvRowSet* o) {
     if (s == nullptr || s->data == nullptr || !aligned16(s->data)) return false;

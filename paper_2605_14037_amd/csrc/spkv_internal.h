@@ -245,3 +245,36 @@ struct SpkvRope {
 hipError_t spkv_launch_rope(const SpkvRope& a, const double* inv_freq, const uint8_t* axis, int head_dim, bool fp32,
                             bool adjacent, bool norm, bool backward, hipStream_t s);
 int spkv_rope_backward_blocks(int64_t n_rows, int n_heads, int head_dim);
+
+// Attention over shared prompts (spkv_prefix.hip).  An active prompt is a sequence of the prompts' cache that holds
+// tokens and that some row of the call continues; the call's rows are taken in the order of the prompts.
+struct SpkvShareCut {
+    float* part;                // [Hkv][slots][n_cols][D] sums, then as many (m, l)
+    int64_t n_out;              // rows * Hq of the call
+    int32_t unit, slots;        // half-pages to a range; most ranges of a list
+    int32_t n_active, n_blocks; // prompts; blocks of columns of the prompt with the most rows
+    int32_t n_cols;             // rows of all prompts * G
+};
+// The rows by prompt: one token a sequence (first, seq; its place is the last of t_own), or tables on the device.
+struct SpkvShareRows {
+    const int2* table;          // null, or [rows] (row, place of its token in the sequence)
+    const int32_t* first_row;   // [n_active + 1], with table
+    const int32_t* t_own;       // [B][Hkv] tokens of the sequences
+    uint16_t first[SPKV_MAX_BATCH + 1], prefix[SPKV_MAX_BATCH], seq[SPKV_MAX_BATCH];
+};
+// ... and by row: its active prompt (-1: none) and its place in the order of the prompts.
+struct SpkvShareMerge {
+    const int2* by_row;         // null: one token a sequence
+    int16_t active[SPKV_MAX_BATCH];
+    uint16_t place[SPKV_MAX_BATCH], prefix[SPKV_MAX_BATCH];
+};
+struct SpkvShareActive {
+    int16_t active[SPKV_MAX_BATCH];       // per sequence
+};
+int spkv_prefix_waves(int n_cols);        // of a workgroup, for the prompt with the most columns
+hipError_t spkv_launch_prefix(const SpkvView& v, const uint16_t* q, float sm_scale, int waves, const SpkvShareCut& cut,
+                              const SpkvShareRows& rows, const SpkvShareMerge& merge, const uint16_t* own_out,
+                              const float* own_lse, uint16_t* out, float* lse, hipStream_t s);
+hipError_t spkv_launch_prefix_rows(const SpkvCu& cu, const SpkvShareActive& a, const int32_t* t_own, int n_seq,
+                                   int n_kv_heads, bool appended, int n_active, int32_t* table, int32_t* by_row,
+                                   int32_t* first_row, hipStream_t s);
