@@ -1635,15 +1635,20 @@ namespace {
 // Shared prompts.  Workspace of a call of n rows: the tables of its rows, their own attention's lse where
 // the caller wants none, and the partial results of the ranges.
 struct ShareCarve {
-    size_t table, by_row, first_row, own_lse, part;
+    size_t table, by_row, first_row, own_lse, own_part, part;
 };
-ShareCarve share_carve(int64_t rows, int n_q_heads) {
+// Sequences whose lists are short are attended in the prompts' launch, in items of at least kShareOwnItem half-pages
+// and at most kShareOwnSlots to a list; only calls of one token a sequence.
+constexpr int kShareOwnSlots = 8, kShareOwnItem = 2;
+ShareCarve share_carve(int64_t rows, int n_q_heads, int head_dim) {
     ShareCarve k;
     k.table = 0;
     k.by_row = align_up((size_t)rows * sizeof(int2));
     k.first_row = k.by_row + align_up((size_t)rows * sizeof(int2));
     k.own_lse = k.first_row + align_up((SPKV_MAX_BATCH + 1) * sizeof(int32_t));
-    k.part = k.own_lse + align_up((size_t)rows * n_q_heads * sizeof(float));
+    k.own_part = k.own_lse + align_up((size_t)rows * n_q_heads * sizeof(float));
+    k.part = k.own_part;
+    if (rows <= SPKV_MAX_BATCH) k.part += align_up((size_t)rows * n_q_heads * kShareOwnSlots * (head_dim + 2) * sizeof(float));
     return k;
 }
 // Bytes that one range of every list needs for the partial results of `rows` rows.
@@ -1677,10 +1682,12 @@ void share_prompts(const spkv_cache* pc, int batch, const int32_t* prefix_of, co
     }
 }
 
-// Ranges of the prompts' lists: about as many workgroups as the chip holds at once.
-constexpr int kShareMinUnit = 4;
-void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_bytes, int* waves, SpkvShareCut* cut) {
-    const int Hkv = c->cfg.n_kv_heads, G = c->carve.G, n = prompts.n;
+// Ranges of the prompts' lists: about as many workgroups as the chip holds at once, every list cut evenly into its
+// share of them.
+constexpr int kShareMinUnit = 2;
+void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_bytes, int* waves, SpkvShareCut* cut,
+               SpkvShareTable* table) {
+    const int Hkv = c->cfg.n_kv_heads, G = c->carve.G, n = prompts.n, n_lists = n * Hkv;
     int64_t most = 0, all_rows = 0;
     for (int a = 0; a < n; ++a) {
         most = std::max<int64_t>(most, prompts.rows[a]);
@@ -1693,14 +1700,10 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
         const int p = prompts.id[a], held = std::min(c->T[p], c->cfg.window);
         return ((int64_t)c->L_ub[p * Hkv + h] + kHalfTokens - 1) / kHalfTokens + (held + kHalfTokens - 1) / kHalfTokens;
     };
-    int64_t work = 0, longest = 1, lists = 0;
+    int64_t work = 0, lists = 0;
     for (int a = 0; a < n; ++a) {
         lists += blocks(a) * Hkv;
-        for (int h = 0; h < Hkv; ++h) {
-            const int64_t x = half_pages(a, h);
-            work += x * blocks(a);
-            longest = std::max(longest, x);
-        }
+        for (int h = 0; h < Hkv; ++h) work += half_pages(a, h) * blocks(a);
     }
     const int cus = spkv_compute_units();
     const int64_t target = (cus > 0 ? cus : 256) * (*waves == 8 ? 1 : 2);
@@ -1714,11 +1717,53 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
     }
     const size_t slot = share_slot_bytes(all_rows, c->cfg.n_q_heads, c->cfg.head_dim);
     const int64_t fit = (int64_t)std::min<size_t>(part_bytes / slot, kShareMaxSlots);
-    cut->unit = (int32_t)unit;
-    cut->slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(fit, ((longest + unit - 1) / unit) | 1));    // odd: see choose_split
-    cut->n_active = n;
+    auto ranges = [&](int a, int h) -> int64_t { return std::max<int64_t>(1, std::min(fit, (half_pages(a, h) + unit - 1) / unit)); };
     cut->n_blocks = (int32_t)((most * G + width - 1) / width);
     cut->n_cols = (int32_t)(all_rows * G);
+    int64_t end = 0, slots = 1;
+    std::fill(table->end, table->end + kShareTablePairs, (uint16_t)65535);
+    for (int a = 0; a < n; ++a)
+        for (int h = 0; h < Hkv; ++h) {
+            const int64_t r = ranges(a, h);
+            slots = std::max(slots, r);
+            end += r * blocks(a);
+            if (a * Hkv + h < kShareTablePairs) {
+                table->end[a * Hkv + h] = (uint16_t)std::min<int64_t>(end, 65535);
+                table->ranges[a * Hkv + h] = (uint8_t)r;
+            }
+        }
+    cut->slots = (int32_t)slots;
+    cut->n_units = (int32_t)end;
+    if (n_lists > kShareTablePairs || end >= 65535) {        // as many for all
+        cut->uniform = (int32_t)std::max<int64_t>(1, std::min(fit, target / std::max<int64_t>(1, lists)));
+        cut->slots = cut->uniform;
+        cut->n_units = (int32_t)((int64_t)n_lists * cut->uniform * cut->n_blocks);
+    }
+}
+
+// Items of the sequences' own lists, in the same launch as the prompts'; part null: not.
+constexpr int kShareOwnLongest = 64;         // half-pages
+void share_own(const spkv_cache* c, char* part, SpkvShareOwn* own) {
+    const int n = c->carve.n_pairs, Hkv = c->cfg.n_kv_heads;
+    int64_t longest = 1;
+    for (int p = 0; p < n; ++p) {
+        const int Tw = std::min(c->T[p / Hkv], c->cfg.window);
+        longest = std::max<int64_t>(longest, (c->L_ub[p] + kHalfTokens - 1) / kHalfTokens + (Tw + kHalfTokens - 1) / kHalfTokens);
+    }
+    if (longest > kShareOwnLongest) return;
+    const SpkvView& v = c->view;
+    own->part = reinterpret_cast<float*>(part);
+    own->ring = v.ring;
+    own->pool = v.pool;
+    own->page_table = v.page_table;
+    own->t_pair = v.t_pair;
+    own->kept_len = v.kept_len;
+    own->n_pairs = n;
+    own->pt_cap = v.pt_cap;
+    own->w = v.w;
+    const int64_t per = std::max<int64_t>(kShareOwnItem, (longest + kShareOwnSlots - 1) / kShareOwnSlots);
+    own->split = SpkvSplit{(int32_t)per, (int32_t)((longest + per - 1) / per), 1, 0, 0, 0};
+    own->n_floats = (int64_t)n * own->split.slots * v.G * v.D;
 }
 
 // Both calls: everything but the sequences' own attention.  cu null: one token per sequence.
@@ -1739,9 +1784,10 @@ int share_check(const spkv_cache* pc, const spkv_cache* c, const int32_t* prefix
     return SPKV_OK;
 }
 
+// own: null, or the sequences' own lists are attended here too (own_out, own_lse are then not read).
 int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, const uint16_t* q, const int32_t* cu,
-                 bool appended, const uint16_t* own_out, const float* own_lse, uint16_t* out, float* lse, float sm_scale,
-                 char* ws, size_t ws_bytes, hipStream_t s) {
+                 bool appended, bool with_own, const uint16_t* own_out, const float* own_lse, uint16_t* out, float* lse,
+                 float sm_scale, char* ws, size_t ws_bytes, hipStream_t s) {
     const int B = c->cfg.batch, Hq = c->cfg.n_q_heads;
     const int64_t total = cu != nullptr ? cu[B] : B;
     if (pc->bound_is_loose) {
@@ -1754,53 +1800,57 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
     }
     SharePrompts prompts;
     share_prompts(pc, B, prefix_of, cu, &prompts);
-    const ShareCarve k = share_carve(total, Hq);
+    const ShareCarve k = share_carve(total, Hq, c->cfg.head_dim);
     SpkvShareCut cut = {};
+    SpkvShareTable table = {};
     int waves = 1;
-    if (prompts.n > 0) {
-        share_cut(pc, prompts, ws_bytes - k.part, &waves, &cut);
-        cut.part = reinterpret_cast<float*>(ws + k.part);
-    } else {
-        cut.unit = cut.slots = cut.n_blocks = 1;
-    }
+    cut.slots = 1;
+    if (prompts.n > 0) share_cut(pc, prompts, ws_bytes - k.part, &waves, &cut, &table);
+    cut.part = reinterpret_cast<float*>(ws + k.part);
     cut.n_out = total * Hq;
+    SpkvShareOwn own = {};
+    if (with_own) share_own(c, ws + k.own_part, &own);
     SpkvShareRows by_prompt = {};
     SpkvShareMerge by_row = {};
-    SpkvShareActive act = {};
     by_prompt.t_own = c->view.t_pair;
-    int at = 0;
-    for (int a = 0; a < prompts.n; ++a) {
-        by_prompt.prefix[a] = by_row.prefix[a] = (uint16_t)prompts.id[a];
-        by_prompt.first[a] = (uint16_t)at;
-        for (int b = 0; cu == nullptr && b < B; ++b)
-            if (prompts.active[b] == a) {
-                by_row.place[b] = (uint16_t)at;
-                by_prompt.seq[at++] = (uint16_t)b;
-            }
-    }
-    by_prompt.first[prompts.n] = (uint16_t)at;
-    for (int b = 0; b < B; ++b) act.active[b] = by_row.active[b] = prompts.active[b];
-    if (cu != nullptr) {
+    std::memcpy(by_row.ranges, table.ranges, sizeof(by_row.ranges));
+    for (int a = 0; a < prompts.n; ++a) by_prompt.prefix[a] = (uint16_t)prompts.id[a];
+    if (cu == nullptr && B <= kShareArgSeqs) {
+        int at = 0;
+        for (int a = 0; a < prompts.n; ++a) {
+            by_prompt.first[a] = (uint16_t)at;
+            for (int b = 0; b < B; ++b)
+                if (prompts.active[b] == a) {
+                    by_row.place[b] = (uint16_t)at;
+                    by_prompt.seq[at++] = (uint16_t)b;
+                }
+        }
+        by_prompt.first[prompts.n] = (uint16_t)at;
+        for (int b = 0; b < B; ++b) by_row.active[b] = prompts.active[b];
+    } else {
         SpkvCu rows_of;
-        std::memcpy(rows_of.v, cu, (size_t)(B + 1) * 4);
-        int32_t* table = reinterpret_cast<int32_t*>(ws + k.table);
+        for (int b = 0; b <= B; ++b) rows_of.v[b] = cu != nullptr ? cu[b] : b;
+        SpkvShareActive act = {};
+        for (int b = 0; b < B; ++b) act.active[b] = prompts.active[b];
+        int32_t* rows = reinterpret_cast<int32_t*>(ws + k.table);
         int32_t* back = reinterpret_cast<int32_t*>(ws + k.by_row);
         int32_t* first = reinterpret_cast<int32_t*>(ws + k.first_row);
-        if (spkv_launch_prefix_rows(rows_of, act, c->view.t_pair, B, c->cfg.n_kv_heads, appended, cut.n_active, table, back,
+        if (spkv_launch_prefix_rows(rows_of, act, c->view.t_pair, B, c->cfg.n_kv_heads, appended, prompts.n, rows, back,
                                     first, s) != hipSuccess)
             return SPKV_E_HIP;
-        by_prompt.table = reinterpret_cast<const int2*>(table);
+        by_prompt.table = reinterpret_cast<const int2*>(rows);
         by_prompt.first_row = first;
         by_row.by_row = reinterpret_cast<const int2*>(back);
     }
-    return spkv_launch_prefix(pc->view, q, sm_scale, waves, cut, by_prompt, by_row, own_out, own_lse, out, lse, s) == hipSuccess
+    return spkv_launch_prefix(pc->view, q, sm_scale, waves, cut, table, by_prompt, by_row, own, own_out, own_lse, out, lse,
+                              s) == hipSuccess
                ? SPKV_OK
                : SPKV_E_HIP;
 }
 
 bool share_workspace_ok(const spkv_cache* c, int64_t rows, const void* ws, size_t bytes) {
     if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & (kAlign - 1)) != 0) return false;
-    const size_t at = share_carve(rows, c->cfg.n_q_heads).part;
+    const size_t at = share_carve(rows, c->cfg.n_q_heads, c->cfg.head_dim).part;
     return bytes >= at && bytes - at >= share_slot_bytes(rows, c->cfg.n_q_heads, c->cfg.head_dim);
 }
 }  // namespace
@@ -1809,7 +1859,7 @@ size_t spkv_prefix_workspace_bytes(const spkv_cache_t* c, int64_t rows) {
     if (c == nullptr || rows <= 0 || rows * c->cfg.n_q_heads > (int64_t)1 << 30) return 0;
     const size_t slot = share_slot_bytes(rows, c->cfg.n_q_heads, c->cfg.head_dim);
     const size_t slots = std::max<size_t>(1, std::min<size_t>(kShareMaxSlots, kSharePartBytes / slot));
-    return share_carve(rows, c->cfg.n_q_heads).part + align_up(slots * slot);
+    return share_carve(rows, c->cfg.n_q_heads, c->cfg.head_dim).part + align_up(slots * slot);
 }
 
 int spkv_prefix_attention(spkv_cache_t* pc, const spkv_cache_t* c, const int32_t* prefix_of, const void* q,
@@ -1823,7 +1873,7 @@ int spkv_prefix_attention(spkv_cache_t* pc, const spkv_cache_t* c, const int32_t
     if (!aligned16(q) || !aligned16(own_out) || !aligned16(own_lse) || !aligned16(out) || !aligned16(lse)) return SPKV_E_INVAL;
     if (!share_workspace_ok(pc, total, workspace, workspace_bytes)) return SPKV_E_INVAL;
     if (!(sm_scale > 0.f)) sm_scale = 1.0f / std::sqrt((float)c->cfg.head_dim);
-    return share_attend(pc, c, prefix_of, static_cast<const uint16_t*>(q), cu_seqlens, appended != 0,
+    return share_attend(pc, c, prefix_of, static_cast<const uint16_t*>(q), cu_seqlens, appended != 0, false,
                         static_cast<const uint16_t*>(own_out), own_lse, static_cast<uint16_t*>(out), lse, sm_scale,
                         static_cast<char*>(workspace), workspace_bytes, static_cast<hipStream_t>(stream));
 }
@@ -1836,13 +1886,28 @@ int spkv_decode_attention_shared(spkv_cache_t* c, spkv_cache_t* pc, const int32_
     if (q == nullptr || out == nullptr || !aligned16(q) || !aligned16(out) || !aligned16(lse)) return SPKV_E_INVAL;
     if (!share_workspace_ok(pc, B, workspace, workspace_bytes)) return SPKV_E_INVAL;
     if (!(sm_scale > 0.f)) sm_scale = 1.0f / std::sqrt((float)c->cfg.head_dim);
+    hipStream_t s = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
-    float* own_lse = lse != nullptr ? lse : reinterpret_cast<float*>(ws + share_carve(B, c->cfg.n_q_heads).own_lse);
+    const uint16_t* qq = static_cast<const uint16_t*>(q);
+    uint16_t* o = static_cast<uint16_t*>(out);
+    bool fused = false;
+    if (!c->timing && !c->split_only) {
+        try {
+            if (c->bound_is_loose) rc = exact_lengths(c, s);
+        } catch (const std::bad_alloc&) {
+            rc = SPKV_E_NOMEM;
+        }
+        if (rc != SPKV_OK) return rc;
+        tighten_bound(c, s);
+        SpkvShareOwn own = {};
+        share_own(c, ws, &own);
+        fused = own.part != nullptr;
+    }
+    if (fused) return share_attend(pc, c, prefix_of, qq, nullptr, true, true, nullptr, nullptr, o, lse, sm_scale, ws, workspace_bytes, s);
+    float* own_lse = lse != nullptr ? lse : reinterpret_cast<float*>(ws + share_carve(B, c->cfg.n_q_heads, c->cfg.head_dim).own_lse);
     rc = spkv_decode_attention(c, q, out, own_lse, sm_scale, stream);
     if (rc != SPKV_OK) return rc;
-    return share_attend(pc, c, prefix_of, static_cast<const uint16_t*>(q), nullptr, true, static_cast<const uint16_t*>(out),
-                        own_lse, static_cast<uint16_t*>(out), lse, sm_scale, ws, workspace_bytes,
-                        static_cast<hipStream_t>(stream));
+    return share_attend(pc, c, prefix_of, qq, nullptr, true, false, o, own_lse, o, lse, sm_scale, ws, workspace_bytes, s);
 }
 
 namespace {

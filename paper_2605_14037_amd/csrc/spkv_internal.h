@@ -251,30 +251,51 @@ int spkv_rope_backward_blocks(int64_t n_rows, int n_heads, int head_dim);
 struct SpkvShareCut {
     float* part;                // [Hkv][slots][n_cols][D] sums, then as many (m, l)
     int64_t n_out;              // rows * Hq of the call
-    int32_t unit, slots;        // half-pages to a range; most ranges of a list
-    int32_t n_active, n_blocks; // prompts; blocks of columns of the prompt with the most rows
+    int32_t n_units;            // workgroups of the prompts' lists
+    int32_t slots;              // most ranges of a list
+    int32_t uniform;            // > 0: every list has this many ranges and n_blocks blocks of columns; 0: SpkvShareTable
+    int32_t n_blocks;           // blocks of columns of the prompt with the most rows
     int32_t n_cols;             // rows of all prompts * G
 };
-// The rows by prompt: one token a sequence (first, seq; its place is the last of t_own), or tables on the device.
+// Workgroups by list (active prompt, KV head): where each list's end, and the ranges of each.
+constexpr int kShareTablePairs = 256;
+struct SpkvShareTable {
+    alignas(8) uint16_t end[kShareTablePairs];       // lists that are not there: 65535
+    uint8_t ranges[kShareTablePairs];
+};
+// The sequences' own lists, where they are attended in the same launch.
+struct SpkvShareOwn {
+    float* part;                // null: not; [n_pairs][split.slots][G][D] sums, then as many (m, l)
+    int64_t n_floats;           // of the sums
+    uint16_t *ring, *pool;
+    int32_t *page_table, *t_pair, *kept_len;
+    int32_t n_pairs, pt_cap, w;
+    SpkvSplit split;
+};
+// The rows by prompt: one token a sequence (first, seq; its place is the last of t_own), or -- more tokens, or more
+// sequences than travel with the launch -- tables on the device.
+constexpr int kShareArgSeqs = 256;
 struct SpkvShareRows {
     const int2* table;          // null, or [rows] (row, place of its token in the sequence)
     const int32_t* first_row;   // [n_active + 1], with table
     const int32_t* t_own;       // [B][Hkv] tokens of the sequences
-    uint16_t first[SPKV_MAX_BATCH + 1], prefix[SPKV_MAX_BATCH], seq[SPKV_MAX_BATCH];
+    uint16_t first[kShareArgSeqs + 1], seq[kShareArgSeqs], prefix[SPKV_MAX_BATCH];
 };
 // ... and by row: its active prompt (-1: none) and its place in the order of the prompts.
 struct SpkvShareMerge {
     const int2* by_row;         // null: one token a sequence
-    int16_t active[SPKV_MAX_BATCH];
-    uint16_t place[SPKV_MAX_BATCH], prefix[SPKV_MAX_BATCH];
+    int16_t active[kShareArgSeqs];
+    uint16_t place[kShareArgSeqs];
+    uint8_t ranges[kShareTablePairs];     // as in SpkvShareTable
 };
 struct SpkvShareActive {
     int16_t active[SPKV_MAX_BATCH];       // per sequence
 };
 int spkv_prefix_waves(int n_cols);        // of a workgroup, for the prompt with the most columns
 hipError_t spkv_launch_prefix(const SpkvView& v, const uint16_t* q, float sm_scale, int waves, const SpkvShareCut& cut,
-                              const SpkvShareRows& rows, const SpkvShareMerge& merge, const uint16_t* own_out,
-                              const float* own_lse, uint16_t* out, float* lse, hipStream_t s);
+                              const SpkvShareTable& table, const SpkvShareRows& rows, const SpkvShareMerge& merge,
+                              const SpkvShareOwn& own, const uint16_t* own_out, const float* own_lse, uint16_t* out,
+                              float* lse, hipStream_t s);
 hipError_t spkv_launch_prefix_rows(const SpkvCu& cu, const SpkvShareActive& a, const int32_t* t_own, int n_seq,
                                    int n_kv_heads, bool appended, int n_active, int32_t* table, int32_t* by_row,
                                    int32_t* first_row, hipStream_t s);

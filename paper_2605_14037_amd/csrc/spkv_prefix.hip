@@ -28,30 +28,147 @@ constexpr int kRingGateTiles = 64;           // half-pages of the ring whose gat
 
 __device__ __forceinline__ unsigned bits_upto8(int n) { return n <= 0 ? 0u : n >= 8 ? 0xffu : (1u << n) - 1u; }
 
+// The sequences' cache as the helpers of spkv_device.h take it: its lists, the shape of the prompts' one.
+__device__ __forceinline__ SpkvView own_view(const SpkvShareOwn& o, const SpkvView& prompts) {
+    SpkvView v = prompts;
+    v.n_pairs = o.n_pairs;
+    v.pt_cap = o.pt_cap;
+    v.ring = o.ring;
+    v.page_table = o.page_table;
+    v.pool = o.pool;
+    v.t_pair = o.t_pair;
+    v.kept_len = o.kept_len;
+    return v;
+}
+// Items that a pair of them is cut into (pair_split).
+__device__ __forceinline__ int own_ranges(const SpkvShareOwn& o, int pair) {
+    const int n_hp = ((o.kept_len[pair] + kHalfTokens - 1) >> 5) + ((min(o.t_pair[pair], o.w) + kHalfTokens - 1) >> 5);
+    return min((n_hp + o.split.hp_per_item - 1) / o.split.hp_per_item, o.split.slots);
+}
+
+// The sequences' own tokens in the same launch (spkv_decode_attention_shared, short lists): one wave per item of a
+// (sequence, KV head), cut as for spkv_decode_split, 16 columns of which the group's heads are used;
+// operands straight from memory, weights in two bf16 parts.
+template <int D>
+__device__ __forceinline__ void own_item(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e, SpkvSplit sp,
+                                         float* part, int item) {
+    constexpr int NS = D / 32, NB = D / 16;
+    const int pair = item / sp.slots, j = item - pair * sp.slots;
+    if (pair >= v.n_pairs) return;
+    const int lane = threadIdx.x & 63, kc = lane >> 4, n = lane & 15;
+    const int32_t* pt = v.page_table + (size_t)pair * v.pt_cap;
+    int pbase = 0, my_page = pt[min(lane, v.pt_cap - 1)];
+    const PairSplit ps = pair_split(v, pair, sp);
+    if (j >= ps.groups) return;
+    const int hp0 = (int)((int64_t)j * ps.nhp / ps.groups), hp1 = (int)((int64_t)(j + 1) * ps.nhp / ps.groups);
+    const int b = pair / v.Hkv, h = pair - b * v.Hkv;
+    bf16x8 qb[NS];
+    const uint16_t* qrow = q + ((size_t)b * v.Hq + (size_t)h * v.G + n) * D + kc * 8;
+#pragma unroll
+    for (int sl = 0; sl < NS; ++sl) {
+        uint4 raw = {0u, 0u, 0u, 0u};
+        if (n < v.G) raw = *reinterpret_cast<const uint4*>(qrow + sl * 32);
+        qb[sl] = __builtin_bit_cast(bf16x8, raw);
+    }
+    f32x4 acc[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    float m = SPKV_NEG_INF, l = 0.f;
+    for (int hp = hp0; hp < hp1; ++hp) {
+        const uint16_t* base;
+        int nvalid;
+        if (hp < ps.ghp) {
+            const int lp = hp >> 1;
+            if (lp >= pbase + 64) {
+                pbase = lp;
+                my_page = pt[min(pbase + lane, v.pt_cap - 1)];
+            }
+            base = pool_page(v, __builtin_amdgcn_readlane(my_page, lp - pbase)) + (hp & 1) * (2 * kHalfTokens * D);
+            nvalid = min(kHalfTokens, ps.L - hp * kHalfTokens);
+        } else {
+            const int r = hp - ps.ghp;
+            base = ring_page(v, pair, r >> 1) + (r & 1) * (2 * kHalfTokens * D);
+            nvalid = min(kHalfTokens, ps.Tw - r * kHalfTokens);
+        }
+        const bool any_kill = nvalid < kHalfTokens;
+        const unsigned kill = any_kill ? 0xffu << min(max(nvalid - kc * 8, 0), 8) : 0u;
+        const uint16_t* kp = base + lane * 8;
+        const uint16_t* vp = base + kHalfTokens * D + lane * 8;
+        bf16x8 ka[2][NS], va[NB];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) ka[t][sl] = load_stream_b128(kp + (t * (D / 8) + sl * 4) * 128);
+#pragma unroll
+        for (int db = 0; db < NB; ++db) va[db] = load_stream_b128(vp + db * 512);
+        attend_half_page<D, true>(ka, va, qb, kill, any_kill, scale_log2e, acc, m, l);
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (n >= v.G) return;
+    const size_t pc = (size_t)item * v.G + n;
+    float* pa = part + pc * D + kc * 4;
+#pragma unroll
+    for (int db = 0; db < NB; ++db) *reinterpret_cast<f32x4*>(pa + db * 16) = acc[db];
+    if (kc == 0) reinterpret_cast<float2*>(part + (size_t)v.n_pairs * sp.slots * v.G * D)[pc] = make_float2(m, l);
+}
+
+// Which list, range and block of columns a workgroup has: id counts workgroups without gaps, the ranges of a list's
+// block of columns next to each other (round-robin over the XCDs).  With up to kShareTablePairs lists the host's
+// table says where each list's workgroups end -- ids with nothing to do in between would fill some
+// XCDs' compute units and leave others idle; with more lists each has as many.
+struct ShareUnit {
+    int list, range, ranges, block;
+};
+__device__ __forceinline__ ShareUnit find_unit(const SpkvShareCut& cut, const SpkvShareTable& table, int id, int n_kv_heads) {
+    ShareUnit u;
+    if (cut.uniform > 0) {
+        const int each = cut.uniform * cut.n_blocks;
+        u.list = id / each;
+        const int rest = id - u.list * each;
+        u.ranges = cut.uniform;
+        u.block = rest / u.ranges;
+        u.range = rest - u.block * u.ranges;
+        return u;
+    }
+    const int lane = threadIdx.x & 63;
+    const uint2 raw = reinterpret_cast<const uint2*>(table.end)[lane];           // four lists a lane
+    const unsigned e[4] = {raw.x & 0xffffu, raw.x >> 16, raw.y & 0xffffu, raw.y >> 16};
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) before += __popcll(__ballot((int)e[i] <= id));
+    u.list = before;
+    const int start = before > 0 ? table.end[before - 1] : 0;
+    u.ranges = table.ranges[before];
+    u.block = (id - start) / u.ranges;
+    u.range = id - start - u.block * u.ranges;
+    return u;
+}
+
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW >= 4 ? 2 : 1, NW >= 4 ? 2 : 1)))
-void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvShareCut cut, SpkvShareRows rows) {
+void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvShareCut cut, SpkvShareTable table,
+                       SpkvShareRows rows, SpkvShareOwn own) {
     constexpr int NS = D / 16, NB = D / 32;
     constexpr int kHalfElems = 2 * kHalfTokens * D;
     constexpr int kHps = NW == 8 ? 2 : 1;                    // half-pages to a step
     constexpr int kSlots = NW == 8 ? 8 : 5;                  // half-pages in LDS
     constexpr int kRowsPerWave = kHps * (D / 8) / NW;        // 1 KB rows of a step that a wave copies
     __shared__ __attribute__((aligned(16))) uint16_t s_tile[kSlots][kHalfElems];
-    // workgroups of one range (its column blocks) run on one XCD, one after the other
-    const int group = (int)blockIdx.x / (8 * cut.n_blocks), rest = (int)blockIdx.x - group * 8 * cut.n_blocks;
-    const int unit = group * 8 + (rest & 7), block = rest >> 3;
-    const int pair_id = unit / cut.slots, j = unit - pair_id * cut.slots;
-    const int act = pair_id / v.Hkv, h = pair_id - act * v.Hkv;
-    if (act >= cut.n_active) return;
+    if ((int)blockIdx.x >= cut.n_units) {                    // behind the prompts': the sequences' own lists
+        const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        own_item<D>(own_view(own, v), q, scale_log2e, own.split, own.part, ((int)blockIdx.x - cut.n_units) * NW + wave);
+        return;
+    }
+    const ShareUnit u = find_unit(cut, table, blockIdx.x, v.Hkv);
+    const int act = u.list / v.Hkv, h = u.list - act * v.Hkv, j = u.range, ranges = u.ranges;
     const int first = rows.table != nullptr ? rows.first_row[act] : rows.first[act];
     const int n_cols = ((rows.table != nullptr ? rows.first_row[act + 1] : rows.first[act + 1]) - first) * v.G;
-    const int col0 = block * (32 * NW);
+    const int col0 = u.block * (32 * NW);
     if (col0 >= n_cols) return;
     const int pair = (int)rows.prefix[act] * v.Hkv + h;
     const int T = v.t_pair[pair], L = v.kept_len[pair], held = min(T, v.w);
     const int nA = (L + kHalfTokens - 1) >> 5, n_hp = nA + ((held + kHalfTokens - 1) >> 5);
-    const int ranges = min((n_hp + cut.unit - 1) / cut.unit, cut.slots);
-    if (j >= ranges) return;
     const int x_begin = (int)((int64_t)j * n_hp / ranges), x_end = (int)((int64_t)(j + 1) * n_hp / ranges), last = x_end - 1;
 
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
@@ -67,6 +184,12 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     } else {
         row = rows.seq[first + in_group];
         place = rows.t_own[row * v.Hkv] - 1;
+    }
+    const size_t pc = ((size_t)h * cut.slots + j) * cut.n_cols + (size_t)first * v.G + c;      // of the partial result
+    float2* part_ml = reinterpret_cast<float2*>(cut.part + (size_t)v.Hkv * cut.slots * cut.n_cols * D);
+    if (x_begin >= x_end) {                                  // fewer half-pages than ranges
+        if (valid && half == 0) part_ml[pc] = make_float2(SPKV_NEG_INF, 0.f);
+        return;
     }
     // page ids of 64 logical pages, one a lane
     const int32_t* pt = v.page_table + (size_t)pair * v.pt_cap;
@@ -329,7 +452,6 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
 
     l += __shfl_xor(l, 32);
     if (!valid) return;
-    const size_t pc = ((size_t)h * cut.slots + j) * cut.n_cols + (size_t)first * v.G + c;
     float* pa = cut.part + pc * D + half * 4;
 #pragma unroll
     for (int db = 0; db < NB; ++db)
@@ -337,24 +459,28 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
         for (int g = 0; g < 4; ++g)
             *reinterpret_cast<f32x4*>(pa + db * 32 + g * 8) =
                 (f32x4){acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]};
-    if (half == 0)
-        reinterpret_cast<float2*>(cut.part + (size_t)v.Hkv * cut.slots * cut.n_cols * D)[pc] = make_float2(m, l);
+    if (half == 0) part_ml[pc] = make_float2(m, l);
 }
 
-// The join: a thread owns four consecutive output elements of one (row, head).  The sequence's own part comes
-// as its bf16 output and fp32 logarithm of the sum: half a step of bf16 more than from sums in 32 bits, on the
-// share that the own tokens have.
-template <int D>
-__global__ __launch_bounds__(256) void spkv_prefix_merge(SpkvView v, SpkvShareCut cut, SpkvShareMerge rows,
-                                                         const uint16_t* own_out, const float* own_lse, uint16_t* out,
-                                                         float* lse) {         // (out may be own_out, lse own_lse)
-    constexpr int TPC = D / 4, CPB = 256 / TPC;
-    const int64_t id = (int64_t)blockIdx.x * CPB + threadIdx.x / TPC;      // row * Hq + head
-    if (id >= cut.n_out) return;
-    const int row = (int)(id / v.Hq), head = (int)(id - (int64_t)row * v.Hq), h = head / v.G, d = ((int)threadIdx.x % TPC) * 4;
-    const uint2 ob = *reinterpret_cast<const uint2*>(own_out + id * D + d);
-    const float z = own_lse[id];
-    int act, at;
+// The join: D / 4 threads own a column (row, head), four consecutive elements each; S such groups share a column,
+// each with every S-th of its partial results, and meet in LDS (few columns of many ranges: 512 columns
+// of 64 ranges in one group each took 14 us, a chain of eight round trips on a quarter of the chip).
+// The sequence's own part is a set of partial results too (own.part), or comes as a call's bf16 output and fp32
+// logarithm of its sum: half a step of bf16 more than from sums in 32 bits, on the share that the own tokens have.
+template <int D, int S>
+__global__ __launch_bounds__(256) void spkv_prefix_merge(SpkvShareCut cut, SpkvShareMerge rows, SpkvShareOwn own, int n_q_heads,
+                                                         int n_kv_heads, const uint16_t* own_out, const float* own_lse,
+                                                         uint16_t* out, float* lse) {      // (out may be own_out, lse own_lse)
+    constexpr int TPC = D / 4, CPB = 256 / TPC, kFold = 8;
+    __shared__ f32x4 s_num[S > 1 ? CPB : 1][S > 1 ? TPC : 1];
+    __shared__ float2 s_ml[S > 1 ? CPB : 1];
+    const int slice = (int)threadIdx.x / TPC, share = slice % S, d = ((int)threadIdx.x % TPC) * 4;
+    const int64_t id = (int64_t)blockIdx.x * (CPB / S) + slice / S;      // row * Hq + head
+    const bool exists = id < cut.n_out;
+    const int G = n_q_heads / n_kv_heads;
+    const int row = exists ? (int)(id / n_q_heads) : 0, head = exists ? (int)(id - (int64_t)row * n_q_heads) : 0;
+    const int h = head / G, g = head - h * G;
+    int act = -1, at = 0;
     if (rows.by_row != nullptr) {
         const int2 e = rows.by_row[row];
         act = e.x;
@@ -363,52 +489,83 @@ __global__ __launch_bounds__(256) void spkv_prefix_merge(SpkvView v, SpkvShareCu
         act = rows.active[row];
         at = rows.place[row];
     }
-    int ranges = 0;
-    if (act >= 0) {
-        const int pair = (int)rows.prefix[act] * v.Hkv + h;
-        const int n_hp = ((v.kept_len[pair] + kHalfTokens - 1) >> 5) + ((min(v.t_pair[pair], v.w) + kHalfTokens - 1) >> 5);
-        ranges = min((n_hp + cut.unit - 1) / cut.unit, cut.slots);
-    }
-    if (ranges == 0) {                                       // no prompt: the own part as it is
-        *reinterpret_cast<uint2*>(out + id * D + d) = ob;
-        if (lse != nullptr && d == 0) lse[id] = z;
-        return;
-    }
-    const bool any_own = z > SPKV_NEG_INF;
-    float M = any_own ? z * 1.4426950408889634f : SPKV_NEG_INF, den = any_own ? 1.f : 0.f;
+    float M = SPKV_NEG_INF, den = 0.f;
     f32x4 num = {0.f, 0.f, 0.f, 0.f};
-    if (any_own)
-        num = (f32x4){__builtin_bit_cast(float, ob.x << 16), __builtin_bit_cast(float, ob.x & 0xffff0000u),
-                      __builtin_bit_cast(float, ob.y << 16), __builtin_bit_cast(float, ob.y & 0xffff0000u)};
-    // ranges kFold at a time, their loads in flight together; only the rescaling is chained
-    constexpr int kFold = 8;
-    const size_t pc0 = (size_t)h * cut.slots * cut.n_cols + (size_t)at * v.G + (head - h * v.G);
-    const float2* ml = reinterpret_cast<const float2*>(cut.part + (size_t)v.Hkv * cut.slots * cut.n_cols * D);
-    for (int r0 = 0; r0 < ranges; r0 += kFold) {
+    const int ranges = act < 0 ? 0 : cut.uniform > 0 ? cut.uniform : rows.ranges[act * n_kv_heads + h];
+    int own_parts = 0;
+    size_t own0 = 0;
+    if (own.part != nullptr) {
+        const SpkvSplit sp = own.split;
+        const int pair = row * n_kv_heads + h;
+        own_parts = own_ranges(own, pair);
+        own0 = (size_t)pair * sp.slots * G + g;
+    } else if (share == 0 && exists) {
+        const uint2 ob = *reinterpret_cast<const uint2*>(own_out + id * D + d);
+        const float z = own_lse[id];
+        if (ranges == 0) {                                   // no prompt: the own part as it is
+            *reinterpret_cast<uint2*>(out + id * D + d) = ob;
+            if (lse != nullptr && d == 0) lse[id] = z;
+        }
+        if (z > SPKV_NEG_INF) {
+            M = z * 1.4426950408889634f;
+            den = 1.f;
+            num = (f32x4){__builtin_bit_cast(float, ob.x << 16), __builtin_bit_cast(float, ob.x & 0xffff0000u),
+                          __builtin_bit_cast(float, ob.y << 16), __builtin_bit_cast(float, ob.y & 0xffff0000u)};
+        }
+    }
+    // partial results kFold at a time, their loads in flight together; only the rescaling is chained
+    const size_t prompt0 = (size_t)h * cut.slots * cut.n_cols + (size_t)at * G + g;
+    const float2* ml = reinterpret_cast<const float2*>(cut.part + (size_t)n_kv_heads * cut.slots * cut.n_cols * D);
+    const float2* own_ml = reinterpret_cast<const float2*>(own.part + own.n_floats);
+    const int parts = exists ? ranges + own_parts : 0;
+    for (int r0 = share; r0 < parts; r0 += kFold * S) {
         float2 x[kFold];
         f32x4 a[kFold];
 #pragma unroll
         for (int u = 0; u < kFold; ++u) {
-            const size_t pc = pc0 + (size_t)min(r0 + u, ranges - 1) * cut.n_cols;      // past the end: re-read, ignored
-            x[u] = ml[pc];
-            a[u] = *reinterpret_cast<const f32x4*>(cut.part + pc * D + d);
+            const int r = min(r0 + u * S, parts - 1);        // past the end: re-read, ignored
+            const bool mine = r >= ranges;
+            const size_t pc = mine ? own0 + (size_t)(r - ranges) * G : prompt0 + (size_t)r * cut.n_cols;
+            x[u] = (mine ? own_ml : ml)[pc];
+            a[u] = *reinterpret_cast<const f32x4*>((mine ? own.part : cut.part) + pc * D + d);
         }
         float m_new = M;
 #pragma unroll
         for (int u = 0; u < kFold; ++u)
-            if (r0 + u < ranges) m_new = fmaxf(m_new, x[u].x);
+            if (r0 + u * S < parts) m_new = fmaxf(m_new, x[u].x);
         const float m_ref = m_new == SPKV_NEG_INF ? 0.f : m_new, so = __builtin_amdgcn_exp2f(M - m_ref);
         den *= so;
         num *= so;
 #pragma unroll
         for (int u = 0; u < kFold; ++u)
-            if (r0 + u < ranges) {
-                const float sc = __builtin_amdgcn_exp2f(x[u].x - m_ref);               // 0 for a range without keys
+            if (r0 + u * S < parts && x[u].x > SPKV_NEG_INF) {       // (a range without keys has written no sums)
+                const float sc = __builtin_amdgcn_exp2f(x[u].x - m_ref);
                 num += a[u] * sc;
                 den += x[u].y * sc;
             }
         M = m_new;
     }
+    if (S > 1) {
+        s_num[slice][(int)threadIdx.x % TPC] = num;
+        if (d == 0) s_ml[slice] = make_float2(M, den);
+        __syncthreads();
+        if (share != 0) return;
+        float top = M;
+#pragma unroll
+        for (int i = 1; i < S; ++i) top = fmaxf(top, s_ml[slice + i].x);
+        const float m_ref = top == SPKV_NEG_INF ? 0.f : top, so = __builtin_amdgcn_exp2f(M - m_ref);
+        num *= so;
+        den *= so;
+#pragma unroll
+        for (int i = 1; i < S; ++i) {
+            const float2 y = s_ml[slice + i];
+            const float sc = __builtin_amdgcn_exp2f(y.x - m_ref);
+            num += s_num[slice + i][(int)threadIdx.x % TPC] * sc;
+            den += y.y * sc;
+        }
+        M = top;
+    }
+    if (!exists || (ranges == 0 && own.part == nullptr)) return;
     const float inv = den > 0.f ? 1.0f / den : 0.f;          // (a row that sees no key at all: zeros)
     uint2 packed;
     packed.x = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)(num[0] * inv)) |
@@ -463,28 +620,37 @@ int spkv_prefix_waves(int n_cols) { return n_cols <= 32 ? 1 : n_cols <= 64 ? 2 :
 
 template <int D>
 static hipError_t launch_prefix(const SpkvView& v, const uint16_t* q, float sl, int waves, const SpkvShareCut& cut,
-                                const SpkvShareRows& rows, const SpkvShareMerge& merge, const uint16_t* own_out,
-                                const float* own_lse, uint16_t* out, float* lse, hipStream_t s) {
-    const int units = cut.n_active * v.Hkv * cut.slots;
-    const dim3 grid((unsigned)((units + 7) / 8 * 8 * cut.n_blocks));
-    if (cut.n_active > 0) {
-        if (waves == 8) spkv_prefix_split<D, 8><<<grid, dim3(512), 0, s>>>(v, q, sl, cut, rows);
-        else if (waves == 4) spkv_prefix_split<D, 4><<<grid, dim3(256), 0, s>>>(v, q, sl, cut, rows);
-        else if (waves == 2) spkv_prefix_split<D, 2><<<grid, dim3(128), 0, s>>>(v, q, sl, cut, rows);
-        else spkv_prefix_split<D, 1><<<grid, dim3(64), 0, s>>>(v, q, sl, cut, rows);
+                                const SpkvShareTable& table, const SpkvShareRows& rows, const SpkvShareMerge& merge,
+                                const SpkvShareOwn& own, const uint16_t* own_out, const float* own_lse, uint16_t* out,
+                                float* lse, hipStream_t s) {
+    const int items = own.part != nullptr ? own.n_pairs * own.split.slots : 0;
+    const dim3 grid((unsigned)(cut.n_units + (items + waves - 1) / waves));
+    if (grid.x > 0) {
+        if (waves == 8) spkv_prefix_split<D, 8><<<grid, dim3(512), 0, s>>>(v, q, sl, cut, table, rows, own);
+        else if (waves == 4) spkv_prefix_split<D, 4><<<grid, dim3(256), 0, s>>>(v, q, sl, cut, table, rows, own);
+        else if (waves == 2) spkv_prefix_split<D, 2><<<grid, dim3(128), 0, s>>>(v, q, sl, cut, table, rows, own);
+        else spkv_prefix_split<D, 1><<<grid, dim3(64), 0, s>>>(v, q, sl, cut, table, rows, own);
     }
-    const int per_block = 256 / (D / 4);
-    spkv_prefix_merge<D><<<dim3((unsigned)((cut.n_out + per_block - 1) / per_block)), dim3(256), 0, s>>>(
-        v, cut, merge, own_out, own_lse, out, lse);
+    // groups to a column: about eight workgroups per compute unit, no more groups than there are ranges
+    constexpr int CPB = 256 / (D / 4);
+    int share = 8;
+    while (share > 1 && (cut.n_out * share / CPB > 4096 || share > cut.slots)) share >>= 1;
+    const int per_block = CPB / share;
+    const dim3 merge_grid((unsigned)((cut.n_out + per_block - 1) / per_block));
+    if (share == 8) spkv_prefix_merge<D, 8><<<merge_grid, dim3(256), 0, s>>>(cut, merge, own, v.Hq, v.Hkv, own_out, own_lse, out, lse);
+    else if (share == 4) spkv_prefix_merge<D, 4><<<merge_grid, dim3(256), 0, s>>>(cut, merge, own, v.Hq, v.Hkv, own_out, own_lse, out, lse);
+    else if (share == 2) spkv_prefix_merge<D, 2><<<merge_grid, dim3(256), 0, s>>>(cut, merge, own, v.Hq, v.Hkv, own_out, own_lse, out, lse);
+    else spkv_prefix_merge<D, 1><<<merge_grid, dim3(256), 0, s>>>(cut, merge, own, v.Hq, v.Hkv, own_out, own_lse, out, lse);
     return hipGetLastError();
 }
 
 hipError_t spkv_launch_prefix(const SpkvView& v, const uint16_t* q, float sm_scale, int waves, const SpkvShareCut& cut,
-                              const SpkvShareRows& rows, const SpkvShareMerge& merge, const uint16_t* own_out,
-                              const float* own_lse, uint16_t* out, float* lse, hipStream_t s) {
+                              const SpkvShareTable& table, const SpkvShareRows& rows, const SpkvShareMerge& merge,
+                              const SpkvShareOwn& own, const uint16_t* own_out, const float* own_lse, uint16_t* out,
+                              float* lse, hipStream_t s) {
     const float sl = sm_scale * 1.4426950408889634f;
-    return v.D == 128 ? launch_prefix<128>(v, q, sl, waves, cut, rows, merge, own_out, own_lse, out, lse, s)
-                      : launch_prefix<64>(v, q, sl, waves, cut, rows, merge, own_out, own_lse, out, lse, s);
+    return v.D == 128 ? launch_prefix<128>(v, q, sl, waves, cut, table, rows, merge, own, own_out, own_lse, out, lse, s)
+                      : launch_prefix<64>(v, q, sl, waves, cut, table, rows, merge, own, own_out, own_lse, out, lse, s);
 }
 
 hipError_t spkv_launch_prefix_rows(const SpkvCu& cu, const SpkvShareActive& a, const int32_t* t_own, int n_seq,

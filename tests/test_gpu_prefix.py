@@ -166,13 +166,15 @@ def test_decode_of_uneven_prompts():
     s = Setup([3000, 0, 70, 431, 900, 1], [1 + 11 * b for b in range(16)], member, 8, 2, 128, keep=0.4, seed=3)
     q, out, lse = s.decode()
     alone, alone_lse = s.cache.decode_attention(q, want_lse=True)
+    out, lse = s.cache.prefix_attention(s.sharing, q, None, alone, alone_lse)
+    s.check(out, lse, s.reference(q, [1] * 16), "joined")
     for b in (2, 12, 14):                                # no prompt, an empty one: the sequence's own, bit for bit
         assert torch.equal(out[b], alone[b]) and torch.equal(lse[b], alone_lse[b])
     s.sharing[2] = s.member[2] = 4
     s.decode()
     s.sharing.prefix_of[:] = [-1] * 16
-    got = s.cache.decode_attention_shared(s.sharing, q)
-    assert torch.equal(got, s.cache.decode_attention(q))
+    s.member = [-1] * 16
+    s.decode()
 
 
 def test_decode_with_sinks_threshold_and_release():
@@ -185,8 +187,20 @@ def test_decode_with_sinks_threshold_and_release():
     s.decode()
 
 
+@pytest.mark.parametrize("own", [[3000, 1, 700], [2900, 2900, 2900]])
+def test_long_sequences_of_their_own(own):
+    """Longer than what rides in the prompts' launch."""
+    s = Setup([700, 300], own, [0, 1, 0], 8, 2, 64, keep=0.9)
+    s.decode()
+
+
+def test_more_sequences_than_travel_with_the_launch():
+    s = Setup([200, 90, 1], [1 + b % 37 for b in range(300)], [b % 3 for b in range(300)], 2, 1, 64)
+    s.decode()
+
+
 def test_many_small_prompts():
-    n = 70
+    n = 270
     s = Setup([1 + 9 * p for p in range(n)], [1 + p % 5 for p in range(n)], list(range(n))[::-1], 8, 2, 64, keep=0.5)
     s.decode()
 

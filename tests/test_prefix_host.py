@@ -122,15 +122,30 @@ def test_one_pass_over_the_lists_whatever_the_number_of_sequences():
                   ["decode", dict(member=[0] * batch)]]
         rc, launches = _run(dict(batch=1), dict(batch=batch), script)[-1]
         mine = [x for x in launches if "prefix" in x[0]]
-        assert rc == 0 and [n for n, _, _ in mine] == [f"spkv_prefix_split<128, {waves}>", "spkv_prefix_merge<128>"], launches
-        assert mine[0][2] == 64 * waves and mine[1][1] == batch * 32 // 8
+        assert rc == 0 and [n.split(",")[0] for n, _, _ in mine] == ["spkv_prefix_split<128", "spkv_prefix_merge<128"], launches
+        assert mine[0][0] == f"spkv_prefix_split<128, {waves}>" and mine[0][2] == 64 * waves
+        own_items = (batch * 8 * 1 + waves - 1) // waves             # (40 tokens or fewer: one item a list)
+        assert mine[0][1] - own_items <= 256 * (1 if waves == 8 else 2)
 
 
 def test_prompts_without_tokens_are_not_visited():
     script = [["append", dict(to="p", counts=[0, 500])], ["append", dict(to="c", counts=[5] * 3)]]
     got = _run(dict(batch=2), dict(batch=3), script + [["join", dict(member=[0, -1, 0])], ["join", dict(member=[0, 1, 0])]])
-    assert [n for n, _, _ in got[2][1]] == ["spkv_prefix_merge<128>"]
-    assert [n for n, _, _ in got[3][1]] == ["spkv_prefix_split<128, 1>", "spkv_prefix_merge<128>"]
+    assert [n.split(",")[0] for n, _, _ in got[2][1]] == ["spkv_prefix_merge<128"]
+    assert [n.split(",")[0] for n, _, _ in got[3][1]] == ["spkv_prefix_split<128", "spkv_prefix_merge<128"]
+
+
+def test_own_lists_ride_in_the_prompts_launch_while_they_are_short():
+    def launches(tokens, kept, options=()):
+        script = [["append", dict(to="p", counts=[9000])], ["lengths", dict(of="p", kept=[2000] * 8)],
+                  ["append", dict(to="c", counts=[tokens] * 2)], ["lengths", dict(of="c", kept=[kept] * 16)],
+                  ["decode", dict(member=[0, 0])]]
+        rc, got = _run(dict(batch=1), dict(batch=2), script)[-1]
+        assert rc == 0
+        return [n.split("<")[0] for n, _, _ in got if "copy" not in n]
+
+    assert launches(5000, 60 * 32) == ["spkv_prefix_split", "spkv_prefix_merge"]
+    assert launches(5000, 60 * 32 + 1) == ["spkv_decode_split", "spkv_decode_combine", "spkv_prefix_split", "spkv_prefix_merge"]
 
 
 if __name__ == "__main__":
