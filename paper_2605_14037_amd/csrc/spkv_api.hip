@@ -1685,7 +1685,7 @@ void share_prompts(const spkv_cache* pc, int batch, const int32_t* prefix_of, co
 // Ranges of the prompts' lists: about as many workgroups as the chip holds at once, every list cut evenly into its
 // share of them.
 constexpr int kShareMinUnit = 2;
-void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_bytes, int* waves, SpkvShareCut* cut,
+void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_bytes, int* groups, SpkvShareCut* cut,
                SpkvShareTable* table) {
     const int Hkv = c->cfg.n_kv_heads, G = c->carve.G, n = prompts.n, n_lists = n * Hkv;
     int64_t most = 0, all_rows = 0;
@@ -1693,8 +1693,8 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
         most = std::max<int64_t>(most, prompts.rows[a]);
         all_rows += prompts.rows[a];
     }
-    *waves = spkv_prefix_waves((int)std::min<int64_t>(most * G, 1 << 20));
-    const int64_t width = 32 * *waves;
+    *groups = spkv_prefix_groups((int)std::min<int64_t>(most * G, 1 << 20));
+    const int64_t width = 16 * *groups;
     auto blocks = [&](int a) -> int64_t { return ((int64_t)prompts.rows[a] * G + width - 1) / width; };
     auto half_pages = [&](int a, int h) -> int64_t {
         const int p = prompts.id[a], held = std::min(c->T[p], c->cfg.window);
@@ -1706,7 +1706,7 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
         for (int h = 0; h < Hkv; ++h) work += half_pages(a, h) * blocks(a);
     }
     const int cus = spkv_compute_units();
-    const int64_t target = (cus > 0 ? cus : 256) * (*waves == 8 ? 1 : 2);
+    const int64_t target = (cus > 0 ? cus : 256) * (*groups == 4 || *groups == 16 ? 1 : 2);
     int64_t unit = std::max<int64_t>(kShareMinUnit, (work + target - 1) / target);
     for (int guard = 0; guard < 64; ++guard) {
         int64_t total = 0;
@@ -1803,9 +1803,9 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
     const ShareCarve k = share_carve(total, Hq, c->cfg.head_dim);
     SpkvShareCut cut = {};
     SpkvShareTable table = {};
-    int waves = 1;
+    int groups = 1;
     cut.slots = 1;
-    if (prompts.n > 0) share_cut(pc, prompts, ws_bytes - k.part, &waves, &cut, &table);
+    if (prompts.n > 0) share_cut(pc, prompts, ws_bytes - k.part, &groups, &cut, &table);
     cut.part = reinterpret_cast<float*>(ws + k.part);
     cut.n_out = total * Hq;
     SpkvShareOwn own = {};
@@ -1842,7 +1842,7 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
         by_prompt.first_row = first;
         by_row.by_row = reinterpret_cast<const int2*>(back);
     }
-    return spkv_launch_prefix(pc->view, q, sm_scale, waves, cut, table, by_prompt, by_row, own, own_out, own_lse, out, lse,
+    return spkv_launch_prefix(pc->view, q, sm_scale, groups, cut, table, by_prompt, by_row, own, own_out, own_lse, out, lse,
                               s) == hipSuccess
                ? SPKV_OK
                : SPKV_E_HIP;

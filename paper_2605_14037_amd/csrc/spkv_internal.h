@@ -291,8 +291,8 @@ struct SpkvShareMerge {
 struct SpkvShareActive {
     int16_t active[SPKV_MAX_BATCH];       // per sequence
 };
-int spkv_prefix_waves(int n_cols);        // of a workgroup, for the prompt with the most columns
-hipError_t spkv_launch_prefix(const SpkvView& v, const uint16_t* q, float sm_scale, int waves, const SpkvShareCut& cut,
+int spkv_prefix_groups(int n_cols);       // of 16 columns of a workgroup, for the prompt with the most columns
+hipError_t spkv_launch_prefix(const SpkvView& v, const uint16_t* q, float sm_scale, int groups, const SpkvShareCut& cut,
                               const SpkvShareTable& table, const SpkvShareRows& rows, const SpkvShareMerge& merge,
                               const SpkvShareOwn& own, const uint16_t* own_out, const float* own_lse, uint16_t* out,
                               float* lse, hipStream_t s);

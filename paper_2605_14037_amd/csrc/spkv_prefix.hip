@@ -16,17 +16,125 @@
 // Bound: with few columns by the read of the lists (once, whatever the number of sequences); 4 D
 // flops per key and column stand against 4 D bytes per key, so past about 300 columns by the matrix units;
 // in between by what the ranges' results cost to write and read again, 4 (D + 2) bytes per column and range.
-//
-// spkv_prefix_split: a workgroup of NW waves takes 32 NW columns (32 a wave, one group of MFMA 32x32x16)
-// and a range of the list's half-pages, which it copies from memory straight into a ring of LDS
-// buffers, in operand order, so that every wave reads its operands as 1 KB in lane order.  The products
-// K Q^T of a half-page stand beside the weights of the one before.  Eight waves fetch two half-pages to
-// a step (as spkv_prefill_attend32, whose pipeline this is); with fewer waves a step is one half-page and
-// two workgroups share a compute unit.
+// Two kernels for the lists, by the columns of the prompt with the most rows:
+//   spkv_prefix_few    up to 64 columns: every wave has all of them and a part of the range to itself, operands straight
+//                      from memory to registers, the next half-page's loads out before this one's products
+//   spkv_prefix_split  more: a workgroup of NW waves has 32 NW columns (32 a wave, one group of MFMA 32x32x16) and
+//                      shares the range's half-pages through a ring of LDS buffers
 constexpr float kSumLimit = 2048.0f;         // a sum of 16 weights above it: the reference is too low
-constexpr int kRingGateTiles = 64;           // half-pages of the ring whose gates a wave looks up beforehand, one a lane
 
-__device__ __forceinline__ unsigned bits_upto8(int n) { return n <= 0 ? 0u : n >= 8 ? 0xffu : (1u << n) - 1u; }
+// Bits e = 0 .. 7 with e < n, with e >= n.
+__device__ __forceinline__ unsigned bits_below(int n) { return 0xffu >> (8 - min(max(n, 0), 8)); }
+__device__ __forceinline__ unsigned bits_from(int n) { return bits_below(n) ^ 0xffu; }
+
+// One prompt's list and ring for a workgroup: half-pages 0 .. nA - 1 are the list's, then those of the ring.
+struct ShareList {
+    int pair, T, L, held, nA, n_hp;
+    int slot0;                  // ring slot of age 0 (negative while the ring is not full)
+};
+__device__ __forceinline__ ShareList share_list(const SpkvView& v, int pair) {
+    ShareList s;
+    s.pair = pair;
+    s.T = v.t_pair[pair];
+    s.L = v.kept_len[pair];
+    s.held = min(s.T, v.w);
+    s.nA = (s.L + kHalfTokens - 1) >> 5;
+    s.n_hp = s.nA + ((s.held + kHalfTokens - 1) >> 5);
+    s.slot0 = s.T >= v.w ? s.T % v.w : s.T - v.w;
+    return s;
+}
+// Does the ring's slot hold a key that passes the gate?
+__device__ __forceinline__ bool ring_gate(const SpkvView& v, const ShareList& s, int at) {
+    const int age = at - s.slot0 + (at < s.slot0 ? v.w : 0);
+    return gate_passes(v, v.ring_logit[(size_t)s.pair * v.w + at], s.T - v.w + age);
+}
+// Keys at0 .. at0 + 7 of the ring that a token at `place` sees: gate on, or of an age above its place (a run of
+// slots from slot0 + place + 1 on, modulo w).
+__device__ __forceinline__ unsigned ring_seen(const SpkvView& v, const ShareList& s, unsigned gates, int at0, int place) {
+    const int from = s.slot0 + place + 1 - at0;
+    return (gates | bits_from(from) | (bits_from(from - v.w) & bits_below(s.slot0 - at0))) & bits_below(s.held - at0);
+}
+// Gates of a wave's ring half-pages, lane t those of half-page ring0 + t; loads four at a time.
+constexpr int kRingGateTiles = 64;
+struct RingGates {
+    int ring0;
+    unsigned mine;
+};
+__device__ __forceinline__ RingGates ring_gates(const SpkvView& v, const ShareList& s, int x_begin, int x_end) {
+    RingGates r = {max(x_begin - s.nA, 0), 0u};
+    const int lane = threadIdx.x & 63, n = min(x_end - s.nA - r.ring0, kRingGateTiles);
+    for (int t = 0; t < n; t += 8) {
+        bool on[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) on[u] = ring_gate(v, s, min((r.ring0 + t + 2 * u) * kHalfTokens + lane, s.held - 1));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const unsigned long long gates = __ballot(on[u]);
+            if (lane == t + 2 * u) r.mine = (unsigned)gates;
+            if (lane == t + 2 * u + 1) r.mine = (unsigned)(gates >> 32);
+        }
+    }
+    return r;
+}
+// Gates (bits 0 .. 7) of ring half-page t's keys k0 .. k0 + 7, t wave-uniform.
+__device__ __forceinline__ unsigned gates_of(const SpkvView& v, const ShareList& s, const RingGates& r, int t, int k0) {
+    if (t - r.ring0 < kRingGateTiles)
+        return ((unsigned)__builtin_amdgcn_readlane((int)r.mine, t - r.ring0) >> k0) & 0xffu;
+    unsigned g = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (ring_gate(v, s, min(t * kHalfTokens + k0 + e, s.held - 1))) g |= 1u << e;
+    return g;
+}
+// Page ids of a list, 64 at a time, one a lane.  The first 256 of the list are sent for before its length is known
+// (share_pages) and those from the range's begin on picked from them.
+struct SharePages {
+    const int32_t* pt;
+    int cap, at, ids;           // ids: of pages at .. at + 63
+};
+__device__ __forceinline__ int page_at(SharePages& p, int lp) {               // lp wave-uniform, never decreasing
+    if (lp >= p.at + 64) {
+        p.at = lp;
+        p.ids = p.pt[min(lp + ((int)threadIdx.x & 63), p.cap - 1)];
+        __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0)
+    }
+    return __builtin_amdgcn_readlane(p.ids, lp - p.at);
+}
+struct FirstPages {
+    int a, b, c, d;             // pages 0 .., 64 .., 128 .., 192 ..
+};
+__device__ __forceinline__ FirstPages first_pages(const SpkvView& v, int pair) {
+    const int32_t* pt = v.page_table + (size_t)pair * v.pt_cap;
+    const int lane = threadIdx.x & 63, end = v.pt_cap - 1;
+    return FirstPages{pt[min(lane, end)], pt[min(64 + lane, end)], pt[min(128 + lane, end)], pt[min(192 + lane, end)]};
+}
+__device__ __forceinline__ SharePages share_pages(const SpkvView& v, int pair, FirstPages f, int from) {
+    SharePages p = {v.page_table + (size_t)pair * v.pt_cap, v.pt_cap, from, 0};
+    const int lp = from + ((int)threadIdx.x & 63), block = from >> 6;        // pages lp lie in two blocks of 64
+    if (block >= 3) {
+        p.ids = p.pt[min(lp, p.cap - 1)];
+        return p;
+    }
+    const int x = block == 0 ? f.a : block == 1 ? f.b : f.c, y = block == 0 ? f.b : block == 1 ? f.c : f.d;
+    const int xs = __shfl(x, lp & 63), ys = __shfl(y, lp & 63);
+    p.ids = (lp >> 6) == block ? xs : ys;
+    return p;
+}
+__device__ __forceinline__ const uint16_t* half_page_at(const SpkvView& v, const ShareList& s, SharePages& p, int x) {
+    const int half = 2 * kHalfTokens * v.D;
+    if (x < s.nA) return pool_page(v, min(max(page_at(p, x >> 1), 0), v.n_pages - 1)) + (x & 1) * half;
+    return ring_page(v, s.pair, (x - s.nA) >> 1) + ((x - s.nA) & 1) * half;
+}
+// 16 bytes of V, eight consecutive keys: those whose bit is not set to zero -- no column sees them, and a weight of
+// zero would turn an infinity among them into a NaN.
+__device__ __forceinline__ bf16x8 keep_keys(bf16x8 x, unsigned seen) {
+    uint4 u = __builtin_bit_cast(uint4, x);
+    u.x &= (seen & 1u ? 0xffffu : 0u) | (seen & 2u ? 0xffff0000u : 0u);
+    u.y &= (seen & 4u ? 0xffffu : 0u) | (seen & 8u ? 0xffff0000u : 0u);
+    u.z &= (seen & 16u ? 0xffffu : 0u) | (seen & 32u ? 0xffff0000u : 0u);
+    u.w &= (seen & 64u ? 0xffffu : 0u) | (seen & 128u ? 0xffff0000u : 0u);
+    return __builtin_bit_cast(bf16x8, u);
+}
 
 // The sequences' cache as the helpers of spkv_device.h take it: its lists, the shape of the prompts' one.
 __device__ __forceinline__ SpkvView own_view(const SpkvShareOwn& o, const SpkvView& prompts) {
@@ -145,8 +253,190 @@ __device__ __forceinline__ ShareUnit find_unit(const SpkvShareCut& cut, const Sp
     return u;
 }
 
+// The query row of column c of an active prompt, its head in the group, and its token's place in the sequence
+// (looked for only where the ring is read).  Columns past the last one repeat the first and are never stored.
+struct ShareRow {
+    int row, head, place;
+};
+__device__ __forceinline__ int share_first(const SpkvShareRows& rows, int act) {
+    return rows.table != nullptr ? rows.first_row[act] : rows.first[act];
+}
+__device__ __forceinline__ ShareRow share_row(const SpkvShareRows& rows, int first, int c, int G, int n_kv_heads, bool ring) {
+    ShareRow r;
+    const int i = c / G;
+    r.head = c - i * G;
+    if (rows.table != nullptr) {
+        const int2 e = rows.table[first + i];
+        r.row = e.x;
+        r.place = e.y;
+    } else {
+        r.row = rows.seq[first + i];
+        r.place = ring ? rows.t_own[r.row * n_kv_heads] - 1 : 0;
+    }
+    return r;
+}
+
+// Up to 16 NQ columns.  Operands of a half-page are loaded as spkv_decode_split does, two half-pages in flight a
+// wave, each used for all NQ groups of 16 columns; weights in two bf16 parts (the read is what takes the time).  The
+// four waves take a quarter of the range each and meet in LDS.
+template <int D, int NQ>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 2 : 1, NQ == 1 ? 2 : 1)))
+void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvShareCut cut, SpkvShareTable table,
+                     SpkvShareRows rows, SpkvShareOwn own) {
+    constexpr int NS = D / 32, NB = D / 16, kRow = D + 4;
+    __shared__ __attribute__((aligned(16))) float s_acc[4][16 * NQ * kRow];
+    __shared__ float2 s_ml[4][16 * NQ];
+    __shared__ __attribute__((aligned(16))) uint16_t s_q[NQ == 1 ? 1 : NQ * NS][512];
+    const int tid = threadIdx.x, lane = tid & 63, kc = lane >> 4, n = lane & 15;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if ((int)blockIdx.x >= cut.n_units) {                    // behind the prompts': the sequences' own lists
+        own_item<D>(own_view(own, v), q, scale_log2e, own.split, own.part, ((int)blockIdx.x - cut.n_units) * 4 + wv);
+        return;
+    }
+    const ShareUnit u = find_unit(cut, table, blockIdx.x, v.Hkv);
+    const int act = u.list / v.Hkv, h = u.list - act * v.Hkv, j = u.range, ranges = u.ranges;
+    const int pair = (int)rows.prefix[act] * v.Hkv + h;
+    const FirstPages first_ids = first_pages(v, pair);
+    const ShareList list = share_list(v, pair);
+    const int first = share_first(rows, act), n_cols = (share_first(rows, act + 1) - first) * v.G;
+    if (n_cols <= 0) return;
+    const int nA = list.nA;
+    const int r_begin = (int)((int64_t)j * list.n_hp / ranges), r_end = (int)((int64_t)(j + 1) * list.n_hp / ranges);
+    const int x_begin = r_begin + (r_end - r_begin) * wv / 4, x_end = r_begin + (r_end - r_begin) * (wv + 1) / 4;
+
+    SharePages pages = share_pages(v, pair, first_ids, x_begin >> 1);
+    struct Tile {
+        bf16x8 k[2][NS], v[NB];
+    };
+    auto load = [&](Tile& t, int x) {
+        const uint16_t* kp = half_page_at(v, list, pages, x) + lane * 8;
+        const uint16_t* vp = kp + kHalfTokens * D;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) t.k[i][sl] = load_stream_b128(kp + (i * (D / 8) + sl * 4) * 128);
+#pragma unroll
+        for (int db = 0; db < NB; ++db) t.v[db] = load_stream_b128(vp + db * 512);
+    };
+    bf16x8 q1[NQ == 1 ? NS : 1];                             // the query operands of one group; of several they lie in LDS
+    int place[NQ], least = 0;
+    const bool ring = x_end > nA;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        const int c = i * 16 + n;
+        const ShareRow sr = share_row(rows, first, c < n_cols ? c : 0, v.G, v.Hkv, ring);
+        place[i] = sr.place;
+        const uint16_t* qrow = q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D + kc * 8;
+        if (NQ == 1) {
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) q1[NQ == 1 ? sl : 0] = *reinterpret_cast<const bf16x8*>(qrow + sl * 32);
+        } else if (i % 4 == wv % NQ) {                       // a wave's share of the groups (NQ = 2: two waves the same)
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl)
+                *reinterpret_cast<bf16x8*>(&s_q[NQ == 1 ? 0 : i * NS + sl][lane * 8]) = *reinterpret_cast<const bf16x8*>(qrow + sl * 32);
+        }
+    }
+    Tile t0, t1;
+    int x = x_begin;
+    if (x < x_end) load(t0, x);
+    if (NQ > 1) __syncthreads();
+    RingGates gates = {0, 0u};
+    if (ring) {
+        gates = ring_gates(v, list, x_begin, x_end);
+        least = place[0];
+#pragma unroll
+        for (int i = 1; i < NQ; ++i) least = min(least, place[i]);
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o));
+    }
+    f32x4 acc[NQ][NB];
+    float m[NQ], l[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        m[i] = SPKV_NEG_INF;
+        l[i] = 0.f;
+#pragma unroll
+        for (int db = 0; db < NB; ++db) acc[i][db] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    const int full = list.L >> 5;                            // half-pages that need no mask
+    auto attend = [&](Tile& t) {
+        unsigned ok[NQ];
+        const bool edge = x >= full;
+        if (edge) {
+            unsigned any;
+            if (x < nA) {
+                any = bits_below(list.L - x * kHalfTokens - kc * 8);
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) ok[i] = any;
+            } else {
+                const int at0 = (x - nA) * kHalfTokens + kc * 8;
+                const unsigned on = gates_of(v, list, gates, x - nA, kc * 8);
+                any = ring_seen(v, list, on, at0, least);
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) ok[i] = ring_seen(v, list, on, at0, place[i]);
+            }
+#pragma unroll
+            for (int db = 0; db < NB; ++db) t.v[db] = keep_keys(t.v[db], any);
+        }
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            bf16x8 qb[NS];
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl)
+                qb[sl] = NQ == 1 ? q1[NQ == 1 ? sl : 0] : *reinterpret_cast<const bf16x8*>(&s_q[NQ == 1 ? 0 : i * NS + sl][lane * 8]);
+            attend_half_page<D, true>(t.k, t.v, qb, ok[i] ^ 0xffu, edge, scale_log2e, acc[i], m[i], l[i]);
+        }
+        ++x;
+    };
+    while (x < x_end) {
+        if (x + 1 < x_end) load(t1, x + 1);
+        attend(t0);
+        if (x >= x_end) break;
+        if (x + 1 < x_end) load(t0, x + 1);
+        attend(t1);
+    }
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        l[i] += __shfl_xor(l[i], 16);
+        l[i] += __shfl_xor(l[i], 32);
+        float* pa = s_acc[wv] + (i * 16 + n) * kRow + kc * 4;
+#pragma unroll
+        for (int db = 0; db < NB; ++db) *reinterpret_cast<f32x4*>(pa + db * 16) = acc[i][db];
+        if (kc == 0) s_ml[wv][i * 16 + n] = make_float2(m[i], l[i]);
+    }
+    __syncthreads();
+    const size_t pc0 = ((size_t)h * cut.slots + j) * cut.n_cols + (size_t)first * v.G;
+    float2* part_ml = reinterpret_cast<float2*>(cut.part + (size_t)v.Hkv * cut.slots * cut.n_cols * D);
+    for (int e = tid; e < n_cols * (D / 4); e += 256) {
+        const int c = e / (D / 4), d = (e - c * (D / 4)) * 4;
+        float2 ml[4];
+        float M = SPKV_NEG_INF;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            ml[w] = s_ml[w][c];
+            M = fmaxf(M, ml[w].x);
+        }
+        const float m_ref = M == SPKV_NEG_INF ? 0.f : M;     // no key at all: every weight 0
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float sc = __builtin_amdgcn_exp2f(ml[w].x - m_ref);
+            a += *reinterpret_cast<const f32x4*>(s_acc[w] + c * kRow + d) * sc;
+            sum += ml[w].y * sc;
+        }
+        *reinterpret_cast<f32x4*>(cut.part + (pc0 + c) * D + d) = a;
+        if (d == 0) part_ml[pc0 + c] = make_float2(M, sum);
+    }
+}
+
+// More columns: the copies of the range's half-pages go from memory straight into LDS, in operand order, so that
+// every wave reads its operands as 1 KB in lane order.  The products K Q^T of a half-page stand beside the
+// weights of the one before.  Eight waves fetch two half-pages to a step (as spkv_prefill_attend32, whose
+// pipeline this is); with four waves a step is one half-page and two workgroups share a compute unit.
+
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW >= 4 ? 2 : 1, NW >= 4 ? 2 : 1)))
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvShareCut cut, SpkvShareTable table,
                        SpkvShareRows rows, SpkvShareOwn own) {
     constexpr int NS = D / 16, NB = D / 32;
@@ -162,83 +452,42 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     }
     const ShareUnit u = find_unit(cut, table, blockIdx.x, v.Hkv);
     const int act = u.list / v.Hkv, h = u.list - act * v.Hkv, j = u.range, ranges = u.ranges;
-    const int first = rows.table != nullptr ? rows.first_row[act] : rows.first[act];
-    const int n_cols = ((rows.table != nullptr ? rows.first_row[act + 1] : rows.first[act + 1]) - first) * v.G;
+    const int pair = (int)rows.prefix[act] * v.Hkv + h;
+    const FirstPages first_ids = first_pages(v, pair);
+    const ShareList list = share_list(v, pair);
+    const int first = share_first(rows, act), n_cols = (share_first(rows, act + 1) - first) * v.G;
     const int col0 = u.block * (32 * NW);
     if (col0 >= n_cols) return;
-    const int pair = (int)rows.prefix[act] * v.Hkv + h;
-    const int T = v.t_pair[pair], L = v.kept_len[pair], held = min(T, v.w);
-    const int nA = (L + kHalfTokens - 1) >> 5, n_hp = nA + ((held + kHalfTokens - 1) >> 5);
-    const int x_begin = (int)((int64_t)j * n_hp / ranges), x_end = (int)((int64_t)(j + 1) * n_hp / ranges), last = x_end - 1;
+    const int nA = list.nA;
+    const int x_begin = (int)((int64_t)j * list.n_hp / ranges), x_end = (int)((int64_t)(j + 1) * list.n_hp / ranges), last = x_end - 1;
 
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
-    const int wv = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = col0 + wv * 32 + col;
     const bool valid = c < n_cols;
-    const int in_group = valid ? c / v.G : 0, g_head = valid ? c - in_group * v.G : 0;
-    int row, place;                                          // this column's query row and its token's place
-    if (rows.table != nullptr) {
-        const int2 e = rows.table[first + in_group];
-        row = e.x;
-        place = e.y;
-    } else {
-        row = rows.seq[first + in_group];
-        place = rows.t_own[row * v.Hkv] - 1;
-    }
     const size_t pc = ((size_t)h * cut.slots + j) * cut.n_cols + (size_t)first * v.G + c;      // of the partial result
     float2* part_ml = reinterpret_cast<float2*>(cut.part + (size_t)v.Hkv * cut.slots * cut.n_cols * D);
     if (x_begin >= x_end) {                                  // fewer half-pages than ranges
         if (valid && half == 0) part_ml[pc] = make_float2(SPKV_NEG_INF, 0.f);
         return;
     }
-    // page ids of 64 logical pages, one a lane
-    const int32_t* pt = v.page_table + (size_t)pair * v.pt_cap;
-    int page_lane0 = x_begin >> 1, my_page = pt[min(page_lane0 + lane, v.pt_cap - 1)];
-    auto page_of = [&](int lp) -> int {                      // lp wave-uniform, never decreasing
-        if (lp >= page_lane0 + 64) {
-            page_lane0 = lp;
-            my_page = pt[min(lp + lane, v.pt_cap - 1)];
-            __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0)
-        }
-        return __builtin_amdgcn_readlane(my_page, lp - page_lane0);
-    };
-    auto base_of = [&](int x) -> const uint16_t* {
-        x = min(x, last);
-        if (x < nA) {
-            const int page = min(max(page_of(x >> 1), 0), v.n_pages - 1);
-            return pool_page(v, page) + (x & 1) * kHalfElems;
-        }
-        return ring_page(v, pair, (x - nA) >> 1) + ((x - nA) & 1) * kHalfElems;
-    };
+    const ShareRow sr = share_row(rows, first, valid ? c : 0, v.G, v.Hkv, x_end > nA);
+    SharePages pages = share_pages(v, pair, first_ids, x_begin >> 1);
     bf16x8 qb[NS];
     {
-        const uint16_t* qrow = q + ((size_t)row * v.Hq + (size_t)h * v.G + g_head) * D + half * 8;
+        const uint16_t* qrow = q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D + half * 8;
 #pragma unroll
-        for (int sl = 0; sl < NS; ++sl) {
-            uint4 raw = {0u, 0u, 0u, 0u};
-            if (valid) raw = *reinterpret_cast<const uint4*>(qrow + sl * 16);
-            qb[sl] = __builtin_bit_cast(bf16x8, raw);
-        }
+        for (int sl = 0; sl < NS; ++sl) qb[sl] = *reinterpret_cast<const bf16x8*>(qrow + sl * 16);
     }
-    // ring: age of a slot's key, 0 = position T - w; does it pass the gate?
-    const int slot0 = T >= v.w ? T % v.w : T - v.w;
-    auto age_of = [&](int at) -> int { return at - slot0 + (at < slot0 ? v.w : 0); };
-    auto ring_gate = [&](int at) -> bool {
-        return gate_passes(v, v.ring_logit[(size_t)pair * v.w + at], T - v.w + age_of(at));
-    };
-    const int ring0 = max(x_begin - nA, 0);                  // this workgroup's first ring half-page
-    unsigned my_gate = 0u;                                   // lane t: the gates of ring half-page ring0 + t
-    for (int t = 0; t < min(x_end - nA - ring0, kRingGateTiles); t += 8) {                // two half-pages a load
-        bool on[4];
+    RingGates gates = {0, 0u};
+    int least = 0;                                           // the smallest place of the wave's columns: it sees most of the ring
+    if (x_end > nA) {
+        gates = ring_gates(v, list, x_begin, x_end);
+        least = sr.place;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) on[u] = ring_gate(min((ring0 + t + 2 * u) * kHalfTokens + lane, held - 1));
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const unsigned long long gates = __ballot(on[u]);
-            if (lane == t + 2 * u) my_gate = (unsigned)gates;
-            if (lane == t + 2 * u + 1) my_gate = (unsigned)(gates >> 32);
-        }
+        for (int o = 1; o < 32; o <<= 1) least = min(least, __shfl_xor(least, o));
     }
+    auto base_of = [&](int x) -> const uint16_t* { return half_page_at(v, list, pages, min(x, last)); };
 
     // A half-page's rows in LDS: K row sl holds, for lane (half, r), d = 16 sl + 8 half .. of key 16 (r >> 4) +
     // 8 ((r >> 2) & 1) + 4 ((r >> 3) & 1) + (r & 3) -- the score of row r of an MFMA then comes out in the
@@ -252,8 +501,8 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
         const unsigned dst = lds0 + (unsigned)slot * (kHalfElems * 2);
 #pragma unroll
         for (int i = 0; i < kRowsPerWave; ++i) {
-            const int row_id = NW == 1 ? i : wq * kRowsPerWave + i;
-            const bool is_k = NW == 1 ? i < NS : wq * kRowsPerWave < NS;
+            const int row_id = wq * kRowsPerWave + i;
+            const bool is_k = wq * kRowsPerWave < NS;
             const int vr = row_id - NS, off = is_k ? row_id * 512 : (vr / NB) * 512 + (vr % NB) * 2048;
             load_row_to_lds(reinterpret_cast<const char*>(base) + off, is_k ? k_lane : v_lane, dst + row_id * 1024);
         }
@@ -263,12 +512,16 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
         else stage_half_page_rows(base_of(x_begin + k), slot);
     };
 
+    // The tiles of the first steps travel with the queries.  Step s + kAhead is sent off in step s.
+    constexpr int kAhead = NW == 8 ? 3 : 4;
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) stage_step(s * kHps, s * kHps);
     f32x16 acc[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
-    float m = valid ? SPKV_NEG_INF : 0.f, l = 0.f;
+    float m = SPKV_NEG_INF, l = 0.f;
     bf16x8 kf[NS];                                           // K operands of the half-page after the current one
     auto load_k = [&](const uint16_t* hp) {
 #pragma unroll
@@ -289,36 +542,23 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const int k0 = 16 * g + 8 * half;
-            unsigned ok;
+            unsigned ok, any;
             if (x < nA) {
-                ok = bits_upto8(L - x * kHalfTokens - k0);
+                ok = any = bits_below(list.L - x * kHalfTokens - k0);
             } else {
-                const int at0 = (x - nA) * kHalfTokens + k0, t = x - nA - ring0;
-                ok = 0u;
-                if (t < kRingGateTiles) {
-                    ok = ((unsigned)__builtin_amdgcn_readlane((int)my_gate, t) >> k0) & 0xffu;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (ring_gate(min(at0 + e, held - 1))) ok |= 1u << e;
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (age_of(at0 + e) > place) ok |= 1u << e;
-                ok &= bits_upto8(held - at0);
+                const unsigned on = gates_of(v, list, gates, x - nA, k0);
+                ok = ring_seen(v, list, on, (x - nA) * kHalfTokens + k0, sr.place);
+                any = ring_seen(v, list, on, (x - nA) * kHalfTokens + k0, least);
             }
-            if (!valid) ok = 0u;
-            seen |= ok << (8 * g);
+            seen |= any << (8 * g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[8 * g + e] = ((ok >> e) & 1u) ? s[8 * g + e] : SPKV_NEG_INF;
         }
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) seen |= __shfl_xor(seen, o);
         return seen;
     };
     // weights against the column's reference as it stands; true (wave-uniform) if one is too low or not set
     bf16x8 pb[2];
-    float psum, neg_ref = valid ? 0.f : -m, limit = valid ? -1.f : kSumLimit;
+    float psum, neg_ref = 0.f, limit = -1.f;
     auto weights = [&](const f32x16& s) -> bool {
         f32x8 p[2];
 #pragma unroll
@@ -361,27 +601,9 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
         for (int db = 0; db < NB; ++db)
             acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[g][db], pb[g], acc[db], 0, 0, 0);
     };
-    // values of keys that no column sees to zero: a weight of zero would turn an infinity among them into a NaN
-    auto clear_v = [&](int g, unsigned seen) {
-        unsigned keep[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned two = seen >> (8 * g + 2 * i);
-            keep[i] = (two & 1u ? 0xffffu : 0u) | (two & 2u ? 0xffff0000u : 0u);
-        }
-#pragma unroll
-        for (int db = 0; db < NB; ++db) {
-            uint4 u = __builtin_bit_cast(uint4, va[g][db]);
-            u.x &= keep[0];
-            u.y &= keep[1];
-            u.z &= keep[2];
-            u.w &= keep[3];
-            va[g][db] = __builtin_bit_cast(bf16x8, u);
-        }
-    };
     // One half-page: its scores are in sc and its first V operands in va[0]; the scores of the next one (hp1)
     // go to sn from kf, which then holds the K operands of hp2.
-    const int full = L >> 5;                                 // half-pages that need no mask
+    const int full = list.L >> 5;                                 // half-pages that need no mask
     auto process = [&](f32x16& sc, f32x16& sn, int x, const uint16_t* hp, const uint16_t* hp1, const uint16_t* hp2,
                        auto&& more) {
         const bool edge = x >= full;
@@ -396,8 +618,11 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
         load_k(hp2);
         __builtin_amdgcn_sched_barrier(0);
         if (edge) {
-            clear_v(0, seen);
-            clear_v(1, seen);
+#pragma unroll
+            for (int db = 0; db < NB; ++db) {
+                va[0][db] = keep_keys(va[0][db], seen);
+                va[1][db] = keep_keys(va[1][db], seen >> 8);
+            }
         }
         l += psum;
         accumulate(0);
@@ -409,13 +634,8 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     };
 
     const int n = x_end - x_begin;
-    __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): queries, page ids, gates
+    __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): queries, gates, the first tiles
     asm volatile("" : : "s"(scale_log2e));
-    // steps 0 .. kAhead - 1 are on their way before the loop; step s + kAhead is sent off in step s
-    constexpr int kAhead = NW == 8 ? 3 : 4;
-#pragma unroll
-    for (int s = 0; s < kAhead; ++s) stage_step(s * kHps, s * kHps);
-    wait_loads_but<kRowsPerWave>();
     __syncthreads();
     f32x16 s0, s1;
     load_k(s_tile[0]);
@@ -451,15 +671,25 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     wait_loads_but<0>();
 
     l += __shfl_xor(l, 32);
-    if (!valid) return;
-    float* pa = cut.part + pc * D + half * 4;
+    if (valid && half == 0) part_ml[pc] = make_float2(m, l);
+    // The sums leave through LDS, a column's row at a time (straight from the registers every store touched 32 rows,
+    // 32 bytes each).  16-byte unit x of column col lies at x ^ col: no bank conflicts either way.
+    __syncthreads();                                         // the tiles are no longer read
+    float* sums = reinterpret_cast<float*>(&s_tile[0][0]) + wv * 32 * D;
 #pragma unroll
     for (int db = 0; db < NB; ++db)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-            *reinterpret_cast<f32x4*>(pa + db * 32 + g * 8) =
+            *reinterpret_cast<f32x4*>(sums + col * D + ((db * 8 + g * 2 + half) ^ (col & (D / 4 - 1))) * 4) =
                 (f32x4){acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]};
-    if (half == 0) part_ml[pc] = make_float2(m, l);
+    __builtin_amdgcn_wave_barrier();
+    constexpr int kUnits = D / 4, kColsPerPass = 64 / kUnits;
+    const int unit = lane % kUnits, n_here = min(32, n_cols - (col0 + wv * 32));
+    float* to = cut.part + (((size_t)h * cut.slots + j) * cut.n_cols + (size_t)first * v.G + col0 + wv * 32) * D;
+#pragma unroll 4
+    for (int i = lane / kUnits; i < n_here; i += kColsPerPass)
+        *reinterpret_cast<f32x4*>(to + (size_t)i * D + unit * 4) =
+            *reinterpret_cast<const f32x4*>(sums + i * D + (unit ^ (i & (D / 4 - 1))) * 4);
 }
 
 // The join: D / 4 threads own a column (row, head), four consecutive elements each; S such groups share a column,
@@ -616,20 +846,21 @@ __global__ __launch_bounds__(256) void spkv_prefix_rows(SpkvCu cu, SpkvShareActi
         }
 }
 
-int spkv_prefix_waves(int n_cols) { return n_cols <= 32 ? 1 : n_cols <= 64 ? 2 : n_cols <= 128 ? 4 : 8; }
+int spkv_prefix_groups(int n_cols) { return n_cols <= 16 ? 1 : n_cols <= 32 ? 2 : n_cols <= 64 ? 4 : n_cols <= 128 ? 8 : 16; }
 
 template <int D>
-static hipError_t launch_prefix(const SpkvView& v, const uint16_t* q, float sl, int waves, const SpkvShareCut& cut,
+static hipError_t launch_prefix(const SpkvView& v, const uint16_t* q, float sl, int groups, const SpkvShareCut& cut,
                                 const SpkvShareTable& table, const SpkvShareRows& rows, const SpkvShareMerge& merge,
                                 const SpkvShareOwn& own, const uint16_t* own_out, const float* own_lse, uint16_t* out,
                                 float* lse, hipStream_t s) {
-    const int items = own.part != nullptr ? own.n_pairs * own.split.slots : 0;
-    const dim3 grid((unsigned)(cut.n_units + (items + waves - 1) / waves));
+    const int items = own.part != nullptr ? own.n_pairs * own.split.slots : 0, waves = groups == 16 ? 8 : 4;
+    const dim3 grid((unsigned)(cut.n_units + (items + waves - 1) / waves)), block(64 * waves);
     if (grid.x > 0) {
-        if (waves == 8) spkv_prefix_split<D, 8><<<grid, dim3(512), 0, s>>>(v, q, sl, cut, table, rows, own);
-        else if (waves == 4) spkv_prefix_split<D, 4><<<grid, dim3(256), 0, s>>>(v, q, sl, cut, table, rows, own);
-        else if (waves == 2) spkv_prefix_split<D, 2><<<grid, dim3(128), 0, s>>>(v, q, sl, cut, table, rows, own);
-        else spkv_prefix_split<D, 1><<<grid, dim3(64), 0, s>>>(v, q, sl, cut, table, rows, own);
+        if (groups == 16) spkv_prefix_split<D, 8><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
+        else if (groups == 8) spkv_prefix_split<D, 4><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
+        else if (groups == 4) spkv_prefix_few<D, 4><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
+        else if (groups == 2) spkv_prefix_few<D, 2><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
+        else spkv_prefix_few<D, 1><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
     }
     // groups to a column: about eight workgroups per compute unit, no more groups than there are ranges
     constexpr int CPB = 256 / (D / 4);
@@ -644,13 +875,13 @@ static hipError_t launch_prefix(const SpkvView& v, const uint16_t* q, float sl, 
     return hipGetLastError();
 }
 
-hipError_t spkv_launch_prefix(const SpkvView& v, const uint16_t* q, float sm_scale, int waves, const SpkvShareCut& cut,
+hipError_t spkv_launch_prefix(const SpkvView& v, const uint16_t* q, float sm_scale, int groups, const SpkvShareCut& cut,
                               const SpkvShareTable& table, const SpkvShareRows& rows, const SpkvShareMerge& merge,
                               const SpkvShareOwn& own, const uint16_t* own_out, const float* own_lse, uint16_t* out,
                               float* lse, hipStream_t s) {
     const float sl = sm_scale * 1.4426950408889634f;
-    return v.D == 128 ? launch_prefix<128>(v, q, sl, waves, cut, table, rows, merge, own, own_out, own_lse, out, lse, s)
-                      : launch_prefix<64>(v, q, sl, waves, cut, table, rows, merge, own, own_out, own_lse, out, lse, s);
+    return v.D == 128 ? launch_prefix<128>(v, q, sl, groups, cut, table, rows, merge, own, own_out, own_lse, out, lse, s)
+                      : launch_prefix<64>(v, q, sl, groups, cut, table, rows, merge, own, own_out, own_lse, out, lse, s);
 }
 
 hipError_t spkv_launch_prefix_rows(const SpkvCu& cu, const SpkvShareActive& a, const int32_t* t_own, int n_seq,

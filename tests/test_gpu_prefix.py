@@ -160,6 +160,15 @@ def test_decode_columns(batch, hq, hk, d):
     s.decode()
 
 
+@pytest.mark.parametrize("batch", [1, 3, 6, 12, 40])
+def test_long_lists_and_wide_windows(batch):
+    """More pages than are sent for beforehand (256), and more of the ring than a wave keeps the gates of."""
+    s = Setup([24000], [1 + 5 * b for b in range(batch)], [0] * batch, 8, 2, 64, keep=0.95, seed=batch)
+    s.decode()
+    s = Setup([6000], [1 + 500 * b for b in range(batch)], [0] * batch, 8, 2, 64, keep=0.3, window=5000, seed=batch, extra=20000)
+    s.decode()
+
+
 def test_decode_of_uneven_prompts():
     """Prompts of unlike lengths and numbers of sequences, some empty, some that nobody continues, none."""
     member = [3, 0, -1, 0, 0, 5, 3, 0, 2, 0, 0, 0, 1, 0, -1, 0]

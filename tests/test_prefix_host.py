@@ -116,23 +116,26 @@ def test_empty_sequences_and_empty_calls():
 
 def test_one_pass_over_the_lists_whatever_the_number_of_sequences():
     """A split and a merge launch; a workgroup as wide as the columns ask; no more workgroups than the chip holds."""
-    for batch, waves in ((1, 1), (8, 1), (9, 2), (16, 2), (17, 4), (32, 4), (33, 8), (64, 8), (200, 8)):
+    few, split = "spkv_prefix_few<128, {}>", "spkv_prefix_split<128, {}>"
+    for batch, name, waves in ((1, few.format(1), 4), (4, few.format(1), 4), (5, few.format(2), 4), (8, few.format(2), 4),
+                               (9, few.format(4), 4), (16, few.format(4), 4), (17, split.format(4), 4),
+                               (32, split.format(4), 4), (33, split.format(8), 8), (64, split.format(8), 8), (200, split.format(8), 8)):
         script = [["append", dict(to="p", counts=[60000])], ["lengths", dict(of="p", kept=[20000, 4000] * 4)],
                   ["append", dict(to="c", counts=[5] * batch)], ["lengths", dict(of="c", kept=[0] * 8 * batch)],
                   ["decode", dict(member=[0] * batch)]]
         rc, launches = _run(dict(batch=1), dict(batch=batch), script)[-1]
         mine = [x for x in launches if "prefix" in x[0]]
-        assert rc == 0 and [n.split(",")[0] for n, _, _ in mine] == ["spkv_prefix_split<128", "spkv_prefix_merge<128"], launches
-        assert mine[0][0] == f"spkv_prefix_split<128, {waves}>" and mine[0][2] == 64 * waves
+        assert rc == 0 and len(mine) == 2 and mine[1][0].startswith("spkv_prefix_merge<128"), launches
+        assert mine[0][0] == name and mine[0][2] == 64 * waves
         own_items = (batch * 8 * 1 + waves - 1) // waves             # (40 tokens or fewer: one item a list)
-        assert mine[0][1] - own_items <= 256 * (1 if waves == 8 else 2)
+        assert mine[0][1] - own_items <= 512
 
 
 def test_prompts_without_tokens_are_not_visited():
     script = [["append", dict(to="p", counts=[0, 500])], ["append", dict(to="c", counts=[5] * 3)]]
     got = _run(dict(batch=2), dict(batch=3), script + [["join", dict(member=[0, -1, 0])], ["join", dict(member=[0, 1, 0])]])
     assert [n.split(",")[0] for n, _, _ in got[2][1]] == ["spkv_prefix_merge<128"]
-    assert [n.split(",")[0] for n, _, _ in got[3][1]] == ["spkv_prefix_split<128", "spkv_prefix_merge<128"]
+    assert [n.split(",")[0] for n, _, _ in got[3][1]] == ["spkv_prefix_few<128", "spkv_prefix_merge<128"]
 
 
 def test_own_lists_ride_in_the_prompts_launch_while_they_are_short():
@@ -144,8 +147,8 @@ def test_own_lists_ride_in_the_prompts_launch_while_they_are_short():
         assert rc == 0
         return [n.split("<")[0] for n, _, _ in got if "copy" not in n]
 
-    assert launches(5000, 60 * 32) == ["spkv_prefix_split", "spkv_prefix_merge"]
-    assert launches(5000, 60 * 32 + 1) == ["spkv_decode_split", "spkv_decode_combine", "spkv_prefix_split", "spkv_prefix_merge"]
+    assert launches(5000, 60 * 32) == ["spkv_prefix_few", "spkv_prefix_merge"]
+    assert launches(5000, 60 * 32 + 1) == ["spkv_decode_split", "spkv_decode_combine", "spkv_prefix_few", "spkv_prefix_merge"]
 
 
 if __name__ == "__main__":
