@@ -1706,7 +1706,7 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
         for (int h = 0; h < Hkv; ++h) work += half_pages(a, h) * blocks(a);
     }
     const int cus = spkv_compute_units();
-    const int64_t target = (cus > 0 ? cus : 256) * (*groups == 4 || *groups == 16 ? 1 : 2);
+    const int64_t target = cus > 0 ? cus : 256;
     int64_t unit = std::max<int64_t>(kShareMinUnit, (work + target - 1) / target);
     for (int guard = 0; guard < 64; ++guard) {
         int64_t total = 0;

@@ -17,7 +17,7 @@
 // flops per key and column stand against 4 D bytes per key, so past about 300 columns by the matrix units;
 // in between by what the ranges' results cost to write and read again, 4 (D + 2) bytes per column and range.
 // Two kernels for the lists, by the columns of the prompt with the most rows:
-//   spkv_prefix_few    up to 64 columns: every wave has all of them and a part of the range to itself, operands straight
+//   spkv_prefix_few    up to 32 columns: every wave has all of them and a part of the range to itself, operands straight
 //                      from memory to registers, the next half-page's loads out before this one's products
 //   spkv_prefix_split  more: a workgroup of NW waves has 32 NW columns (32 a wave, one group of MFMA 32x32x16) and
 //                      shares the range's half-pages through a ring of LDS buffers
@@ -276,11 +276,15 @@ __device__ __forceinline__ ShareRow share_row(const SpkvShareRows& rows, int fir
     return r;
 }
 
-// Up to 16 NQ columns.  Operands of a half-page are loaded as spkv_decode_split does, two half-pages in flight a
-// wave, each used for all NQ groups of 16 columns; weights in two bf16 parts (the read is what takes the time).  The
-// four waves take a quarter of the range each and meet in LDS.
+// Up to 16 NQ columns.  A half-page's operands come straight from memory (1 KB a load, as in spkv_decode_split) and are
+// used for all NQ groups of 16 columns: scores of all groups -- the next half-page's keys are sent for -- then
+// weights against the references as they stand -- raised, and sums and accumulators rescaled, only where some lane's
+// eight weights add up to more than kSumLimit -- then the products with V, the weights as two bf16 parts (16 bits: the
+// lists' read takes the time, not these products) -- and the next values are sent for.  One body for every half-page:
+// two of them in turn on two sets of operands were slower where a wave has only a few (cold instructions).  The four
+// waves take a quarter of the range each and meet in LDS.
 template <int D, int NQ>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NQ == 1 ? 2 : 1, NQ == 1 ? 2 : 1)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, NQ == 1 ? 3 : 2)))
 void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvShareCut cut, SpkvShareTable table,
                      SpkvShareRows rows, SpkvShareOwn own) {
     constexpr int NS = D / 32, NB = D / 16, kRow = D + 4;
@@ -305,18 +309,16 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
     const int x_begin = r_begin + (r_end - r_begin) * wv / 4, x_end = r_begin + (r_end - r_begin) * (wv + 1) / 4;
 
     SharePages pages = share_pages(v, pair, first_ids, x_begin >> 1);
-    struct Tile {
-        bf16x8 k[2][NS], v[NB];
-    };
-    auto load = [&](Tile& t, int x) {
-        const uint16_t* kp = half_page_at(v, list, pages, x) + lane * 8;
-        const uint16_t* vp = kp + kHalfTokens * D;
+    bf16x8 k[2][NS], va[NB];
+    auto load_k = [&](const uint16_t* page) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int sl = 0; sl < NS; ++sl) t.k[i][sl] = load_stream_b128(kp + (i * (D / 8) + sl * 4) * 128);
+            for (int sl = 0; sl < NS; ++sl) k[i][sl] = load_stream_b128(page + lane * 8 + (i * (D / 8) + sl * 4) * 128);
+    };
+    auto load_v = [&](const uint16_t* page) {
 #pragma unroll
-        for (int db = 0; db < NB; ++db) t.v[db] = load_stream_b128(vp + db * 512);
+        for (int db = 0; db < NB; ++db) va[db] = load_stream_b128(page + kHalfTokens * D + lane * 8 + db * 512);
     };
     bf16x8 q1[NQ == 1 ? NS : 1];                             // the query operands of one group; of several they lie in LDS
     int place[NQ], least = 0;
@@ -336,9 +338,11 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
                 *reinterpret_cast<bf16x8*>(&s_q[NQ == 1 ? 0 : i * NS + sl][lane * 8]) = *reinterpret_cast<const bf16x8*>(qrow + sl * 32);
         }
     }
-    Tile t0, t1;
-    int x = x_begin;
-    if (x < x_end) load(t0, x);
+    if (x_begin < x_end) {
+        const uint16_t* page = half_page_at(v, list, pages, x_begin);
+        load_k(page);
+        load_v(page);
+    }
     if (NQ > 1) __syncthreads();
     RingGates gates = {0, 0u};
     if (ring) {
@@ -359,41 +363,87 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
         for (int db = 0; db < NB; ++db) acc[i][db] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     const int full = list.L >> 5;                            // half-pages that need no mask
-    auto attend = [&](Tile& t) {
-        unsigned ok[NQ];
-        const bool edge = x >= full;
-        if (edge) {
-            unsigned any;
-            if (x < nA) {
-                any = bits_below(list.L - x * kHalfTokens - kc * 8);
+#pragma unroll 1
+    for (int x = x_begin; x < x_end; ++x) {
+        const bool more = x + 1 < x_end;
+        const uint16_t* next = more ? half_page_at(v, list, pages, x + 1) : nullptr;
+        f32x8 s[NQ];
 #pragma unroll
-                for (int i = 0; i < NQ; ++i) ok[i] = any;
-            } else {
-                const int at0 = (x - nA) * kHalfTokens + kc * 8;
-                const unsigned on = gates_of(v, list, gates, x - nA, kc * 8);
-                any = ring_seen(v, list, on, at0, least);
+        for (int i = 0; i < NQ; ++i) {
+            f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < NQ; ++i) ok[i] = ring_seen(v, list, on, at0, place[i]);
+            for (int sl = 0; sl < NS; ++sl) {
+                const bf16x8 qb = NQ == 1 ? q1[NQ == 1 ? sl : 0]
+                                          : *reinterpret_cast<const bf16x8*>(&s_q[NQ == 1 ? 0 : i * NS + sl][lane * 8]);
+                s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[0][sl], qb, s0, 0, 0, 0);
+                s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[1][sl], qb, s1, 0, 0, 0);
             }
 #pragma unroll
-            for (int db = 0; db < NB; ++db) t.v[db] = keep_keys(t.v[db], any);
+            for (int e = 0; e < 4; ++e) {
+                s[i][e] = s0[e];
+                s[i][4 + e] = s1[e];
+            }
+        }
+        if (more) load_k(next);
+        if (x >= full) {
+            unsigned any, on = 0u;
+            const int at0 = (x - nA) * kHalfTokens + kc * 8;
+            if (x < nA) any = bits_below(list.L - x * kHalfTokens - kc * 8);
+            else any = ring_seen(v, list, on = gates_of(v, list, gates, x - nA, kc * 8), at0, least);
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                const unsigned ok = x < nA ? any : ring_seen(v, list, on, at0, place[i]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[i][e] = ((ok >> e) & 1u) ? s[i][e] : SPKV_NEG_INF;
+            }
+#pragma unroll
+            for (int db = 0; db < NB; ++db) va[db] = keep_keys(va[db], any);
+        }
+        f32x8 p[NQ];
+        float psum[NQ];
+        auto weights = [&]() -> bool {
+            bool low = false;
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                const bool unset = m[i] == SPKV_NEG_INF;
+                const float neg_ref = unset ? 0.f : -m[i];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) p[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], scale_log2e, neg_ref));
+                psum[i] = ((p[i][0] + p[i][1]) + (p[i][2] + p[i][3])) + ((p[i][4] + p[i][5]) + (p[i][6] + p[i][7]));
+                low = low || unset || !(psum[i] <= kSumLimit);
+            }
+            return __ballot(low) != 0ull;
+        };
+#pragma unroll 1
+        for (bool again = true; weights() && again; again = false) {
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                float cm = fmaxf(fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3])),
+                                 fmaxf(fmaxf(s[i][4], s[i][5]), fmaxf(s[i][6], s[i][7]))) * scale_log2e;
+                cm = fmaxf(cm, __shfl_xor(cm, 16));
+                cm = fmaxf(cm, __shfl_xor(cm, 32));
+                const float m_new = fmaxf(m[i], cm);
+                // (no key so far: the reference stays unset, sums and accumulators are zero)
+                const float alpha = __builtin_amdgcn_exp2f(m[i] - (m_new == SPKV_NEG_INF ? 0.f : m_new));
+                m[i] = m_new;
+                l[i] *= alpha;
+                if (x > x_begin) {
+#pragma unroll
+                    for (int db = 0; db < NB; ++db) acc[i][db] *= alpha;
+                }
+            }
         }
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
-            bf16x8 qb[NS];
+            l[i] += psum[i];
+            const bf16x8 hi = __builtin_convertvector(p[i], bf16x8);
+            const bf16x8 lo = __builtin_convertvector(p[i] - __builtin_convertvector(hi, f32x8), bf16x8);
 #pragma unroll
-            for (int sl = 0; sl < NS; ++sl)
-                qb[sl] = NQ == 1 ? q1[NQ == 1 ? sl : 0] : *reinterpret_cast<const bf16x8*>(&s_q[NQ == 1 ? 0 : i * NS + sl][lane * 8]);
-            attend_half_page<D, true>(t.k, t.v, qb, ok[i] ^ 0xffu, edge, scale_log2e, acc[i], m[i], l[i]);
+            for (int db = 0; db < NB; ++db) acc[i][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[db], hi, acc[i][db], 0, 0, 0);
+#pragma unroll
+            for (int db = 0; db < NB; ++db) acc[i][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[db], lo, acc[i][db], 0, 0, 0);
         }
-        ++x;
-    };
-    while (x < x_end) {
-        if (x + 1 < x_end) load(t1, x + 1);
-        attend(t0);
-        if (x >= x_end) break;
-        if (x + 1 < x_end) load(t0, x + 1);
-        attend(t1);
+        if (more) load_v(next);
     }
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
@@ -701,16 +751,17 @@ template <int D, int S>
 __global__ __launch_bounds__(256) void spkv_prefix_merge(SpkvShareCut cut, SpkvShareMerge rows, SpkvShareOwn own, int n_q_heads,
                                                          int n_kv_heads, const uint16_t* own_out, const float* own_lse,
                                                          uint16_t* out, float* lse) {      // (out may be own_out, lse own_lse)
-    constexpr int TPC = D / 4, CPB = 256 / TPC, kFold = 8;
+    constexpr int TPC = D / 4, CPB = 256 / TPC, kFold = 8, kCols = CPB / S;
     __shared__ f32x4 s_num[S > 1 ? CPB : 1][S > 1 ? TPC : 1];
     __shared__ float2 s_ml[S > 1 ? CPB : 1];
     const int slice = (int)threadIdx.x / TPC, share = slice % S, d = ((int)threadIdx.x % TPC) * 4;
-    const int64_t id = (int64_t)blockIdx.x * (CPB / S) + slice / S;      // row * Hq + head
-    const bool exists = id < cut.n_out;
-    const int G = n_q_heads / n_kv_heads;
-    const int row = exists ? (int)(id / n_q_heads) : 0, head = exists ? (int)(id - (int64_t)row * n_q_heads) : 0;
-    const int h = head / G, g = head - h * G;
-    int act = -1, at = 0;
+    // a workgroup's columns are heads of one row: what belongs to the row is looked up once, in scalar registers
+    const int per_row = (n_q_heads + kCols - 1) / kCols, row = (int)blockIdx.x / per_row;
+    const int head0 = ((int)blockIdx.x - row * per_row) * kCols;
+    const bool exists = head0 + slice / S < n_q_heads;
+    const int G = n_q_heads / n_kv_heads, head = exists ? head0 + slice / S : head0, h = head / G, g = head - h * G;
+    const int64_t id = (int64_t)row * n_q_heads + head;
+    int act, at;
     if (rows.by_row != nullptr) {
         const int2 e = rows.by_row[row];
         act = e.x;
@@ -721,15 +772,38 @@ __global__ __launch_bounds__(256) void spkv_prefix_merge(SpkvShareCut cut, SpkvS
     }
     float M = SPKV_NEG_INF, den = 0.f;
     f32x4 num = {0.f, 0.f, 0.f, 0.f};
-    const int ranges = act < 0 ? 0 : cut.uniform > 0 ? cut.uniform : rows.ranges[act * n_kv_heads + h];
-    int own_parts = 0;
-    size_t own0 = 0;
-    if (own.part != nullptr) {
-        const SpkvSplit sp = own.split;
-        const int pair = row * n_kv_heads + h;
-        own_parts = own_ranges(own, pair);
-        own0 = (size_t)pair * sp.slots * G + g;
-    } else if (share == 0 && exists) {
+    const int h_first = head0 / G, h_last = (min(head0 + kCols, n_q_heads) - 1) / G;      // (one, or the table is asked per lane)
+    const int ranges = act < 0 ? 0 : cut.uniform > 0 ? cut.uniform
+                     : h_first == h_last ? rows.ranges[act * n_kv_heads + h_first] : rows.ranges[act * n_kv_heads + h];
+    // partial results kFold at a time, their loads in flight together; only the rescaling is chained
+    auto fold = [&](const float* sums, const float2* ml, size_t pc0, size_t step, int n) {
+        for (int r0 = share; r0 < n; r0 += kFold * S) {
+            float2 x[kFold];
+            f32x4 a[kFold];
+#pragma unroll
+            for (int u = 0; u < kFold; ++u) {
+                const size_t pc = pc0 + (size_t)min(r0 + u * S, n - 1) * step;       // past the end: re-read, ignored
+                x[u] = ml[pc];
+                a[u] = *reinterpret_cast<const f32x4*>(sums + pc * D + d);
+            }
+            float m_new = M;
+#pragma unroll
+            for (int u = 0; u < kFold; ++u)
+                if (r0 + u * S < n) m_new = fmaxf(m_new, x[u].x);
+            const float m_ref = m_new == SPKV_NEG_INF ? 0.f : m_new, so = __builtin_amdgcn_exp2f(M - m_ref);
+            den *= so;
+            num *= so;
+#pragma unroll
+            for (int u = 0; u < kFold; ++u)
+                if (r0 + u * S < n && x[u].x > SPKV_NEG_INF) {       // (a range without keys has written no sums)
+                    const float sc = __builtin_amdgcn_exp2f(x[u].x - m_ref);
+                    num += a[u] * sc;
+                    den += x[u].y * sc;
+                }
+            M = m_new;
+        }
+    };
+    if (own.part == nullptr && share == 0 && exists) {
         const uint2 ob = *reinterpret_cast<const uint2*>(own_out + id * D + d);
         const float z = own_lse[id];
         if (ranges == 0) {                                   // no prompt: the own part as it is
@@ -743,37 +817,12 @@ __global__ __launch_bounds__(256) void spkv_prefix_merge(SpkvShareCut cut, SpkvS
                           __builtin_bit_cast(float, ob.y << 16), __builtin_bit_cast(float, ob.y & 0xffff0000u)};
         }
     }
-    // partial results kFold at a time, their loads in flight together; only the rescaling is chained
-    const size_t prompt0 = (size_t)h * cut.slots * cut.n_cols + (size_t)at * G + g;
-    const float2* ml = reinterpret_cast<const float2*>(cut.part + (size_t)n_kv_heads * cut.slots * cut.n_cols * D);
-    const float2* own_ml = reinterpret_cast<const float2*>(own.part + own.n_floats);
-    const int parts = exists ? ranges + own_parts : 0;
-    for (int r0 = share; r0 < parts; r0 += kFold * S) {
-        float2 x[kFold];
-        f32x4 a[kFold];
-#pragma unroll
-        for (int u = 0; u < kFold; ++u) {
-            const int r = min(r0 + u * S, parts - 1);        // past the end: re-read, ignored
-            const bool mine = r >= ranges;
-            const size_t pc = mine ? own0 + (size_t)(r - ranges) * G : prompt0 + (size_t)r * cut.n_cols;
-            x[u] = (mine ? own_ml : ml)[pc];
-            a[u] = *reinterpret_cast<const f32x4*>((mine ? own.part : cut.part) + pc * D + d);
-        }
-        float m_new = M;
-#pragma unroll
-        for (int u = 0; u < kFold; ++u)
-            if (r0 + u * S < parts) m_new = fmaxf(m_new, x[u].x);
-        const float m_ref = m_new == SPKV_NEG_INF ? 0.f : m_new, so = __builtin_amdgcn_exp2f(M - m_ref);
-        den *= so;
-        num *= so;
-#pragma unroll
-        for (int u = 0; u < kFold; ++u)
-            if (r0 + u * S < parts && x[u].x > SPKV_NEG_INF) {       // (a range without keys has written no sums)
-                const float sc = __builtin_amdgcn_exp2f(x[u].x - m_ref);
-                num += a[u] * sc;
-                den += x[u].y * sc;
-            }
-        M = m_new;
+    fold(cut.part, reinterpret_cast<const float2*>(cut.part + (size_t)n_kv_heads * cut.slots * cut.n_cols * D),
+         (size_t)h * cut.slots * cut.n_cols + (size_t)at * G + g, cut.n_cols, ranges);
+    if (own.part != nullptr) {
+        const int pair = row * n_kv_heads + h;
+        fold(own.part, reinterpret_cast<const float2*>(own.part + own.n_floats), (size_t)pair * own.split.slots * G + g, G,
+             own_ranges(own, pair));
     }
     if (S > 1) {
         s_num[slice][(int)threadIdx.x % TPC] = num;
@@ -848,26 +897,29 @@ __global__ __launch_bounds__(256) void spkv_prefix_rows(SpkvCu cu, SpkvShareActi
 
 int spkv_prefix_groups(int n_cols) { return n_cols <= 16 ? 1 : n_cols <= 32 ? 2 : n_cols <= 64 ? 4 : n_cols <= 128 ? 8 : 16; }
 
+constexpr int kMergeRound = 1280;
 template <int D>
 static hipError_t launch_prefix(const SpkvView& v, const uint16_t* q, float sl, int groups, const SpkvShareCut& cut,
                                 const SpkvShareTable& table, const SpkvShareRows& rows, const SpkvShareMerge& merge,
                                 const SpkvShareOwn& own, const uint16_t* own_out, const float* own_lse, uint16_t* out,
                                 float* lse, hipStream_t s) {
-    const int items = own.part != nullptr ? own.n_pairs * own.split.slots : 0, waves = groups == 16 ? 8 : 4;
+    const int items = own.part != nullptr ? own.n_pairs * own.split.slots : 0, waves = groups == 16 ? 8 : groups == 4 ? 2 : 4;
     const dim3 grid((unsigned)(cut.n_units + (items + waves - 1) / waves)), block(64 * waves);
     if (grid.x > 0) {
         if (groups == 16) spkv_prefix_split<D, 8><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
         else if (groups == 8) spkv_prefix_split<D, 4><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
-        else if (groups == 4) spkv_prefix_few<D, 4><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
+        else if (groups == 4) spkv_prefix_split<D, 2><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
         else if (groups == 2) spkv_prefix_few<D, 2><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
         else spkv_prefix_few<D, 1><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
     }
-    // groups to a column: about eight workgroups per compute unit, no more groups than there are ranges
+    // groups to a column: as many as one round of workgroups (five on a compute unit) leaves room for, no more than
+    // there are ranges
     constexpr int CPB = 256 / (D / 4);
+    const int64_t rows_out = cut.n_out / v.Hq;
     int share = 8;
-    while (share > 1 && (cut.n_out * share / CPB > 4096 || share > cut.slots)) share >>= 1;
-    const int per_block = CPB / share;
-    const dim3 merge_grid((unsigned)((cut.n_out + per_block - 1) / per_block));
+    while (share > 1 && (rows_out * ((v.Hq * share + CPB - 1) / CPB) > kMergeRound || share > cut.slots)) share >>= 1;
+    const int cols = CPB / share;
+    const dim3 merge_grid((unsigned)(rows_out * ((v.Hq + cols - 1) / cols)));
     if (share == 8) spkv_prefix_merge<D, 8><<<merge_grid, dim3(256), 0, s>>>(cut, merge, own, v.Hq, v.Hkv, own_out, own_lse, out, lse);
     else if (share == 4) spkv_prefix_merge<D, 4><<<merge_grid, dim3(256), 0, s>>>(cut, merge, own, v.Hq, v.Hkv, own_out, own_lse, out, lse);
     else if (share == 2) spkv_prefix_merge<D, 2><<<merge_grid, dim3(256), 0, s>>>(cut, merge, own, v.Hq, v.Hkv, own_out, own_lse, out, lse);
