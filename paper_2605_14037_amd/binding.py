@@ -63,10 +63,6 @@ class SPKVRope(C.Structure):
                 ("n_axes", C.c_int32), ("inv_freq", C.c_void_p), ("axis", C.c_void_p)]
 
 
-class SPKVHeads(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
-
-
 class SPKVError(RuntimeError):
     def __init__(self, code, where):
         self.code = code
@@ -135,7 +131,7 @@ def load_library():
     lib.spkv_prefix_attention.argtypes = [vp, vp, P(i32), vp, P(i32), i32, vp, vp, vp, vp, f32, vp, C.c_size_t, vp]
     lib.spkv_decode_attention_shared.restype = C.c_int
     lib.spkv_decode_attention_shared.argtypes = [vp, vp, P(i32), vp, vp, vp, f32, vp, C.c_size_t, vp]
-    ph, pr = P(SPKVHeads), P(SPKVRope)
+    ph, pr = vp, P(SPKVRope)                 # (heads: addresses into one block of memory, see _block)
     lib.spkv_qk_norm_rope.restype = C.c_int
     lib.spkv_qk_norm_rope.argtypes = [ph, ph, ph, vp, vp, f32, vp, pr, i32, i64, i32, i32, ph, ph, ph, vp]
     lib.spkv_qk_norm_rope_backward_workspace_bytes.restype = C.c_size_t
@@ -291,22 +287,36 @@ class Rope:
 
 
 def _heads(t, dtype, shape, name):
-    if not t.is_cuda or t.dtype != dtype or t.shape != shape or (t.stride(2) != 1 and shape[2] != 1):
+    """Address and strides of one set of heads (the fields of spkv_heads_t)."""
+    st = t.stride()
+    if not t.is_cuda or t.dtype != dtype or t.shape != shape or (st[2] != 1 and shape[2] != 1):
         raise ValueError(f"{name}: need a cuda {dtype} tensor of shape {tuple(shape)} with dense heads, "
-                         f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
-    return SPKVHeads(t.data_ptr(), t.stride(0), t.stride(1))
+                         f"got {t.dtype} {tuple(t.shape)} strides {st} on {t.device}")
+    return t.data_ptr(), st[0], st[1]
+
+
+_NO_HEADS = (0, 0, 0)
+
+
+def _block(sets):
+    """Sets of heads as one block of memory, and the address of each (None where there is none)."""
+    flat = [x for h in sets for x in h]
+    block = (C.c_int64 * len(flat))(*flat)
+    at = C.addressof(block)
+    return block, [None if h is _NO_HEADS else at + 24 * i for i, h in enumerate(sets)]
 
 
 def _rope_call(q, k, v, positions, rope, q_weight, k_weight, eps, names):
     """What both directions check and pass: shapes, type, weights, norm, positions."""
-    if q.dim() != 3 or k.dim() != 3 or q.dtype not in _HEAD_TYPES:
+    dtype = q.dtype
+    if q.dim() != 3 or k.dim() != 3 or dtype not in _HEAD_TYPES:
         raise ValueError(f"{names[0]}, {names[1]}: need bf16 or fp32 [tokens, heads, head_dim]")
     n, hq, d = q.shape
     if d != rope.head_dim:
         raise ValueError(f"{names[0]}: heads of {d} elements, rope made for {rope.head_dim}")
     hk = k.shape[1]
-    ins = [_heads(q, q.dtype, (n, hq, d), names[0]), _heads(k, q.dtype, (n, hk, d), names[1]),
-           None if v is None else _heads(v, q.dtype, (n, hk, d), names[2])]
+    ins = [_heads(q, dtype, (n, hq, d), names[0]), _heads(k, dtype, (n, hk, d), names[1]),
+           _NO_HEADS if v is None else _heads(v, dtype, (n, hk, d), names[2])]
     shape = (n,) if rope.n_axes == 1 and positions.dim() == 1 else (rope.n_axes, n)
     pp = _dev_ptr(positions, torch.int32, shape, "positions")
     if eps is None:
@@ -320,22 +330,27 @@ def _rope_call(q, k, v, positions, rope, q_weight, k_weight, eps, names):
     return n, hq, hk, d, ins, pp, qw, kw, float(eps)
 
 
+def _rope_out(out, q, v, n, hq, hk, d):
+    """Tensors to write: those given, or new dense ones."""
+    if out is not None:
+        return (out[0], out[1], None) if v is None else out
+    dtype, device = q.dtype, q.device
+    return (torch.empty((n, hq, d), dtype=dtype, device=device), torch.empty((n, hk, d), dtype=dtype, device=device),
+            None if v is None else torch.empty((n, hk, d), dtype=dtype, device=device))
+
+
 def qk_norm_rope(q, k, positions, rope, q_weight=None, k_weight=None, eps=None, v=None, out=None):
     """RMS norm of every head (eps None: no norm), rotation by positions, dense layout, in one launch
     (spkv_qk_norm_rope).  q: bf16 or fp32 [tokens, H_q, D]; k, v: [tokens, H_kv, D], slices of a
     projection's rows as they are; positions: int32 [tokens] or [axes, tokens].  out: tensors to write
     (the inputs themselves may be passed).  Returns (q, k) or, with v, (q, k, v)."""
     n, hq, hk, d, ins, pp, qw, kw, eps = _rope_call(q, k, v, positions, rope, q_weight, k_weight, eps, "qkv")
-    if out is None:
-        out = (torch.empty((n, hq, d), dtype=q.dtype, device=q.device),
-               torch.empty((n, hk, d), dtype=q.dtype, device=q.device),
-               None if v is None else torch.empty((n, hk, d), dtype=q.dtype, device=q.device))
-    elif v is None:
-        out = (out[0], out[1], None)
-    outs = [_heads(out[0], q.dtype, (n, hq, d), "out[0]"), _heads(out[1], q.dtype, (n, hk, d), "out[1]"),
-            None if v is None else _heads(out[2], q.dtype, (n, hk, d), "out[2]")]
-    _check(load_library().spkv_qk_norm_rope(*ins, qw, kw, eps, pp, rope.struct, _HEAD_TYPES[q.dtype], n, hq, hk, *outs,
-                                            _stream()), "spkv_qk_norm_rope")
+    out, dtype = _rope_out(out, q, v, n, hq, hk, d), q.dtype
+    outs = [_heads(out[0], dtype, (n, hq, d), "out[0]"), _heads(out[1], dtype, (n, hk, d), "out[1]"),
+            _NO_HEADS if v is None else _heads(out[2], dtype, (n, hk, d), "out[2]")]
+    block, at = _block(ins + outs)
+    _check((_LIB or load_library()).spkv_qk_norm_rope(at[0], at[1], at[2], qw, kw, eps, pp, rope.struct, _HEAD_TYPES[dtype],
+                                                      n, hq, hk, at[3], at[4], at[5], _stream()), "spkv_qk_norm_rope")
     return tuple(out[:2]) if v is None else tuple(out)
 
 
@@ -348,21 +363,17 @@ def qk_norm_rope_backward(dq, dk, positions, rope, q=None, k=None, q_weight=None
     fp32 gradients of both weights."""
     n, hq, hk, d, ins, pp, qw, kw, eps = _rope_call(dq, dk, dv, positions, rope, q_weight, k_weight, eps,
                                                     ("dq", "dk", "dv"))
-    given = out is not None
-    if not given:
-        out = (torch.empty((n, hq, d), dtype=dq.dtype, device=dq.device),
-               torch.empty((n, hk, d), dtype=dq.dtype, device=dq.device),
-               None if dv is None else torch.empty((n, hk, d), dtype=dq.dtype, device=dq.device))
-    outs = [_heads(out[0], dq.dtype, (n, hq, d), "out[0]"), _heads(out[1], dq.dtype, (n, hk, d), "out[1]"),
-            None if dv is None else _heads(out[2], dq.dtype, (n, hk, d), "out[2]")]
-    xs, weights = [None, None], ()
+    given, dtype = out is not None, dq.dtype
+    out = _rope_out(out, dq, dv, n, hq, hk, d)
+    outs = [_heads(out[0], dtype, (n, hq, d), "out[0]"), _heads(out[1], dtype, (n, hk, d), "out[1]"),
+            _NO_HEADS if dv is None else _heads(out[2], dtype, (n, hk, d), "out[2]")]
+    xs, weights = [_NO_HEADS, _NO_HEADS], ()
     if eps >= 0.0:
         if q is None or k is None:
             raise ValueError("q, k: the forward's inputs are needed with a norm")
-        xs = [_heads(q, dq.dtype, (n, hq, d), "q"), _heads(k, dq.dtype, (n, hk, d), "k")]
+        xs = [_heads(q, dtype, (n, hq, d), "q"), _heads(k, dtype, (n, hk, d), "k")]
         if want_weights is None or want_weights:
-            weights = (torch.empty(d, dtype=torch.float32, device=dq.device),
-                       torch.empty(d, dtype=torch.float32, device=dq.device))
+            weights = tuple(torch.empty((2, d), dtype=torch.float32, device=dq.device).unbind(0))
     elif want_weights:
         raise ValueError("want_weights: there are no weights without a norm")
     lib = load_library()
@@ -371,11 +382,11 @@ def qk_norm_rope_backward(dq, dk, positions, rope, q=None, k=None, q_weight=None
                                 dtype=torch.uint8, device=dq.device)
     if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous uint8 device tensor")
-    _check(lib.spkv_qk_norm_rope_backward(*ins, *xs, qw, kw, eps, pp, rope.struct, _HEAD_TYPES[dq.dtype], n, hq, hk, *outs,
-                                          *([w.data_ptr() for w in weights] or [None, None]),
-                                          workspace.data_ptr() if workspace is not None else None,
-                                          workspace.numel() if workspace is not None else 0, _stream()),
-           "spkv_qk_norm_rope_backward")
+    block, at = _block(ins + xs + outs)
+    dqw, dkw = (weights[0].data_ptr(), weights[1].data_ptr()) if weights else (None, None)
+    ws, ws_bytes = (workspace.data_ptr(), workspace.numel()) if workspace is not None else (None, 0)
+    _check(lib.spkv_qk_norm_rope_backward(*at[:5], qw, kw, eps, pp, rope.struct, _HEAD_TYPES[dtype], n, hq, hk, *at[5:],
+                                          dqw, dkw, ws, ws_bytes, _stream()), "spkv_qk_norm_rope_backward")
     first = () if given else tuple(out[:2]) if dv is None else tuple(out)
     return first + weights
 

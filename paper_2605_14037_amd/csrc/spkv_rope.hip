@@ -456,8 +456,8 @@ hipError_t spkv_launch_rope(const SpkvRope& a, const double* inv_freq, const uin
     RopeTable table = {};
     for (int i = 0; i < a.rot_dim / 2; ++i) {
         // frequency in turns per position, its whole part dropped: positions are whole numbers
-        const long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559005768L;
-        const long double part = turns - floorl(turns);
+        long double part = (long double)inv_freq[i] * 0.159154943091895335768883763372514362L;
+        if (!(part >= 0.0L && part < 1.0L)) part -= floorl(part);
         table.turn[i] = part >= 1.0L ? 0u : (uint64_t)(part * 18446744073709551616.0L);
         table.axis[i] = axis != nullptr ? axis[i] : 0;
     }

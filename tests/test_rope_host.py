@@ -13,6 +13,11 @@ E_INVAL = -1
 PTR = 1 << 20          # a 16-byte aligned address that is never followed
 
 
+class Heads(C.Structure):
+    """spkv_heads_t"""
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
 def _call(rope=None, backward=False, **kw):
     a = dict(q=(PTR, 4 * 128, 128), k=(PTR, 2 * 128, 128), v=None, q_weight=None, k_weight=None, eps=1e-6,
              positions=PTR, dtype=B.BF16, n=5, hq=4, hk=2, q_out=(PTR, 4 * 128, 128), k_out=(PTR, 2 * 128, 128),
@@ -22,7 +27,7 @@ def _call(rope=None, backward=False, **kw):
     s = r.struct if isinstance(r, spkv.Rope) else r
 
     def heads(t):
-        return None if t is None else B.SPKVHeads(*t)
+        return None if t is None else C.byref(Heads(*t))
 
     lib = spkv.load_library()
     io = [heads(a["q"]), heads(a["k"]), heads(a["v"])]
