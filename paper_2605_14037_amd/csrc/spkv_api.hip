@@ -1637,8 +1637,8 @@ namespace {
 struct ShareCarve {
     size_t table, by_row, first_row, own_lse, own_part, part;
 };
-// Sequences whose lists are short are attended in the prompts' launch, in items of at least kShareOwnItem half-pages
-// and at most kShareOwnSlots to a list; only calls of one token a sequence.
+// Sequences whose lists are short are attended in the prompts' launch, at most kShareOwnSlots items to a list (two
+// half-pages each in the longest); only calls of one token a sequence.
 constexpr int kShareOwnSlots = 8, kShareOwnItem = 2;
 ShareCarve share_carve(int64_t rows, int n_q_heads, int head_dim) {
     ShareCarve k;
@@ -1684,11 +1684,11 @@ void share_prompts(const spkv_cache* pc, int batch, const int32_t* prefix_of, co
 
 // Ranges of the prompts' lists: about as many workgroups as the chip holds at once, every list cut evenly into its
 // share of them.
-constexpr int kShareMinUnit = 2;
+constexpr int kShareMinUnit = 2, kShareStart = 16;
 void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_bytes, int* groups, SpkvShareCut* cut,
                SpkvShareTable* table) {
     const int Hkv = c->cfg.n_kv_heads, G = c->carve.G, n = prompts.n, n_lists = n * Hkv;
-    int64_t most = 0, all_rows = 0;
+    int64_t most = 0, all_rows = 0, lists = 0;
     for (int a = 0; a < n; ++a) {
         most = std::max<int64_t>(most, prompts.rows[a]);
         all_rows += prompts.rows[a];
@@ -1696,54 +1696,67 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
     *groups = spkv_prefix_groups((int)std::min<int64_t>(most * G, 1 << 20));
     const int64_t width = 16 * *groups;
     auto blocks = [&](int a) -> int64_t { return ((int64_t)prompts.rows[a] * G + width - 1) / width; };
-    auto half_pages = [&](int a, int h) -> int64_t {
-        const int p = prompts.id[a], held = std::min(c->T[p], c->cfg.window);
-        return ((int64_t)c->L_ub[p * Hkv + h] + kHalfTokens - 1) / kHalfTokens + (held + kHalfTokens - 1) / kHalfTokens;
-    };
-    int64_t work = 0, lists = 0;
-    for (int a = 0; a < n; ++a) {
-        lists += blocks(a) * Hkv;
-        for (int h = 0; h < Hkv; ++h) work += half_pages(a, h) * blocks(a);
-    }
-    const int cus = spkv_compute_units();
-    const int64_t target = cus > 0 ? cus : 256;
-    int64_t unit = std::max<int64_t>(kShareMinUnit, (work + target - 1) / target);
-    for (int guard = 0; guard < 64; ++guard) {
-        int64_t total = 0;
-        for (int a = 0; a < n; ++a)
-            for (int h = 0; h < Hkv; ++h) total += (half_pages(a, h) + unit - 1) / unit * blocks(a);
-        if (total <= target || total <= lists) break;
-        unit += std::max<int64_t>(1, unit / 16);
-    }
-    const size_t slot = share_slot_bytes(all_rows, c->cfg.n_q_heads, c->cfg.head_dim);
-    const int64_t fit = (int64_t)std::min<size_t>(part_bytes / slot, kShareMaxSlots);
-    auto ranges = [&](int a, int h) -> int64_t { return std::max<int64_t>(1, std::min(fit, (half_pages(a, h) + unit - 1) / unit)); };
+    for (int a = 0; a < n; ++a) lists += blocks(a) * Hkv;
     cut->n_blocks = (int32_t)((most * G + width - 1) / width);
     cut->n_cols = (int32_t)(all_rows * G);
-    int64_t end = 0, slots = 1;
+    const size_t slot = share_slot_bytes(all_rows, c->cfg.n_q_heads, c->cfg.head_dim);
+    const int64_t fit = (int64_t)std::min<size_t>(part_bytes / slot, kShareMaxSlots);
+    const int cus = spkv_compute_units(), round = cus > 0 ? cus : 256;
     std::fill(table->end, table->end + kShareTablePairs, (uint16_t)65535);
-    for (int a = 0; a < n; ++a)
-        for (int h = 0; h < Hkv; ++h) {
-            const int64_t r = ranges(a, h);
-            slots = std::max(slots, r);
-            end += r * blocks(a);
-            if (a * Hkv + h < kShareTablePairs) {
-                table->end[a * Hkv + h] = (uint16_t)std::min<int64_t>(end, 65535);
-                table->ranges[a * Hkv + h] = (uint8_t)r;
-            }
-        }
-    cut->slots = (int32_t)slots;
-    cut->n_units = (int32_t)end;
-    if (n_lists > kShareTablePairs || end >= 65535) {        // as many for all
-        cut->uniform = (int32_t)std::max<int64_t>(1, std::min(fit, target / std::max<int64_t>(1, lists)));
-        cut->slots = cut->uniform;
+    if (n_lists > kShareTablePairs || lists > 16384) {       // as many ranges for all
+        cut->uniform = cut->slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(fit, round / lists));
         cut->n_units = (int32_t)((int64_t)n_lists * cut->uniform * cut->n_blocks);
+        return;
     }
+    int32_t hp[kShareTablePairs], copies[kShareTablePairs];
+    int64_t work = 0;
+    for (int a = 0; a < n; ++a) {
+        const int p = prompts.id[a], held = std::min(c->T[p], c->cfg.window);
+        for (int h = 0; h < Hkv; ++h) {
+            const int i = a * Hkv + h;
+            hp[i] = (c->L_ub[p * Hkv + h] + kHalfTokens - 1) / kHalfTokens + (held + kHalfTokens - 1) / kHalfTokens;
+            copies[i] = (int32_t)blocks(a);
+            work += (int64_t)hp[i] * copies[i];
+        }
+    }
+    // One workgroup per compute unit and round.  A range of n half-pages takes about as long as n + kShareStart of them
+    // (start, first references, and what its results cost), so one round unless the lists are so many that they
+    // fill it badly: two or three of shorter ranges then.  Questions of 1632 tokens behind 30 MB of lists in 208 blocks
+    // of columns and heads, one round / two 291 / 247 us; of 256 tokens, 32 such blocks, 56 / 71.
+    int64_t unit = 0, best = 0;
+    for (int k = 1; k <= 3; ++k) {
+        const int64_t target = (int64_t)k * round;
+        int64_t u = std::max<int64_t>(kShareMinUnit, (work + target - 1) / target), total = 0, longest = 0;
+        for (int guard = 0; guard < 64; ++guard) {
+            total = longest = 0;
+            for (int i = 0; i < n_lists; ++i) {
+                const int64_t r = std::max<int64_t>(1, (hp[i] + u - 1) / u);
+                total += r * copies[i];
+                longest = std::max(longest, (hp[i] + r - 1) / r);
+            }
+            if (total <= target || total <= lists) break;
+            u += std::max<int64_t>(1, u / 16);
+        }
+        const int64_t time = (total + round - 1) / round * (longest + kShareStart);
+        if (k > 1 && time >= best) continue;
+        best = time;
+        unit = u;
+    }
+    int64_t end = 0;
+    for (int i = 0; i < n_lists; ++i) {
+        const int64_t r = std::max<int64_t>(1, std::min(fit, (hp[i] + unit - 1) / unit));
+        cut->slots = std::max(cut->slots, (int32_t)r);
+        end += r * copies[i];
+        table->end[i] = (uint16_t)end;                       // (below 65535: at most three rounds beyond a range for each)
+        table->ranges[i] = (uint8_t)r;
+    }
+    cut->n_units = (int32_t)end;
 }
 
-// Items of the sequences' own lists, in the same launch as the prompts'; part null: not.
+// Items of the sequences' own lists, in the same launch as the prompts'; part null: not.  Every list in the same number
+// of items, as many as fill the chip once with one to a wave.
 constexpr int kShareOwnLongest = 64;         // half-pages
-void share_own(const spkv_cache* c, char* part, SpkvShareOwn* own) {
+void share_own(const spkv_cache* c, int waves, char* part, SpkvShareOwn* own) {
     const int n = c->carve.n_pairs, Hkv = c->cfg.n_kv_heads;
     int64_t longest = 1;
     for (int p = 0; p < n; ++p) {
@@ -1761,9 +1774,11 @@ void share_own(const spkv_cache* c, char* part, SpkvShareOwn* own) {
     own->n_pairs = n;
     own->pt_cap = v.pt_cap;
     own->w = v.w;
-    const int64_t per = std::max<int64_t>(kShareOwnItem, (longest + kShareOwnSlots - 1) / kShareOwnSlots);
-    own->split = SpkvSplit{(int32_t)per, (int32_t)((longest + per - 1) / per), 1, 0, 0, 0};
-    own->n_floats = (int64_t)n * own->split.slots * v.G * v.D;
+    const int cus = spkv_compute_units();
+    const int64_t fill = (int64_t)(cus > 0 ? cus : 256) * waves / n;
+    const int64_t slots = std::max<int64_t>(1, std::min({fill, (longest + kShareOwnItem - 1) / kShareOwnItem, (int64_t)kShareOwnSlots}));
+    own->split = SpkvSplit{1, (int32_t)slots, 1, 0, 0, 0};
+    own->n_floats = (int64_t)n * slots * v.G * v.D;
 }
 
 // Both calls: everything but the sequences' own attention.  cu null: one token per sequence.
@@ -1809,7 +1824,7 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
     cut.part = reinterpret_cast<float*>(ws + k.part);
     cut.n_out = total * Hq;
     SpkvShareOwn own = {};
-    if (with_own) share_own(c, ws + k.own_part, &own);
+    if (with_own) share_own(c, spkv_prefix_kernel_waves(groups), ws + k.own_part, &own);
     SpkvShareRows by_prompt = {};
     SpkvShareMerge by_row = {};
     by_prompt.t_own = c->view.t_pair;
@@ -1900,7 +1915,7 @@ int spkv_decode_attention_shared(spkv_cache_t* c, spkv_cache_t* pc, const int32_
         if (rc != SPKV_OK) return rc;
         tighten_bound(c, s);
         SpkvShareOwn own = {};
-        share_own(c, ws, &own);
+        share_own(c, 1, ws, &own);
         fused = own.part != nullptr;
     }
     if (fused) return share_attend(pc, c, prefix_of, qq, nullptr, true, true, nullptr, nullptr, o, lse, sm_scale, ws, workspace_bytes, s);

@@ -270,6 +270,7 @@ struct SpkvShareOwn {
     uint16_t *ring, *pool;
     int32_t *page_table, *t_pair, *kept_len;
     int32_t n_pairs, pt_cap, w;
+    int32_t n_blocks;           // workgroups of the launch that belong to them, its first ones
     SpkvSplit split;
 };
 // The rows by prompt: one token a sequence (first, seq; its place is the last of t_own), or -- more tokens, or more
@@ -291,6 +292,7 @@ struct SpkvShareMerge {
 struct SpkvShareActive {
     int16_t active[SPKV_MAX_BATCH];       // per sequence
 };
+int spkv_prefix_kernel_waves(int groups); // of a workgroup
 int spkv_prefix_groups(int n_cols);       // of 16 columns of a workgroup, for the prompt with the most columns
 hipError_t spkv_launch_prefix(const SpkvView& v, const uint16_t* q, float sm_scale, int groups, const SpkvShareCut& cut,
                               const SpkvShareTable& table, const SpkvShareRows& rows, const SpkvShareMerge& merge,

@@ -182,9 +182,10 @@ __device__ __forceinline__ void own_item(const SpkvView& v, const uint16_t* __re
 #pragma unroll
     for (int i = 0; i < NB; ++i) acc[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m = SPKV_NEG_INF, l = 0.f;
-    for (int hp = hp0; hp < hp1; ++hp) {
+    // two half-pages in flight: what limits an item is its round trips to memory
+    bf16x8 ka[2][2][NS], va[2][NB];
+    auto load = [&](int at, int hp) {
         const uint16_t* base;
-        int nvalid;
         if (hp < ps.ghp) {
             const int lp = hp >> 1;
             if (lp >= pbase + 64) {
@@ -192,24 +193,28 @@ __device__ __forceinline__ void own_item(const SpkvView& v, const uint16_t* __re
                 my_page = pt[min(pbase + lane, v.pt_cap - 1)];
             }
             base = pool_page(v, __builtin_amdgcn_readlane(my_page, lp - pbase)) + (hp & 1) * (2 * kHalfTokens * D);
-            nvalid = min(kHalfTokens, ps.L - hp * kHalfTokens);
         } else {
             const int r = hp - ps.ghp;
             base = ring_page(v, pair, r >> 1) + (r & 1) * (2 * kHalfTokens * D);
-            nvalid = min(kHalfTokens, ps.Tw - r * kHalfTokens);
         }
-        const bool any_kill = nvalid < kHalfTokens;
-        const unsigned kill = any_kill ? 0xffu << min(max(nvalid - kc * 8, 0), 8) : 0u;
-        const uint16_t* kp = base + lane * 8;
-        const uint16_t* vp = base + kHalfTokens * D + lane * 8;
-        bf16x8 ka[2][NS], va[NB];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int sl = 0; sl < NS; ++sl) ka[t][sl] = load_stream_b128(kp + (t * (D / 8) + sl * 4) * 128);
+            for (int sl = 0; sl < NS; ++sl) ka[at][t][sl] = load_stream_b128(base + lane * 8 + (t * (D / 8) + sl * 4) * 128);
 #pragma unroll
-        for (int db = 0; db < NB; ++db) va[db] = load_stream_b128(vp + db * 512);
-        attend_half_page<D, true>(ka, va, qb, kill, any_kill, scale_log2e, acc, m, l);
+        for (int db = 0; db < NB; ++db) va[at][db] = load_stream_b128(base + kHalfTokens * D + lane * 8 + db * 512);
+    };
+    auto attend = [&](int at, int hp) {
+        const int nvalid = hp < ps.ghp ? ps.L - hp * kHalfTokens : ps.Tw - (hp - ps.ghp) * kHalfTokens;
+        const bool any_kill = nvalid < kHalfTokens;
+        const unsigned kill = any_kill ? bits_from(nvalid - kc * 8) : 0u;
+        attend_half_page<D, true>(ka[at], va[at], qb, kill, any_kill, scale_log2e, acc, m, l);
+    };
+    for (int hp = hp0; hp < hp1; hp += 2) {
+        load(0, hp);
+        if (hp + 1 < hp1) load(1, hp + 1);
+        attend(0, hp);
+        if (hp + 1 < hp1) attend(1, hp + 1);
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -293,11 +298,11 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
     __shared__ __attribute__((aligned(16))) uint16_t s_q[NQ == 1 ? 1 : NQ * NS][512];
     const int tid = threadIdx.x, lane = tid & 63, kc = lane >> 4, n = lane & 15;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    if ((int)blockIdx.x >= cut.n_units) {                    // behind the prompts': the sequences' own lists
-        own_item<D>(own_view(own, v), q, scale_log2e, own.split, own.part, ((int)blockIdx.x - cut.n_units) * 4 + wv);
+    if ((int)blockIdx.x < own.n_blocks) {
+        own_item<D>(own_view(own, v), q, scale_log2e, own.split, own.part, (int)blockIdx.x * 4 + wv);
         return;
     }
-    const ShareUnit u = find_unit(cut, table, blockIdx.x, v.Hkv);
+    const ShareUnit u = find_unit(cut, table, (int)blockIdx.x - own.n_blocks, v.Hkv);
     const int act = u.list / v.Hkv, h = u.list - act * v.Hkv, j = u.range, ranges = u.ranges;
     const int pair = (int)rows.prefix[act] * v.Hkv + h;
     const FirstPages first_ids = first_pages(v, pair);
@@ -495,12 +500,12 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     constexpr int kSlots = NW == 8 ? 8 : 5;                  // half-pages in LDS
     constexpr int kRowsPerWave = kHps * (D / 8) / NW;        // 1 KB rows of a step that a wave copies
     __shared__ __attribute__((aligned(16))) uint16_t s_tile[kSlots][kHalfElems];
-    if ((int)blockIdx.x >= cut.n_units) {                    // behind the prompts': the sequences' own lists
-        const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-        own_item<D>(own_view(own, v), q, scale_log2e, own.split, own.part, ((int)blockIdx.x - cut.n_units) * NW + wave);
+    if ((int)blockIdx.x < own.n_blocks) {
+        own_item<D>(own_view(own, v), q, scale_log2e, own.split, own.part,
+                    (int)blockIdx.x * NW + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6));
         return;
     }
-    const ShareUnit u = find_unit(cut, table, blockIdx.x, v.Hkv);
+    const ShareUnit u = find_unit(cut, table, (int)blockIdx.x - own.n_blocks, v.Hkv);
     const int act = u.list / v.Hkv, h = u.list - act * v.Hkv, j = u.range, ranges = u.ranges;
     const int pair = (int)rows.prefix[act] * v.Hkv + h;
     const FirstPages first_ids = first_pages(v, pair);
@@ -748,10 +753,10 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
 // The sequence's own part is a set of partial results too (own.part), or comes as a call's bf16 output and fp32
 // logarithm of its sum: half a step of bf16 more than from sums in 32 bits, on the share that the own tokens have.
 template <int D, int S>
-__global__ __launch_bounds__(256) void spkv_prefix_merge(SpkvShareCut cut, SpkvShareMerge rows, SpkvShareOwn own, int n_q_heads,
+__global__ __launch_bounds__(256, 8) void spkv_prefix_merge(SpkvShareCut cut, SpkvShareMerge rows, SpkvShareOwn own, int n_q_heads,
                                                          int n_kv_heads, const uint16_t* own_out, const float* own_lse,
                                                          uint16_t* out, float* lse) {      // (out may be own_out, lse own_lse)
-    constexpr int TPC = D / 4, CPB = 256 / TPC, kFold = 8, kCols = CPB / S;
+    constexpr int TPC = D / 4, CPB = 256 / TPC, kFold = S > 1 ? 5 : 2, kCols = CPB / S;
     __shared__ f32x4 s_num[S > 1 ? CPB : 1][S > 1 ? TPC : 1];
     __shared__ float2 s_ml[S > 1 ? CPB : 1];
     const int slice = (int)threadIdx.x / TPC, share = slice % S, d = ((int)threadIdx.x % TPC) * 4;
@@ -775,34 +780,7 @@ __global__ __launch_bounds__(256) void spkv_prefix_merge(SpkvShareCut cut, SpkvS
     const int h_first = head0 / G, h_last = (min(head0 + kCols, n_q_heads) - 1) / G;      // (one, or the table is asked per lane)
     const int ranges = act < 0 ? 0 : cut.uniform > 0 ? cut.uniform
                      : h_first == h_last ? rows.ranges[act * n_kv_heads + h_first] : rows.ranges[act * n_kv_heads + h];
-    // partial results kFold at a time, their loads in flight together; only the rescaling is chained
-    auto fold = [&](const float* sums, const float2* ml, size_t pc0, size_t step, int n) {
-        for (int r0 = share; r0 < n; r0 += kFold * S) {
-            float2 x[kFold];
-            f32x4 a[kFold];
-#pragma unroll
-            for (int u = 0; u < kFold; ++u) {
-                const size_t pc = pc0 + (size_t)min(r0 + u * S, n - 1) * step;       // past the end: re-read, ignored
-                x[u] = ml[pc];
-                a[u] = *reinterpret_cast<const f32x4*>(sums + pc * D + d);
-            }
-            float m_new = M;
-#pragma unroll
-            for (int u = 0; u < kFold; ++u)
-                if (r0 + u * S < n) m_new = fmaxf(m_new, x[u].x);
-            const float m_ref = m_new == SPKV_NEG_INF ? 0.f : m_new, so = __builtin_amdgcn_exp2f(M - m_ref);
-            den *= so;
-            num *= so;
-#pragma unroll
-            for (int u = 0; u < kFold; ++u)
-                if (r0 + u * S < n && x[u].x > SPKV_NEG_INF) {       // (a range without keys has written no sums)
-                    const float sc = __builtin_amdgcn_exp2f(x[u].x - m_ref);
-                    num += a[u] * sc;
-                    den += x[u].y * sc;
-                }
-            M = m_new;
-        }
-    };
+    const int pair = row * n_kv_heads + h, parts = ranges + (own.part != nullptr ? own_ranges(own, pair) : 0);
     if (own.part == nullptr && share == 0 && exists) {
         const uint2 ob = *reinterpret_cast<const uint2*>(own_out + id * D + d);
         const float z = own_lse[id];
@@ -817,12 +795,37 @@ __global__ __launch_bounds__(256) void spkv_prefix_merge(SpkvShareCut cut, SpkvS
                           __builtin_bit_cast(float, ob.y << 16), __builtin_bit_cast(float, ob.y & 0xffff0000u)};
         }
     }
-    fold(cut.part, reinterpret_cast<const float2*>(cut.part + (size_t)n_kv_heads * cut.slots * cut.n_cols * D),
-         (size_t)h * cut.slots * cut.n_cols + (size_t)at * G + g, cut.n_cols, ranges);
-    if (own.part != nullptr) {
-        const int pair = row * n_kv_heads + h;
-        fold(own.part, reinterpret_cast<const float2*>(own.part + own.n_floats), (size_t)pair * own.split.slots * G + g, G,
-             own_ranges(own, pair));
+    // partial results, the prompt's and then the own ones, kFold at a time: their loads in flight together, only the
+    // rescaling is chained
+    const float2* ml = reinterpret_cast<const float2*>(cut.part + (size_t)n_kv_heads * cut.slots * cut.n_cols * D);
+    const float2* own_ml = reinterpret_cast<const float2*>(own.part + own.n_floats);
+    const size_t prompt0 = (size_t)h * cut.slots * cut.n_cols + (size_t)at * G + g, own0 = (size_t)pair * own.split.slots * G + g;
+    for (int r0 = share; r0 < parts; r0 += kFold * S) {
+        float2 x[kFold];
+        f32x4 a[kFold];
+#pragma unroll
+        for (int u = 0; u < kFold; ++u) {
+            const int r = min(r0 + u * S, parts - 1);        // past the end: re-read, ignored
+            const bool mine = r >= ranges;
+            const size_t pc = mine ? own0 + (size_t)(r - ranges) * G : prompt0 + (size_t)r * cut.n_cols;
+            x[u] = (mine ? own_ml : ml)[pc];
+            a[u] = *reinterpret_cast<const f32x4*>((mine ? own.part : cut.part) + pc * D + d);
+        }
+        float m_new = M;
+#pragma unroll
+        for (int u = 0; u < kFold; ++u)
+            if (r0 + u * S < parts) m_new = fmaxf(m_new, x[u].x);
+        const float m_ref = m_new == SPKV_NEG_INF ? 0.f : m_new, so = __builtin_amdgcn_exp2f(M - m_ref);
+        den *= so;
+        num *= so;
+#pragma unroll
+        for (int u = 0; u < kFold; ++u)
+            if (r0 + u * S < parts && x[u].x > SPKV_NEG_INF) {       // (a range without keys has written no sums)
+                const float sc = __builtin_amdgcn_exp2f(x[u].x - m_ref);
+                num += a[u] * sc;
+                den += x[u].y * sc;
+            }
+        M = m_new;
     }
     if (S > 1) {
         s_num[slice][(int)threadIdx.x % TPC] = num;
@@ -897,14 +900,17 @@ __global__ __launch_bounds__(256) void spkv_prefix_rows(SpkvCu cu, SpkvShareActi
 
 int spkv_prefix_groups(int n_cols) { return n_cols <= 16 ? 1 : n_cols <= 32 ? 2 : n_cols <= 64 ? 4 : n_cols <= 128 ? 8 : 16; }
 
-constexpr int kMergeRound = 1280;
+constexpr int kMergeRound = 2048;
+int spkv_prefix_kernel_waves(int groups) { return groups == 16 ? 8 : groups == 4 ? 2 : 4; }
+
 template <int D>
 static hipError_t launch_prefix(const SpkvView& v, const uint16_t* q, float sl, int groups, const SpkvShareCut& cut,
                                 const SpkvShareTable& table, const SpkvShareRows& rows, const SpkvShareMerge& merge,
-                                const SpkvShareOwn& own, const uint16_t* own_out, const float* own_lse, uint16_t* out,
-                                float* lse, hipStream_t s) {
-    const int items = own.part != nullptr ? own.n_pairs * own.split.slots : 0, waves = groups == 16 ? 8 : groups == 4 ? 2 : 4;
-    const dim3 grid((unsigned)(cut.n_units + (items + waves - 1) / waves)), block(64 * waves);
+                                SpkvShareOwn own, const uint16_t* own_out, const float* own_lse, uint16_t* out, float* lse,
+                                hipStream_t s) {
+    const int items = own.part != nullptr ? own.n_pairs * own.split.slots : 0, waves = spkv_prefix_kernel_waves(groups);
+    own.n_blocks = (items + waves - 1) / waves;
+    const dim3 grid((unsigned)(own.n_blocks + cut.n_units)), block(64 * waves);
     if (grid.x > 0) {
         if (groups == 16) spkv_prefix_split<D, 8><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
         else if (groups == 8) spkv_prefix_split<D, 4><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
@@ -912,7 +918,7 @@ static hipError_t launch_prefix(const SpkvView& v, const uint16_t* q, float sl, 
         else if (groups == 2) spkv_prefix_few<D, 2><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
         else spkv_prefix_few<D, 1><<<grid, block, 0, s>>>(v, q, sl, cut, table, rows, own);
     }
-    // groups to a column: as many as one round of workgroups (five on a compute unit) leaves room for, no more than
+    // groups to a column: as many as one round of workgroups (eight on a compute unit) leaves room for, no more than
     // there are ranges
     constexpr int CPB = 256 / (D / 4);
     const int64_t rows_out = cut.n_out / v.Hq;
