@@ -1708,23 +1708,23 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
         cut->n_units = (int32_t)((int64_t)n_lists * cut->uniform * cut->n_blocks);
         return;
     }
-    int32_t hp[kShareTablePairs], copies[kShareTablePairs];
+    int32_t hp[kShareTablePairs], copies[kShareTablePairs];      // half-pages, the ring's twice (ShareList::begin)
     int64_t work = 0;
     for (int a = 0; a < n; ++a) {
         const int p = prompts.id[a], held = std::min(c->T[p], c->cfg.window);
         for (int h = 0; h < Hkv; ++h) {
             const int i = a * Hkv + h;
-            hp[i] = (c->L_ub[p * Hkv + h] + kHalfTokens - 1) / kHalfTokens + (held + kHalfTokens - 1) / kHalfTokens;
+            hp[i] = (c->L_ub[p * Hkv + h] + kHalfTokens - 1) / kHalfTokens + 2 * ((held + kHalfTokens - 1) / kHalfTokens);
             copies[i] = (int32_t)blocks(a);
             work += (int64_t)hp[i] * copies[i];
         }
     }
     // One workgroup per compute unit and round.  A range of n half-pages takes about as long as n + kShareStart of them
     // (start, first references, and what its results cost), so one round unless the lists are so many that they
-    // fill it badly: two or three of shorter ranges then.  Questions of 1632 tokens behind 30 MB of lists in 208 blocks
-    // of columns and heads, one round / two 291 / 247 us; of 256 tokens, 32 such blocks, 56 / 71.
+    // fill it badly: two of shorter ranges then.  Questions of 1632 tokens behind 30 MB of lists in 208 blocks of columns
+    // and heads, one round / two / three 291 / 247 / 271 us; of 256 tokens, 32 such blocks, 56 / 71 / 85.
     int64_t unit = 0, best = 0;
-    for (int k = 1; k <= 3; ++k) {
+    for (int k = 1; k <= 2; ++k) {
         const int64_t target = (int64_t)k * round;
         int64_t u = std::max<int64_t>(kShareMinUnit, (work + target - 1) / target), total = 0, longest = 0;
         for (int guard = 0; guard < 64; ++guard) {
@@ -1747,7 +1747,7 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
         const int64_t r = std::max<int64_t>(1, std::min(fit, (hp[i] + unit - 1) / unit));
         cut->slots = std::max(cut->slots, (int32_t)r);
         end += r * copies[i];
-        table->end[i] = (uint16_t)end;                       // (below 65535: at most three rounds beyond a range for each)
+        table->end[i] = (uint16_t)end;                       // (below 65535: at most two rounds beyond a range for each)
         table->ranges[i] = (uint8_t)r;
     }
     cut->n_units = (int32_t)end;

@@ -31,6 +31,12 @@ __device__ __forceinline__ unsigned bits_from(int n) { return bits_below(n) ^ 0x
 struct ShareList {
     int pair, T, L, held, nA, n_hp;
     int slot0;                  // ring slot of age 0 (negative while the ring is not full)
+    // Begin of the j-th of n ranges.  A half-page of the ring counts twice: its mask takes about as long as its
+    // products (16 sequences behind 30 MB of lists: workgroups with the ring 3.5 us behind the others, of 16).
+    __device__ __forceinline__ int begin(int j, int n) const {
+        const int x = (int)((int64_t)j * (2 * n_hp - nA) / n);
+        return x <= nA ? x : nA + (x - nA + 1) / 2;
+    }
 };
 __device__ __forceinline__ ShareList share_list(const SpkvView& v, int pair) {
     ShareList s;
@@ -310,7 +316,7 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
     const int first = share_first(rows, act), n_cols = (share_first(rows, act + 1) - first) * v.G;
     if (n_cols <= 0) return;
     const int nA = list.nA;
-    const int r_begin = (int)((int64_t)j * list.n_hp / ranges), r_end = (int)((int64_t)(j + 1) * list.n_hp / ranges);
+    const int r_begin = list.begin(j, ranges), r_end = list.begin(j + 1, ranges);
     const int x_begin = r_begin + (r_end - r_begin) * wv / 4, x_end = r_begin + (r_end - r_begin) * (wv + 1) / 4;
 
     SharePages pages = share_pages(v, pair, first_ids, x_begin >> 1);
@@ -514,7 +520,7 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     const int col0 = u.block * (32 * NW);
     if (col0 >= n_cols) return;
     const int nA = list.nA;
-    const int x_begin = (int)((int64_t)j * list.n_hp / ranges), x_end = (int)((int64_t)(j + 1) * list.n_hp / ranges), last = x_end - 1;
+    const int x_begin = list.begin(j, ranges), x_end = list.begin(j + 1, ranges), last = x_end - 1;
 
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -533,14 +539,6 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
         const uint16_t* qrow = q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D + half * 8;
 #pragma unroll
         for (int sl = 0; sl < NS; ++sl) qb[sl] = *reinterpret_cast<const bf16x8*>(qrow + sl * 16);
-    }
-    RingGates gates = {0, 0u};
-    int least = 0;                                           // the smallest place of the wave's columns: it sees most of the ring
-    if (x_end > nA) {
-        gates = ring_gates(v, list, x_begin, x_end);
-        least = sr.place;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) least = min(least, __shfl_xor(least, o));
     }
     auto base_of = [&](int x) -> const uint16_t* { return half_page_at(v, list, pages, min(x, last)); };
 
@@ -571,6 +569,14 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     constexpr int kAhead = NW == 8 ? 3 : 4;
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) stage_step(s * kHps, s * kHps);
+    RingGates gates = {0, 0u};
+    int least = 0;                                           // the smallest place of the wave's columns: it sees most of the ring
+    if (x_end > nA) {
+        gates = ring_gates(v, list, x_begin, x_end);
+        least = sr.place;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) least = min(least, __shfl_xor(least, o));
+    }
     f32x16 acc[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i)
