@@ -216,7 +216,15 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_forward(SpkvRope a, Ro
     __syncthreads();
     for (; r < n_rows; r += RPP) {
         const RowPlace here = at;
-        const Raw8<T> h0 = x0, h1 = x1;
+        T* o = row_of<T>(a.out, here);
+        float f0[8], f1[8];
+        if (here.kind < 2) {
+            widen8(x0, f0);
+            widen8(x1, f1);
+        } else {                                               // values: as they are
+            store8(x0, o + rc.c0 * 8);
+            store8(x1, o + rc.c1 * 8);
+        }
         if (r + RPP < n_rows) {                                // the next row travels meanwhile
             hh += RPP;
             while (hh >= a.n_heads) {
@@ -228,58 +236,54 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_forward(SpkvRope a, Ro
             load8(x0, p + rc.c0 * 8);
             load8(x1, p + rc.c1 * 8);
         }
-        T* o = row_of<T>(a.out, here);
-        Raw8<T> y0 = h0, y1 = h1;
-        // (values share the exchanges of the sum: lanes of a wave may hold rows of different kinds)
-        float f0[8], f1[8], r_norm = 1.f;
-        widen8(h0, f0);
-        widen8(h1, f1);
+        if (here.kind == 2) continue;                          // (a row's lanes go the same way)
         if (NORM) {
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum += f0[e] * f0[e] + f1[e] * f1[e];
-            sum = row_sum<LPR>(sum);
-            r_norm = rsqrtf(sum * (1.f / D) + a.eps);
-        }
-        if (here.kind < 2) {
-            if (NORM) {
-                const float* w = s_w + here.kind * D;
+            const float r_norm = rsqrtf(row_sum<LPR>(sum) * (1.f / D) + a.eps);
+            const float* w = s_w + here.kind * D;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    f0[e] *= r_norm * w[rc.c0 * 8 + e];
-                    f1[e] *= r_norm * w[rc.c1 * 8 + e];
-                }
+            for (int e = 0; e < 8; ++e) {
+                f0[e] *= r_norm * w[rc.c0 * 8 + e];
+                f1[e] *= r_norm * w[rc.c1 * 8 + e];
             }
-            rotate16<D, ADJ, false>(rc, a.rot_dim, s_cs + (here.token - first) * (a.rot_dim >> 1), f0, f1);
-            round8(y0, f0);
-            round8(y1, f1);
         }
-        store8(y0, o + rc.c0 * 8);
-        store8(y1, o + rc.c1 * 8);
+        rotate16<D, ADJ, false>(rc, a.rot_dim, s_cs + (here.token - first) * (a.rot_dim >> 1), f0, f1);
+        Raw8<T> y;
+        round8(y, f0);
+        store8(y, o + rc.c0 * 8);
+        round8(y, f1);
+        store8(y, o + rc.c1 * 8);
     }
 }
 
 // Gradients.  in: those of the rotated heads (and values), x: the forward's inputs (NORM), out: the
 // gradients of those.  A workgroup walks every gridDim-th tile and keeps its share of the weights'
-// gradients in registers, sixteen columns a lane for queries and for keys; they meet in LDS at
+// gradients, sixteen columns a lane: those of queries in registers, those of the fewer keys in LDS (both in
+// registers left room for three waves on a SIMD instead of four).  They meet in LDS at
 // the end and leave as one partial row of 2 D floats, which spkv_rope_weight_sum adds up in a
 // fixed order (no atomics: equal calls give equal bits).
 template <typename T, int D, bool ADJ, bool NORM>
-__global__ __launch_bounds__(kRopeThreads) void spkv_rope_backward(SpkvRope a, RopeTable table) {
+__global__ __launch_bounds__(kRopeThreads, sizeof(T) == 2 ? 4 : 3) void spkv_rope_backward(SpkvRope a, RopeTable table) {
     constexpr int LPR = D / 16, RPP = kRopeThreads / LPR;
     extern __shared__ __attribute__((aligned(16))) float s_rope[];
     float* s_w = s_rope;
-    float2* s_cs = reinterpret_cast<float2*>(s_rope + (NORM ? 2 * D : 0));
+    f32x4* s_dwk = reinterpret_cast<f32x4*>(s_rope + 2 * D) + threadIdx.x;       // this lane's four units, kRopeThreads apart
+    float2* s_cs = reinterpret_cast<float2*>(s_rope + (NORM ? 2 * D + 16 * kRopeThreads : 0));
     const int tid = threadIdx.x, c = tid & (LPR - 1), lane_row = tid / LPR;
     const RowChunks rc = row_chunks<D, ADJ>(c, a.rot_dim);
-    if (NORM)
+    if (NORM) {
         for (int i = tid; i < 2 * D; i += kRopeThreads) {
             const float* w = i < D ? a.q_weight : a.k_weight;
             s_w[i] = w != nullptr ? w[i & (D - 1)] : 1.f;
         }
-    float dwq[16], dwk[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) dwq[e] = dwk[e] = 0.f;
+        for (int i = 0; i < 4; ++i) s_dwk[i * kRopeThreads] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    float dwq[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dwq[e] = 0.f;
 
     for (int tile = blockIdx.x; tile < a.n_tiles; tile += gridDim.x) {
         const int row0 = tile * a.tile_rows, n_rows = min(a.tile_rows, a.n_rows - row0);
@@ -305,7 +309,19 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_backward(SpkvRope a, R
         __syncthreads();
         for (; r < n_rows; r += RPP) {
             const RowPlace here = at;
-            const Raw8<T> hg0 = g0, hg1 = g1, hx0 = x0, hx1 = x1;
+            T* o = row_of<T>(a.out, here);
+            float f0[8], f1[8], v0[8], v1[8];
+            if (here.kind < 2) {
+                widen8(g0, f0);
+                widen8(g1, f1);
+                if (NORM) {
+                    widen8(x0, v0);
+                    widen8(x1, v1);
+                }
+            } else {                                           // values: as they are
+                store8(g0, o + rc.c0 * 8);
+                store8(g1, o + rc.c1 * 8);
+            }
             if (r + RPP < n_rows) {
                 hh += RPP;
                 while (hh >= a.n_heads) {
@@ -314,17 +330,10 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_backward(SpkvRope a, R
                 }
                 load_row();
             }
-            T* o = row_of<T>(a.out, here);
-            Raw8<T> y0 = hg0, y1 = hg1;
             if (here.kind < 2) {                               // a row's lanes go the same way
-                float f0[8], f1[8];
-                widen8(hg0, f0);
-                widen8(hg1, f1);
                 rotate16<D, ADJ, true>(rc, a.rot_dim, s_cs + (here.token - first) * (a.rot_dim >> 1), f0, f1);
                 if (NORM) {
-                    float v0[8], v1[8], square = 0.f, dot = 0.f;
-                    widen8(hx0, v0);
-                    widen8(hx1, v1);
+                    float square = 0.f, dot = 0.f;
                     const float* w = s_w + here.kind * D;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -336,27 +345,44 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_backward(SpkvRope a, R
                     dot = row_sum<LPR>(dot);
                     const float rn = rsqrtf(square * (1.f / D) + a.eps);
                     const float back = rn * rn * dot * (1.f / D);
-                    const bool is_q = here.kind == 0;
+                    if (here.kind == 0) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            dwq[e] += f0[e] * (v0[e] * rn);
+                            dwq[8 + e] += f1[e] * (v1[e] * rn);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            f32x4 p0 = s_dwk[i * kRopeThreads], p1 = s_dwk[(2 + i) * kRopeThreads];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                p0[e] += f0[4 * i + e] * (v0[4 * i + e] * rn);
+                                p1[e] += f1[4 * i + e] * (v1[4 * i + e] * rn);
+                            }
+                            s_dwk[i * kRopeThreads] = p0;
+                            s_dwk[(2 + i) * kRopeThreads] = p1;
+                        }
+                    }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float p0 = f0[e] * (v0[e] * rn), p1 = f1[e] * (v1[e] * rn);
-                        dwq[e] += is_q ? p0 : 0.f;
-                        dwq[8 + e] += is_q ? p1 : 0.f;
-                        dwk[e] += is_q ? 0.f : p0;
-                        dwk[8 + e] += is_q ? 0.f : p1;
                         f0[e] = rn * (f0[e] * w[rc.c0 * 8 + e] - v0[e] * back);
                         f1[e] = rn * (f1[e] * w[rc.c1 * 8 + e] - v1[e] * back);
                     }
                 }
-                round8(y0, f0);
-                round8(y1, f1);
+                Raw8<T> y;
+                round8(y, f0);
+                store8(y, o + rc.c0 * 8);
+                round8(y, f1);
+                store8(y, o + rc.c1 * 8);
             }
-            store8(y0, o + rc.c0 * 8);
-            store8(y1, o + rc.c1 * 8);
         }
     }
     if (!NORM || a.partial == nullptr) return;
     // rows of a wave meet by exchanges, waves in LDS
+    float dwk[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dwk[e] = s_dwk[(e >> 2) * kRopeThreads][e & 3];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
 #pragma unroll
@@ -385,23 +411,25 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_backward(SpkvRope a, R
     }
 }
 
-// Column sums of the partial rows: a workgroup takes eight columns, 32 threads each.
+// Column sums of the partial rows: a workgroup takes sixteen columns, four a thread, its threads every 64th row.
 template <int D>
 __global__ __launch_bounds__(256) void spkv_rope_weight_sum(const float* __restrict__ partial, int n,
                                                             float* __restrict__ dq, float* __restrict__ dk) {
-    __shared__ float s[4][8];
-    const int col = (int)blockIdx.x * 8 + (threadIdx.x & 7), lane = threadIdx.x & 63;
-    float sum = 0.f;
-#pragma unroll 8
-    for (int r = threadIdx.x >> 3; r < n; r += 32) sum += partial[(size_t)r * 2 * D + col];
+    __shared__ f32x4 s[4][4];
+    const int unit = threadIdx.x & 3, lane = threadIdx.x & 63, col = ((int)blockIdx.x * 4 + unit) * 4;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 16
+    for (int r = threadIdx.x >> 2; r < n; r += 64) sum += *reinterpret_cast<const f32x4*>(partial + (size_t)r * 2 * D + col);
 #pragma unroll
-    for (int o = 8; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-    if (lane < 8) s[threadIdx.x >> 6][lane] = sum;
+    for (int o = 4; o < 64; o <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], o);
+    if (lane < 4) s[threadIdx.x >> 6][lane] = sum;
     __syncthreads();
-    if (threadIdx.x < 8) {
+    if (threadIdx.x < 4) {
         sum = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
         float* out = col < D ? dq : dk;
-        if (out != nullptr) out[col & (D - 1)] = sum;
+        if (out != nullptr) *reinterpret_cast<f32x4*>(out + (col & (D - 1))) = sum;
     }
 }
 
@@ -434,10 +462,10 @@ static hipError_t launch_rope(SpkvRope a, const RopeTable& table, bool backward,
         return hipGetLastError();
     }
     const int blocks = spkv_rope_backward_blocks(a.n_rows, a.n_heads, D);
-    if (NORM) lds = std::max(lds, (size_t)(kRopeThreads / 64) * 2 * D * sizeof(float));
+    if (NORM) lds += (size_t)kRopeThreads * 16 * sizeof(float);      // (also room for what the waves meet in)
     spkv_rope_backward<T, D, ADJ, NORM><<<dim3(blocks), dim3(kRopeThreads), lds, s>>>(a, table);
     if (NORM && a.partial != nullptr)
-        spkv_rope_weight_sum<D><<<dim3(2 * D / 8), dim3(256), 0, s>>>(a.partial, blocks, a.dq_weight, a.dk_weight);
+        spkv_rope_weight_sum<D><<<dim3(2 * D / 16), dim3(256), 0, s>>>(a.partial, blocks, a.dq_weight, a.dk_weight);
     return hipGetLastError();
 }
 
