@@ -7,7 +7,10 @@ memory (the arena and the tensors) and the current stream.
 from __future__ import annotations
 
 import ctypes as C
+import itertools
 import os
+import struct
+import threading
 
 import torch
 
@@ -298,12 +301,24 @@ def _heads(t, dtype, shape, name):
 _NO_HEADS = (0, 0, 0)
 
 
-def _block(sets):
-    """Sets of heads as one block of memory, and the address of each (None where there is none)."""
-    flat = [x for h in sets for x in h]
-    block = (C.c_int64 * len(flat))(*flat)
-    at = C.addressof(block)
-    return block, [None if h is _NO_HEADS else at + 24 * i for i, h in enumerate(sets)]
+class _Block(threading.local):
+    """Memory for the sets of heads of a call (the calls read them before they return): each thread's own."""
+
+    def __init__(self):
+        self.block = (C.c_int64 * 24)()
+        at = C.addressof(self.block)
+        self.at = [at + 24 * i for i in range(8)]
+
+
+_block = _Block()
+_PACK = {n: struct.Struct(f"{3 * n}q").pack_into for n in (6, 8)}
+
+
+def _packed(sets):
+    """Address of each set of heads (None where there is none)."""
+    block = _block
+    _PACK[len(sets)](block.block, 0, *itertools.chain.from_iterable(sets))
+    return [None if h is _NO_HEADS else at for h, at in zip(sets, block.at)]
 
 
 def _rope_call(q, k, v, positions, rope, q_weight, k_weight, eps, names):
@@ -334,9 +349,11 @@ def _rope_out(out, q, v, n, hq, hk, d):
     """Tensors to write: those given, or new dense ones."""
     if out is not None:
         return (out[0], out[1], None) if v is None else out
-    dtype, device = q.dtype, q.device
-    return (torch.empty((n, hq, d), dtype=dtype, device=device), torch.empty((n, hk, d), dtype=dtype, device=device),
-            None if v is None else torch.empty((n, hk, d), dtype=dtype, device=device))
+    dtype, device = q.dtype, q.device          # (empty_strided takes less host time than empty)
+    few, of_few = (n, hk, d), (hk * d, d, 1)
+    return (torch.empty_strided((n, hq, d), (hq * d, d, 1), dtype=dtype, device=device),
+            torch.empty_strided(few, of_few, dtype=dtype, device=device),
+            None if v is None else torch.empty_strided(few, of_few, dtype=dtype, device=device))
 
 
 def qk_norm_rope(q, k, positions, rope, q_weight=None, k_weight=None, eps=None, v=None, out=None):
@@ -348,7 +365,7 @@ def qk_norm_rope(q, k, positions, rope, q_weight=None, k_weight=None, eps=None, 
     out, dtype = _rope_out(out, q, v, n, hq, hk, d), q.dtype
     outs = [_heads(out[0], dtype, (n, hq, d), "out[0]"), _heads(out[1], dtype, (n, hk, d), "out[1]"),
             _NO_HEADS if v is None else _heads(out[2], dtype, (n, hk, d), "out[2]")]
-    block, at = _block(ins + outs)
+    at = _packed(ins + outs)
     _check((_LIB or load_library()).spkv_qk_norm_rope(at[0], at[1], at[2], qw, kw, eps, pp, rope.struct, _HEAD_TYPES[dtype],
                                                       n, hq, hk, at[3], at[4], at[5], _stream()), "spkv_qk_norm_rope")
     return tuple(out[:2]) if v is None else tuple(out)
@@ -373,7 +390,7 @@ def qk_norm_rope_backward(dq, dk, positions, rope, q=None, k=None, q_weight=None
             raise ValueError("q, k: the forward's inputs are needed with a norm")
         xs = [_heads(q, dtype, (n, hq, d), "q"), _heads(k, dtype, (n, hk, d), "k")]
         if want_weights is None or want_weights:
-            weights = tuple(torch.empty((2, d), dtype=torch.float32, device=dq.device).unbind(0))
+            weights = torch.empty_strided((2, d), (d, 1), dtype=torch.float32, device=dq.device).unbind(0)
     elif want_weights:
         raise ValueError("want_weights: there are no weights without a norm")
     lib = load_library()
@@ -382,13 +399,13 @@ def qk_norm_rope_backward(dq, dk, positions, rope, q=None, k=None, q_weight=None
                                 dtype=torch.uint8, device=dq.device)
     if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous uint8 device tensor")
-    block, at = _block(ins + xs + outs)
+    at = _packed(ins + xs + outs)
     dqw, dkw = (weights[0].data_ptr(), weights[1].data_ptr()) if weights else (None, None)
     ws, ws_bytes = (workspace.data_ptr(), workspace.numel()) if workspace is not None else (None, 0)
     _check(lib.spkv_qk_norm_rope_backward(*at[:5], qw, kw, eps, pp, rope.struct, _HEAD_TYPES[dtype], n, hq, hk, *at[5:],
                                           dqw, dkw, ws, ws_bytes, _stream()), "spkv_qk_norm_rope_backward")
     first = () if given else tuple(out[:2]) if dv is None else tuple(out)
-    return first + weights
+    return first + tuple(weights)
 
 
 def _check(code, where):
@@ -663,7 +680,7 @@ class SPKVCache:
         if sharing.batch != self.cfg.batch:
             raise ValueError(f"sharing: made for {sharing.batch} sequences, the cache has {self.cfg.batch}")
         if workspace is None:
-            workspace = torch.empty(sharing.workspace_bytes(rows), dtype=torch.uint8, device=device)
+            workspace = torch.empty_strided((sharing.workspace_bytes(rows),), (1,), dtype=torch.uint8, device=device)
         if workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous uint8 device tensor")
         return workspace
@@ -677,10 +694,10 @@ class SPKVCache:
         qp = _dev_ptr(q, torch.bfloat16, shape, "q")
         workspace = self._share_workspace(sharing, cfg.batch, workspace, q.device)
         if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+            out = torch.empty_strided(shape, (shape[1] * shape[2], shape[2], 1), dtype=torch.bfloat16, device=q.device)
         op = _dev_ptr(out, torch.bfloat16, shape, "out")
         if lse is None and want_lse:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
+            lse = torch.empty_strided(shape[:2], (shape[1], 1), dtype=torch.float32, device=q.device)
         lp = _dev_ptr(lse, torch.float32, shape[:2], "lse") if lse is not None else None
         _check(self.lib.spkv_decode_attention_shared(self.handle, sharing.prefix.handle, sharing.prefix_of, qp, op, lp,
                                                      float(sm_scale), workspace.data_ptr(), workspace.numel(),
@@ -701,9 +718,9 @@ class SPKVCache:
         zp = _dev_ptr(own_lse, torch.float32, shape[:2], "own_lse")
         workspace = self._share_workspace(sharing, max(total, 1), workspace, q.device)
         if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+            out = torch.empty_strided(shape, (shape[1] * shape[2], shape[2], 1), dtype=torch.bfloat16, device=q.device)
         if lse is None:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
+            lse = torch.empty_strided(shape[:2], (shape[1], 1), dtype=torch.float32, device=q.device)
         op = _dev_ptr(out, torch.bfloat16, shape, "out")
         lp = _dev_ptr(lse, torch.float32, shape[:2], "lse")
         _check(self.lib.spkv_prefix_attention(sharing.prefix.handle, self.handle, sharing.prefix_of, qp, cu, int(appended), ip, zp,

@@ -142,6 +142,49 @@ __device__ __forceinline__ bf16x8 keep_keys(bf16x8 x, unsigned seen) {
     return __builtin_bit_cast(bf16x8, u);
 }
 
+// Where some columns of a wave see a key and others do not, infinities and NaN among its values would reach the others
+// too, with a weight of zero: they are left out of the products (bounded_keys) and added at the end to the columns that
+// do see them (add_unbounded: a weight above zero leaves an infinity and a NaN what they are).
+// (An infinity that all see may come out as a NaN: the second part of its weight may be negative.)
+__device__ __forceinline__ bf16x8 bounded_keys(bf16x8 x, unsigned some, bool& found) {
+    const uint4 u = __builtin_bit_cast(uint4, x);
+    unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const bool lo = (w[e] & 0x7f80u) == 0x7f80u && ((some >> (2 * e)) & 1u);
+        const bool hi = (w[e] & 0x7f800000u) == 0x7f800000u && ((some >> (2 * e + 1)) & 1u);
+        w[e] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+        found = found || lo || hi;
+    }
+    return __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+}
+// Half-pages x_begin .. x_end - 1 of a ring for a lane's column, of a token at `place`; least, most: over the wave's
+// columns.  add(u) for u = 0 .. N - 1 gives sum u, which is element dim(u) of the head.
+template <int D, int N, class Dim, class Sum>
+__device__ __forceinline__ void add_unbounded(const SpkvView& v, const ShareList& s, const RingGates& r, int x_begin, int x_end,
+                                              int place, int least, int most, Dim dim, Sum sum) {
+#pragma unroll 1
+    for (int t = max(x_begin - s.nA, 0); t < x_end - s.nA; ++t) {
+        const uint16_t* values = ring_page(v, s.pair, t >> 1) + (2 * (t & 1) + 1) * kHalfTokens * D;
+#pragma unroll 1
+        for (int k0 = 0; k0 < kHalfTokens; k0 += 8) {
+            const unsigned on = gates_of(v, s, r, t, k0);
+            const unsigned mine = ring_seen(v, s, on, t * kHalfTokens + k0, place);
+            const unsigned some = ring_seen(v, s, on, t * kHalfTokens + k0, least) & ~ring_seen(v, s, on, t * kHalfTokens + k0, most);
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+                if (!((some >> e) & 1u)) continue;
+#pragma unroll
+                for (int u = 0; u < N; ++u) {
+                    const int d = dim(u);
+                    const unsigned x = values[(d >> 4) * 512 + (k0 * 2 + (d & 15)) * 8 + e];
+                    if ((x & 0x7f80u) == 0x7f80u && ((mine >> e) & 1u)) sum(u) += __builtin_bit_cast(float, x << 16);
+                }
+            }
+        }
+    }
+}
+
 // The sequences' cache as the helpers of spkv_device.h take it: its lists, the shape of the prompts' one.
 __device__ __forceinline__ SpkvView own_view(const SpkvShareOwn& o, const SpkvView& prompts) {
     SpkvView v = prompts;
@@ -332,8 +375,9 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
         for (int db = 0; db < NB; ++db) va[db] = load_stream_b128(page + kHalfTokens * D + lane * 8 + db * 512);
     };
     bf16x8 q1[NQ == 1 ? NS : 1];                             // the query operands of one group; of several they lie in LDS
-    int place[NQ], least = 0;
+    int place[NQ], least = 0, most = 0;                      // of the wave's columns, the smallest sees most of the ring
     const bool ring = x_end > nA;
+    bool unbounded = false;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
         const int c = i * 16 + n;
@@ -358,11 +402,19 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
     RingGates gates = {0, 0u};
     if (ring) {
         gates = ring_gates(v, list, x_begin, x_end);
-        least = place[0];
+        least = most = place[0];
 #pragma unroll
-        for (int i = 1; i < NQ; ++i) least = min(least, place[i]);
+        for (int i = 1; i < NQ; ++i) {
+            least = min(least, place[i]);
+            most = max(most, place[i]);
+        }
 #pragma unroll
-        for (int o = 1; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o));
+        for (int o = 1; o < 16; o <<= 1) {
+            least = min(least, __shfl_xor(least, o));
+            most = max(most, __shfl_xor(most, o));
+        }
+        least = __builtin_amdgcn_readfirstlane(least);
+        most = __builtin_amdgcn_readfirstlane(most);
     }
     f32x4 acc[NQ][NB];
     float m[NQ], l[NQ];
@@ -409,6 +461,11 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
             }
 #pragma unroll
             for (int db = 0; db < NB; ++db) va[db] = keep_keys(va[db], any);
+            if (x >= nA && least != most) {
+                const unsigned some = any & ~ring_seen(v, list, on, at0, most);
+#pragma unroll
+                for (int db = 0; db < NB; ++db) va[db] = bounded_keys(va[db], some, unbounded);
+            }
         }
         f32x8 p[NQ];
         float psum[NQ];
@@ -458,6 +515,10 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
     }
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
+        if (__builtin_expect(__ballot(unbounded) != 0ull, 0))
+            add_unbounded<D, 4 * NB>(v, list, gates, x_begin, x_end, place[i], least, most,
+                                     [&](int u) { return (u >> 2) * 16 + kc * 4 + (u & 3); },
+                                     [&](int u) -> float& { return reinterpret_cast<float*>(&acc[i][u >> 2])[u & 3]; });
         l[i] += __shfl_xor(l[i], 16);
         l[i] += __shfl_xor(l[i], 32);
         float* pa = s_acc[wv] + (i * 16 + n) * kRow + kc * 4;
@@ -497,7 +558,7 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
 // pipeline this is); with four waves a step is one half-page and two workgroups share a compute unit.
 
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 2 ? 1 : 2, 2)))
 void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvShareCut cut, SpkvShareTable table,
                        SpkvShareRows rows, SpkvShareOwn own) {
     constexpr int NS = D / 16, NB = D / 32;
@@ -570,12 +631,18 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) stage_step(s * kHps, s * kHps);
     RingGates gates = {0, 0u};
-    int least = 0;                                           // the smallest place of the wave's columns: it sees most of the ring
+    int least = 0, most = 0;                                 // places of the wave's columns: the smallest sees most of the ring
+    bool unbounded = false;
     if (x_end > nA) {
         gates = ring_gates(v, list, x_begin, x_end);
-        least = sr.place;
+        least = most = sr.place;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) least = min(least, __shfl_xor(least, o));
+        for (int o = 1; o < 32; o <<= 1) {
+            least = min(least, __shfl_xor(least, o));
+            most = max(most, __shfl_xor(most, o));
+        }
+        least = __builtin_amdgcn_readfirstlane(least);
+        most = __builtin_amdgcn_readfirstlane(most);
     }
     f32x16 acc[NB];
 #pragma unroll
@@ -597,21 +664,23 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
         for (int sl = 1; sl < NS; ++sl) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[sl], qb[sl], s, 0, 0, 0);
     };
     // Excluded keys to -inf: past the list's end, past the ring's, gate off and outside the column's window.
-    // Returns the keys (bit 8 g + e: 16 g + 8 half + e) that some column of the wave sees.
+    // Returns the keys (bit 8 g + e: 16 g + 8 half + e) that some column of the wave sees, and from bit 16 on those of
+    // them that not all do.
     auto mask = [&](f32x16& s, int x) -> unsigned {
         unsigned seen = 0u;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const int k0 = 16 * g + 8 * half;
-            unsigned ok, any;
+            unsigned ok, any, some = 0u;
             if (x < nA) {
                 ok = any = bits_below(list.L - x * kHalfTokens - k0);
             } else {
                 const unsigned on = gates_of(v, list, gates, x - nA, k0);
                 ok = ring_seen(v, list, on, (x - nA) * kHalfTokens + k0, sr.place);
                 any = ring_seen(v, list, on, (x - nA) * kHalfTokens + k0, least);
+                some = any & ~ring_seen(v, list, on, (x - nA) * kHalfTokens + k0, most);
             }
-            seen |= any << (8 * g);
+            seen |= any << (8 * g) | some << (16 + 8 * g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[8 * g + e] = ((ok >> e) & 1u) ? s[8 * g + e] : SPKV_NEG_INF;
         }
@@ -684,6 +753,13 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
                 va[0][db] = keep_keys(va[0][db], seen);
                 va[1][db] = keep_keys(va[1][db], seen >> 8);
             }
+            if (least != most) {
+#pragma unroll
+                for (int db = 0; db < NB; ++db) {
+                    va[0][db] = bounded_keys(va[0][db], seen >> 16, unbounded);
+                    va[1][db] = bounded_keys(va[1][db], seen >> 24, unbounded);
+                }
+            }
         }
         l += psum;
         accumulate(0);
@@ -731,6 +807,10 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     }
     wait_loads_but<0>();
 
+    if (__builtin_expect(__ballot(unbounded) != 0ull, 0))
+        add_unbounded<D, 16 * NB>(v, list, gates, x_begin, x_end, sr.place, least, most,
+                                  [&](int u) { return (u >> 4) * 32 + ((u >> 2) & 3) * 8 + half * 4 + (u & 3); },
+                                  [&](int u) -> float& { return reinterpret_cast<float*>(&acc[u >> 4])[u & 15]; });
     l += __shfl_xor(l, 32);
     if (valid && half == 0) part_ml[pc] = make_float2(m, l);
     // The sums leave through LDS, a column's row at a time (straight from the registers every store touched 32 rows,
@@ -794,7 +874,7 @@ __global__ __launch_bounds__(256, 8) void spkv_prefix_merge(SpkvShareCut cut, Sp
             *reinterpret_cast<uint2*>(out + id * D + d) = ob;
             if (lse != nullptr && d == 0) lse[id] = z;
         }
-        if (z > SPKV_NEG_INF) {
+        if (z != SPKV_NEG_INF) {                             // (a NaN shows)
             M = z * 1.4426950408889634f;
             den = 1.f;
             num = (f32x4){__builtin_bit_cast(float, ob.x << 16), __builtin_bit_cast(float, ob.x & 0xffff0000u),
@@ -826,7 +906,7 @@ __global__ __launch_bounds__(256, 8) void spkv_prefix_merge(SpkvShareCut cut, Sp
         num *= so;
 #pragma unroll
         for (int u = 0; u < kFold; ++u)
-            if (r0 + u * S < parts && x[u].x > SPKV_NEG_INF) {       // (a range without keys has written no sums)
+            if (r0 + u * S < parts && (x[u].x != SPKV_NEG_INF || x[u].y != 0.f)) {       // (a range without keys has written no sums)
                 const float sc = __builtin_amdgcn_exp2f(x[u].x - m_ref);
                 num += a[u] * sc;
                 den += x[u].y * sc;
@@ -854,14 +934,14 @@ __global__ __launch_bounds__(256, 8) void spkv_prefix_merge(SpkvShareCut cut, Sp
         M = top;
     }
     if (!exists || (ranges == 0 && own.part == nullptr)) return;
-    const float inv = den > 0.f ? 1.0f / den : 0.f;          // (a row that sees no key at all: zeros)
+    const float inv = den == 0.f ? 0.f : 1.0f / den;         // (a row that sees no key at all: zeros; a NaN shows)
     uint2 packed;
     packed.x = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)(num[0] * inv)) |
                ((unsigned)__builtin_bit_cast(uint16_t, (__bf16)(num[1] * inv)) << 16);
     packed.y = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)(num[2] * inv)) |
                ((unsigned)__builtin_bit_cast(uint16_t, (__bf16)(num[3] * inv)) << 16);
     *reinterpret_cast<uint2*>(out + id * D + d) = packed;
-    if (lse != nullptr && d == 0) lse[id] = den > 0.f ? (M + log2f(den)) * 0.6931471805599453f : SPKV_NEG_INF;
+    if (lse != nullptr && d == 0) lse[id] = den == 0.f ? SPKV_NEG_INF : (M + log2f(den)) * 0.6931471805599453f;
 }
 
 // Rows of a call with several tokens a sequence, grouped by prompt: one workgroup per sequence.

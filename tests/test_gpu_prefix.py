@@ -355,3 +355,55 @@ def test_captured_steps_replay_as_sequences_grow():
             into[:] = [torch.cat([into[b], t[b:b + 1].double().cpu()]) for b in range(3)]
         s.held = [n + 1 for n in s.held]
         s.check(out, lse, s.reference(q, [1] * 3), f"replay {step}")
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("hq,hk,d,batch", [(4, 4, 64, 3), (8, 2, 128, 7), (8, 2, 128, 14), (16, 2, 64, 15), (16, 1, 128, 20)])
+def test_what_one_row_sees_does_not_show_in_another(hq, hk, d, batch, bad):
+    """Keys with their gate off that are still inside the window of some sequences, their values not finite: the
+    sequences that see them get them, the others what they would without."""
+    own = [1 + (5 * b) % 60 for b in range(batch)]
+    s = Setup([0], own, [0] * batch, hq, hk, d, window=48, keep=0.0, extra=400, seed=batch)
+    k, v, f = s.tokens([300])
+    f = s.randn(300, hk) - 9.0
+    f[290:] += 18.0
+    there = [260, 275, 281]
+    for i, at in enumerate(there):
+        v[at, :, 5 * i::7] = bad
+    s._feed(s.prefix, s.prompt, [300], (k, v, f))
+    q = s.randn(batch, hq, d).bfloat16()
+    out, lse = s.cache.decode_attention_shared(s.sharing, q, want_lse=True)
+    got = out.clone()
+    for b in range(batch):
+        for i, at in enumerate(there):
+            if 300 + own[b] - 1 - at < 48:
+                x = got[b, :, 5 * i::7]
+                assert not torch.isfinite(x).any(), (b, at)      # (weights in two parts: an infinity may come out as a NaN)
+                x.zero_()
+    assert torch.isfinite(got).all()
+    s.prompt[1][0] = s.prompt[1][0].nan_to_num(0.0, 0.0, 0.0)
+    ref = s.reference(q, [1] * batch)
+    for b in range(batch):
+        for i, at in enumerate(there):
+            if 300 + own[b] - 1 - at < 48:
+                ref[0][b, :, 5 * i::7] = 0.0
+    s.check(got, lse, ref, "finite part")
+
+
+def test_a_query_that_is_not_a_number_shows():
+    """... in its own rows alone, in the output and in lse, whether or not the sequence has keys of its own."""
+    s = Setup([500, 40], [3, 80, 7, 1], [0, 0, 1, 0], 8, 2, 64)
+    q, out, lse = s.decode()
+    q[1, 3, 5] = float("nan")
+    bad, bad_lse = s.cache.decode_attention_shared(s.sharing, q, want_lse=True)
+    assert torch.isnan(bad[1, 3]).all() and torch.isnan(bad_lse[1, 3])
+    bad[1, 3], bad_lse[1, 3] = out[1, 3], lse[1, 3]
+    assert torch.equal(bad, out) and torch.equal(bad_lse, lse)
+    own, own_lse = s.randn(4, 8, 64).bfloat16(), s.randn(4, 8)
+    own_lse[2] = -math.inf
+    bad, bad_lse = s.cache.prefix_attention(s.sharing, q, None, own, own_lse)
+    assert torch.isnan(bad[1, 3]).all() and torch.isnan(bad_lse[1, 3])
+    assert torch.isfinite(bad[0]).all() and torch.isfinite(bad[2:]).all()
+    own_lse[0, 2] = float("nan")
+    bad, bad_lse = s.cache.prefix_attention(s.sharing, q, None, own, own_lse)
+    assert torch.isnan(bad[0, 2]).all() and torch.isnan(bad_lse[0, 2])
