@@ -142,47 +142,84 @@ __device__ __forceinline__ bf16x8 keep_keys(bf16x8 x, unsigned seen) {
     return __builtin_bit_cast(bf16x8, u);
 }
 
-// Where some columns of a wave see a key and others do not, infinities and NaN among its values would reach the others
-// too, with a weight of zero: they are left out of the products (bounded_keys) and added at the end to the columns that
-// do see them (add_unbounded: a weight above zero leaves an infinity and a NaN what they are).
-// (An infinity that all see may come out as a NaN: the second part of its weight may be negative.)
-__device__ __forceinline__ bf16x8 bounded_keys(bf16x8 x, unsigned some, bool& found) {
-    const uint4 u = __builtin_bit_cast(uint4, x);
-    unsigned w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const bool lo = (w[e] & 0x7f80u) == 0x7f80u && ((some >> (2 * e)) & 1u);
-        const bool hi = (w[e] & 0x7f800000u) == 0x7f800000u && ((some >> (2 * e + 1)) & 1u);
-        w[e] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
-        found = found || lo || hi;
-    }
-    return __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+// Where some columns of a wave see a ring key and others do not, an infinity or NaN among its values reaches the others
+// too, with a weight of zero.  A column whose sums are not finite though its weights are, in a range with such keys, is
+// summed up once more, key by key (careful_sums).  Calls, so that the loops keep their registers: with the
+// values looked at and set aside on the way 64 sequences behind 128k took 50.7 us instead of 45.8.  (An infinity that all
+// columns see may come out as a NaN: the second part of its weight may be negative.)
+struct CarefulRange {
+    const uint16_t *pool, *ring;        // pages: of the pool, of this list's ring
+    const float* logit;                 // of the ring
+    const int32_t* pages;               // of the list
+    float theta, scale_log2e;
+    int n_sink, w, n_pages, T, L, held, nA, slot0, x_begin, x_end;
+};
+__device__ __forceinline__ CarefulRange careful_range(const SpkvView& v, const ShareList& s, float scale_log2e, int x_begin,
+                                                      int x_end) {
+    return CarefulRange{v.pool, ring_page(v, s.pair, 0), v.ring_logit + (size_t)s.pair * v.w, v.page_table + (size_t)s.pair * v.pt_cap,
+                        v.theta, scale_log2e, v.n_sink, v.w, v.n_pages, s.T, s.L, s.held, s.nA, s.slot0, x_begin, x_end};
 }
-// Half-pages x_begin .. x_end - 1 of a ring for a lane's column, of a token at `place`; least, most: over the wave's
-// columns.  add(u) for u = 0 .. N - 1 gives sum u, which is element dim(u) of the head.
-template <int D, int N, class Dim, class Sum>
-__device__ __forceinline__ void add_unbounded(const SpkvView& v, const ShareList& s, const RingGates& r, int x_begin, int x_end,
-                                              int place, int least, int most, Dim dim, Sum sum) {
-#pragma unroll 1
-    for (int t = max(x_begin - s.nA, 0); t < x_end - s.nA; ++t) {
-        const uint16_t* values = ring_page(v, s.pair, t >> 1) + (2 * (t & 1) + 1) * kHalfTokens * D;
-#pragma unroll 1
-        for (int k0 = 0; k0 < kHalfTokens; k0 += 8) {
-            const unsigned on = gates_of(v, s, r, t, k0);
-            const unsigned mine = ring_seen(v, s, on, t * kHalfTokens + k0, place);
-            const unsigned some = ring_seen(v, s, on, t * kHalfTokens + k0, least) & ~ring_seen(v, s, on, t * kHalfTokens + k0, most);
-#pragma unroll 1
-            for (int e = 0; e < 8; ++e) {
-                if (!((some >> e) & 1u)) continue;
-#pragma unroll
-                for (int u = 0; u < N; ++u) {
-                    const int d = dim(u);
-                    const unsigned x = values[(d >> 4) * 512 + (k0 * 2 + (d & 15)) * 8 + e];
-                    if ((x & 0x7f80u) == 0x7f80u && ((mine >> e) & 1u)) sum(u) += __builtin_bit_cast(float, x << 16);
-                }
-            }
+__device__ __forceinline__ bool careful_seen(const CarefulRange& r, int at, int place) {          // the ring's slot, by a token there
+    const int age = at - r.slot0 + (at < r.slot0 ? r.w : 0);
+    return age > place || r.logit[at] >= r.theta || r.T - r.w + age < r.n_sink;
+}
+__device__ __forceinline__ float bf16_at(const uint16_t* p) { return __builtin_bit_cast(float, (unsigned)*p << 16); }
+// Is there a key that a token at `least` sees and one at `most` does not, with a value that is not finite?  (The whole wave.)
+template <int D>
+__device__ __attribute__((noinline)) bool careful_needed(CarefulRange r, int least, int most) {
+    bool odd = false;
+    for (int at = max(r.x_begin - r.nA, 0) * kHalfTokens; at < min((r.x_end - r.nA) * kHalfTokens, r.held); ++at) {
+        if (!careful_seen(r, at, least) || careful_seen(r, at, most)) continue;
+        for (int d = threadIdx.x & 63; d < D; d += 64) {
+            const float x = bf16_at(r.ring + (size_t)(at >> 6) * spkv_page_elems(D) + spkv_v_off(D, at & 63, d));
+            odd = odd || !(x - x == 0.f);
         }
     }
+    return __ballot(odd) != 0ull;
+}
+// Sums of the range for the column of a query row (in memory) and place, against its reference m.  (The whole wave.)
+template <int D>
+__device__ __attribute__((noinline)) void careful_sums(CarefulRange r, const uint16_t* qrow, int place, float m, float* sums) {
+    const int lane = threadIdx.x & 63;
+    float q[D / 64], acc[D / 64];
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) {
+        q[e] = bf16_at(qrow + e * 64 + lane);
+        acc[e] = 0.f;
+    }
+    const int end = r.nA * kHalfTokens;                      // place of the ring's slots in the numbering of keys below
+    for (int k = r.x_begin * kHalfTokens; k < r.x_end * kHalfTokens; ++k) {
+        const uint16_t* page;
+        if (k < end) {
+            if (k >= r.L) continue;
+            page = r.pool + (size_t)min(max(r.pages[k >> 6], 0), r.n_pages - 1) * spkv_page_elems(D);
+        } else {
+            if (k - end >= r.held || !careful_seen(r, k - end, place)) continue;
+            page = r.ring + (size_t)((k - end) >> 6) * spkv_page_elems(D);
+        }
+        const int in = (k < end ? k : k - end) & 63;
+        float x = 0.f;
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) x += q[e] * bf16_at(page + spkv_k_off(D, in, e * 64 + lane));
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x, r.scale_log2e, -m));
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) acc[e] += p * bf16_at(page + spkv_v_off(D, in, e * 64 + lane));
+    }
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) sums[e * 64 + lane] = acc[e];
+}
+// Are the weights' sum finite and the n sums not?  (0 * x is a NaN where x is not finite.)
+template <class Acc>
+__device__ __forceinline__ bool odd_sums(const Acc* acc, int n, float l) {
+    Acc t = acc[0] * 0.f;
+#pragma unroll
+    for (int i = 1; i < n; ++i) t += acc[i] * 0.f;
+    float sum = t[0];
+#pragma unroll
+    for (int e = 1; e < (int)(sizeof(Acc) / sizeof(float)); ++e) sum += t[e];
+    return sum != 0.f && l - l == 0.f;
 }
 
 // The sequences' cache as the helpers of spkv_device.h take it: its lists, the shape of the prompts' one.
@@ -377,7 +414,6 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
     bf16x8 q1[NQ == 1 ? NS : 1];                             // the query operands of one group; of several they lie in LDS
     int place[NQ], least = 0, most = 0;                      // of the wave's columns, the smallest sees most of the ring
     const bool ring = x_end > nA;
-    bool unbounded = false;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
         const int c = i * 16 + n;
@@ -461,11 +497,6 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
             }
 #pragma unroll
             for (int db = 0; db < NB; ++db) va[db] = keep_keys(va[db], any);
-            if (x >= nA && least != most) {
-                const unsigned some = any & ~ring_seen(v, list, on, at0, most);
-#pragma unroll
-                for (int db = 0; db < NB; ++db) va[db] = bounded_keys(va[db], some, unbounded);
-            }
         }
         f32x8 p[NQ];
         float psum[NQ];
@@ -515,16 +546,27 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
     }
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        if (__builtin_expect(__ballot(unbounded) != 0ull, 0))
-            add_unbounded<D, 4 * NB>(v, list, gates, x_begin, x_end, place[i], least, most,
-                                     [&](int u) { return (u >> 2) * 16 + kc * 4 + (u & 3); },
-                                     [&](int u) -> float& { return reinterpret_cast<float*>(&acc[i][u >> 2])[u & 3]; });
         l[i] += __shfl_xor(l[i], 16);
         l[i] += __shfl_xor(l[i], 32);
         float* pa = s_acc[wv] + (i * 16 + n) * kRow + kc * 4;
 #pragma unroll
         for (int db = 0; db < NB; ++db) *reinterpret_cast<f32x4*>(pa + db * 16) = acc[i][db];
         if (kc == 0) s_ml[wv][i * 16 + n] = make_float2(m[i], l[i]);
+    }
+    if (ring && least != most) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) odd = odd || odd_sums(acc[i], NB, l[i]);
+        if (__builtin_expect(__ballot(odd) != 0ull, 0)) {
+            const CarefulRange range = careful_range(v, list, scale_log2e, x_begin, x_end);
+            if (careful_needed<D>(range, least, most))
+                for (int c = 0; c < min(16 * NQ, n_cols); ++c) {
+                    const ShareRow sr = share_row(rows, first, c, v.G, v.Hkv, true);
+                    __builtin_amdgcn_wave_barrier();
+                    careful_sums<D>(range, q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D, sr.place, s_ml[wv][c].x,
+                                    s_acc[wv] + c * kRow);
+                }
+        }
     }
     __syncthreads();
     const size_t pc0 = ((size_t)h * cut.slots + j) * cut.n_cols + (size_t)first * v.G;
@@ -632,7 +674,6 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     for (int s = 0; s < kAhead; ++s) stage_step(s * kHps, s * kHps);
     RingGates gates = {0, 0u};
     int least = 0, most = 0;                                 // places of the wave's columns: the smallest sees most of the ring
-    bool unbounded = false;
     if (x_end > nA) {
         gates = ring_gates(v, list, x_begin, x_end);
         least = most = sr.place;
@@ -664,23 +705,21 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
         for (int sl = 1; sl < NS; ++sl) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[sl], qb[sl], s, 0, 0, 0);
     };
     // Excluded keys to -inf: past the list's end, past the ring's, gate off and outside the column's window.
-    // Returns the keys (bit 8 g + e: 16 g + 8 half + e) that some column of the wave sees, and from bit 16 on those of
-    // them that not all do.
+    // Returns the keys (bit 8 g + e: 16 g + 8 half + e) that some column of the wave sees.
     auto mask = [&](f32x16& s, int x) -> unsigned {
         unsigned seen = 0u;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const int k0 = 16 * g + 8 * half;
-            unsigned ok, any, some = 0u;
+            unsigned ok, any;
             if (x < nA) {
                 ok = any = bits_below(list.L - x * kHalfTokens - k0);
             } else {
                 const unsigned on = gates_of(v, list, gates, x - nA, k0);
                 ok = ring_seen(v, list, on, (x - nA) * kHalfTokens + k0, sr.place);
                 any = ring_seen(v, list, on, (x - nA) * kHalfTokens + k0, least);
-                some = any & ~ring_seen(v, list, on, (x - nA) * kHalfTokens + k0, most);
             }
-            seen |= any << (8 * g) | some << (16 + 8 * g);
+            seen |= any << (8 * g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[8 * g + e] = ((ok >> e) & 1u) ? s[8 * g + e] : SPKV_NEG_INF;
         }
@@ -753,13 +792,6 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
                 va[0][db] = keep_keys(va[0][db], seen);
                 va[1][db] = keep_keys(va[1][db], seen >> 8);
             }
-            if (least != most) {
-#pragma unroll
-                for (int db = 0; db < NB; ++db) {
-                    va[0][db] = bounded_keys(va[0][db], seen >> 16, unbounded);
-                    va[1][db] = bounded_keys(va[1][db], seen >> 24, unbounded);
-                }
-            }
         }
         l += psum;
         accumulate(0);
@@ -807,12 +839,9 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     }
     wait_loads_but<0>();
 
-    if (__builtin_expect(__ballot(unbounded) != 0ull, 0))
-        add_unbounded<D, 16 * NB>(v, list, gates, x_begin, x_end, sr.place, least, most,
-                                  [&](int u) { return (u >> 4) * 32 + ((u >> 2) & 3) * 8 + half * 4 + (u & 3); },
-                                  [&](int u) -> float& { return reinterpret_cast<float*>(&acc[u >> 4])[u & 15]; });
     l += __shfl_xor(l, 32);
     if (valid && half == 0) part_ml[pc] = make_float2(m, l);
+    const bool odd = x_end > nA && least != most && odd_sums(acc, NB, l);
     // The sums leave through LDS, a column's row at a time (straight from the registers every store touched 32 rows,
     // 32 bytes each).  16-byte unit x of column col lies at x ^ col: no bank conflicts either way.
     __syncthreads();                                         // the tiles are no longer read
@@ -831,6 +860,17 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
     for (int i = lane / kUnits; i < n_here; i += kColsPerPass)
         *reinterpret_cast<f32x4*>(to + (size_t)i * D + unit * 4) =
             *reinterpret_cast<const f32x4*>(sums + i * D + (unit ^ (i & (D / 4 - 1))) * 4);
+    if (__builtin_expect(__ballot(odd) != 0ull, 0)) {
+        const CarefulRange range = careful_range(v, list, scale_log2e, x_begin, x_end);
+        if (careful_needed<D>(range, least, most)) {
+            __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0): the stores above come first
+            for (int i = 0; i < n_here; ++i) {
+                const ShareRow at = share_row(rows, first, col0 + wv * 32 + i, v.G, v.Hkv, true);
+                careful_sums<D>(range, q + ((size_t)at.row * v.Hq + (size_t)h * v.G + at.head) * D, at.place, __shfl(m, i),
+                                to + (size_t)i * D);
+            }
+        }
+    }
 }
 
 // The join: D / 4 threads own a column (row, head), four consecutive elements each; S such groups share a column,
