@@ -63,10 +63,18 @@ template <typename T> struct Raw8;
 template <> struct Raw8<uint16_t> { uint4 u; };
 template <> struct Raw8<float> { uint4 u, w; };
 
-__device__ __forceinline__ void load8(Raw8<uint16_t>& r, const uint16_t* p) { r.u = *reinterpret_cast<const uint4*>(p); }
+// STREAM (see Streaming below): past the caches' retention.
+template <bool STREAM>
+__device__ __forceinline__ uint4 load_unit(const void* p) {
+    if (STREAM) return __builtin_bit_cast(uint4, load_stream_b128(static_cast<const uint16_t*>(p)));
+    return *static_cast<const uint4*>(p);
+}
+template <bool STREAM>
+__device__ __forceinline__ void load8(Raw8<uint16_t>& r, const uint16_t* p) { r.u = load_unit<STREAM>(p); }
+template <bool STREAM>
 __device__ __forceinline__ void load8(Raw8<float>& r, const float* p) {
-    r.u = *reinterpret_cast<const uint4*>(p);
-    r.w = *reinterpret_cast<const uint4*>(p + 4);
+    r.u = load_unit<STREAM>(p);
+    r.w = load_unit<STREAM>(p + 4);
 }
 __device__ __forceinline__ void store8(const Raw8<uint16_t>& r, uint16_t* p) { *reinterpret_cast<uint4*>(p) = r.u; }
 __device__ __forceinline__ void store8(const Raw8<float>& r, float* p) {
@@ -186,7 +194,7 @@ __device__ __forceinline__ T* row_of(const SpkvRowSet (&s)[3], const RowPlace& r
 }
 
 // One tile of rows: tile_rows consecutive rows of the order (token, head).
-template <typename T, int D, bool ADJ, bool NORM>
+template <typename T, int D, bool ADJ, bool NORM, bool STREAM>
 __global__ __launch_bounds__(kRopeThreads) void spkv_rope_forward(SpkvRope a, RopeTable table) {
     constexpr int LPR = D / 16, RPP = kRopeThreads / LPR;      // lanes per row, rows per pass
     extern __shared__ __attribute__((aligned(16))) float s_rope[];
@@ -204,8 +212,8 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_forward(SpkvRope a, Ro
     if (r < n_rows) {
         at = place_of(a, token, hh);
         const T* p = row_of<const T>(a.in, at);
-        load8(x0, p + rc.c0 * 8);
-        load8(x1, p + rc.c1 * 8);
+        load8<STREAM>(x0, p + rc.c0 * 8);
+        load8<STREAM>(x1, p + rc.c1 * 8);
     }
     if (NORM)
         for (int i = tid; i < 2 * D; i += kRopeThreads) {
@@ -233,8 +241,8 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_forward(SpkvRope a, Ro
             }
             at = place_of(a, token, hh);
             const T* p = row_of<const T>(a.in, at);
-            load8(x0, p + rc.c0 * 8);
-            load8(x1, p + rc.c1 * 8);
+            load8<STREAM>(x0, p + rc.c0 * 8);
+            load8<STREAM>(x1, p + rc.c1 * 8);
         }
         if (here.kind == 2) continue;                          // (a row's lanes go the same way)
         if (NORM) {
@@ -264,7 +272,7 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_forward(SpkvRope a, Ro
 // registers left room for three waves on a SIMD instead of four).  They meet in LDS at
 // the end and leave as one partial row of 2 D floats, which spkv_rope_weight_sum adds up in a
 // fixed order (no atomics: equal calls give equal bits).
-template <typename T, int D, bool ADJ, bool NORM>
+template <typename T, int D, bool ADJ, bool NORM, bool STREAM>
 __global__ __launch_bounds__(kRopeThreads, sizeof(T) == 2 ? 4 : 3) void spkv_rope_backward(SpkvRope a, RopeTable table) {
     constexpr int LPR = D / 16, RPP = kRopeThreads / LPR;
     extern __shared__ __attribute__((aligned(16))) float s_rope[];
@@ -295,12 +303,12 @@ __global__ __launch_bounds__(kRopeThreads, sizeof(T) == 2 ? 4 : 3) void spkv_rop
         auto load_row = [&]() {
             at = place_of(a, token, hh);
             const T* p = row_of<const T>(a.in, at);
-            load8(g0, p + rc.c0 * 8);
-            load8(g1, p + rc.c1 * 8);
+            load8<STREAM>(g0, p + rc.c0 * 8);
+            load8<STREAM>(g1, p + rc.c1 * 8);
             if (NORM && at.kind < 2) {
                 const T* q = row_of<const T>(a.x, at);
-                load8(x0, q + rc.c0 * 8);
-                load8(x1, q + rc.c1 * 8);
+                load8<STREAM>(x0, q + rc.c0 * 8);
+                load8<STREAM>(x1, q + rc.c1 * 8);
             }
         };
         if (r < n_rows) load_row();
@@ -451,22 +459,36 @@ int spkv_rope_backward_blocks(int64_t n_rows, int n_heads, int head_dim) {
     return (int)std::min<int64_t>((n_rows + rows - 1) / rows, kRopeGradBlocks);
 }
 
-template <typename T, int D, bool ADJ, bool NORM>
+// Streaming.  Once a call moves more than the 256 MB of the last cache hold, what it reads is not there and need not
+// stay: loads that ask for no retention then leave the cache to the writes.  bf16, D = 128, gradients of 8192 /
+// 10000 / 16384 tokens (285, 348, 570 MB): 57.8 -> 55.4, 78.7 -> 69.3, 121 -> 101 us; forward of 12000 / 16384 / 32768
+// (295, 403, 805 MB): 51.1 -> 50.2, 82.8 -> 66.1, 157 -> 159; fp32 gradients, D = 64, 9000 / 10000 (313, 348 MB):
+// 64.7 -> 68.3, 76.7 -> 76.1.  Below 200 MB they cost up to a tenth.
+constexpr int64_t kStreamBytes = (int64_t)320 << 20;
+
+template <typename T, int D, bool ADJ, bool NORM, bool STREAM>
 static hipError_t launch_rope(SpkvRope a, const RopeTable& table, bool backward, hipStream_t s) {
     a.tile_rows = tile_rows(a.n_rows, a.n_heads, D, backward ? kRopeGradBlocks : kRopeBlocks);
     a.n_tiles = (a.n_rows - 1) / a.tile_rows + 1;
     const int tokens = std::min(tile_tokens(a.tile_rows, a.n_heads), a.n_tokens);       // of a tile, at most
     size_t lds = (NORM ? 2 * D * sizeof(float) : 0) + (size_t)tokens * (a.rot_dim / 2) * sizeof(float2);
     if (!backward) {
-        spkv_rope_forward<T, D, ADJ, NORM><<<dim3(a.n_tiles), dim3(kRopeThreads), lds, s>>>(a, table);
+        spkv_rope_forward<T, D, ADJ, NORM, STREAM><<<dim3(a.n_tiles), dim3(kRopeThreads), lds, s>>>(a, table);
         return hipGetLastError();
     }
     const int blocks = spkv_rope_backward_blocks(a.n_rows, a.n_heads, D);
     if (NORM) lds += (size_t)kRopeThreads * 16 * sizeof(float);      // (also room for what the waves meet in)
-    spkv_rope_backward<T, D, ADJ, NORM><<<dim3(blocks), dim3(kRopeThreads), lds, s>>>(a, table);
+    spkv_rope_backward<T, D, ADJ, NORM, STREAM><<<dim3(blocks), dim3(kRopeThreads), lds, s>>>(a, table);
     if (NORM && a.partial != nullptr)
         spkv_rope_weight_sum<D><<<dim3(2 * D / 16), dim3(256), 0, s>>>(a.partial, blocks, a.dq_weight, a.dk_weight);
     return hipGetLastError();
+}
+
+template <typename T, int D, bool ADJ, bool NORM>
+static hipError_t launch_rope(const SpkvRope& a, const RopeTable& table, bool backward, hipStream_t s) {
+    const int64_t moved = ((int64_t)a.n_rows * 2 + (backward && NORM ? (int64_t)a.n_tokens * (a.n_q + a.n_kv) : 0)) * D * sizeof(T);
+    return moved > kStreamBytes ? launch_rope<T, D, ADJ, NORM, true>(a, table, backward, s)
+                                : launch_rope<T, D, ADJ, NORM, false>(a, table, backward, s);
 }
 
 template <typename T, int D>

@@ -315,3 +315,33 @@ def test_captured_calls_replay():
         torch.cuda.synchronize()
         for a, b in zip(got, (*out, grad, *want_w)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype,d,adjacent", [(torch.bfloat16, 128, False), (torch.float32, 64, True)], ids=["bf16", "fp32"])
+def test_more_than_the_caches_hold(dtype, d, adjacent):
+    """Calls that move more than the last cache holds take other loads: the same bits as in pieces.  Weights' gradients, as
+    sums in another order, differ by the errors of both: under 136 u of the products' magnitudes each."""
+    t, hq, hk, piece = 14001, 32, 8, 2000
+    rope = _rope(d, adjacent=adjacent)
+    qkv, q, k, v, qw, kw, g = _inputs(t, hq, hk, d, dtype)
+    dy = torch.randn(t, hq + 2 * hk, d, generator=g, device="cuda").to(dtype)
+    dq, dk, dv = dy[:, :hq], dy[:, hq:hq + hk], dy[:, hq + hk:]
+    pos = _positions(rope, t, g)
+    norm = dict(q_weight=qw, k_weight=kw, eps=1e-6)
+    whole = spkv.qk_norm_rope(q, k, pos, rope, v=v, **norm)
+    back = spkv.qk_norm_rope_backward(dq, dk, pos, rope, q=q, k=k, dv=dv, **norm)
+    sums = [torch.zeros(d, dtype=torch.float64, device="cuda") for _ in range(2)]
+    for at in range(0, t, piece):
+        s = slice(at, min(at + piece, t))
+        for x, y in zip(whole, spkv.qk_norm_rope(q[s], k[s], pos[s].contiguous(), rope, v=v[s], **norm)):
+            assert torch.equal(x[s], y)
+        part = spkv.qk_norm_rope_backward(dq[s], dk[s], pos[s].contiguous(), rope, q=q[s], k=k[s], dv=dv[s], **norm)
+        for x, y in zip(back[:3], part):
+            assert torch.equal(x[s], y)
+        for x, y in zip(sums, part[3:]):
+            x += y
+    for x, y, heads, grad in ((sums[0], back[3], q, dq), (sums[1], back[4], k, dk)):
+        # |g| <= |a| + |b| of its pair: the magnitudes' sum is at least that of the products
+        r = torch.rsqrt(heads.float().pow(2).mean(-1, keepdim=True) + 1e-6)
+        size = (_pair_size(rope, grad.float()) * heads.float().abs() * r).double().sum((0, 1))
+        assert ((x - y).abs() <= 2 * 136 * U * size).all()
