@@ -350,9 +350,9 @@ int spkv_soft_gated_attention(const void* q, const void* k, const void* v, const
  *   workspace    device, 256-byte aligned, spkv_prefix_workspace_bytes(prefix, total) bytes
  *                are enough for any call of at most `total` rows (with less, down to one range per list, a
  *                call is slower); contents disposable
- * Two launches (three with cu_seqlens); waits once for the lengths after the prompt's append, as
- * spkv_decode_attention does, and never in steady state.  May be captured: the place of a row is read on the
- * device.  Copies of a sequence get results that agree to rounding.
+ * Two launches (three if, by cu_seqlens, more than 64 sequences have both rows and a prompt); waits once for
+ * the lengths after the prompt's append, as spkv_decode_attention does, and never in steady state.  May be
+ * captured: the place of a row is read on the device.  Copies of a sequence get results that agree to rounding.
  * Errors: SPKV_E_INVAL for shapes that differ, indices out of range, bad pointers, a workspace without
  * room for one range; SPKV_E_STATE if a sequence holds fewer tokens than the call has appended. */
 size_t spkv_prefix_workspace_bytes(const spkv_cache_t* prefix, int64_t max_total_rows);

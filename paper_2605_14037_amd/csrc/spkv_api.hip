@@ -1660,14 +1660,14 @@ constexpr int kShareMaxSlots = 255;
 
 // The prompts of a call that hold tokens and are continued by some row of it.  (No container: nothing here allocates.)
 struct SharePrompts {
-    int32_t n;
+    int32_t n, seqs;                       // prompts, sequences that continue them
     int32_t id[SPKV_MAX_BATCH], rows[SPKV_MAX_BATCH];
     int16_t active[SPKV_MAX_BATCH];        // of every sequence; -1: none
 };
 void share_prompts(const spkv_cache* pc, int batch, const int32_t* prefix_of, const int32_t* cu, SharePrompts* s) {
     int16_t at[SPKV_MAX_BATCH];
     std::fill(at, at + SPKV_MAX_BATCH, (int16_t)-1);
-    s->n = 0;
+    s->n = s->seqs = 0;
     for (int b = 0; b < batch; ++b) {
         const int p = prefix_of[b];
         s->active[b] = -1;
@@ -1678,6 +1678,7 @@ void share_prompts(const spkv_cache* pc, int batch, const int32_t* prefix_of, co
             s->rows[s->n++] = 0;
         }
         s->active[b] = at[p];
+        ++s->seqs;
         s->rows[at[p]] += tokens_for(cu, b);
     }
 }
@@ -1842,6 +1843,24 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
         }
         by_prompt.first[prompts.n] = (uint16_t)at;
         for (int b = 0; b < B; ++b) by_row.active[b] = prompts.active[b];
+    } else if (cu != nullptr && prompts.n > 0 && prompts.seqs <= kShareSpans) {
+        SpkvShareSpans& sp = by_prompt.spans;
+        sp = {};
+        sp.appended = appended ? 1 : 0;
+        for (int a = 0; a < prompts.n; ++a) {
+            sp.first[a] = sp.start[sp.n];
+            for (int b = 0; b < B; ++b)
+                if (prompts.active[b] == a) {
+                    sp.row[sp.n] = cu[b];
+                    sp.seq[sp.n] = (int16_t)b;
+                    sp.act[sp.n] = (int16_t)a;
+                    sp.start[sp.n + 1] = sp.start[sp.n] + tokens_for(cu, b);
+                    ++sp.n;
+                }
+        }
+        sp.first[prompts.n] = sp.start[sp.n];
+        by_prompt.in_spans = by_row.in_spans = 1;
+        by_row.spans = sp;
     } else {
         SpkvCu rows_of;
         for (int b = 0; b <= B; ++b) rows_of.v[b] = cu != nullptr ? cu[b] : b;

@@ -273,20 +273,40 @@ struct SpkvShareOwn {
     int32_t n_blocks;           // workgroups of the launch that belong to them, its first ones
     SpkvSplit split;
 };
-// The rows by prompt: one token a sequence (first, seq; its place is the last of t_own), or -- more tokens, or more
-// sequences than travel with the launch -- tables on the device.
-constexpr int kShareArgSeqs = 256;
+// The rows by prompt: one token a sequence (first, seq; its place is the last of t_own), spans of more tokens each, or --
+// more sequences than travel with the launch -- tables on the device.
+constexpr int kShareArgSeqs = 256, kShareSpans = 64;
+struct SpkvShareSpans {                   // sequences with rows that continue a prompt, in the order of the prompts
+    int32_t n, appended;
+    int32_t start[kShareSpans + 1];       // rows before each in that order
+    int32_t row[kShareSpans];             // its first row in the call
+    int32_t first[kShareSpans + 1];       // rows before each active prompt
+    int16_t seq[kShareSpans], act[kShareSpans];
+};
 struct SpkvShareRows {
     const int2* table;          // null, or [rows] (row, place of its token in the sequence)
     const int32_t* first_row;   // [n_active + 1], with table
     const int32_t* t_own;       // [B][Hkv] tokens of the sequences
-    uint16_t first[kShareArgSeqs + 1], seq[kShareArgSeqs], prefix[SPKV_MAX_BATCH];
+    int32_t in_spans;
+    union {
+        struct {
+            uint16_t first[kShareArgSeqs + 1], seq[kShareArgSeqs];
+        };
+        SpkvShareSpans spans;
+    };
+    uint16_t prefix[SPKV_MAX_BATCH];
 };
 // ... and by row: its active prompt (-1: none) and its place in the order of the prompts.
 struct SpkvShareMerge {
-    const int2* by_row;         // null: one token a sequence
-    int16_t active[kShareArgSeqs];
-    uint16_t place[kShareArgSeqs];
+    const int2* by_row;         // null: one token a sequence, or spans
+    int32_t in_spans;
+    union {
+        struct {
+            int16_t active[kShareArgSeqs];
+            uint16_t place[kShareArgSeqs];
+        };
+        SpkvShareSpans spans;
+    };
     uint8_t ranges[kShareTablePairs];     // as in SpkvShareTable
 };
 struct SpkvShareActive {

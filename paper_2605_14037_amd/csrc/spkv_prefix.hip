@@ -350,13 +350,24 @@ struct ShareRow {
     int row, head, place;
 };
 __device__ __forceinline__ int share_first(const SpkvShareRows& rows, int act) {
-    return rows.table != nullptr ? rows.first_row[act] : rows.first[act];
+    return rows.in_spans ? rows.spans.first[act] : rows.table != nullptr ? rows.first_row[act] : rows.first[act];
 }
 __device__ __forceinline__ ShareRow share_row(const SpkvShareRows& rows, int first, int c, int G, int n_kv_heads, bool ring) {
     ShareRow r;
     const int i = c / G;
     r.head = c - i * G;
-    if (rows.table != nullptr) {
+    if (rows.in_spans) {                                     // lane k has span k; all lanes of the wave are here
+        const SpkvShareSpans& sp = rows.spans;
+        const int k = min((int)threadIdx.x & 63, sp.n - 1), start = sp.start[k], shift = sp.row[k] - start;
+        int place = 0;
+        if (ring) place = rows.t_own[(int)sp.seq[k] * n_kv_heads] - (sp.appended ? sp.start[k + 1] : start);
+        r.row = r.place = 0;
+        for (int x = 0; x < sp.n; ++x)
+            if (first + i >= __builtin_amdgcn_readlane(start, x)) {
+                r.row = first + i + __builtin_amdgcn_readlane(shift, x);
+                r.place = first + i + __builtin_amdgcn_readlane(place, x);
+            }
+    } else if (rows.table != nullptr) {
         const int2 e = rows.table[first + i];
         r.row = e.x;
         r.place = e.y;
@@ -779,8 +790,12 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
         unsigned seen = 0xffffu;
         if (edge) seen = mask(sc, x);
         __builtin_amdgcn_sched_barrier(0);
+        // (the waves that are here first: the matrix and vector work of this part side by side with the products of the
+        // other waves' last one; questions of 1632 tokens behind 30 MB of lists 230 -> 224 us)
+        __builtin_amdgcn_s_setprio(1);
         scores(sn);
         const bool low = weights(sc);
+        __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         if (__builtin_expect(low, 0)) rescale(sc);
         load_v(hp, 1);
@@ -893,7 +908,14 @@ __global__ __launch_bounds__(256, 8) void spkv_prefix_merge(SpkvShareCut cut, Sp
     const int G = n_q_heads / n_kv_heads, head = exists ? head0 + slice / S : head0, h = head / G, g = head - h * G;
     const int64_t id = (int64_t)row * n_q_heads + head;
     int act, at;
-    if (rows.by_row != nullptr) {
+    if (rows.in_spans) {                                     // the span that holds the row, if any
+        const SpkvShareSpans& sp = rows.spans;
+        const int lane = (int)threadIdx.x & 63, k = min(lane, sp.n - 1), off = row - sp.row[k];
+        const unsigned long long here = __ballot(lane < sp.n && off >= 0 && off < sp.start[k + 1] - sp.start[k]);
+        const int x = here != 0ull ? __builtin_ctzll(here) : 0;
+        act = here != 0ull ? (int)sp.act[x] : -1;
+        at = sp.start[x] + row - sp.row[x];
+    } else if (rows.by_row != nullptr) {
         const int2 e = rows.by_row[row];
         act = e.x;
         at = e.y;

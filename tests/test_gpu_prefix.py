@@ -407,3 +407,31 @@ def test_a_query_that_is_not_a_number_shows():
     own_lse[0, 2] = float("nan")
     bad, bad_lse = s.cache.prefix_attention(s.sharing, q, None, own, own_lse)
     assert torch.isnan(bad[0, 2]).all() and torch.isnan(bad_lse[0, 2])
+
+
+@pytest.mark.parametrize("asking", [64, 65])
+@pytest.mark.parametrize("appended", [True, False], ids=["appended", "drafts"])
+def test_questions_of_many_sequences(asking, appended):
+    """Up to 64 sequences with rows and a prompt travel with the launches, more by tables; others have neither."""
+    batch = 90
+    counts = [0 if b % 7 == 3 else 1 + (5 * b) % 9 for b in range(batch)]
+    member, n = [], 0
+    for b in range(batch):
+        use = counts[b] > 0 and n < asking
+        member.append((0, 2, 1)[b % 3] if use else -1 if b % 2 else 3)
+        n += use
+    assert n == asking
+    s = Setup([700, 90, 300, 0], [(11 * b) % 60 for b in range(batch)], member, 8, 2, 64, window=64, keep=0.3, seed=asking)
+    cu = [sum(counts[:b]) for b in range(batch + 1)]
+    k, v, f = s.tokens(counts)
+    q = s.randn(cu[-1], 8, 64).bfloat16()
+    if appended:
+        own, own_lse = s.cache.prefill_attention(k, v, f, q, cu, want_lse=True)
+        s.held = [a + n for a, n in zip(s.held, counts)]
+    else:
+        own, own_lse = s.cache.score_chunk(k, v, q, cu, want_lse=True)
+    out, lse = s.cache.prefix_attention(s.sharing, q, cu, own, own_lse, appended=appended)
+    s.check(out, lse, s.reference(q, counts, (own, own_lse), appended=appended), "given the own part")
+    for b in range(batch):
+        if member[b] in (-1, 3):
+            assert torch.equal(out[cu[b]:cu[b + 1]], own[cu[b]:cu[b + 1]]) and torch.equal(lse[cu[b]:cu[b + 1]], own_lse[cu[b]:cu[b + 1]])

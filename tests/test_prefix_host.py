@@ -151,5 +151,15 @@ def test_own_lists_ride_in_the_prompts_launch_while_they_are_short():
     assert launches(5000, 60 * 32 + 1) == ["spkv_decode_split", "spkv_decode_combine", "spkv_prefix_few", "spkv_prefix_merge"]
 
 
+@pytest.mark.parametrize("asking,launches", [(1, 2), (64, 2), (65, 3)])
+def test_rows_of_up_to_64_sequences_travel_with_the_launch(asking, launches):
+    """More tokens a sequence: a table on the device, in a launch before, from more sequences with rows and a prompt on."""
+    script = [["append", dict(to="p", counts=[9000])], ["append", dict(to="c", counts=[5] * 100)],
+              ["join", dict(member=[0] * asking + [-1] * (100 - asking), counts=[3] * 100)],
+              ["join", dict(member=[0] * 100, counts=[3] * asking + [0] * (100 - asking))]]
+    for rc, got in _run(dict(batch=1), dict(batch=100), script)[2:]:
+        assert rc == 0 and len(got) == launches and (got[0][0] == "spkv_prefix_rows") == (launches == 3), got
+
+
 if __name__ == "__main__":
     _main()
