@@ -63,23 +63,31 @@ template <typename T> struct Raw8;
 template <> struct Raw8<uint16_t> { uint4 u; };
 template <> struct Raw8<float> { uint4 u, w; };
 
-// STREAM (see Streaming below): past the caches' retention.
-template <bool STREAM>
+// STREAM (see Streaming below): 1: loads, 2: stores too ask the caches for no retention.
+template <int STREAM>
 __device__ __forceinline__ uint4 load_unit(const void* p) {
-    if (STREAM) return __builtin_bit_cast(uint4, load_stream_b128(static_cast<const uint16_t*>(p)));
+    if (STREAM > 0) return __builtin_bit_cast(uint4, load_stream_b128(static_cast<const uint16_t*>(p)));
     return *static_cast<const uint4*>(p);
 }
-template <bool STREAM>
+template <int STREAM>
+__device__ __forceinline__ void store_unit(uint4 u, void* p) {
+    typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+    if (STREAM > 1) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, u), static_cast<u32x4*>(p));
+    else *static_cast<uint4*>(p) = u;
+}
+template <int STREAM>
 __device__ __forceinline__ void load8(Raw8<uint16_t>& r, const uint16_t* p) { r.u = load_unit<STREAM>(p); }
-template <bool STREAM>
+template <int STREAM>
 __device__ __forceinline__ void load8(Raw8<float>& r, const float* p) {
     r.u = load_unit<STREAM>(p);
     r.w = load_unit<STREAM>(p + 4);
 }
-__device__ __forceinline__ void store8(const Raw8<uint16_t>& r, uint16_t* p) { *reinterpret_cast<uint4*>(p) = r.u; }
+template <int STREAM>
+__device__ __forceinline__ void store8(const Raw8<uint16_t>& r, uint16_t* p) { store_unit<STREAM>(r.u, p); }
+template <int STREAM>
 __device__ __forceinline__ void store8(const Raw8<float>& r, float* p) {
-    *reinterpret_cast<uint4*>(p) = r.u;
-    *reinterpret_cast<uint4*>(p + 4) = r.w;
+    store_unit<STREAM>(r.u, p);
+    store_unit<STREAM>(r.w, p + 4);
 }
 __device__ __forceinline__ void widen8(const Raw8<uint16_t>& r, float (&x)[8]) {
     const unsigned w[4] = {r.u.x, r.u.y, r.u.z, r.u.w};
@@ -194,7 +202,7 @@ __device__ __forceinline__ T* row_of(const SpkvRowSet (&s)[3], const RowPlace& r
 }
 
 // One tile of rows: tile_rows consecutive rows of the order (token, head).
-template <typename T, int D, bool ADJ, bool NORM, bool STREAM>
+template <typename T, int D, bool ADJ, bool NORM, int STREAM>
 __global__ __launch_bounds__(kRopeThreads) void spkv_rope_forward(SpkvRope a, RopeTable table) {
     constexpr int LPR = D / 16, RPP = kRopeThreads / LPR;      // lanes per row, rows per pass
     extern __shared__ __attribute__((aligned(16))) float s_rope[];
@@ -230,8 +238,8 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_forward(SpkvRope a, Ro
             widen8(x0, f0);
             widen8(x1, f1);
         } else {                                               // values: as they are
-            store8(x0, o + rc.c0 * 8);
-            store8(x1, o + rc.c1 * 8);
+            store8<STREAM>(x0, o + rc.c0 * 8);
+            store8<STREAM>(x1, o + rc.c1 * 8);
         }
         if (r + RPP < n_rows) {                                // the next row travels meanwhile
             hh += RPP;
@@ -260,9 +268,9 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_forward(SpkvRope a, Ro
         rotate16<D, ADJ, false>(rc, a.rot_dim, s_cs + (here.token - first) * (a.rot_dim >> 1), f0, f1);
         Raw8<T> y;
         round8(y, f0);
-        store8(y, o + rc.c0 * 8);
+        store8<STREAM>(y, o + rc.c0 * 8);
         round8(y, f1);
-        store8(y, o + rc.c1 * 8);
+        store8<STREAM>(y, o + rc.c1 * 8);
     }
 }
 
@@ -272,7 +280,7 @@ __global__ __launch_bounds__(kRopeThreads) void spkv_rope_forward(SpkvRope a, Ro
 // registers left room for three waves on a SIMD instead of four).  They meet in LDS at
 // the end and leave as one partial row of 2 D floats, which spkv_rope_weight_sum adds up in a
 // fixed order (no atomics: equal calls give equal bits).
-template <typename T, int D, bool ADJ, bool NORM, bool STREAM>
+template <typename T, int D, bool ADJ, bool NORM, int STREAM>
 __global__ __launch_bounds__(kRopeThreads, sizeof(T) == 2 ? 4 : 3) void spkv_rope_backward(SpkvRope a, RopeTable table) {
     constexpr int LPR = D / 16, RPP = kRopeThreads / LPR;
     extern __shared__ __attribute__((aligned(16))) float s_rope[];
@@ -327,8 +335,8 @@ __global__ __launch_bounds__(kRopeThreads, sizeof(T) == 2 ? 4 : 3) void spkv_rop
                     widen8(x1, v1);
                 }
             } else {                                           // values: as they are
-                store8(g0, o + rc.c0 * 8);
-                store8(g1, o + rc.c1 * 8);
+                store8<STREAM>(g0, o + rc.c0 * 8);
+                store8<STREAM>(g1, o + rc.c1 * 8);
             }
             if (r + RPP < n_rows) {
                 hh += RPP;
@@ -380,9 +388,9 @@ __global__ __launch_bounds__(kRopeThreads, sizeof(T) == 2 ? 4 : 3) void spkv_rop
                 }
                 Raw8<T> y;
                 round8(y, f0);
-                store8(y, o + rc.c0 * 8);
+                store8<STREAM>(y, o + rc.c0 * 8);
                 round8(y, f1);
-                store8(y, o + rc.c1 * 8);
+                store8<STREAM>(y, o + rc.c1 * 8);
             }
         }
     }
@@ -459,14 +467,15 @@ int spkv_rope_backward_blocks(int64_t n_rows, int n_heads, int head_dim) {
     return (int)std::min<int64_t>((n_rows + rows - 1) / rows, kRopeGradBlocks);
 }
 
-// Streaming.  Once a call moves more than the 256 MB of the last cache hold, what it reads is not there and need not
-// stay: loads that ask for no retention then leave the cache to the writes.  bf16, D = 128, gradients of 8192 /
-// 10000 / 16384 tokens (285, 348, 570 MB): 57.8 -> 55.4, 78.7 -> 69.3, 121 -> 101 us; forward of 12000 / 16384 / 32768
-// (295, 403, 805 MB): 51.1 -> 50.2, 82.8 -> 66.1, 157 -> 159; fp32 gradients, D = 64, 9000 / 10000 (313, 348 MB):
-// 64.7 -> 68.3, 76.7 -> 76.1.  Below 200 MB they cost up to a tenth.
-constexpr int64_t kStreamBytes = (int64_t)320 << 20;
+// Streaming.  Once a call moves more than the 256 MB of the last cache, what it reads is not there and need not stay: loads
+// without retention leave the cache to what is written, for whoever reads that next -- unless that alone is more than it
+// holds.  bf16, D = 128, gradients of 16384 tokens (570 MB, 201 of them written): into buffers that are not in the
+// cache 120.8 -> 117.9 us, into the last call's 121 -> 101; 8192 tokens (285 MB) 64.9 either way; forward of 16384 tokens 82.7
+// either way, 82.6 -> 66.2 into the last call's; of 32768 (805 MB, 403 written) plain 156, loads 159, stores too 153.
+// fp32 gradients, D = 64, 10000 tokens (348 MB): 77.9 -> 80.8, the same into the last call's.
+constexpr int64_t kStreamBytes = (int64_t)320 << 20, kStreamWritten = (int64_t)256 << 20;
 
-template <typename T, int D, bool ADJ, bool NORM, bool STREAM>
+template <typename T, int D, bool ADJ, bool NORM, int STREAM>
 static hipError_t launch_rope(SpkvRope a, const RopeTable& table, bool backward, hipStream_t s) {
     a.tile_rows = tile_rows(a.n_rows, a.n_heads, D, backward ? kRopeGradBlocks : kRopeBlocks);
     a.n_tiles = (a.n_rows - 1) / a.tile_rows + 1;
@@ -486,9 +495,11 @@ static hipError_t launch_rope(SpkvRope a, const RopeTable& table, bool backward,
 
 template <typename T, int D, bool ADJ, bool NORM>
 static hipError_t launch_rope(const SpkvRope& a, const RopeTable& table, bool backward, hipStream_t s) {
-    const int64_t moved = ((int64_t)a.n_rows * 2 + (backward && NORM ? (int64_t)a.n_tokens * (a.n_q + a.n_kv) : 0)) * D * sizeof(T);
-    return moved > kStreamBytes ? launch_rope<T, D, ADJ, NORM, true>(a, table, backward, s)
-                                : launch_rope<T, D, ADJ, NORM, false>(a, table, backward, s);
+    const int64_t written = (int64_t)a.n_rows * D * sizeof(T);
+    const int64_t moved = 2 * written + (backward && NORM ? (int64_t)a.n_tokens * (a.n_q + a.n_kv) * D * sizeof(T) : 0);
+    if (moved <= kStreamBytes) return launch_rope<T, D, ADJ, NORM, 0>(a, table, backward, s);
+    return written <= kStreamWritten ? launch_rope<T, D, ADJ, NORM, 1>(a, table, backward, s)
+                                     : launch_rope<T, D, ADJ, NORM, 2>(a, table, backward, s);
 }
 
 template <typename T, int D>

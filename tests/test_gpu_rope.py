@@ -317,11 +317,14 @@ def test_captured_calls_replay():
             assert torch.equal(a, b)
 
 
-@pytest.mark.parametrize("dtype,d,adjacent", [(torch.bfloat16, 128, False), (torch.float32, 64, True)], ids=["bf16", "fp32"])
-def test_more_than_the_caches_hold(dtype, d, adjacent):
-    """Calls that move more than the last cache holds take other loads: the same bits as in pieces.  Weights' gradients, as
-    sums in another order, differ by the errors of both: under 136 u of the products' magnitudes each."""
-    t, hq, hk, piece = 14001, 32, 8, 2000
+@pytest.mark.parametrize("dtype,d,adjacent,t", [
+    (torch.bfloat16, 128, False, 14001), (torch.float32, 64, True, 14001), (torch.bfloat16, 128, False, 22003),
+    (torch.float32, 64, True, 23003)], ids=["bf16", "fp32", "bf16-longer", "fp32-longer"])
+def test_more_than_the_caches_hold(dtype, d, adjacent, t):
+    """Calls that move more than the last cache holds take other loads, and other stores where what they write alone is more:
+    the same bits as in pieces.  Weights' gradients, as sums in another order, differ by the errors of both: under 136 u of
+    the products' magnitudes each."""
+    hq, hk, piece = 32, 8, 2000
     rope = _rope(d, adjacent=adjacent)
     qkv, q, k, v, qw, kw, g = _inputs(t, hq, hk, d, dtype)
     dy = torch.randn(t, hq + 2 * hk, d, generator=g, device="cuda").to(dtype)
