@@ -1843,7 +1843,7 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
         }
         by_prompt.first[prompts.n] = (uint16_t)at;
         for (int b = 0; b < B; ++b) by_row.active[b] = prompts.active[b];
-    } else if (cu != nullptr && prompts.n > 0 && prompts.seqs <= kShareSpans) {
+    } else if (cu != nullptr && prompts.seqs <= kShareSpans) {
         SpkvShareSpans& sp = by_prompt.spans;
         sp = {};
         sp.appended = appended ? 1 : 0;

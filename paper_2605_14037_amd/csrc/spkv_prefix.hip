@@ -914,7 +914,7 @@ __global__ __launch_bounds__(256, 8) void spkv_prefix_merge(SpkvShareCut cut, Sp
     int act, at;
     if (rows.in_spans) {                                     // the span that holds the row, if any
         const SpkvShareSpans& sp = rows.spans;
-        const int lane = (int)threadIdx.x & 63, k = min(lane, sp.n - 1), off = row - sp.row[k];
+        const int lane = (int)threadIdx.x & 63, k = max(min(lane, sp.n - 1), 0), off = row - sp.row[k];
         const unsigned long long here = __ballot(lane < sp.n && off >= 0 && off < sp.start[k + 1] - sp.start[k]);
         const int x = here != 0ull ? __builtin_ctzll(here) : 0;
         act = here != 0ull ? (int)sp.act[x] : -1;

@@ -435,3 +435,11 @@ def test_questions_of_many_sequences(asking, appended):
     for b in range(batch):
         if member[b] in (-1, 3):
             assert torch.equal(out[cu[b]:cu[b + 1]], own[cu[b]:cu[b + 1]]) and torch.equal(lse[cu[b]:cu[b + 1]], own_lse[cu[b]:cu[b + 1]])
+
+
+def test_questions_without_any_prompt():
+    """No sequence continues a prompt, or only an empty one: the own part, bit for bit."""
+    s = Setup([0, 50], [5, 9, 1], [-1, 0, -1], 8, 2, 128)
+    own, own_lse = s.randn(11, 8, 128).bfloat16(), s.randn(11, 8)
+    out, lse = s.cache.prefix_attention(s.sharing, s.randn(11, 8, 128).bfloat16(), [0, 3, 10, 11], own, own_lse)
+    assert torch.equal(out, own) and torch.equal(lse, own_lse)

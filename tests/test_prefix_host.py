@@ -156,9 +156,12 @@ def test_rows_of_up_to_64_sequences_travel_with_the_launch(asking, launches):
     """More tokens a sequence: a table on the device, in a launch before, from more sequences with rows and a prompt on."""
     script = [["append", dict(to="p", counts=[9000])], ["append", dict(to="c", counts=[5] * 100)],
               ["join", dict(member=[0] * asking + [-1] * (100 - asking), counts=[3] * 100)],
-              ["join", dict(member=[0] * 100, counts=[3] * asking + [0] * (100 - asking))]]
-    for rc, got in _run(dict(batch=1), dict(batch=100), script)[2:]:
+              ["join", dict(member=[0] * 100, counts=[3] * asking + [0] * (100 - asking))],
+              ["join", dict(member=[-1] * 100, counts=[3] * 100)]]
+    *asked, none = _run(dict(batch=1), dict(batch=100), script)[2:]
+    for rc, got in asked:
         assert rc == 0 and len(got) == launches and (got[0][0] == "spkv_prefix_rows") == (launches == 3), got
+    assert none[0] == 0 and [n.split("<")[0] for n, _, _ in none[1]] == ["spkv_prefix_merge"]
 
 
 if __name__ == "__main__":
