@@ -346,14 +346,19 @@ def _rope_call(q, k, v, positions, rope, q_weight, k_weight, eps, names):
 
 
 def _rope_out(out, q, v, n, hq, hk, d):
-    """Tensors to write: those given, or new dense ones."""
+    """Tensors to write -- those given, or new dense ones -- and the sets of heads that they are."""
+    dtype, many, few = q.dtype, (n, hq, d), (n, hk, d)
     if out is not None:
-        return (out[0], out[1], None) if v is None else out
-    dtype, device = q.dtype, q.device          # (empty_strided takes less host time than empty)
-    few, of_few = (n, hk, d), (hk * d, d, 1)
-    return (torch.empty_strided((n, hq, d), (hq * d, d, 1), dtype=dtype, device=device),
-            torch.empty_strided(few, of_few, dtype=dtype, device=device),
-            None if v is None else torch.empty_strided(few, of_few, dtype=dtype, device=device))
+        out = (out[0], out[1], None) if v is None else out
+        return out, [_heads(out[0], dtype, many, "out[0]"), _heads(out[1], dtype, few, "out[1]"),
+                     _NO_HEADS if v is None else _heads(out[2], dtype, few, "out[2]")]
+    device, of_many, of_few = q.device, (hq * d, d, 1), (hk * d, d, 1)       # (empty_strided takes less host time than empty)
+    a = torch.empty_strided(many, of_many, dtype=dtype, device=device)
+    b = torch.empty_strided(few, of_few, dtype=dtype, device=device)
+    if v is None:
+        return (a, b, None), [(a.data_ptr(), hq * d, d), (b.data_ptr(), hk * d, d), _NO_HEADS]
+    c = torch.empty_strided(few, of_few, dtype=dtype, device=device)
+    return (a, b, c), [(a.data_ptr(), hq * d, d), (b.data_ptr(), hk * d, d), (c.data_ptr(), hk * d, d)]
 
 
 def qk_norm_rope(q, k, positions, rope, q_weight=None, k_weight=None, eps=None, v=None, out=None):
@@ -362,11 +367,9 @@ def qk_norm_rope(q, k, positions, rope, q_weight=None, k_weight=None, eps=None, 
     projection's rows as they are; positions: int32 [tokens] or [axes, tokens].  out: tensors to write
     (the inputs themselves may be passed).  Returns (q, k) or, with v, (q, k, v)."""
     n, hq, hk, d, ins, pp, qw, kw, eps = _rope_call(q, k, v, positions, rope, q_weight, k_weight, eps, "qkv")
-    out, dtype = _rope_out(out, q, v, n, hq, hk, d), q.dtype
-    outs = [_heads(out[0], dtype, (n, hq, d), "out[0]"), _heads(out[1], dtype, (n, hk, d), "out[1]"),
-            _NO_HEADS if v is None else _heads(out[2], dtype, (n, hk, d), "out[2]")]
+    out, outs = _rope_out(out, q, v, n, hq, hk, d)
     at = _packed(ins + outs)
-    _check((_LIB or load_library()).spkv_qk_norm_rope(at[0], at[1], at[2], qw, kw, eps, pp, rope.struct, _HEAD_TYPES[dtype],
+    _check((_LIB or load_library()).spkv_qk_norm_rope(at[0], at[1], at[2], qw, kw, eps, pp, rope.struct, _HEAD_TYPES[q.dtype],
                                                       n, hq, hk, at[3], at[4], at[5], _stream()), "spkv_qk_norm_rope")
     return tuple(out[:2]) if v is None else tuple(out)
 
@@ -381,9 +384,7 @@ def qk_norm_rope_backward(dq, dk, positions, rope, q=None, k=None, q_weight=None
     n, hq, hk, d, ins, pp, qw, kw, eps = _rope_call(dq, dk, dv, positions, rope, q_weight, k_weight, eps,
                                                     ("dq", "dk", "dv"))
     given, dtype = out is not None, dq.dtype
-    out = _rope_out(out, dq, dv, n, hq, hk, d)
-    outs = [_heads(out[0], dtype, (n, hq, d), "out[0]"), _heads(out[1], dtype, (n, hk, d), "out[1]"),
-            _NO_HEADS if dv is None else _heads(out[2], dtype, (n, hk, d), "out[2]")]
+    out, outs = _rope_out(out, dq, dv, n, hq, hk, d)
     xs, weights = [_NO_HEADS, _NO_HEADS], ()
     if eps >= 0.0:
         if q is None or k is None:
