@@ -681,7 +681,7 @@ class SPKVCache:
         if sharing.batch != self.cfg.batch:
             raise ValueError(f"sharing: made for {sharing.batch} sequences, the cache has {self.cfg.batch}")
         if workspace is None:
-            workspace = torch.empty_strided((sharing.workspace_bytes(rows),), (1,), dtype=torch.uint8, device=device)
+            return torch.empty_strided((sharing.workspace_bytes(rows),), (1,), dtype=torch.uint8, device=device)
         if workspace.dtype != torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous uint8 device tensor")
         return workspace
@@ -696,10 +696,16 @@ class SPKVCache:
         workspace = self._share_workspace(sharing, cfg.batch, workspace, q.device)
         if out is None:
             out = torch.empty_strided(shape, (shape[1] * shape[2], shape[2], 1), dtype=torch.bfloat16, device=q.device)
-        op = _dev_ptr(out, torch.bfloat16, shape, "out")
-        if lse is None and want_lse:
+            op = out.data_ptr()
+        else:
+            op = _dev_ptr(out, torch.bfloat16, shape, "out")
+        if lse is not None:
+            lp = _dev_ptr(lse, torch.float32, shape[:2], "lse")
+        elif want_lse:
             lse = torch.empty_strided(shape[:2], (shape[1], 1), dtype=torch.float32, device=q.device)
-        lp = _dev_ptr(lse, torch.float32, shape[:2], "lse") if lse is not None else None
+            lp = lse.data_ptr()
+        else:
+            lp = None
         _check(self.lib.spkv_decode_attention_shared(self.handle, sharing.prefix.handle, sharing.prefix_of, qp, op, lp,
                                                      float(sm_scale), workspace.data_ptr(), workspace.numel(),
                                                      _stream()), "spkv_decode_attention_shared")
