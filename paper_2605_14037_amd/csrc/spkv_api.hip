@@ -1829,6 +1829,7 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
     SpkvShareRows by_prompt = {};
     SpkvShareMerge by_row = {};
     by_prompt.t_own = c->view.t_pair;
+    by_prompt.appended = appended ? 1 : 0;
     std::memcpy(by_row.ranges, table.ranges, sizeof(by_row.ranges));
     for (int a = 0; a < prompts.n; ++a) by_prompt.prefix[a] = (uint16_t)prompts.id[a];
     if (cu == nullptr && B <= kShareArgSeqs) {
@@ -1846,7 +1847,6 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
     } else if (cu != nullptr && prompts.seqs <= kShareSpans) {
         SpkvShareSpans& sp = by_prompt.spans;
         sp = {};
-        sp.appended = appended ? 1 : 0;
         for (int a = 0; a < prompts.n; ++a) {
             sp.first[a] = sp.start[sp.n];
             for (int b = 0; b < B; ++b)

@@ -273,11 +273,12 @@ struct SpkvShareOwn {
     int32_t n_blocks;           // workgroups of the launch that belong to them, its first ones
     SpkvSplit split;
 };
-// The rows by prompt: one token a sequence (first, seq; its place is the last of t_own), spans of more tokens each, or --
+// The rows by prompt: one token a sequence (first, seq; its place is the last of t_own, or the one behind it if the call
+// has not appended), spans of more tokens each, or --
 // more sequences than travel with the launch -- tables on the device.
 constexpr int kShareArgSeqs = 256, kShareSpans = 64;
 struct SpkvShareSpans {                   // sequences with rows that continue a prompt, in the order of the prompts
-    int32_t n, appended;
+    int32_t n;
     int32_t start[kShareSpans + 1];       // rows before each in that order
     int32_t row[kShareSpans];             // its first row in the call
     int32_t first[kShareSpans + 1];       // rows before each active prompt
@@ -287,7 +288,7 @@ struct SpkvShareRows {
     const int2* table;          // null, or [rows] (row, place of its token in the sequence)
     const int32_t* first_row;   // [n_active + 1], with table
     const int32_t* t_own;       // [B][Hkv] tokens of the sequences
-    int32_t in_spans;
+    int32_t in_spans, appended;
     union {
         struct {
             uint16_t first[kShareArgSeqs + 1], seq[kShareArgSeqs];

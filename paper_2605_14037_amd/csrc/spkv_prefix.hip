@@ -362,7 +362,7 @@ __device__ __forceinline__ ShareRow share_row(const SpkvShareRows& rows, int fir
         const SpkvShareSpans& sp = rows.spans;
         const int k = min((int)threadIdx.x & 63, sp.n - 1), start = sp.start[k], shift = sp.row[k] - start;
         int place = 0;
-        if (ring) place = rows.t_own[(int)sp.seq[k] * n_kv_heads] - (sp.appended ? sp.start[k + 1] : start);
+        if (ring) place = rows.t_own[(int)sp.seq[k] * n_kv_heads] - (rows.appended ? sp.start[k + 1] : start);
         r.row = r.place = 0;
         for (int x = 0; x < sp.n; ++x)
             if (first + i >= __builtin_amdgcn_readlane(start, x)) {
@@ -375,7 +375,7 @@ __device__ __forceinline__ ShareRow share_row(const SpkvShareRows& rows, int fir
         r.place = e.y;
     } else {
         r.row = rows.seq[first + i];
-        r.place = ring ? rows.t_own[r.row * n_kv_heads] - 1 : 0;
+        r.place = ring ? rows.t_own[r.row * n_kv_heads] - rows.appended : 0;
     }
     return r;
 }
