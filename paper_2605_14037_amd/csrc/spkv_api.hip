@@ -1632,23 +1632,22 @@ int spkv_utility_logits(const void* hidden, const void* w1, const float* b1, con
 }
 
 namespace {
-// Shared prompts.  Workspace of a call of n rows: the tables of its rows, their own attention's lse where
-// the caller wants none, and the partial results of the ranges.
+// Shared prompts.  Workspace of a call of n rows: the tables of its rows, in a decoding step their own attention's lse
+// where the caller wants none and the partial results of the own items, and the partial results of the ranges.
 struct ShareCarve {
     size_t table, by_row, first_row, own_lse, own_part, part;
 };
 // Sequences whose lists are short are attended in the prompts' launch, at most kShareOwnSlots items to a list (two
 // half-pages each in the longest); only calls of one token a sequence.
 constexpr int kShareOwnSlots = 8, kShareOwnItem = 2;
-ShareCarve share_carve(int64_t rows, int n_q_heads, int head_dim) {
+ShareCarve share_carve(int64_t rows, int n_q_heads, int head_dim, bool decode) {
     ShareCarve k;
     k.table = 0;
     k.by_row = align_up((size_t)rows * sizeof(int2));
     k.first_row = k.by_row + align_up((size_t)rows * sizeof(int2));
     k.own_lse = k.first_row + align_up((SPKV_MAX_BATCH + 1) * sizeof(int32_t));
-    k.own_part = k.own_lse + align_up((size_t)rows * n_q_heads * sizeof(float));
-    k.part = k.own_part;
-    if (rows <= SPKV_MAX_BATCH) k.part += align_up((size_t)rows * n_q_heads * kShareOwnSlots * (head_dim + 2) * sizeof(float));
+    k.own_part = k.own_lse + (decode ? align_up((size_t)rows * n_q_heads * sizeof(float)) : 0);
+    k.part = k.own_part + (decode ? align_up((size_t)rows * n_q_heads * kShareOwnSlots * (head_dim + 2) * sizeof(float)) : 0);
     return k;
 }
 // Bytes that one range of every list needs for the partial results of `rows` rows.
@@ -1657,6 +1656,11 @@ size_t share_slot_bytes(int64_t rows, int n_q_heads, int head_dim) {
 }
 constexpr size_t kSharePartBytes = (size_t)96 << 20;     // ranges are no more than fit, beyond the first
 constexpr int kShareMaxSlots = 255;
+// Bytes of the ranges' partial results; never less for more rows.
+size_t share_part_bytes(int64_t rows, int n_q_heads, int head_dim) {
+    const size_t slot = share_slot_bytes(rows, n_q_heads, head_dim);
+    return std::max(slot, std::min(kShareMaxSlots * slot, kSharePartBytes));
+}
 
 // The prompts of a call that hold tokens and are continued by some row of it.  (No container: nothing here allocates.)
 struct SharePrompts {
@@ -1701,7 +1705,8 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
     cut->n_blocks = (int32_t)((most * G + width - 1) / width);
     cut->n_cols = (int32_t)(all_rows * G);
     const size_t slot = share_slot_bytes(all_rows, c->cfg.n_q_heads, c->cfg.head_dim);
-    const int64_t fit = (int64_t)std::min<size_t>(part_bytes / slot, kShareMaxSlots);
+    // (of a larger workspace no more than a call's own size has: the ranges do not depend on it)
+    const int64_t fit = (int64_t)std::max<size_t>(1, std::min<size_t>(std::min(part_bytes, kSharePartBytes) / slot, kShareMaxSlots));
     const int cus = spkv_compute_units(), round = cus > 0 ? cus : 256;
     std::fill(table->end, table->end + kShareTablePairs, (uint16_t)65535);
     if (n_lists > kShareTablePairs || lists > 16384) {       // as many ranges for all
@@ -1800,9 +1805,10 @@ int share_check(const spkv_cache* pc, const spkv_cache* c, const int32_t* prefix
     return SPKV_OK;
 }
 
-// own: null, or the sequences' own lists are attended here too (own_out, own_lse are then not read).
+// with_own: the sequences' own lists are attended here too (own_out, own_lse are then not read); decode: the workspace
+// is a decoding step's.
 int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, const uint16_t* q, const int32_t* cu,
-                 bool appended, bool with_own, const uint16_t* own_out, const float* own_lse, uint16_t* out, float* lse,
+                 bool appended, bool decode, bool with_own, const uint16_t* own_out, const float* own_lse, uint16_t* out, float* lse,
                  float sm_scale, char* ws, size_t ws_bytes, hipStream_t s) {
     const int B = c->cfg.batch, Hq = c->cfg.n_q_heads;
     const int64_t total = cu != nullptr ? cu[B] : B;
@@ -1816,7 +1822,7 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
     }
     SharePrompts prompts;
     share_prompts(pc, B, prefix_of, cu, &prompts);
-    const ShareCarve k = share_carve(total, Hq, c->cfg.head_dim);
+    const ShareCarve k = share_carve(total, Hq, c->cfg.head_dim, decode);
     SpkvShareCut cut = {};
     SpkvShareTable table = {};
     int groups = 1;
@@ -1882,18 +1888,19 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
                : SPKV_E_HIP;
 }
 
-bool share_workspace_ok(const spkv_cache* c, int64_t rows, const void* ws, size_t bytes) {
+bool share_workspace_ok(const spkv_cache* c, int64_t rows, bool decode, const void* ws, size_t bytes) {
     if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & (kAlign - 1)) != 0) return false;
-    const size_t at = share_carve(rows, c->cfg.n_q_heads, c->cfg.head_dim).part;
+    const size_t at = share_carve(rows, c->cfg.n_q_heads, c->cfg.head_dim, decode).part;
     return bytes >= at && bytes - at >= share_slot_bytes(rows, c->cfg.n_q_heads, c->cfg.head_dim);
 }
 }  // namespace
 
 size_t spkv_prefix_workspace_bytes(const spkv_cache_t* c, int64_t rows) {
     if (c == nullptr || rows <= 0 || rows * c->cfg.n_q_heads > (int64_t)1 << 30) return 0;
-    const size_t slot = share_slot_bytes(rows, c->cfg.n_q_heads, c->cfg.head_dim);
-    const size_t slots = std::max<size_t>(1, std::min<size_t>(kShareMaxSlots, kSharePartBytes / slot));
-    return share_carve(rows, c->cfg.n_q_heads, c->cfg.head_dim).part + align_up(slots * slot);
+    const int Hq = c->cfg.n_q_heads, D = c->cfg.head_dim;
+    const int64_t seqs = std::min<int64_t>(rows, SPKV_MAX_BATCH);          // of the largest decoding step
+    const size_t own = share_carve(seqs, Hq, D, true).part - share_carve(seqs, Hq, D, false).part;
+    return share_carve(rows, Hq, D, false).part + own + align_up(share_part_bytes(rows, Hq, D));
 }
 
 int spkv_prefix_attention(spkv_cache_t* pc, const spkv_cache_t* c, const int32_t* prefix_of, const void* q,
@@ -1905,9 +1912,9 @@ int spkv_prefix_attention(spkv_cache_t* pc, const spkv_cache_t* c, const int32_t
     if (total == 0) return SPKV_OK;
     if (q == nullptr || own_out == nullptr || own_lse == nullptr || out == nullptr) return SPKV_E_INVAL;
     if (!aligned16(q) || !aligned16(own_out) || !aligned16(own_lse) || !aligned16(out) || !aligned16(lse)) return SPKV_E_INVAL;
-    if (!share_workspace_ok(pc, total, workspace, workspace_bytes)) return SPKV_E_INVAL;
+    if (!share_workspace_ok(pc, total, false, workspace, workspace_bytes)) return SPKV_E_INVAL;
     if (!(sm_scale > 0.f)) sm_scale = 1.0f / std::sqrt((float)c->cfg.head_dim);
-    return share_attend(pc, c, prefix_of, static_cast<const uint16_t*>(q), cu_seqlens, appended != 0, false,
+    return share_attend(pc, c, prefix_of, static_cast<const uint16_t*>(q), cu_seqlens, appended != 0, false, false,
                         static_cast<const uint16_t*>(own_out), own_lse, static_cast<uint16_t*>(out), lse, sm_scale,
                         static_cast<char*>(workspace), workspace_bytes, static_cast<hipStream_t>(stream));
 }
@@ -1918,7 +1925,7 @@ int spkv_decode_attention_shared(spkv_cache_t* c, spkv_cache_t* pc, const int32_
     if (rc != SPKV_OK) return rc;
     const int B = c->cfg.batch;
     if (q == nullptr || out == nullptr || !aligned16(q) || !aligned16(out) || !aligned16(lse)) return SPKV_E_INVAL;
-    if (!share_workspace_ok(pc, B, workspace, workspace_bytes)) return SPKV_E_INVAL;
+    if (!share_workspace_ok(pc, B, true, workspace, workspace_bytes)) return SPKV_E_INVAL;
     if (!(sm_scale > 0.f)) sm_scale = 1.0f / std::sqrt((float)c->cfg.head_dim);
     hipStream_t s = static_cast<hipStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
@@ -1937,11 +1944,11 @@ int spkv_decode_attention_shared(spkv_cache_t* c, spkv_cache_t* pc, const int32_
         share_own(c, 1, ws, &own);
         fused = own.part != nullptr;
     }
-    if (fused) return share_attend(pc, c, prefix_of, qq, nullptr, true, true, nullptr, nullptr, o, lse, sm_scale, ws, workspace_bytes, s);
-    float* own_lse = lse != nullptr ? lse : reinterpret_cast<float*>(ws + share_carve(B, c->cfg.n_q_heads, c->cfg.head_dim).own_lse);
+    if (fused) return share_attend(pc, c, prefix_of, qq, nullptr, true, true, true, nullptr, nullptr, o, lse, sm_scale, ws, workspace_bytes, s);
+    float* own_lse = lse != nullptr ? lse : reinterpret_cast<float*>(ws + share_carve(B, c->cfg.n_q_heads, c->cfg.head_dim, true).own_lse);
     rc = spkv_decode_attention(c, q, out, own_lse, sm_scale, stream);
     if (rc != SPKV_OK) return rc;
-    return share_attend(pc, c, prefix_of, qq, nullptr, true, false, o, own_lse, o, lse, sm_scale, ws, workspace_bytes, s);
+    return share_attend(pc, c, prefix_of, qq, nullptr, true, true, false, o, own_lse, o, lse, sm_scale, ws, workspace_bytes, s);
 }
 
 namespace {
