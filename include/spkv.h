@@ -354,7 +354,9 @@ int spkv_soft_gated_attention(const void* q, const void* k, const void* v, const
  * the lengths after the prompt's append, as spkv_decode_attention does, and never in steady state.  May be
  * captured: the place of a row is read on the device.  Copies of a sequence get results that agree to rounding.
  * Errors: SPKV_E_INVAL for shapes that differ, indices out of range, bad pointers, a workspace without
- * room for one range; SPKV_E_STATE if a sequence holds fewer tokens than the call has appended. */
+ * room for one range, more rows than a launch holds (2^24 - 1 over n_q_heads * head_dim / 1024, rounded up; fewer
+ * with more than 256 lists, active prompts times KV heads, of very uneven numbers of rows); SPKV_E_STATE if a sequence
+ * holds fewer tokens than the call has appended. */
 size_t spkv_prefix_workspace_bytes(const spkv_cache_t* prefix, int64_t max_total_rows);
 int spkv_prefix_attention(spkv_cache_t* prefix, const spkv_cache_t* cache, const int32_t* prefix_of,
                           const void* q, const int32_t* cu_seqlens, int32_t appended,

@@ -1656,6 +1656,12 @@ size_t share_slot_bytes(int64_t rows, int n_q_heads, int head_dim) {
 }
 constexpr size_t kSharePartBytes = (size_t)96 << 20;     // ranges are no more than fit, beyond the first
 constexpr int kShareMaxSlots = 255;
+constexpr int64_t kShareLaunchThreads = ((int64_t)1 << 32) - 1;          // of a launch, at most
+// Does the join of a call of this many rows fit a launch (spkv_launch_prefix)?
+bool share_rows_ok(int64_t rows, int n_q_heads, int head_dim) {
+    const int columns = 1024 / head_dim;                     // of a workgroup of 256 threads
+    return rows <= kShareLaunchThreads / 256 / ((n_q_heads + columns - 1) / columns);
+}
 // Bytes of the ranges' partial results; never less for more rows.
 size_t share_part_bytes(int64_t rows, int n_q_heads, int head_dim) {
     const size_t slot = share_slot_bytes(rows, n_q_heads, head_dim);
@@ -1690,7 +1696,8 @@ void share_prompts(const spkv_cache* pc, int batch, const int32_t* prefix_of, co
 // Ranges of the prompts' lists: about as many workgroups as the chip holds at once, every list cut evenly into its
 // share of them.
 constexpr int kShareMinUnit = 2, kShareStart = 16;
-void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_bytes, int* groups, SpkvShareCut* cut,
+// False: more workgroups than a launch holds.
+bool share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_bytes, int* groups, SpkvShareCut* cut,
                SpkvShareTable* table) {
     const int Hkv = c->cfg.n_kv_heads, G = c->carve.G, n = prompts.n, n_lists = n * Hkv;
     int64_t most = 0, all_rows = 0, lists = 0;
@@ -1711,8 +1718,10 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
     std::fill(table->end, table->end + kShareTablePairs, (uint16_t)65535);
     if (n_lists > kShareTablePairs || lists > 16384) {       // as many ranges for all
         cut->uniform = cut->slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(fit, round / lists));
-        cut->n_units = (int32_t)((int64_t)n_lists * cut->uniform * cut->n_blocks);
-        return;
+        const int64_t units = (int64_t)n_lists * cut->uniform * cut->n_blocks;
+        if (units * 64 * spkv_prefix_kernel_waves(*groups) > kShareLaunchThreads) return false;
+        cut->n_units = (int32_t)units;
+        return true;
     }
     int32_t hp[kShareTablePairs], copies[kShareTablePairs];      // half-pages, the ring's twice (ShareList::begin)
     int64_t work = 0;
@@ -1757,6 +1766,7 @@ void share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
         table->ranges[i] = (uint8_t)r;
     }
     cut->n_units = (int32_t)end;
+    return true;
 }
 
 // Items of the sequences' own lists, in the same launch as the prompts'; part null: not.  Every list in the same number
@@ -1798,8 +1808,7 @@ int share_check(const spkv_cache* pc, const spkv_cache* c, const int32_t* prefix
         if (prefix_of[b] < -1 || prefix_of[b] >= x.batch || (pc == c && prefix_of[b] == b)) return SPKV_E_INVAL;
         if (cu != nullptr && cu[b + 1] < cu[b]) return SPKV_E_INVAL;
     }
-    // (the partial results are addressed by row * heads in 32 bits)
-    if (cu != nullptr && (int64_t)cu[y.batch] * y.n_q_heads > (int64_t)1 << 30) return SPKV_E_INVAL;
+    if (cu != nullptr && !share_rows_ok(cu[y.batch], y.n_q_heads, y.head_dim)) return SPKV_E_INVAL;
     for (int b = 0; b < y.batch; ++b)
         if (appended && c->T[b] < tokens_for(cu, b)) return SPKV_E_STATE;
     return SPKV_OK;
@@ -1827,7 +1836,7 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
     SpkvShareTable table = {};
     int groups = 1;
     cut.slots = 1;
-    if (prompts.n > 0) share_cut(pc, prompts, ws_bytes - k.part, &groups, &cut, &table);
+    if (prompts.n > 0 && !share_cut(pc, prompts, ws_bytes - k.part, &groups, &cut, &table)) return SPKV_E_INVAL;
     cut.part = reinterpret_cast<float*>(ws + k.part);
     cut.n_out = total * Hq;
     SpkvShareOwn own = {};
@@ -1896,7 +1905,7 @@ bool share_workspace_ok(const spkv_cache* c, int64_t rows, bool decode, const vo
 }  // namespace
 
 size_t spkv_prefix_workspace_bytes(const spkv_cache_t* c, int64_t rows) {
-    if (c == nullptr || rows <= 0 || rows * c->cfg.n_q_heads > (int64_t)1 << 30) return 0;
+    if (c == nullptr || rows <= 0 || !share_rows_ok(rows, c->cfg.n_q_heads, c->cfg.head_dim)) return 0;
     const int Hq = c->cfg.n_q_heads, D = c->cfg.head_dim;
     const int64_t seqs = std::min<int64_t>(rows, SPKV_MAX_BATCH);          // of the largest decoding step
     const size_t own = share_carve(seqs, Hq, D, true).part - share_carve(seqs, Hq, D, false).part;

@@ -100,5 +100,28 @@ def test_less_than_one_range_is_refused():
     assert got[0][0] == 0 and got[1][0] == -1
 
 
+def _fit(rows, heads):
+    """A launch has fewer than 2^32 threads: one of four elements of every output, rows filled up to workgroups of 256."""
+    return rows * -(-heads // 8) * 256 < 1 << 32
+
+
+@pytest.mark.parametrize("heads", [8, 24, 32, 128])
+def test_more_rows_than_a_launch_holds(heads):
+    most = ((1 << 24) - 1) // (heads // 8)
+    assert _fit(most, heads) and not _fit(most + 1, heads)
+    fits, more = _run(heads, 1, [["join", most, most], ["join", most + 1, most]])
+    assert fits[0] == 0 and fits[1] > 0 and len(fits[2]) == 2 and all(x * t < 1 << 32 for _, x, t in fits[2])
+    assert more[0] == -1 and more[2] == []
+    assert _run(heads, 1, [["join", 1, most + 1]])[0][1] == 0          # no size either
+
+
+def test_more_workgroups_than_a_launch_holds():
+    """Many prompts, whose lists all have as many blocks of columns as the widest one."""
+    rows = 1 << 21
+    few, many = _run(32, 40, [["join", rows, rows]], prompts=[70] * 20)[0], _run(32, 40, [["join", rows, rows]], prompts=[70] * 40)[0]
+    assert few[0] == 0 and all(x * t < 1 << 32 for _, x, t in few[2])
+    assert many[0] == -1 and many[2] == []
+
+
 if __name__ == "__main__":
     _main()
