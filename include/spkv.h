@@ -333,8 +333,8 @@ int spkv_soft_gated_attention(const void* q, const void* k, const void* v, const
  * window, and else if that key's gate is on -- the keys it would see had the prompt been
  * appended to its own sequence (Eq. 3-5).  (Keys are stored as they are given: rotary positions of
  * the sequence's tokens start at P.)  One pass over a prompt's lists serves all rows that
- * continue it.  The prompts' cache is only read, and may serve any number of caches; appending to it
- * changes what is attended to from then on.
+ * continue it.  The prompts' cache is only read, and may serve any number of caches, from as many threads and streams,
+ * as long as no call that changes it runs beside them; appending to it changes what is attended to from then on.
  *
  * spkv_prefix_attention joins the attention of a call's tokens over their own sequences, which
  * any of the calls above has left, with that over their prompts:

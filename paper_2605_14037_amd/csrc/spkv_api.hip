@@ -8,6 +8,7 @@
 #include <cstdint>
 #include <cstdlib>
 #include <cstring>
+#include <exception>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -181,6 +182,7 @@ struct spkv_cache {
     bool split_only;
     std::vector<hipEvent_t> events;   // pairs (before, after)
     int n_timed;
+    std::mutex prompt_lengths;        // held while a call over shared prompts reads this (prompts') cache's lengths back
 };
 
 namespace {
@@ -1821,13 +1823,16 @@ int share_attend(spkv_cache* pc, const spkv_cache* c, const int32_t* prefix_of, 
                  float sm_scale, char* ws, size_t ws_bytes, hipStream_t s) {
     const int B = c->cfg.batch, Hq = c->cfg.n_q_heads;
     const int64_t total = cu != nullptr ? cu[B] : B;
-    if (pc->bound_is_loose) {
-        try {
+    try {
+        // One prompts' cache serves any number of caches, whose calls may come from threads of their own: the first one after
+        // its append reads the lengths, the others wait for that.
+        std::lock_guard<std::mutex> lock(pc->prompt_lengths);
+        if (pc->bound_is_loose) {
             const int rc = exact_lengths(pc, s);
             if (rc != SPKV_OK) return rc;
-        } catch (const std::bad_alloc&) {
-            return SPKV_E_NOMEM;
         }
+    } catch (const std::exception&) {                        // no memory; no lock
+        return SPKV_E_NOMEM;
     }
     SharePrompts prompts;
     share_prompts(pc, B, prefix_of, cu, &prompts);
