@@ -365,7 +365,14 @@ def qk_norm_rope(q, k, positions, rope, q_weight=None, k_weight=None, eps=None, 
     """RMS norm of every head (eps None: no norm), rotation by positions, dense layout, in one launch
     (spkv_qk_norm_rope).  q: bf16 or fp32 [tokens, H_q, D]; k, v: [tokens, H_kv, D], slices of a
     projection's rows as they are; positions: int32 [tokens] or [axes, tokens].  out: tensors to write
-    (the inputs themselves may be passed).  Returns (q, k) or, with v, (q, k, v)."""
+    (the inputs themselves may be passed).  Returns (q, k) or, with v, (q, k, v); where an input or a weight
+    requires a gradient (and none is given to write), outputs whose backward pass is qk_norm_rope_backward."""
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or (v is not None and v.requires_grad) or
+                                    (q_weight is not None and q_weight.requires_grad) or
+                                    (k_weight is not None and k_weight.requires_grad)):
+        if out is not None:
+            raise ValueError("out: no gradient passes through tensors to write; leave it out, or call under torch.no_grad()")
+        return _NormRope.apply(q, k, v, q_weight, k_weight, positions, rope, eps)
     n, hq, hk, d, ins, pp, qw, kw, eps = _rope_call(q, k, v, positions, rope, q_weight, k_weight, eps, "qkv")
     out, outs = _rope_out(out, q, v, n, hq, hk, d)
     at = _packed(ins + outs)
@@ -380,7 +387,7 @@ def qk_norm_rope_backward(dq, dk, positions, rope, q=None, k=None, q_weight=None
     q, k: the forward's inputs (only with a norm).  out: tensors for the inputs' gradients, for example
     slices of one buffer for the projection's rows.  Returns (dq, dk), with dv (dq, dk, dv) -- or nothing
     of these if `out` was given -- and then, with a norm and unless want_weights is False, the
-    fp32 gradients of both weights."""
+    fp32 gradients of both weights.  What it returns carries no gradient of its own."""
     n, hq, hk, d, ins, pp, qw, kw, eps = _rope_call(dq, dk, dv, positions, rope, q_weight, k_weight, eps,
                                                     ("dq", "dk", "dv"))
     given, dtype = out is not None, dq.dtype
@@ -407,6 +414,36 @@ def qk_norm_rope_backward(dq, dk, positions, rope, q=None, k=None, q_weight=None
                                           dqw, dkw, ws, ws_bytes, _stream()), "spkv_qk_norm_rope_backward")
     first = () if given else tuple(out[:2]) if dv is None else tuple(out)
     return first + tuple(weights)
+
+
+def _as_heads(t):
+    """t, or a dense copy where its strides or address are not those of a set of heads."""
+    unit, st = 16 // t.element_size(), t.stride()
+    if st[2] == 1 and st[1] % unit == 0 and st[0] % unit == 0 and t.data_ptr() % 16 == 0:
+        return t
+    return t.clone(memory_format=torch.contiguous_format)
+
+
+class _NormRope(torch.autograd.Function):
+    """qk_norm_rope with qk_norm_rope_backward as its gradient; the values' is theirs as it comes."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, q_weight, k_weight, positions, rope, eps):
+        ctx.rope, ctx.eps = rope, eps
+        ctx.save_for_backward(positions, *((q, k, q_weight, k_weight) if eps is not None else ()))
+        return qk_norm_rope(q, k, positions, rope, q_weight, k_weight, eps, v)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq, dk, dv=None):
+        need = ctx.needs_input_grad
+        if not (need[0] or need[1] or need[3] or need[4]):
+            return None, None, dv, None, None, None, None, None
+        positions, *x = ctx.saved_tensors
+        norm = dict(zip(("q", "k", "q_weight", "k_weight"), x), eps=ctx.eps, want_weights=need[3] or need[4]) if x else {}
+        got = qk_norm_rope_backward(_as_heads(dq), _as_heads(dk), positions, ctx.rope, **norm) + (None, None)
+        wanted = [g if n else None for g, n in zip((got[0], got[1], dv, got[2], got[3]), need)]
+        return (*wanted, None, None, None)
 
 
 def _check(code, where):
