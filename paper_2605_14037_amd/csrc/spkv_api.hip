@@ -1718,9 +1718,9 @@ bool share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
     const int64_t fit = (int64_t)std::max<size_t>(1, std::min<size_t>(std::min(part_bytes, kSharePartBytes) / slot, kShareMaxSlots));
     const int cus = spkv_compute_units(), round = cus > 0 ? cus : 256;
     std::fill(table->end, table->end + kShareTablePairs, (uint16_t)65535);
-    if (n_lists > kShareTablePairs || lists > 16384) {       // as many ranges for all
-        cut->uniform = cut->slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(fit, round / lists));
-        const int64_t units = (int64_t)n_lists * cut->uniform * cut->n_blocks;
+    if (n_lists > kShareTablePairs || lists > 16384) {       // more than the table holds, more than compute units in any case:
+        cut->whole = cut->slots = 1;                         // one range each, however unlike their lengths are
+        const int64_t units = (int64_t)n_lists * cut->n_blocks;
         if (units * 64 * spkv_prefix_kernel_waves(*groups) > kShareLaunchThreads) return false;
         cut->n_units = (int32_t)units;
         return true;

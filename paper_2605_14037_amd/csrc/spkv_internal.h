@@ -253,7 +253,7 @@ struct SpkvShareCut {
     int64_t n_out;              // rows * Hq of the call
     int32_t n_units;            // workgroups of the prompts' lists
     int32_t slots;              // most ranges of a list
-    int32_t uniform;            // > 0: every list has this many ranges and n_blocks blocks of columns; 0: SpkvShareTable
+    int32_t whole;              // 1: every list is one range, of n_blocks blocks of columns; 0: SpkvShareTable
     int32_t n_blocks;           // blocks of columns of the prompt with the most rows
     int32_t n_cols;             // rows of all prompts * G
 };

@@ -317,19 +317,17 @@ __device__ __forceinline__ void own_item(const SpkvView& v, const uint16_t* __re
 // Which list, range and block of columns a workgroup has: id counts workgroups without gaps, the ranges of a list's
 // block of columns next to each other (round-robin over the XCDs).  With up to kShareTablePairs lists the host's
 // table says where each list's workgroups end -- ids with nothing to do in between would fill some
-// XCDs' compute units and leave others idle; with more lists each has as many.
+// XCDs' compute units and leave others idle; with more lists each is one range.
 struct ShareUnit {
     int list, range, ranges, block;
 };
 __device__ __forceinline__ ShareUnit find_unit(const SpkvShareCut& cut, const SpkvShareTable& table, int id, int n_kv_heads) {
     ShareUnit u;
-    if (cut.uniform > 0) {
-        const int each = cut.uniform * cut.n_blocks;
-        u.list = id / each;
-        const int rest = id - u.list * each;
-        u.ranges = cut.uniform;
-        u.block = rest / u.ranges;
-        u.range = rest - u.block * u.ranges;
+    if (cut.whole != 0) {
+        u.list = id / cut.n_blocks;
+        u.block = id - u.list * cut.n_blocks;
+        u.range = 0;
+        u.ranges = 1;
         return u;
     }
     const int lane = threadIdx.x & 63;
@@ -930,7 +928,7 @@ __global__ __launch_bounds__(256, 8) void spkv_prefix_merge(SpkvShareCut cut, Sp
     float M = SPKV_NEG_INF, den = 0.f;
     f32x4 num = {0.f, 0.f, 0.f, 0.f};
     const int h_first = head0 / G, h_last = (min(head0 + kCols, n_q_heads) - 1) / G;      // (one, or the table is asked per lane)
-    const int ranges = act < 0 ? 0 : cut.uniform > 0 ? cut.uniform
+    const int ranges = act < 0 ? 0 : cut.whole != 0 ? 1
                      : h_first == h_last ? rows.ranges[act * n_kv_heads + h_first] : rows.ranges[act * n_kv_heads + h];
     const int pair = row * n_kv_heads + h, parts = ranges + (own.part != nullptr ? own_ranges(own, pair) : 0);
     if (own.part == nullptr && share == 0 && exists) {
