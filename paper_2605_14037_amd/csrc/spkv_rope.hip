@@ -64,7 +64,7 @@ template <typename T> struct Raw8;
 template <> struct Raw8<uint16_t> { uint4 u; };
 template <> struct Raw8<float> { uint4 u, w; };
 
-// STREAM (see Streaming below): 1: loads, 2: stores too ask the caches for no retention.
+// STREAM (see Streaming below; bf16): 1: loads, 2: stores too ask the caches for no retention.
 template <int STREAM>
 __device__ __forceinline__ uint4 load_unit(const void* p) {
     if (STREAM > 0) return __builtin_bit_cast(uint4, load_stream_b128(static_cast<const uint16_t*>(p)));
@@ -80,15 +80,15 @@ template <int STREAM>
 __device__ __forceinline__ void load8(Raw8<uint16_t>& r, const uint16_t* p) { r.u = load_unit<STREAM>(p); }
 template <int STREAM>
 __device__ __forceinline__ void load8(Raw8<float>& r, const float* p) {
-    r.u = load_unit<STREAM>(p);
-    r.w = load_unit<STREAM>(p + 4);
+    r.u = *reinterpret_cast<const uint4*>(p);
+    r.w = *reinterpret_cast<const uint4*>(p + 4);
 }
 template <int STREAM>
 __device__ __forceinline__ void store8(const Raw8<uint16_t>& r, uint16_t* p) { store_unit<STREAM>(r.u, p); }
 template <int STREAM>
 __device__ __forceinline__ void store8(const Raw8<float>& r, float* p) {
-    store_unit<STREAM>(r.u, p);
-    store_unit<STREAM>(r.w, p + 4);
+    *reinterpret_cast<uint4*>(p) = r.u;
+    *reinterpret_cast<uint4*>(p + 4) = r.w;
 }
 __device__ __forceinline__ void widen8(const Raw8<uint16_t>& r, float (&x)[8]) {
     const unsigned w[4] = {r.u.x, r.u.y, r.u.z, r.u.w};
@@ -468,12 +468,15 @@ int spkv_rope_backward_blocks(int64_t n_rows, int n_heads, int head_dim) {
     return (int)std::min<int64_t>((n_rows + rows - 1) / rows, kRopeGradBlocks);
 }
 
-// Streaming.  Once a call moves more than the 256 MB of the last cache, what it reads is not there and need not stay: loads
+// Streaming.  Once a bf16 call moves more than the 256 MB of the last cache, what it reads is not there and need not stay: loads
 // without retention leave the cache to what is written, for whoever reads that next -- unless that alone is more than it
-// holds.  bf16, D = 128, gradients of 16384 tokens (570 MB, 201 of them written): into buffers that are not in the
-// cache 120.8 -> 117.9 us, into the last call's 121 -> 101; 8192 tokens (285 MB) 64.9 either way; forward of 16384 tokens 82.7
-// either way, 82.6 -> 66.2 into the last call's; of 32768 (805 MB, 403 written) plain 156, loads 159, stores too 153.
-// fp32 gradients, D = 64, 10000 tokens (348 MB): 77.9 -> 80.8, the same into the last call's.
+// holds.  D = 128, 40 normed heads of 48, us plain / such loads / stores too, into buffers that are not in the cache: gradients of
+// 6800 tokens (251 MB) 57.6 / 53.9 / 55.4, 16384 (604 MB, 201 of them written) 121 / 118 / 112, 32768 (1208, 403 written)
+// 229 / 226 / 216; forward of 14000 (344) 70.8 / 70.6 / 68.1, 32768 (805, 403 written) 156 / 157 / 151.  Into the last call's
+// buffers, where loads alone leave what is written for the next kernel: 6800 tokens 47.7 / 51.4 / 53.4, 16384 120 / 102 / 111, 32768
+// 229 / 227 / 214; forward of 14000 67.9 / 58.1 / 67.8, 32768 156 / 157 / 150.
+// fp32 calls, two loads and stores a chunk, do without: forward of 16384 tokens (805 MB) 158 / 164 / 168, gradients of 8192 (604 MB)
+// 122 / 129 / 133, with D = 64 of 20000 (461 MB) 98 / 103 / 105; into the last call's buffers 158 / 163 / 168, 122 / 121 / 133, 97 / 98 / 104.
 constexpr int64_t kStreamBytes = (int64_t)320 << 20, kStreamWritten = (int64_t)256 << 20;
 
 template <typename T, int D, bool ADJ, bool NORM, int STREAM>
@@ -498,9 +501,12 @@ template <typename T, int D, bool ADJ, bool NORM>
 static hipError_t launch_rope(const SpkvRope& a, const RopeTable& table, bool backward, hipStream_t s) {
     const int64_t written = (int64_t)a.n_rows * D * sizeof(T);
     const int64_t moved = 2 * written + (backward && NORM ? (int64_t)a.n_tokens * (a.n_q + a.n_kv) * D * sizeof(T) : 0);
-    if (moved <= kStreamBytes) return launch_rope<T, D, ADJ, NORM, 0>(a, table, backward, s);
-    return written <= kStreamWritten ? launch_rope<T, D, ADJ, NORM, 1>(a, table, backward, s)
-                                     : launch_rope<T, D, ADJ, NORM, 2>(a, table, backward, s);
+    if constexpr (sizeof(T) == 2) {
+        if (moved > kStreamBytes)
+            return written <= kStreamWritten ? launch_rope<T, D, ADJ, NORM, 1>(a, table, backward, s)
+                                             : launch_rope<T, D, ADJ, NORM, 2>(a, table, backward, s);
+    }
+    return launch_rope<T, D, ADJ, NORM, 0>(a, table, backward, s);
 }
 
 template <typename T, int D>
