@@ -837,7 +837,8 @@ class SPKVCache:
 
 class PrefixSharing:
     """Which sequence of `prefix`, a cache that holds prompts, every sequence of another cache continues
-    (-1: none).  Host memory only; prefix_of may be changed in place (sharing[b] = p) as sequences come and go."""
+    (-1: none).  Host memory only; prefix_of may be changed in place (sharing[b] = p) as sequences come and go: calls
+    from then on see it, launches captured before keep what they were captured with."""
 
     def __init__(self, prefix, prefix_of):
         self.prefix, self.batch = prefix, len(prefix_of)

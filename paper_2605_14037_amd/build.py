@@ -22,7 +22,9 @@ FLAGS = [
 # register count depends on how the compiler schedules loads against MFMAs): the library
 # adapts its work-item count to whatever the runtime reports, but a drop costs bandwidth.
 EXPECTED_OCCUPANCY = {"spkv_decode_splitILi128E": 3,      # every mode and merge width at head_dim 128
-                      "spkv_decode_split_compactILi128E": 3}
+                      "spkv_decode_split_compactILi128E": 3,
+                      "spkv_prefix_fewILi128E": 2, "spkv_prefix_splitILi128ELi4E": 2, "spkv_prefix_splitILi128ELi8E": 2,
+                      "spkv_rope_forwardItLi128E": 7, "spkv_rope_backwardItLi128E": 4}
 
 
 def _check_occupancy(remarks: str) -> list:

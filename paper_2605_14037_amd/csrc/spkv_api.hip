@@ -1641,6 +1641,9 @@ struct ShareCarve {
 };
 // Sequences whose lists are short are attended in the prompts' launch, at most kShareOwnSlots items to a list (two
 // half-pages each in the longest); only calls of one token a sequence.
+// (32 heads over 8 of 128, replayed from a graph, us with 4 / 8 / 16 items: one sequence of 22 half-pages behind 2k 14.3 / 10.3 / 9.7, of 54
+// 24.7 / 16.1 / 12.1; four of 54 behind 32k 28.6 / 20.3 / 18.7; 16 and 64 the same with any; twice the workspace with 16.  Items of
+// 1 / 2 / 4 half-pages: four of 6 behind 32k 14.1 / 14.9 / 15.5, 16 22.5 / 21.9 / 22.1, 64 behind 128k 57.2 / 55.0 / 55.5.)
 constexpr int kShareOwnSlots = 8, kShareOwnItem = 2;
 ShareCarve share_carve(int64_t rows, int n_q_heads, int head_dim, bool decode) {
     ShareCarve k;
@@ -1773,6 +1776,9 @@ bool share_cut(const spkv_cache* c, const SharePrompts& prompts, size_t part_byt
 
 // Items of the sequences' own lists, in the same launch as the prompts'; part null: not.  Every list in the same number
 // of items, as many as fill the chip once with one to a wave.
+// Longer lists take spkv_decode_attention's launches before.  us in the prompts' launch / before it, replayed from a graph: one
+// sequence behind 32k with 41 half-pages 16.8 / 20.6, 64 19.5 / 21.0, 91 24.2 / 21.5, 254 50 / 26; 16 with 41 30 / 41, 91 50 / 56, 254
+// 109 / 106; 64 behind 128k with 41 99 / 108, 129 206 / 217.  The limit is one sequence's, whose list has the fewest waves.
 constexpr int kShareOwnLongest = 64;         // half-pages
 void share_own(const spkv_cache* c, int waves, char* part, SpkvShareOwn* own) {
     const int n = c->carve.n_pairs, Hkv = c->cfg.n_kv_heads;

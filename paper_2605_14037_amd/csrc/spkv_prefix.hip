@@ -892,7 +892,9 @@ void spkv_prefix_split(SpkvView v, const uint16_t* __restrict__ q, float scale_l
 
 // The join: D / 4 threads own a column (row, head), four consecutive elements each; S such groups share a column,
 // each with every S-th of its partial results, and meet in LDS (few columns of many ranges: 512 columns
-// of 64 ranges in one group each took 14 us, a chain of eight round trips on a quarter of the chip).
+// of 64 ranges in one group each took 14 us, a chain of eight round trips on a quarter of the chip).  kFold results are loaded
+// before any is used.  Call, joins included, with 2 / 5 / 8: one sequence behind 32k (S = 8) 13.2 / 12.5 / 14.0 us, 16 21.4 / 21.4 /
+// 25.6; four questions of 512 tokens behind 2k (S = 1, few ranges and many columns) 49.2 / 52.3 / 49.3.
 // The sequence's own part is a set of partial results too (own.part), or comes as a call's bf16 output and fp32
 // logarithm of its sum: half a step of bf16 more than from sums in 32 bits, on the share that the own tokens have.
 template <int D, int S>
