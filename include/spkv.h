@@ -61,6 +61,7 @@ extern "C" {
 #define SPKV_MAX_BATCH     512 /* sequences per cache                                       */
 #define SPKV_PAGE_TOKENS   64  /* key/value pairs per long-term page                        */
 #define SPKV_MAX_CHUNK_TOKENS 16 /* new tokens per sequence in one spkv_decode_chunk call   */
+#define SPKV_MAX_TREE_NODES 64 /* drafts per sequence of a tree, rows of one append of them  */
 
 typedef struct spkv_cache spkv_cache_t;   /* opaque host object */
 
@@ -382,6 +383,47 @@ int spkv_prefix_attention(spkv_cache_t* prefix, const spkv_cache_t* cache, const
 int spkv_decode_attention_shared(spkv_cache_t* cache, spkv_cache_t* prefix, const int32_t* prefix_of,
                                  const void* q, void* out, float* lse, float sm_scale,
                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* Append of chosen rows: spkv_append of the tokens k[rows[i]], v[rows[i]], util_logits[rows[i]].  The drafts of a
+ * tree that were accepted lie here and there in its buffers; this takes them from where they are.
+ *   k, v         device bf16 [n_rows, n_kv_heads, head_dim]    util_logits device fp32 [n_rows, n_kv_heads]
+ *   rows         device int32 [cu_seqlens[batch]]: sequence b's tokens, in order, are the rows
+ *                rows[cu_seqlens[b]] .. rows[cu_seqlens[b + 1] - 1]; any order, the same row more than once
+ *   cu_seqlens   host int32 [batch + 1], at most SPKV_MAX_TREE_NODES tokens a sequence
+ * A row that is not in 0 .. n_rows - 1 makes the cache's state an error (spkv_cache_stats: SPKV_E_DEVICE); no memory
+ * outside the rows is read.  One launch.  Errors as for spkv_append; SPKV_E_INVAL if a sequence has more tokens. */
+int spkv_append_rows(spkv_cache_t* cache, const void* k, const void* v, const float* util_logits,
+                     const int32_t* rows, int32_t n_rows, const int32_t* cu_seqlens, void* stream);
+
+/* Sequences that become others, all at once: parallel samples of a prompt, beams that take each other's places,
+ * sequences taken over from the cache that their prompts were fed into, slots given back.
+ *   source   host int32 [batch of cache]: sequence b becomes what sequence source[b] of `from` was before the call;
+ *            SPKV_FORK_KEEP: stays as it is; SPKV_FORK_EMPTY: holds no token any more, its pages are the pool's
+ *   from     the cache that is copied from, with the same heads, head_dim and window; NULL or `cache`: itself.  Another
+ *            cache is only read; its threshold and sinks have decided over what its lists hold, those of `cache`
+ *            decide over what leaves the windows from then on
+ * Within a cache the first sequence that takes the contents of one that is itself replaced or emptied has its pages;
+ * only further ones are copied, so beams that trade places move page ids and windows.  The same sequence may be taken by any
+ * number of others.  Copies are the same to the last bit, and independent of each other from then on.
+ * Two launches at most.  Waits once for the lengths after a prompt's append to `from`, as spkv_decode_attention does, and
+ * where the pool might not hold the copies; else it does not synchronise (a sequence is given back without waiting, too).
+ * Errors: SPKV_E_INVAL for shapes that differ and sources out of range; SPKV_E_CAPACITY if the pool or max_context cannot hold
+ * the result (nothing is changed); SPKV_E_STATE under stream capture -- a replay would move sequences that the
+ * host's bookkeeping knows nothing of -- unless nothing is to be done. */
+#define SPKV_FORK_KEEP  -1
+#define SPKV_FORK_EMPTY -2
+int spkv_cache_fork(spkv_cache_t* cache, spkv_cache_t* from, const int32_t* source, void* stream);
+
+/* What sequences hold, as dense rows: for every KV head the pairs of its long-term list and then those of the window,
+ * positions ascending -- what attention reads, for a host store, another kernel, a test.
+ *   sequences    host int32 [n], any of them more than once, n * n_kv_heads <= 65535; NULL: the first n
+ *   k, v         device bf16 [n, n_kv_heads, rows, head_dim]
+ *   util_logits  device fp32 [n, n_kv_heads, rows]     positions  device int32 [n, n_kv_heads, rows]
+ *   counts       device int32 [n, n_kv_heads]: pairs held
+ * Any of the outputs may be NULL.  A head that holds more than `rows` pairs gives its first ones (counts says how many there
+ * are); rows behind the last pair are left as they were.  One launch, no synchronisation; may be captured. */
+int spkv_cache_gather(spkv_cache_t* cache, const int32_t* sequences, int32_t n, int64_t rows, void* k, void* v,
+                      float* util_logits, int32_t* positions, int32_t* counts, void* stream);
 
 /* Forget sequence b (for example when its request has finished): its window and long-term
  * entries are dropped, its pages return to the pool for reuse by any sequence, and slot b

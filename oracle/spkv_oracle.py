@@ -240,6 +240,22 @@ class SPKVOracle:
         self._fbuf[b] = np.zeros((0, self.Hkv), np.float32)
         self._len[b] = 0
 
+    def fork(self, source, other=None):
+        """Sequence b becomes what sequence source[b] (of `other`, or of this oracle) was before the call;
+        -1: it stays, -2: it holds nothing any more."""
+        of = self if other is None else other
+        fields = ("_kbuf", "_vbuf", "_fbuf", "_len", "_theta_hist", "_prunes")
+        before = {name: list(getattr(of, name)) for name in fields}
+        for b, s in enumerate(source):
+            if s == -2:
+                self.release_sequence(b)
+            elif s >= 0:
+                for name in fields:
+                    x = before[name][s]
+                    getattr(self, name)[b] = x.copy() if hasattr(x, "copy") else x
+                if other is not None:                  # this one's threshold decides from here on
+                    self._theta_hist[b].append((self._len[b], self.theta))
+
     # ------------------------------------------------------------- bookkeeping
     def seq_len(self, b):
         return self._len[b]
@@ -299,6 +315,11 @@ class SPKVOracle:
         stored position t: s <= t and (t - s < w or z_s)."""
         s = np.arange(t + 1)
         return ((t - s) < self.w) | self.gate(b, h)[:t + 1]
+
+    def held(self, b, h):
+        """Positions whose pairs the cache of (b, h) holds, ascending: the kept ones, then the window's."""
+        T = self.seq_len(b)
+        return np.concatenate([self.kept_positions(b, h), np.arange(max(0, T - self.w), T, dtype=np.int32)])
 
     def stats(self):
         """Eq. 8 in both readings, plus byte counts at 2 bytes per element."""
@@ -403,3 +424,41 @@ class SPKVOracle:
             with ThreadPoolExecutor(max_workers=workers) as ex:
                 list(ex.map(job, pairs))
         return out, lse
+
+    def score_tree(self, k, v, util_logits, q, parents, counts):
+        """Outputs of the drafts of a tree, the history left as it is.  Draft i of sequence b hangs behind draft
+        parents[i] of the same sequence (an index within it; anything but 0 .. i - 1: behind the newest token) and
+        stands at the position behind it.  It attends as if the drafts on the path to it, and no others, had been
+        appended (Eq. 3-5).  k, v: [sum(counts), H_kv, D], util_logits fp32 [sum(counts), H_kv], q [sum(counts), H_q,
+        D], packed by sequence.  A draft sees at least itself.  Returns (out, lse) in fp64."""
+        q = np.asarray(q, np.float64)
+        k, v = np.asarray(k, np.float64), np.asarray(v, np.float64)
+        f = np.asarray(util_logits)
+        if f.dtype != np.float32:
+            raise TypeError("utility logits must be float32")
+        out, lse, row0 = np.zeros(q.shape), np.zeros(q.shape[:2]), 0
+        for b in range(self.B):
+            T, paths = self.seq_len(b), []
+            for i in range(int(counts[b])):
+                p = int(parents[row0 + i])
+                paths.append((paths[p] if 0 <= p < i else []) + [i])
+                path, t = [row0 + j for j in paths[i]], T + len(paths[i]) - 1
+                for h in range(self.Hkv):
+                    s = np.arange(t + 1)
+                    gate = np.concatenate([self.gate_now(b, h), (f[path, h] >= self.theta)]) | (s < self.n_sink)
+                    seen = (t - s < self.w) | gate
+                    K = np.concatenate([self._k(b)[:, h].astype(np.float64), k[path, h]])[seen]
+                    V = np.concatenate([self._v(b)[:, h].astype(np.float64), v[path, h]])[seen]
+                    x = self.scale * (K @ q[row0 + i, h * self.G:(h + 1) * self.G].T)
+                    m = x.max(axis=0)
+                    e = np.exp(x - m)
+                    den = e.sum(axis=0)
+                    out[row0 + i, h * self.G:(h + 1) * self.G] = (e.T @ V) / den[:, None]
+                    lse[row0 + i, h * self.G:(h + 1) * self.G] = m + np.log(den)
+            row0 += int(counts[b])
+        return out, lse
+
+    def gate_now(self, b, h):
+        """z_s of every stored position as attention sees it: decided when it left the window, by the threshold
+        in force now while it has not."""
+        return self.gate(b, h)

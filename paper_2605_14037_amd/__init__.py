@@ -11,4 +11,5 @@ from .binding import (  # noqa: F401
     PrefixSharing, Rope, qk_norm_rope, qk_norm_rope_backward,
     EXPORTED_SYMBOLS,
     OPT_ITEM_TARGET, OPT_KERNEL_TIMING, OPT_SPLIT_ONLY, OPT_SINK_TOKENS, OPT_MERGE_WAVES, OPT_STEP_LAUNCHES,
+    FORK_KEEP, FORK_EMPTY, MAX_TREE_NODES,
 )

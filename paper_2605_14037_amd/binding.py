@@ -20,7 +20,8 @@ _LIB = None
 OK, E_INVAL, E_STATE, E_CAPACITY, E_HIP, E_NOMEM, E_DEVICE = 0, -1, -2, -3, -4, -5, -6
 OPT_ITEM_TARGET, OPT_KERNEL_TIMING, OPT_SPLIT_ONLY, OPT_SINK_TOKENS, OPT_MERGE_WAVES = 1, 2, 3, 4, 5
 OPT_STEP_LAUNCHES = 6
-MAX_BATCH, PAGE_TOKENS = 512, 64
+MAX_BATCH, PAGE_TOKENS, MAX_TREE_NODES = 512, 64, 64
+FORK_KEEP, FORK_EMPTY = -1, -2
 
 EXPORTED_SYMBOLS = [
     "spkv_cache_required_bytes", "spkv_cache_create", "spkv_cache_destroy", "spkv_cache_grow",
@@ -34,6 +35,7 @@ EXPORTED_SYMBOLS = [
     "spkv_debug_layout_offset", "spkv_debug_copy", "spkv_debug_read", "spkv_strerror",
     "spkv_qk_norm_rope", "spkv_qk_norm_rope_backward", "spkv_qk_norm_rope_backward_workspace_bytes",
     "spkv_prefix_workspace_bytes", "spkv_prefix_attention", "spkv_decode_attention_shared",
+    "spkv_append_rows", "spkv_cache_fork", "spkv_cache_gather",
 ]
 
 BF16, FP32 = 0, 1
@@ -142,6 +144,12 @@ def load_library():
     lib.spkv_qk_norm_rope_backward.restype = C.c_int
     lib.spkv_qk_norm_rope_backward.argtypes = [ph, ph, ph, ph, ph, vp, vp, f32, vp, pr, i32, i64, i32, i32,
                                                ph, ph, ph, vp, vp, vp, C.c_size_t, vp]
+    lib.spkv_append_rows.restype = C.c_int
+    lib.spkv_append_rows.argtypes = [vp, vp, vp, vp, vp, i32, P(i32), vp]
+    lib.spkv_cache_fork.restype = C.c_int
+    lib.spkv_cache_fork.argtypes = [vp, vp, P(i32), vp]
+    lib.spkv_cache_gather.restype = C.c_int
+    lib.spkv_cache_gather.argtypes = [vp, P(i32), i32, i64, vp, vp, vp, vp, vp, vp]
     lib.spkv_cache_prune.restype = C.c_int
     lib.spkv_cache_prune.argtypes = [vp, vp]
     lib.spkv_cache_safe_steps.restype = C.c_int
@@ -771,6 +779,61 @@ class SPKVCache:
                                               op, lp, float(sm_scale), workspace.data_ptr(), workspace.numel(),
                                               _stream()), "spkv_prefix_attention")
         return out, lse
+
+    # ---- sequences that branch
+    def append_rows(self, k, v, util_logits, rows, cu_seqlens):
+        """Append the rows `rows` (int32 [total], on the device) of k, v, util_logits: sequence b's tokens are
+        rows[cu[b]:cu[b + 1]] (spkv_append_rows).  For the drafts of a tree that were accepted."""
+        cfg = self.cfg
+        cu = cu_seqlens if isinstance(cu_seqlens, C.Array) else self.make_cu(cu_seqlens)
+        total, n = cu[cfg.batch], k.shape[0]
+        kv_shape = (n, cfg.n_kv_heads, cfg.head_dim)
+        kp = _dev_ptr(k, torch.bfloat16, kv_shape, "k")
+        vp = _dev_ptr(v, torch.bfloat16, kv_shape, "v")
+        fp = _dev_ptr(util_logits, torch.float32, kv_shape[:2], "util_logits")
+        rp = _dev_ptr(rows, torch.int32, (total,), "rows")
+        _check(self.lib.spkv_append_rows(self.handle, kp, vp, fp, rp, n, cu, _stream()), "spkv_append_rows")
+
+    def fork(self, source, other=None):
+        """Sequence b becomes what sequence source[b] -- of `other`, or of this cache -- was before the call; FORK_KEEP
+        leaves it, FORK_EMPTY empties it and gives its pages back (spkv_cache_fork)."""
+        if not isinstance(source, C.Array):
+            source = (C.c_int32 * len(source))(*[int(x) for x in source])
+        if len(source) != self.cfg.batch:
+            raise ValueError(f"source: need one entry for each of {self.cfg.batch} sequences, got {len(source)}")
+        _check(self.lib.spkv_cache_fork(self.handle, other.handle if other is not None else None, source, _stream()),
+               "spkv_cache_fork")
+
+    def gather(self, sequences=None, rows=None, out=None):
+        """The pairs that sequences hold (all of them by default), kept ones and then the window's, positions ascending, as
+        (k, v, util_logits, positions, counts): bf16 [n, H_kv, rows, D] twice, fp32 and int32 [n, H_kv, rows], int32
+        [n, H_kv] (spkv_cache_gather).  rows None: as many as the longest head holds (synchronises).  out: those five
+        tensors, to write; rows behind a head's last pair are left as they were (undefined in new tensors)."""
+        cfg = self.cfg
+        if sequences is None:
+            n, which = cfg.batch, None
+        else:
+            n, which = len(sequences), (C.c_int32 * max(len(sequences), 1))(*[int(b) for b in sequences])
+        if out is None:
+            if rows is None:
+                counts = torch.zeros(n, cfg.n_kv_heads, dtype=torch.int32, device=self.device)
+                _check(self.lib.spkv_cache_gather(self.handle, which, n, 0, None, None, None, None, counts.data_ptr(), _stream()),
+                       "spkv_cache_gather")
+                rows = int(counts.max()) if n > 0 else 0
+            shape = (n, cfg.n_kv_heads, int(rows))
+            k, v = (torch.empty(*shape, cfg.head_dim, dtype=torch.bfloat16, device=self.device) for _ in range(2))
+            out = (k, v, torch.empty(shape, dtype=torch.float32, device=self.device),
+                   torch.empty(shape, dtype=torch.int32, device=self.device),
+                   torch.empty(shape[:2], dtype=torch.int32, device=self.device))
+        k, v, f, positions, counts = out
+        shape = (n, cfg.n_kv_heads, k.shape[2] if k.dim() == 4 else -1)
+        kp = _dev_ptr(k, torch.bfloat16, (*shape, cfg.head_dim), "out[0]")
+        vp = _dev_ptr(v, torch.bfloat16, (*shape, cfg.head_dim), "out[1]")
+        fp = _dev_ptr(f, torch.float32, shape, "out[2]")
+        pp = _dev_ptr(positions, torch.int32, shape, "out[3]")
+        cp = _dev_ptr(counts, torch.int32, shape[:2], "out[4]")
+        _check(self.lib.spkv_cache_gather(self.handle, which, n, shape[2], kp, vp, fp, pp, cp, _stream()), "spkv_cache_gather")
+        return k, v, f, positions, counts
 
     # ---- bookkeeping
     def reset(self):

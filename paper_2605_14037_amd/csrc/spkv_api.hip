@@ -1972,6 +1972,200 @@ int spkv_decode_attention_shared(spkv_cache_t* c, spkv_cache_t* pc, const int32_
 }
 
 namespace {
+// What spkv_cache_fork makes of its sources: moves in an order in which every sequence is read before it is replaced
+// (spkv_fork_move), and the sequences that need pages of their own afterwards.
+struct ForkPlan {
+    SpkvForkMoves moves;
+    SpkvSequences copies;
+    int n_copies;
+};
+// same: the sources are sequences of the cache itself.
+void plan_fork(int B, const int32_t* source, bool same, ForkPlan* p) {
+    // Sequences that hang together: each points towards the one that stands for its component.
+    int16_t towards[SPKV_MAX_BATCH], next[SPKV_MAX_BATCH], first[SPKV_MAX_BATCH], readers[SPKV_MAX_BATCH];
+    bool replaced[SPKV_MAX_BATCH], made[SPKV_MAX_BATCH], taken[SPKV_MAX_BATCH], wanted[SPKV_MAX_BATCH];
+    for (int b = 0; b < B; ++b) {
+        towards[b] = (int16_t)b;
+        first[b] = -1;
+        readers[b] = 0;
+        made[b] = taken[b] = wanted[b] = false;
+        replaced[b] = source[b] == SPKV_FORK_EMPTY || (source[b] >= 0 && !(same && source[b] == b));
+    }
+    auto root = [&](int b) -> int {
+        while (towards[b] != b) b = towards[b] = towards[towards[b]];
+        return b;
+    };
+    for (int b = 0; same && b < B; ++b) {
+        const int s = source[b];
+        if (!replaced[b] || s < 0 || !replaced[s]) continue;
+        wanted[s] = true;
+        ++readers[s];
+        towards[root(b)] = (int16_t)root(s);
+    }
+    for (int b = B - 1; b >= 0; --b)
+        if (replaced[b]) {
+            const int r = root(b);
+            next[b] = first[r];
+            first[r] = (int16_t)b;
+        }
+    int at = 0;
+    p->moves.n = p->n_copies = 0;
+    auto emit = [&](int b, int dst_flags, int src_flags) {
+        const int s = source[b];
+        made[b] = true;
+        if (!wanted[b]) dst_flags |= kForkFree;              // (of another cache: nothing here is read)
+        p->moves.dst[at] = (uint16_t)(b | dst_flags);
+        p->moves.src[at++] = (uint16_t)(s < 0 ? kForkNothing : s | src_flags);
+        if (s < 0) return;
+        if (same && replaced[s] && !taken[s]) taken[s] = true;
+        else p->copies.seq[p->n_copies++] = (uint16_t)b;
+    };
+    for (int r = 0; r < B; ++r) {
+        if (first[r] < 0) continue;
+        p->moves.start[p->moves.n++] = (uint16_t)at;
+        int16_t ready[SPKV_MAX_BATCH];
+        int n_ready = 0;
+        for (int b = first[r]; b >= 0; b = next[b])
+            if (readers[b] == 0) ready[n_ready++] = (int16_t)b;
+        while (n_ready > 0) {
+            const int b = ready[--n_ready], s = source[b];
+            emit(b, 0, 0);
+            if (same && s >= 0 && replaced[s] && --readers[s] == 0) ready[n_ready++] = (int16_t)s;
+        }
+        for (int c = first[r]; c >= 0; c = next[c]) {        // what is left is one cycle
+            if (made[c]) continue;
+            emit(c, kForkSave, 0);
+            int b = source[c];
+            for (; source[b] != c; b = source[b]) emit(b, 0, 0);
+            emit(b, 0, kForkSaved);
+        }
+    }
+    p->moves.start[p->moves.n] = (uint16_t)at;
+}
+SpkvForkSource fork_source(const SpkvView& v) {
+    return SpkvForkSource{v.ring, v.pool, v.ring_logit, v.logit_pool, v.page_table, v.pos_pool, v.t_pair, v.kept_len, v.gate_on,
+                          v.pt_cap, v.n_pages};
+}
+constexpr int kMaxPairs = 16384;                             // (config_ok)
+}  // namespace
+
+int spkv_cache_fork(spkv_cache_t* c, spkv_cache_t* other, const int32_t* source, void* stream) {
+    if (c == nullptr || source == nullptr) return SPKV_E_INVAL;
+    spkv_cache* from = other == nullptr ? c : other;
+    const bool same = from == c;
+    const spkv_config_t &x = from->cfg, &y = c->cfg;
+    if (x.n_q_heads != y.n_q_heads || x.n_kv_heads != y.n_kv_heads || x.head_dim != y.head_dim || x.window != y.window)
+        return SPKV_E_INVAL;
+    const int B = y.batch, Hkv = y.n_kv_heads;
+    for (int b = 0; b < B; ++b)
+        if (source[b] < SPKV_FORK_EMPTY || source[b] >= x.batch) return SPKV_E_INVAL;
+    for (int b = 0; b < B; ++b)
+        if (source[b] >= 0 && from->T[source[b]] > y.max_context) return SPKV_E_CAPACITY;
+    ForkPlan plan;
+    plan_fork(B, source, same, &plan);
+    if (plan.moves.n == 0) return SPKV_OK;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (being_captured(s)) return SPKV_E_STATE;              // a replay would move sequences that the host knows nothing of
+    auto length_after = [&](int b, int h) -> int32_t {
+        return source[b] == SPKV_FORK_KEEP ? c->L_ub[b * Hkv + h] : source[b] < 0 ? 0 : from->L_ub[source[b] * Hkv + h];
+    };
+    auto pages_after = [&]() -> int64_t {
+        int64_t pages = 0;
+        for (int b = 0; b < B; ++b)
+            for (int h = 0; h < Hkv; ++h) pages += pages_for(length_after(b, h));
+        return pages;
+    };
+    try {
+        std::unique_lock<std::mutex> lock;
+        if (!same) lock = std::unique_lock<std::mutex>(from->prompt_lengths);
+        int rc = from->bound_is_loose ? exact_lengths(from, s) : SPKV_OK;
+        if (rc == SPKV_OK && pages_after() > c->carve.n_pages) {
+            rc = exact_lengths(from, s);
+            if (rc == SPKV_OK && !same) rc = exact_lengths(c, s);
+        }
+        if (rc != SPKV_OK) return rc;
+    } catch (const std::exception&) {                        // no memory; no lock
+        return SPKV_E_NOMEM;
+    }
+    if (pages_after() > c->carve.n_pages) return SPKV_E_CAPACITY;
+
+    const SpkvForkSource src = fork_source(from->view);
+    if (spkv_launch_fork_move(c->view, src, plan.moves, s) != hipSuccess) return SPKV_E_HIP;
+    int64_t most = 0;
+    for (int i = 0; i < plan.n_copies; ++i)
+        for (int h = 0; h < Hkv; ++h) most = std::max(most, pages_for(length_after(plan.copies.seq[i], h)));
+    if (most > 0 && spkv_launch_fork_pages(c->view, src, plan.copies, plan.n_copies, (int)most, s) != hipSuccess)
+        return SPKV_E_HIP;
+
+    int32_t len[kMaxPairs], tokens[SPKV_MAX_BATCH], since[SPKV_MAX_BATCH];
+    c->slack = 0;
+    for (int b = 0; b < B; ++b) {
+        const int a = source[b];
+        tokens[b] = a == SPKV_FORK_KEEP ? c->T[b] : a < 0 ? 0 : from->T[a];
+        since[b] = a == SPKV_FORK_KEEP ? c->since_exact[b] : a < 0 ? 0 : from->since_exact[a];
+        c->slack += (int64_t)since[b] * Hkv;
+        for (int h = 0; h < Hkv; ++h) len[b * Hkv + h] = length_after(b, h);
+    }
+    c->pages_ub = pages_after();
+    std::copy(len, len + B * Hkv, c->L_ub.begin());
+    std::copy(tokens, tokens + B, c->T.begin());
+    std::copy(since, since + B, c->since_exact.begin());
+    c->lists_known = c->lists_known && from->lists_known;
+    c->snap_pending = c->sent = false;                       // lengths on their way are other sequences' by now
+    return SPKV_OK;
+}
+
+int spkv_cache_gather(spkv_cache_t* c, const int32_t* sequences, int32_t n, int64_t rows, void* k, void* v, float* util_logits,
+                      int32_t* positions, int32_t* counts, void* stream) {
+    if (c == nullptr || n < 0 || n > SPKV_MAX_BATCH || rows < 0 || rows > INT32_MAX) return SPKV_E_INVAL;
+    if (sequences == nullptr && n > c->cfg.batch) return SPKV_E_INVAL;
+    SpkvSequences of = {};
+    int64_t most = 0;
+    const int Hkv = c->cfg.n_kv_heads;
+    for (int i = 0; i < n; ++i) {
+        const int b = sequences != nullptr ? sequences[i] : i;
+        if (b < 0 || b >= c->cfg.batch) return SPKV_E_INVAL;
+        of.seq[i] = (uint16_t)b;
+        const int held = (std::min(c->T[b], c->cfg.window) + kHalfTokens - 1) / kHalfTokens;
+        for (int h = 0; h < Hkv; ++h)
+            most = std::max<int64_t>(most, (c->L_ub[b * Hkv + h] + kHalfTokens - 1) / kHalfTokens + held);
+    }
+    if ((int64_t)n * Hkv > 65535) return SPKV_E_INVAL;       // (of a launch; the same sequence many times)
+    if (!aligned16(k) || !aligned16(v) || !aligned16(util_logits) || !aligned16(positions) || !aligned16(counts)) return SPKV_E_INVAL;
+    if (n == 0) return SPKV_OK;
+    const SpkvPairRows out = {static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), util_logits, positions, counts, rows};
+    return spkv_launch_gather_pairs(c->view, of, n, (int)most, out, static_cast<hipStream_t>(stream)) == hipSuccess ? SPKV_OK
+                                                                                                               : SPKV_E_HIP;
+}
+
+int spkv_append_rows(spkv_cache_t* c, const void* k, const void* v, const float* util_logits, const int32_t* rows,
+                     int32_t n_rows, const int32_t* cu_seqlens, void* stream) {
+    if (c == nullptr || cu_seqlens == nullptr || cu_seqlens[0] != 0) return SPKV_E_INVAL;
+    const int B = c->cfg.batch;
+    for (int b = 0; b < B; ++b) {
+        const int64_t n = (int64_t)cu_seqlens[b + 1] - cu_seqlens[b];
+        if (n < 0 || n > SPKV_MAX_TREE_NODES) return SPKV_E_INVAL;
+    }
+    if (cu_seqlens[B] == 0) return SPKV_OK;
+    if (k == nullptr || v == nullptr || util_logits == nullptr || rows == nullptr || n_rows < 1) return SPKV_E_INVAL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(util_logits) || !aligned16(rows)) return SPKV_E_INVAL;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    try {
+        const int rc = reserve_capacity(c, cu_seqlens, s);
+        if (rc != SPKV_OK) return rc;
+    } catch (const std::exception&) {
+        return SPKV_E_NOMEM;
+    }
+    SpkvCu cu;
+    std::memcpy(cu.v, cu_seqlens, (size_t)(B + 1) * 4);
+    if (spkv_launch_append_rows(c->view, static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), util_logits, rows,
+                                n_rows, cu, s) != hipSuccess)
+        return SPKV_E_HIP;
+    commit_lengths(c, cu_seqlens);
+    return SPKV_OK;
+}
+
+namespace {
 // A set of heads as the kernels take it; false if it is not one of `size`-byte elements.
 bool heads_ok(const spkv_heads_t* s, int64_t n_tokens, int n_heads, int head_dim, int size, bool written, SpkvRowSet* o) {
     if (s == nullptr || s->data == nullptr || !aligned16(s->data)) return false;

@@ -1,0 +1,257 @@
+// Sequences that branch, on gfx950: copies, moves and releases of whole sequences, what sequences hold as
+// dense rows, and the append of rows that lie here and there.
+#include "spkv_device.h"
+
+// ---------------------------------------------------------------- sequences become others
+// All sequences of a call change at once: sequence b becomes what source[b] was.  What a sequence holds is its
+// window ring, its counters and, per head, a row of the page table.  Rows move as they are: the first sequence that
+// takes over one whose own place is taken has its pages, without a copy; further ones hold the same page ids for the
+// length of this launch and get pages of their own in the next (spkv_fork_pages).  Pages that nobody takes go back
+// onto the stack, in this launch alone, and pages are handed out in the next alone.
+//
+// Order.  Sequences that hang together (one is the source of another and is itself replaced) are a component; the
+// host has put its moves into an order in which every sequence is read before it is replaced, a cycle being opened by
+// saving its first one (the flag kForkSave).  Every thread carries its own units -- 16 bytes of a ring, an entry of a
+// page table row, a logit -- through all moves of the component before it takes the next, so the order of one
+// thread's loads and stores is all that is needed, and what is saved is one register.
+// Counters are read before any of them is written.
+constexpr int kForkThreads = 256, kForkUnits = 4;             // 16 KB of a ring to a workgroup
+__device__ __forceinline__ int fork_ring_units(const SpkvView& v) { return v.n_ring_pages * (spkv_page_elems(v.D) / 8); }
+
+__global__ __launch_bounds__(kForkThreads) void spkv_fork_move(SpkvView v, SpkvForkSource from, SpkvForkMoves mv) {
+    const int tid = threadIdx.x, h = blockIdx.y;
+    const int m0 = mv.start[blockIdx.x], m1 = mv.start[blockIdx.x + 1];
+    if (blockIdx.z > 0) {                                     // rings
+        const int units = fork_ring_units(v), step = kForkThreads * kForkUnits;
+        uint4* to = reinterpret_cast<uint4*>(v.ring);
+        const uint4* src = reinterpret_cast<const uint4*>(from.ring);
+        for (int u0 = ((int)blockIdx.z - 1) * step; u0 < units; u0 += ((int)gridDim.z - 1) * step) {
+            uint4 saved[kForkUnits];
+            for (int m = m0; m < m1; ++m) {
+                const int d = mv.dst[m], s = mv.src[m];
+                uint4* at = to + ((size_t)(d & kForkIndex) * v.Hkv + h) * units;
+                const uint4* of = src + ((size_t)(s & kForkIndex) * v.Hkv + h) * units;
+                uint4 x[kForkUnits];
+#pragma unroll
+                for (int i = 0; i < kForkUnits; ++i) {
+                    const int u = u0 + i * kForkThreads + tid;
+                    x[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (u < units && (s & (kForkSaved | kForkNothing)) == 0) x[i] = of[u];
+                }
+                if ((s & kForkSaved) != 0) {
+#pragma unroll
+                    for (int i = 0; i < kForkUnits; ++i) x[i] = saved[i];
+                }
+                if ((d & kForkSave) != 0) {
+#pragma unroll
+                    for (int i = 0; i < kForkUnits; ++i) {
+                        const int u = u0 + i * kForkThreads + tid;
+                        if (u < units) saved[i] = at[u];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kForkUnits; ++i) {
+                    const int u = u0 + i * kForkThreads + tid;
+                    if (u < units) at[u] = x[i];
+                }
+            }
+        }
+        return;
+    }
+    __shared__ int s_len[SPKV_MAX_BATCH], s_tokens[SPKV_MAX_BATCH], s_on[SPKV_MAX_BATCH];   // what move m brings
+    __shared__ int s_old[SPKV_MAX_BATCH], s_at[SPKV_MAX_BATCH];   // pages that move m gives back, their place on the stack
+    __shared__ int s_most;
+    if (tid == 0) s_most = 0;
+    __syncthreads();
+    for (int m = m0 + tid; m < m1; m += kForkThreads) {
+        const int d = mv.dst[m], s = mv.src[m], i = m - m0;
+        const int to = (d & kForkIndex) * v.Hkv + h, of = (s & kForkIndex) * v.Hkv + h;
+        const bool nothing = (s & kForkNothing) != 0;
+        s_len[i] = nothing ? 0 : from.kept_len[of];
+        s_tokens[i] = nothing ? 0 : from.t_pair[of];
+        s_on[i] = nothing ? 0 : from.gate_on[of];
+        s_old[i] = (d & kForkFree) != 0 ? (v.kept_len[to] + kPageTokens - 1) / kPageTokens : 0;
+        s_at[i] = s_old[i] > 0 ? atomicAdd(v.free_top, s_old[i]) : 0;
+        atomicMax(&s_most, max(s_old[i], (s_len[i] + kPageTokens - 1) / kPageTokens));
+    }
+    __syncthreads();
+    const int most = s_most;
+    for (int i = tid; i < most; i += kForkThreads) {          // page table rows
+        int saved = 0;
+        for (int m = m0; m < m1; ++m) {
+            const int d = mv.dst[m], s = mv.src[m];
+            int32_t* at = v.page_table + ((size_t)(d & kForkIndex) * v.Hkv + h) * v.pt_cap;
+            const int n = (s_len[m - m0] + kPageTokens - 1) / kPageTokens;
+            const int old = i < v.pt_cap ? at[i] : 0;
+            int x = saved;
+            if ((s & (kForkSaved | kForkNothing)) == 0 && i < n)
+                x = from.page_table[((size_t)(s & kForkIndex) * v.Hkv + h) * from.pt_cap + i];
+            if (i < s_old[m - m0]) v.free_pages[s_at[m - m0] + i] = old;
+            if ((d & kForkSave) != 0) saved = old;
+            if (i < min(n, v.pt_cap)) at[i] = x;
+        }
+    }
+    for (int i = tid; i < v.w; i += kForkThreads) {           // logits of the rings
+        float saved = 0.f;
+        for (int m = m0; m < m1; ++m) {
+            const int d = mv.dst[m], s = mv.src[m];
+            float* at = v.ring_logit + ((size_t)(d & kForkIndex) * v.Hkv + h) * v.w;
+            float x = 0.f;
+            if ((s & kForkSaved) != 0) x = saved;
+            else if ((s & kForkNothing) == 0) x = from.ring_logit[((size_t)(s & kForkIndex) * v.Hkv + h) * v.w + i];
+            if ((d & kForkSave) != 0) saved = at[i];
+            at[i] = x;
+        }
+    }
+    for (int m = m0 + tid; m < m1; m += kForkThreads) {       // (all counters were read before the barrier)
+        const int to = (mv.dst[m] & kForkIndex) * v.Hkv + h;
+        v.kept_len[to] = s_len[m - m0];
+        v.t_pair[to] = s_tokens[m - m0];
+        v.gate_on[to] = s_on[m - m0];
+    }
+}
+
+// Pages of their own for the sequences that hold another one's: kForkPages pages to a workgroup and turn, ids by one
+// atomic, then the pages with their positions and logits.
+constexpr int kForkPages = 4;
+template <int D>
+__global__ __launch_bounds__(kForkThreads) void spkv_fork_pages(SpkvView v, SpkvForkSource from, SpkvSequences dst) {
+    const int tid = threadIdx.x, pair = dst.seq[blockIdx.z] * v.Hkv + blockIdx.y;
+    const int n = min((v.kept_len[pair] + kPageTokens - 1) / kPageTokens, v.pt_cap);
+    int32_t* row = v.page_table + (size_t)pair * v.pt_cap;
+    __shared__ int s_from[kForkPages], s_to[kForkPages];
+    for (int p0 = blockIdx.x * kForkPages; p0 < n; p0 += gridDim.x * kForkPages) {
+        const int here = min(kForkPages, n - p0);
+        if (tid == 0) {
+            const PageBatch pb = alloc_page_batch(v, here);
+            for (int i = 0; i < here; ++i) {
+                const int to = batch_page(v, pb, i);
+                s_from[i] = min(max(row[p0 + i], 0), from.n_pages - 1);
+                s_to[i] = to;
+                row[p0 + i] = max(to, 0);
+                if (to < 0) *v.err_flag = 1;
+            }
+        }
+        __syncthreads();
+        for (int i = 0; i < here; ++i) {
+            if (s_to[i] < 0) continue;
+            const int a = s_from[i], b = s_to[i];
+            const uint4* src = reinterpret_cast<const uint4*>(from.pool + (size_t)a * spkv_page_elems(D));
+            uint4* to = reinterpret_cast<uint4*>(pool_page(v, b));
+            constexpr int kUnits = 2 * kPageTokens * D / 8 / kForkThreads;
+            uint4 x[kUnits];
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) x[u] = src[u * kForkThreads + tid];
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) to[u * kForkThreads + tid] = x[u];
+            if (tid < kPageTokens) v.pos_pool[(size_t)b * kPageTokens + tid] = from.pos_pool[(size_t)a * kPageTokens + tid];
+            else if (tid < 2 * kPageTokens)
+                v.logit_pool[(size_t)b * kPageTokens + tid - kPageTokens] = from.logit_pool[(size_t)a * kPageTokens + tid - kPageTokens];
+        }
+        __syncthreads();
+    }
+}
+
+hipError_t spkv_launch_fork_move(const SpkvView& v, const SpkvForkSource& from, const SpkvForkMoves& mv, hipStream_t s) {
+    const int units = v.n_ring_pages * (spkv_page_elems(v.D) / 8), step = kForkThreads * kForkUnits;
+    spkv_fork_move<<<dim3(mv.n, v.Hkv, 1 + std::min((units + step - 1) / step, 1024)), dim3(kForkThreads), 0, s>>>(v, from, mv);
+    return hipGetLastError();
+}
+
+hipError_t spkv_launch_fork_pages(const SpkvView& v, const SpkvForkSource& from, const SpkvSequences& dst, int n, int most_pages,
+                                  hipStream_t s) {
+    const dim3 grid((unsigned)std::max(1, std::min((most_pages + kForkPages - 1) / kForkPages, 65535)), v.Hkv, n);
+    if (v.D == 128) spkv_fork_pages<128><<<grid, dim3(kForkThreads), 0, s>>>(v, from, dst);
+    else spkv_fork_pages<64><<<grid, dim3(kForkThreads), 0, s>>>(v, from, dst);
+    return hipGetLastError();
+}
+
+// -------------------------------------------------------------- what sequences hold, as rows
+// A workgroup takes a half-page (32 pairs) at a time.  Rows of keys: four consecutive keys lie in 64 bytes of every
+// chunk of eight elements, so a wave that takes four keys reads whole pieces of 64 bytes and writes whole rows.
+// Values come as units of eight keys of one element and are turned in LDS.
+template <int D>
+__global__ __launch_bounds__(256) void spkv_gather_pairs(SpkvView v, SpkvSequences of, SpkvPairRows out) {
+    constexpr int kChunks = D / 8;
+    __shared__ __attribute__((aligned(16))) uint16_t s_v[kHalfTokens][D + 8];
+    const int tid = threadIdx.x, i = blockIdx.y / v.Hkv, h = blockIdx.y - i * v.Hkv, pair = of.seq[i] * v.Hkv + h;
+    const int T = v.t_pair[pair], L = v.kept_len[pair], held = min(T, v.w), first = T % v.w;
+    const int nA = (L + kHalfTokens - 1) >> 5, n_hp = nA + ((held + kHalfTokens - 1) >> 5);
+    const int32_t* row = v.page_table + (size_t)pair * v.pt_cap;
+    const size_t row0 = (size_t)blockIdx.y * out.rows;
+    if (blockIdx.x == 0 && tid == 0 && out.counts != nullptr) out.counts[blockIdx.y] = L + held;
+    // a ring slot's place among the window's pairs, oldest first
+    auto age = [&](int slot) -> int { return T < v.w ? slot : slot - first + (slot < first ? v.w : 0); };
+    for (int x = blockIdx.x; x < n_hp; x += gridDim.x) {
+        const bool ring = x >= nA;
+        const int k0 = (ring ? x - nA : x) * kHalfTokens, n = min((ring ? held : L) - k0, kHalfTokens);
+        const int page = ring ? 0 : min(max(row[x >> 1], 0), v.n_pages - 1);
+        const uint16_t* base = ring ? ring_page(v, pair, k0 >> 6) : pool_page(v, page);
+        const int in0 = k0 & 63;
+        auto place = [&](int r) -> int { return ring ? L + age(k0 + r) : k0 + r; };
+        if (out.k != nullptr) {
+            for (int u = tid; u < kHalfTokens * kChunks; u += 256) {
+                const int r = u / kChunks, c = u - r * kChunks;
+                if (r >= n || place(r) >= out.rows) continue;
+                *reinterpret_cast<uint4*>(out.k + (row0 + place(r)) * D + c * 8) =
+                    *reinterpret_cast<const uint4*>(base + spkv_k_off(D, in0 + r, c * 8));
+            }
+        }
+        if (out.v != nullptr) {
+            for (int u = tid; u < kHalfTokens / 8 * D; u += 256) {
+                const int kc = u / D, d = u - kc * D;
+                const uint4 q = *reinterpret_cast<const uint4*>(base + spkv_v_off(D, in0 + 8 * kc, d));
+                const unsigned w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s_v[8 * kc + e][d] = (uint16_t)(w[e >> 1] >> ((e & 1) * 16));
+            }
+            __syncthreads();
+            for (int u = tid; u < kHalfTokens * kChunks; u += 256) {
+                const int r = u / kChunks, c = u - r * kChunks;
+                if (r < n && place(r) < out.rows)
+                    *reinterpret_cast<uint4*>(out.v + (row0 + place(r)) * D + c * 8) = *reinterpret_cast<const uint4*>(&s_v[r][c * 8]);
+            }
+            __syncthreads();
+        }
+        if (tid < n && place(tid) < out.rows) {
+            const size_t e = (size_t)page * kPageTokens + in0 + tid;
+            if (out.logits != nullptr) out.logits[row0 + place(tid)] = ring ? v.ring_logit[(size_t)pair * v.w + k0 + tid] : v.logit_pool[e];
+            if (out.positions != nullptr) out.positions[row0 + place(tid)] = ring ? T - held + age(k0 + tid) : v.pos_pool[e];
+        }
+    }
+}
+
+hipError_t spkv_launch_gather_pairs(const SpkvView& v, const SpkvSequences& of, int n, int most_half_pages, const SpkvPairRows& out,
+                                    hipStream_t s) {
+    const dim3 grid((unsigned)std::max(1, std::min(most_half_pages, 65535)), n * v.Hkv);
+    if (v.D == 128) spkv_gather_pairs<128><<<grid, dim3(256), 0, s>>>(v, of, out);
+    else spkv_gather_pairs<64><<<grid, dim3(256), 0, s>>>(v, of, out);
+    return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ append of chosen rows
+// append_few in rounds of up to kFewTokens tokens, and no more than the window holds: none enters and leaves it
+// within a round.  Token i of a sequence is row rows[cu[b] + i]; a row that is not there is flagged.
+template <int D>
+__global__ __launch_bounds__(256) void spkv_append_rows(SpkvView v, const uint16_t* __restrict__ k,
+                                                        const uint16_t* __restrict__ vv, const float* __restrict__ f,
+                                                        const int32_t* __restrict__ rows, int n_rows, SpkvCu cu) {
+    const int pair = blockIdx.x, b = pair / v.Hkv, h = pair - b * v.Hkv;
+    const int row0 = cu.v[b], n = cu.v[b + 1] - row0, round = min(kFewTokens, v.w);
+    int T = v.t_pair[pair], L = v.kept_len[pair];
+    for (int i0 = 0; i0 < n; i0 += round) {
+        if (i0 > 0) __syncthreads();                         // the last round's rows and page are there
+        append_few_rows<D>(v, pair, h, min(round, n - i0), T, L, k, vv, f, [&](int i) -> int {
+            const int r = rows[row0 + i0 + i];
+            if (r < 0 || r >= n_rows) *v.err_flag = 1;
+            return min(max(r, 0), n_rows - 1);
+        });
+    }
+}
+
+hipError_t spkv_launch_append_rows(const SpkvView& v, const uint16_t* k, const uint16_t* vv, const float* f,
+                                   const int32_t* rows, int n_rows, const SpkvCu& cu, hipStream_t s) {
+    if (v.D == 128) spkv_append_rows<128><<<dim3(v.n_pairs), dim3(256), 0, s>>>(v, k, vv, f, rows, n_rows, cu);
+    else spkv_append_rows<64><<<dim3(v.n_pairs), dim3(256), 0, s>>>(v, k, vv, f, rows, n_rows, cu);
+    return hipGetLastError();
+}

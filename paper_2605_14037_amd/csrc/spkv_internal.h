@@ -322,3 +322,38 @@ hipError_t spkv_launch_prefix(const SpkvView& v, const uint16_t* q, float sm_sca
 hipError_t spkv_launch_prefix_rows(const SpkvCu& cu, const SpkvShareActive& a, const int32_t* t_own, int n_seq,
                                    int n_kv_heads, bool appended, int n_active, int32_t* table, int32_t* by_row,
                                    int32_t* first_row, hipStream_t s);
+
+// Sequences that branch (spkv_branch.hip).  Moves by component, in the order in which they are made: start[c] ..
+// start[c + 1] - 1 are those of component c.
+constexpr int kForkIndex = 0x1ff;                // sequence, in dst and src
+constexpr int kForkSave = 0x4000;                // dst: what it held is saved first
+constexpr int kForkFree = 0x8000;                // dst: nobody takes its pages, they go back
+constexpr int kForkNothing = 0x4000;             // src: none, the sequence is emptied
+constexpr int kForkSaved = 0x8000;               // src: what was saved (the index says whose it was)
+struct SpkvForkMoves {
+    int32_t n;                                   // components
+    uint16_t start[SPKV_MAX_BATCH + 1], dst[SPKV_MAX_BATCH], src[SPKV_MAX_BATCH];
+};
+struct SpkvForkSource {                          // the cache that is copied from: the same one or another
+    const uint16_t *ring, *pool;
+    const float *ring_logit, *logit_pool;
+    const int32_t *page_table, *pos_pool, *t_pair, *kept_len, *gate_on;
+    int32_t pt_cap, n_pages;
+};
+struct SpkvSequences {
+    uint16_t seq[SPKV_MAX_BATCH];
+};
+struct SpkvPairRows {                            // [sequences][Hkv][rows], any of them null
+    uint16_t *k, *v;
+    float* logits;
+    int32_t *positions, *counts;                 // counts: [sequences][Hkv]
+    int64_t rows;
+};
+hipError_t spkv_launch_fork_move(const SpkvView& v, const SpkvForkSource& from, const SpkvForkMoves& mv, hipStream_t s);
+// most_pages: of a head of these sequences, by the host's bound.
+hipError_t spkv_launch_fork_pages(const SpkvView& v, const SpkvForkSource& from, const SpkvSequences& dst, int n, int most_pages,
+                                  hipStream_t s);
+hipError_t spkv_launch_gather_pairs(const SpkvView& v, const SpkvSequences& of, int n, int most_half_pages, const SpkvPairRows& out,
+                                    hipStream_t s);
+hipError_t spkv_launch_append_rows(const SpkvView& v, const uint16_t* k, const uint16_t* vv, const float* f,
+                                   const int32_t* rows, int n_rows, const SpkvCu& cu, hipStream_t s);

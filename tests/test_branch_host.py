@@ -1,0 +1,188 @@
+"""What the calls on branching sequences refuse, launch and count, without a GPU (see tests/recorder: the library's host
+code against a HIP runtime that writes launches down)."""
+
+import ctypes as C
+import json
+import os
+import subprocess
+import sys
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+sys.path.insert(0, ROOT)
+
+AT = 1 << 40                                             # an aligned address that nothing touches
+KEEP, EMPTY = -1, -2
+
+
+def _run(configs, script):
+    from tests import recorder
+    out = subprocess.run([sys.executable, os.path.abspath(__file__), recorder._runtime(), recorder.LIB],
+                         input=json.dumps([configs, script]), capture_output=True, text=True, timeout=120)
+    assert out.returncode == 0, out.stderr
+    return [(rc, [(recorder._readable(n), int(x), int(b)) for n, x, _, b in ls]) for rc, ls in json.loads(out.stdout)]
+
+
+def _main():
+    """Runs one script, [[op, args], ..] on the caches "a" and "b", and prints [[rc, launches], ..]."""
+    rt = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)          # before the library: its names win
+    lib = C.CDLL(sys.argv[2])
+
+    class Config(C.Structure):
+        _fields_ = [("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                    ("window", C.c_int32), ("page_tokens", C.c_int32), ("tau", C.c_float), ("max_context", C.c_int32),
+                    ("max_total_kept_tokens", C.c_int64)]
+
+    configs, script = json.load(sys.stdin)
+    handles, cfgs = {}, {}
+    lib.spkv_cache_required_bytes.restype = C.c_size_t
+    for name, config in zip("ab", configs):
+        cfgs[name] = Config(**{**dict(batch=3, n_q_heads=32, n_kv_heads=8, head_dim=128, window=128, page_tokens=0, tau=0.5,
+                                      max_context=1 << 16, max_total_kept_tokens=1 << 20), **config})
+        handles[name] = C.c_void_p()
+        need = lib.spkv_cache_required_bytes(C.byref(cfgs[name]))
+        assert lib.spkv_cache_create(C.byref(cfgs[name]), C.c_void_p(AT), C.c_size_t(need), None, C.byref(handles[name])) == 0
+
+    def ints(x):
+        return None if x is None else (C.c_int32 * max(len(x), 1))(*x)
+
+    def cu(counts):
+        return None if counts is None else ints([sum(counts[:b]) for b in range(len(counts) + 1)])
+
+    def taken():
+        buf, got = C.create_string_buffer(1024), []
+        while rt.rec_take(buf, 1024) >= 0:
+            got.append(buf.value.decode().rsplit(" ", 3))
+        return got
+
+    taken()
+    calls, ptr = [], C.c_void_p
+    for op, a in script:
+        who = handles.get(a.get("on", "a"))
+        if op == "append":
+            rc = lib.spkv_append(who, ptr(AT), ptr(AT), ptr(AT), cu(a["counts"]), None)
+        elif op == "lengths":
+            x = ints(a["kept"])
+            rt.rec_device_bytes(x, C.c_size_t(4 * len(x)))
+            rc = lib.spkv_cache_stats(who, (C.c_byte * 4096)(), None, None)
+        elif op == "later":                               # what the next read-back of lengths finds
+            x = ints(a["kept"])
+            rt.rec_device_bytes(x, C.c_size_t(4 * len(x)))
+            rc = 0
+        elif op == "capture":
+            rt.rec_capture(a["status"], 0)
+            rc = 0
+        elif op == "steps":
+            n = C.c_int64()
+            rc = lib.spkv_cache_safe_steps(who, None, C.byref(n))
+            rc = n.value if rc == 0 else rc
+        elif op == "fork":
+            rc = lib.spkv_cache_fork(who, handles.get(a.get("of")), ints(a["source"]), None)
+        elif op == "gather":
+            rc = lib.spkv_cache_gather(who, ints(a.get("which")), a.get("n", 3), C.c_int64(a.get("rows", 10)), ptr(a.get("k", AT)),
+                                       ptr(a.get("v", AT)), ptr(a.get("f", AT)), ptr(a.get("p", AT)), ptr(a.get("counts", AT)), None)
+        elif op == "rows":
+            rc = lib.spkv_append_rows(who, ptr(a.get("k", AT)), ptr(a.get("v", AT)), ptr(a.get("f", AT)), ptr(a.get("rows", AT)),
+                                      a.get("n_rows", 100), cu(a["counts"]), None)
+        else:
+            raise ValueError(op)
+        calls.append([rc, taken()])
+    json.dump(calls, sys.stdout)
+
+
+FED = [["append", dict(counts=[9000, 50, 0])], ["lengths", dict(kept=[2000] * 8 + [0] * 16)]]
+
+
+@pytest.mark.parametrize("bad", [dict(on="none"), dict(source=None), dict(source=[0, 3, 1]), dict(source=[-3, 0, 1])])
+def test_forks_that_are_refused(bad):
+    assert _run([{}], FED + [["fork", dict(source=[0, 0, 0], **bad) if "source" not in bad else bad]])[-1] == (-1, [])
+
+
+@pytest.mark.parametrize("other", [dict(n_q_heads=16), dict(n_kv_heads=4), dict(head_dim=64), dict(window=64)])
+def test_forks_from_caches_of_other_shapes(other):
+    assert _run([{}, other], FED + [["fork", dict(of="b", source=[0, 0, 0])]])[-1] == (-1, [])
+
+
+def test_launches_of_a_fork():
+    def launches(source, of=None):
+        rc, got = _run([{}, {}], FED + [["append", dict(on="b", counts=[9000, 50, 0])],
+                                        ["lengths", dict(on="b", kept=[2000] * 8 + [0] * 16)], ["fork", dict(of=of, source=source)]])[-1]
+        assert rc == 0
+        return [n for n, _, _ in got]
+
+    move, pages = "spkv_fork_move", "spkv_fork_pages<128>"
+    assert launches([KEEP, 1, KEEP]) == []                   # nothing to do
+    assert launches([1, 0, KEEP]) == [move]                  # pages change hands
+    assert launches([EMPTY, EMPTY, 0]) == [move]
+    assert launches([KEEP, KEEP, 0]) == [move, pages]        # a copy
+    assert launches([KEEP, KEEP, 1]) == [move]               # of a sequence that is all window
+    assert launches([2, 0, 0]) == [move, pages]              # one takes the pages, one has copies
+    assert launches([0, 1, 2], of="b") == [move, pages]      # of another cache always
+    assert launches([KEEP, KEEP, 0], of="b") == [move, pages]
+    assert launches([1, EMPTY, 2], of="b") == [move]
+
+
+def test_components_are_moved_side_by_side():
+    """One workgroup row for each: a chain is one, sequences copied from one that stays are one each."""
+    for source, n in (([KEEP, 0, 0], 2), ([1, 2, 0], 1), ([EMPTY, 0, 1], 1), ([EMPTY, EMPTY, EMPTY], 3)):
+        assert _run([{}], FED + [["fork", dict(source=source)]])[-1][1][0][1] == n
+
+
+def test_a_fork_under_capture_is_refused():
+    got = _run([{}], FED + [["capture", dict(status=1)], ["fork", dict(source=[1, 0, KEEP])], ["fork", dict(source=[0, KEEP, 2])]])
+    assert got[-2] == (-2, []) and got[-1] == (0, [])
+
+
+def test_a_pool_that_cannot_hold_the_copies():
+    """Judged by the exact lengths, and nothing launched: 2000 kept pairs are 32 pages a head."""
+    small = dict(max_total_kept_tokens=64 * 8 * 40)          # 320 pages, and one for every pair: 344
+    fed = [["append", dict(counts=[2128, 50, 0])], ["lengths", dict(kept=[2000] * 8 + [0] * 16)]]
+    assert _run([small], fed + [["fork", dict(source=[KEEP, 0, KEEP])]])[-1] == (-3, [])
+    assert _run([small], fed + [["fork", dict(source=[EMPTY, 0, KEEP])]])[-1][0] == 0
+    got = _run([small], fed + [["later", dict(kept=[1000] * 8 + [0] * 16)], ["fork", dict(source=[KEEP, 0, KEEP])]])
+    assert got[-1][0] == 0                                   # (it was the bound that did not fit)
+
+
+def test_contexts_that_are_too_long():
+    assert _run([dict(max_context=8000), {}], [["append", dict(on="b", counts=[9000, 50, 0])], ["fork", dict(of="b", source=[0, KEEP, KEEP])]])[-1] == (-3, [])
+    assert _run([dict(max_context=8000), {}], [["append", dict(on="b", counts=[9000, 50, 0])], ["fork", dict(of="b", source=[1, 1, 2])]])[-1][0] == 0
+
+
+def test_token_counts_follow_the_sequences():
+    cfg = dict(max_context=10000)
+    steps = ["steps", {}]
+    got = _run([cfg], FED + [steps, ["fork", dict(source=[EMPTY, 0, KEEP])], steps, ["fork", dict(source=[KEEP, EMPTY, 1])], steps,
+                             ["fork", dict(source=[EMPTY, EMPTY, EMPTY])], ["later", dict(kept=[0] * 24)], steps])
+    assert [rc for rc, _ in got[2::2][:3]] == [1000] * 3 and got[-1][0] == 10000
+
+
+@pytest.mark.parametrize("bad", [dict(on="none"), dict(n=-1), dict(n=4), dict(rows=-1), dict(rows=1 << 31), dict(which=[0, 1, 3]),
+                                 dict(which=[0, -1, 1]), dict(k=AT + 8), dict(v=AT + 8), dict(f=AT + 4), dict(p=AT + 4), dict(counts=AT + 8),
+                                 dict(n=513, which=[0] * 513)])
+def test_gathers_that_are_refused(bad):
+    assert _run([{}], FED + [["gather", bad]])[-1] == (-1, [])
+
+
+def test_gathers_that_are_not():
+    got = _run([{}], FED + [["gather", {}], ["gather", dict(n=5, which=[0, 0, 2, 1, 0], k=0, v=0, f=0, p=0)], ["gather", dict(n=0)],
+                            ["gather", dict(rows=0)]])[2:]
+    assert [(rc, [n for n, _, _ in ls]) for rc, ls in got] == [(0, ["spkv_gather_pairs<128>"])] * 2 + [(0, []), (0, ["spkv_gather_pairs<128>"])]
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(on="none"), -1), (dict(k=0), -1), (dict(v=0), -1), (dict(f=0), -1), (dict(rows=0), -1), (dict(n_rows=0), -1), (dict(k=AT + 2), -1),
+    (dict(rows=AT + 4), -1), (dict(counts=None), -1), (dict(counts=[1, 65, 0]), -1), (dict(counts=[1, -1, 0]), -1),
+    (dict(counts=[0, 64, 0], on="b"), -3)])
+def test_appends_of_rows_that_are_refused(bad, code):
+    fed = FED + [["append", dict(on="b", counts=[0, 37, 0])]]
+    assert _run([{}, dict(max_context=100)], fed + [["rows", {**dict(counts=[1, 2, 0]), **bad}]])[-1] == (code, [])
+
+
+def test_appends_of_rows():
+    got = _run([{}], FED + [["rows", dict(counts=[1, 64, 0])], ["rows", dict(counts=[0, 0, 0], k=0, rows=0)]])[2:]
+    assert got == [(0, [("spkv_append_rows<128>", 24, 256)]), (0, [])]
+
+
+if __name__ == "__main__":
+    _main()

@@ -1,0 +1,348 @@
+"""Sequences that branch, on the GPU: copies, moves and releases of whole sequences (fork), the append of chosen rows
+(append_rows), and what sequences hold as dense rows (gather), against histories kept by the oracle.
+
+What is copied is compared to the last bit.  Attention afterwards: the tolerances of tests/harness.py."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_14037_amd as spkv
+from oracle.spkv_oracle import SPKVOracle
+from paper_2605_14037_amd.inputs import to_numpy_f32
+from tests import harness as H
+
+pytestmark = pytest.mark.gpu
+KEEP, EMPTY = spkv.FORK_KEEP, spkv.FORK_EMPTY
+
+
+class Both:
+    """A cache and the oracle of it, given the same calls."""
+
+    def __init__(self, batch, hq=8, hk=2, d=64, window=128, tau=0.5, seed=0, context=4096, kept=None, keep=0.4, sinks=0):
+        self.shape = (batch, hq, hk, d)
+        self.g = torch.Generator(device="cuda")
+        self.g.manual_seed(seed)
+        self.mu = float(torch.special.ndtri(torch.tensor(keep, dtype=torch.float64)))
+        self.cache = spkv.SPKVCache(batch, hq, hk, d, max_context=context, window=window, tau=tau,
+                                    max_total_kept_tokens=batch * hk * context if kept is None else kept)
+        if sinks:
+            self.cache.set_option(spkv.OPT_SINK_TOKENS, sinks)
+        self.oracle = SPKVOracle(batch, hq, hk, d, window=window, tau=tau, n_sink=sinks)
+
+    def rows(self, n):
+        _, _, hk, d = self.shape
+        theta = max(min(self.cache.threshold_logit(), 30.0), -30.0)
+        x = [torch.randn(n, hk, d, generator=self.g, device="cuda").bfloat16() for _ in range(2)]
+        return x + [torch.randn(n, hk, generator=self.g, device="cuda") + self.mu + theta]
+
+    @staticmethod
+    def cu(counts):
+        return [sum(counts[:b]) for b in range(len(counts) + 1)]
+
+    def append(self, counts):
+        k, v, f = self.rows(sum(counts))
+        self.cache.append(k, v, f, self.cu(counts))
+        self.oracle.append(to_numpy_f32(k), to_numpy_f32(v), to_numpy_f32(f), self.cu(counts))
+
+    def append_rows(self, n_rows, rows, counts):
+        k, v, f = self.rows(n_rows)
+        rows = [int(r) for r in rows]
+        self.cache.append_rows(k, v, f, torch.tensor(rows, dtype=torch.int32, device="cuda"), self.cu(counts))
+        self.oracle.append(to_numpy_f32(k)[rows], to_numpy_f32(v)[rows], to_numpy_f32(f)[rows], self.cu(counts))
+
+    def fork(self, source, other=None):
+        self.cache.fork(source, other.cache if other is not None else None)
+        self.oracle.fork(source, other.oracle if other is not None else None)
+
+    def check(self, attend=True):
+        batch, hq, hk, d = self.shape
+        st, kept = self.cache.stats(with_kept_len=True)
+        assert st.device_error == 0
+        assert np.array_equal(np.array(kept), self.oracle.kept_len())
+        # every page that is in use is some list's
+        assert st.pool_pages_used == sum((n + 63) // 64 for row in kept for n in row)
+        want = self.oracle.stats()
+        for name in ("total_tokens", "evicted_tokens", "window_tokens", "kept_tokens", "gate_on_tokens"):
+            assert getattr(st, name) == want[name], name
+        k, v, f, positions, counts = self.cache.gather()
+        for b in range(batch):
+            for h in range(hk):
+                at = self.oracle.held(b, h)
+                n = len(at)
+                assert counts[b, h] == n, (b, h)
+                assert positions[b, h, :n].tolist() == at.tolist(), (b, h)
+                for got, history in ((k, self.oracle._k(b)), (v, self.oracle._v(b)), (f, self.oracle._f(b))):
+                    assert np.array_equal(to_numpy_f32(got[b, h, :n]), np.asarray(history[at, h], np.float32)), (b, h)
+        if attend and min(self.oracle._len) > 0:
+            q = torch.randn(batch, hq, d, generator=self.g, device="cuda").bfloat16()
+            out, lse = self.cache.decode_attention(q, want_lse=True)
+            ref, ref_lse = self.oracle.decode(to_numpy_f32(q))
+            H.check_output(out, ref)
+            H.check_lse(lse, ref_lse)
+
+
+# ------------------------------------------------------------------------------------ gather
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window", [1, 31, 64, 100, 128])
+def test_rows_of_what_is_held(window, d):
+    x = Both(7, d=d, window=window, seed=window + d)
+    for counts in ([0, 1, 31, 32, 33, 500, 1000], [0, 0, 1, 1, 40, 300, 1], [0, 1, 0, 5, 7, 1, 200]):
+        x.append(counts)
+        x.check()
+
+
+def test_rows_of_some_sequences_and_fewer_rows_than_pairs():
+    x = Both(3, window=20, seed=5)
+    x.append([300, 0, 70])
+    k, v, f, positions, counts = whole = x.cache.gather()
+    room = k.shape[2]
+    for which, rows in (([2, 0, 2], room), ([0], 1), ([1, 0, 2], 45), ([0, 2], 0)):
+        n = len(which)
+        out = (torch.full((n, 2, rows, 64), 7.0, dtype=torch.bfloat16, device="cuda"),
+               torch.full((n, 2, rows, 64), 7.0, dtype=torch.bfloat16, device="cuda"),
+               torch.full((n, 2, rows), 7.0, device="cuda"), torch.full((n, 2, rows), 7, dtype=torch.int32, device="cuda"),
+               torch.full((n, 2), 7, dtype=torch.int32, device="cuda"))
+        x.cache.gather(which, out=out)
+        assert torch.equal(out[4], counts[which])
+        for i, b in enumerate(which):
+            for h in range(2):
+                m = min(rows, int(counts[b, h]))
+                for got, all_of in zip(out[:4], whole):
+                    assert torch.equal(got[i, h, :m], all_of[b, h, :m])
+                    assert bool((got[i, h, m:] == 7).all())          # rows behind are left as they were
+    assert [t.shape[0] for t in x.cache.gather([])] == [0] * 5
+
+
+def test_rows_in_a_graph_follow_the_lists():
+    x = Both(2, window=20, seed=6)
+    x.append([300, 70])
+    x.check()
+    hk, d = 2, 64
+    out = (torch.zeros(2, hk, 700, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, hk, 700, d, dtype=torch.bfloat16, device="cuda"),
+           torch.zeros(2, hk, 700, device="cuda"), torch.zeros(2, hk, 700, dtype=torch.int32, device="cuda"),
+           torch.zeros(2, hk, dtype=torch.int32, device="cuda"))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.cache.gather(out=out)
+    for counts in ([0, 0], [350, 1], [1, 400]):
+        x.append(counts)
+        graph.replay()
+        eager = x.cache.gather()
+        for a, b in zip(out, eager):
+            if a.dim() == 2:
+                assert torch.equal(a, b)
+                continue
+            for s in range(2):
+                for h in range(hk):
+                    n = int(eager[4][s, h])
+                    assert torch.equal(a[s, h, :n], b[s, h, :n])
+
+
+# -------------------------------------------------------------------------------------- fork
+SOURCES = {
+    "one_to_all": [2] * 8,
+    "swap": [1, 0, KEEP, 3, 4, 5, 7, 6],
+    "cycle": [1, 2, 3, 4, 5, 6, 7, 0],
+    "chain": [KEEP, 0, 1, 2, 3, 4, 5, 6],
+    "cycle_with_tails": [3, 0, 0, 1, 3, 4, KEEP, 4],
+    "two_cycles_shared": [1, 0, 3, 4, 2, 0, 2, KEEP],
+    "emptied_and_taken": [EMPTY, 0, 0, EMPTY, KEEP, 3, EMPTY, 6],
+    "emptied": [EMPTY, KEEP, EMPTY, 3, KEEP, KEEP, KEEP, EMPTY],
+    "all_emptied": [EMPTY] * 8,
+    "stay": [KEEP, 1, 2, KEEP, 4, 5, 6, 7],
+}
+
+
+@pytest.mark.parametrize("d,window", [(64, 128), (128, 100), (64, 1)])
+@pytest.mark.parametrize("name", SOURCES)
+def test_sequences_take_each_others_places(name, d, window):
+    x = Both(8, d=d, window=window, seed=len(name) + d)
+    x.append([0, 1, 900, 64, 130, 333, 2000, 128])
+    x.check(attend=False)
+    for _ in range(2):
+        x.fork(SOURCES[name])
+        x.check()
+        x.append([3, 70, 0, 1, 1, 200, 1, 5])         # they go their own ways
+        x.check()
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_random_turns(seed):
+    """Forks, steps, prompts, prunes and releases in any order."""
+    rng = np.random.default_rng(seed)
+    batch = int(rng.integers(1, 12))
+    x = Both(batch, d=64 if seed % 2 else 128, window=int(rng.integers(1, 150)), seed=seed, sinks=int(rng.integers(0, 3)) * 4, context=30000)
+    x.append([int(n) for n in rng.integers(0, 700, batch)])
+    for turn in range(12):
+        kind = int(rng.integers(0, 6))
+        if kind <= 2:
+            x.fork([int(s) if s >= -2 else KEEP for s in rng.integers(-2, batch, batch)])
+        elif kind == 3:
+            x.append([int(n) for n in rng.integers(0, 40, batch)])
+        elif kind == 4:
+            counts = [int(n) for n in rng.integers(0, 65, batch)]
+            x.append_rows(50, rng.integers(0, 50, sum(counts)), counts)
+        else:
+            x.append([1] * batch)
+        x.check(attend=turn % 3 == 2)
+
+
+@pytest.mark.parametrize("d,window", [(64, 128), (128, 33)])
+def test_sequences_of_another_cache(d, window):
+    prompts = Both(3, d=d, window=window, seed=1, context=2000)
+    prompts.append([1500, 7, 0])
+    x = Both(6, d=d, window=window, seed=2, context=3000, tau=0.7, keep=0.2)
+    x.append([100, 0, 600, 5, 0, 1])
+    for source in ([0, 0, 1, 2, KEEP, 0], [1, 0, EMPTY, 0, 0, KEEP], [0, 0, 0, 0, 0, 0]):
+        x.fork(source, prompts)
+        x.check()
+        x.append([2, 300, 1, 1, 64, 9])               # (the gates from here on: the second cache's threshold)
+        k, _, _, positions, counts = x.cache.gather()
+        for b in range(6):
+            for h in range(2):
+                assert positions[b, h, :int(counts[b, h])].tolist() == x.oracle.held(b, h).tolist()
+        prompts.check()
+
+
+def test_a_pool_of_just_the_pages_that_are_needed():
+    """Forks give back as many pages as they take: the pool never runs out, and a call that it cannot serve changes nothing."""
+    x = Both(4, window=16, seed=3, context=1500, kept=4 * 2 * 1000, keep=0.9)
+    x.append([1000, 900, 100, 0])
+    x.check(attend=False)
+    for _ in range(20):
+        for source in ([0, 0, 0, 0], [KEEP, EMPTY, EMPTY, EMPTY], [EMPTY, 0, KEEP, 0], [1, 3, 1, KEEP]):
+            x.fork(source)
+    x.check(attend=False)
+    big = Both(4, window=16, seed=4, context=3000, kept=4 * 2 * 2000, keep=0.9)
+    big.append([2900, 0, 10, 0])
+    for other, source in ((big, [0, 0, 0, 0]), (None, None)):
+        if other is None:
+            x.cache.fork([EMPTY] * 4)
+            x.oracle.fork([EMPTY] * 4)
+            x.append([600, 600, 600, 600])
+            continue
+        with pytest.raises(spkv.SPKVError, match="capacity"):
+            x.cache.fork(source, other.cache)         # longer than max_context
+        x.check(attend=False)
+    tight = Both(4, window=16, seed=5, context=3000, kept=3000, keep=0.9)
+    tight.append([1200, 0, 0, 0])
+    with pytest.raises(spkv.SPKVError, match="capacity"):
+        tight.cache.fork([KEEP, 0, 0, 0])
+    tight.check(attend=False)
+    tight.fork([EMPTY, KEEP, 0, KEEP])
+    tight.check(attend=False)
+
+
+def test_what_a_window_held_does_not_show():
+    """Infinities and NaN of a sequence that is replaced or emptied, in the ring and in pages given back."""
+    x = Both(4, window=40, seed=7, keep=0.9)
+    k, v, f = x.rows(600)
+    v[:] = float("inf")
+    v[::3] = float("nan")
+    k[::2] = float("nan")
+    x.cache.append(k, v, f, [0, 300, 600, 600, 600])
+    x.oracle._len = [0] * 4                           # (their histories are never looked at)
+    x.fork([2, EMPTY, 1, KEEP])
+    x.fork([KEEP, KEEP, EMPTY, KEEP])
+    x.append([5, 3, 37, 41])
+    x.check()
+    x.append([60, 100, 1, 300])
+    x.check()
+    x.fork([3, 3, 3, 0])
+    x.check()
+
+
+def test_beams_of_a_wide_batch():
+    """As many sequences as a cache has; groups that trade places among themselves."""
+    x = Both(512, hq=2, hk=1, window=20, seed=8, context=300, keep=0.5)
+    x.append([20 + b % 37 for b in range(512)])
+    rng = np.random.default_rng(0)
+    for _ in range(2):
+        x.fork([b // 4 * 4 + int(rng.integers(0, 4)) for b in range(512)])
+        x.append([1] * 512)
+    x.check()
+    x.fork([int(s) for s in rng.permutation(512)])
+    x.check()
+
+
+def test_fork_is_refused_under_capture_and_for_other_shapes():
+    x = Both(2, window=20, seed=9)
+    x.append([50, 3])
+    x.check()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        torch.zeros(8, device="cuda").add_(1)
+        with pytest.raises(spkv.SPKVError, match="-2"):
+            x.cache.fork([1, 1])
+        x.cache.fork([0, KEEP])                       # nothing to do
+    for other in (Both(2, window=21), Both(2, hk=4), Both(2, d=128), Both(2, hq=4)):
+        with pytest.raises(spkv.SPKVError, match="invalid"):
+            x.cache.fork([0, 0], other.cache)
+    for bad in ([0, 2], [-3, 0]):
+        with pytest.raises(spkv.SPKVError, match="invalid"):
+            x.cache.fork(bad)
+    with pytest.raises(ValueError):
+        x.cache.fork([0])
+    x.check()
+
+
+def test_steps_after_a_fork_are_counted():
+    """What the host knows of the lengths follows the sequences: safe steps, captured steps, copies' bits."""
+    x = Both(6, window=32, seed=10, context=900, keep=0.5)
+    x.append([500, 3, 0, 40, 100, 1])
+    x.fork([0, 0, 0, KEEP, 0, 3])
+    assert x.cache.safe_steps() == 400
+    _, hq, hk, d = x.shape
+    q = torch.randn(1, hq, d, generator=x.g, device="cuda").bfloat16().expand(6, hq, d).contiguous()
+    out = x.cache.decode_attention(q)
+    for b in (1, 2, 4):
+        assert torch.equal(out[b], out[0])
+    assert torch.equal(out[5], out[3])
+    for _ in range(50):
+        x.append([1] * 6)
+    x.check()
+
+
+# -------------------------------------------------------------------------------- append_rows
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window", [1, 2, 15, 16, 17, 50, 128])
+def test_chosen_rows_are_appended(window, d):
+    rng = np.random.default_rng(window)
+    x = Both(7, d=d, window=window, seed=window)
+    x.append([0, 1, 15, 60, 127, 300, 0])
+    for counts in ([1, 0, 2, 16, 17, 64, 0], [64, 33, 1, 0, 5, 16, 1], [1] * 7, [0, 0, 0, 31, 0, 0, 0]):
+        x.append_rows(90, rng.integers(0, 90, sum(counts)), counts)
+        x.check()
+
+
+def test_rows_that_are_not_there_are_flagged():
+    x = Both(2, window=20, seed=11)
+    x.append([30, 30])
+    k, v, f = x.rows(10)
+    x.cache.append_rows(k, v, f, torch.tensor([0, 9, 10], dtype=torch.int32, device="cuda"), [0, 2, 3])
+    with pytest.raises(spkv.SPKVError, match="inconsistent"):
+        x.cache.stats()
+    x.cache.reset()
+    x.cache.append_rows(k, v, f, torch.tensor([-1], dtype=torch.int32, device="cuda"), [0, 0, 1])
+    with pytest.raises(spkv.SPKVError, match="inconsistent"):
+        x.cache.stats()
+    x.cache.reset()
+    assert x.cache.stats().total_tokens == 0
+
+
+def test_refused_appends_change_nothing():
+    x = Both(2, window=20, seed=12, context=100, kept=640)
+    x.append([60, 95])
+    k, v, f = x.rows(70)
+    rows = torch.arange(70, dtype=torch.int32, device="cuda")
+    with pytest.raises(spkv.SPKVError, match="capacity"):
+        x.cache.append_rows(k, v, f, rows[:6], [0, 0, 6])
+    with pytest.raises(spkv.SPKVError, match="invalid"):
+        x.cache.append_rows(k, v, f, rows[:65], [0, 65, 65])
+    with pytest.raises(ValueError):
+        x.cache.append_rows(k, v, f, rows.long()[:1], [0, 1, 1])
+    with pytest.raises(ValueError):
+        x.cache.append_rows(k, v, f[:3], rows[:1], [0, 1, 1])
+    x.cache.append_rows(k, v, f, rows[:0], [0, 0, 0])
+    x.check()
