@@ -384,6 +384,27 @@ int spkv_decode_attention_shared(spkv_cache_t* cache, spkv_cache_t* prefix, cons
                                  const void* q, void* out, float* lse, float sm_scale,
                                  void* workspace, size_t workspace_bytes, void* stream);
 
+/* Scoring of a tree of drafted tokens: several continuations of every sequence at once, the cache left exactly as it
+ * was.  Draft i of a sequence hangs behind draft parents[i] of the same sequence, and attends as if the drafts on the path from
+ * the newest token to it -- and no others -- had been appended before it (Eq. 3-5): with d drafts before it on its
+ * path it stands at position T + d, and sees the cached keys inside its window or past the gate, the drafts of its
+ * path (past the window only those with their gate on), and itself.  A chain of drafts is spkv_score_chunk's case.
+ * Accepted paths are appended by spkv_append_rows.
+ *   k, v         device bf16 [total, n_kv_heads, head_dim]    q, out  device bf16 [total, n_q_heads, head_dim]
+ *   util_logits  device fp32 [total, n_kv_heads], or NULL where no sequence has more drafts than the window tokens
+ *   parents      device int32 [total]: -1 (or anything that is not 0 .. i - 1): the draft hangs behind the newest token,
+ *                else the index, within its sequence's drafts, of an earlier one
+ *   cu_seqlens   host int32 [batch + 1]: sequence b's drafts are rows cu[b] .. cu[b+1]-1, at most SPKV_MAX_TREE_NODES
+ *   lse          device fp32 [total, n_q_heads] or NULL
+ * A sequence may hold no token.  One pass over the cache serves all drafts of a sequence.  Needs no workspace (partial results
+ * lie in the cache's own buffers); two launches, more for hundreds of (sequence, KV head) pairs with many columns each.  Waits
+ * once for the lengths after a prompt's append, as spkv_decode_attention does.  May be captured; a replay takes the parents and
+ * the lists as they are by then.  Copies of a sequence get results that agree to rounding.
+ * Errors: SPKV_E_INVAL for bad shapes and pointers; never SPKV_E_STATE. */
+int spkv_score_tree(spkv_cache_t* cache, const void* k, const void* v, const float* util_logits, const void* q,
+                    const int32_t* parents, const int32_t* cu_seqlens, void* out, float* lse, float sm_scale,
+                    void* stream);
+
 /* Append of chosen rows: spkv_append of the tokens k[rows[i]], v[rows[i]], util_logits[rows[i]].  The drafts of a
  * tree that were accepted lie here and there in its buffers; this takes them from where they are.
  *   k, v         device bf16 [n_rows, n_kv_heads, head_dim]    util_logits device fp32 [n_rows, n_kv_heads]

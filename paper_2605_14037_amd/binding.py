@@ -35,7 +35,7 @@ EXPORTED_SYMBOLS = [
     "spkv_debug_layout_offset", "spkv_debug_copy", "spkv_debug_read", "spkv_strerror",
     "spkv_qk_norm_rope", "spkv_qk_norm_rope_backward", "spkv_qk_norm_rope_backward_workspace_bytes",
     "spkv_prefix_workspace_bytes", "spkv_prefix_attention", "spkv_decode_attention_shared",
-    "spkv_append_rows", "spkv_cache_fork", "spkv_cache_gather",
+    "spkv_score_tree", "spkv_append_rows", "spkv_cache_fork", "spkv_cache_gather",
 ]
 
 BF16, FP32 = 0, 1
@@ -144,6 +144,8 @@ def load_library():
     lib.spkv_qk_norm_rope_backward.restype = C.c_int
     lib.spkv_qk_norm_rope_backward.argtypes = [ph, ph, ph, ph, ph, vp, vp, f32, vp, pr, i32, i64, i32, i32,
                                                ph, ph, ph, vp, vp, vp, C.c_size_t, vp]
+    lib.spkv_score_tree.restype = C.c_int
+    lib.spkv_score_tree.argtypes = [vp, vp, vp, vp, vp, vp, P(i32), vp, vp, f32, vp]
     lib.spkv_append_rows.restype = C.c_int
     lib.spkv_append_rows.argtypes = [vp, vp, vp, vp, vp, i32, P(i32), vp]
     lib.spkv_cache_fork.restype = C.c_int
@@ -781,6 +783,34 @@ class SPKVCache:
         return out, lse
 
     # ---- sequences that branch
+    def score_tree(self, k, v, q, parents, cu_seqlens, util_logits=None, out=None, lse=None, sm_scale=0.0, want_lse=False):
+        """Attention outputs of a tree of up to 64 drafts per sequence, the cache left unchanged (spkv_score_tree).
+        parents: int32 [total] on the device, the index of an earlier draft of the same sequence or -1.  util_logits: the
+        drafts', needed where a sequence has more drafts than the window has tokens."""
+        cfg = self.cfg
+        cu = cu_seqlens if isinstance(cu_seqlens, C.Array) else self.make_cu(cu_seqlens)
+        total = cu[cfg.batch]
+        if total == 0:
+            _check(self.lib.spkv_score_tree(self.handle, None, None, None, None, None, cu, None, None, float(sm_scale),
+                                            _stream()), "spkv_score_tree")
+            return None
+        kv_shape = (total, cfg.n_kv_heads, cfg.head_dim)
+        shape = (total, cfg.n_q_heads, cfg.head_dim)
+        kp = _dev_ptr(k, torch.bfloat16, kv_shape, "k")
+        vp = _dev_ptr(v, torch.bfloat16, kv_shape, "v")
+        qp = _dev_ptr(q, torch.bfloat16, shape, "q")
+        fp = _dev_ptr(util_logits, torch.float32, kv_shape[:2], "util_logits") if util_logits is not None else None
+        pp = _dev_ptr(parents, torch.int32, (total,), "parents")
+        if out is None:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+        op = _dev_ptr(out, torch.bfloat16, shape, "out")
+        if lse is None and want_lse:
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
+        lp = _dev_ptr(lse, torch.float32, shape[:2], "lse") if lse is not None else None
+        _check(self.lib.spkv_score_tree(self.handle, kp, vp, fp, qp, pp, cu, op, lp, float(sm_scale), _stream()),
+               "spkv_score_tree")
+        return (out, lse) if lse is not None else out
+
     def append_rows(self, k, v, util_logits, rows, cu_seqlens):
         """Append the rows `rows` (int32 [total], on the device) of k, v, util_logits: sequence b's tokens are
         rows[cu[b]:cu[b + 1]] (spkv_append_rows).  For the drafts of a tree that were accepted."""

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspkv.so")
 SOURCES = ["spkv_api.hip", "spkv_write.hip", "spkv_decode.hip", "spkv_decode_short.hip",
            "spkv_prefill.hip", "spkv_predictor.hip", "spkv_rope.hip", "spkv_prefix.hip",
-           "spkv_branch.hip"]
+           "spkv_branch.hip", "spkv_tree.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1972,6 +1972,119 @@ int spkv_decode_attention_shared(spkv_cache_t* c, spkv_cache_t* pc, const int32_
 }
 
 namespace {
+// Ranges of the lists of a launch (pairs tree->pair0 .. + n_pairs - 1): about as many workgroups as the chip holds at
+// once, every list cut evenly into its share of them; a half-page of the ring counts twice (ShareList::begin).
+constexpr int kTreeMinUnit = 2, kTreeStart = 16;
+int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, int width, int64_t fit, SpkvTree* tree, SpkvTreeTable* table) {
+    const int Hkv = c->cfg.n_kv_heads, G = c->carve.G;
+    int32_t hp[kTreePairs], copies[kTreePairs];
+    int64_t work = 0, lists = 0;
+    for (int i = 0; i < n_pairs; ++i) {
+        const int p = tree->pair0 + i, b = p / Hkv;
+        copies[i] = ((cu[b + 1] - cu[b]) * G + width - 1) / width;
+        hp[i] = (c->L_ub[p] + kHalfTokens - 1) / kHalfTokens + 2 * ((std::min(c->T[b], c->cfg.window) + kHalfTokens - 1) / kHalfTokens);
+        work += (int64_t)hp[i] * copies[i];
+        lists += copies[i];
+    }
+    const int cus = spkv_compute_units();
+    const int64_t round = cus > 0 ? cus : 256;
+    int64_t unit = 0, best = 0;
+    for (int k = 1; k <= 2; ++k) {
+        const int64_t target = std::min(fit, (int64_t)k * round);
+        int64_t u = std::max<int64_t>(kTreeMinUnit, (work + target - 1) / target), total = 0, longest = 0;
+        for (int guard = 0; guard < 64; ++guard) {
+            total = longest = 0;
+            for (int i = 0; i < n_pairs; ++i) {
+                const int64_t r = std::min<int64_t>(255, std::max<int64_t>(1, (hp[i] + u - 1) / u));
+                total += r * copies[i];
+                longest = std::max(longest, (hp[i] + r - 1) / r);
+            }
+            if (total <= target || total <= lists) break;
+            u += std::max<int64_t>(1, u / 16);
+        }
+        const int64_t time = (total + round - 1) / round * (longest + kTreeStart);
+        if (k > 1 && time >= best) continue;
+        best = time;
+        unit = total > fit ? (int64_t)1 << 40 : u;           // (no room for ranges: one each)
+    }
+    int64_t end = 0;
+    int most = 1;
+    for (int i = 0; i < kTreePairs; ++i) {
+        if (i >= n_pairs) {
+            table->end[i] = 65535;
+            table->ranges[i] = 1;
+            continue;
+        }
+        const int64_t r = std::min<int64_t>(255, std::max<int64_t>(1, (hp[i] + unit - 1) / unit));
+        most = std::max(most, (int)r);
+        end += r * copies[i];
+        table->end[i] = (uint16_t)end;
+        table->ranges[i] = (uint8_t)r;
+    }
+    tree->n_units = (int32_t)end;
+    return most;
+}
+}  // namespace
+
+int spkv_score_tree(spkv_cache_t* c, const void* k, const void* v, const float* util_logits, const void* q,
+                    const int32_t* parents, const int32_t* cu_seqlens, void* out, float* lse, float sm_scale, void* stream) {
+    if (c == nullptr || cu_seqlens == nullptr || cu_seqlens[0] != 0) return SPKV_E_INVAL;
+    const int B = c->cfg.batch, Hkv = c->cfg.n_kv_heads, G = c->carve.G;
+    int n_max = 0;
+    for (int b = 0; b < B; ++b) {
+        const int64_t n = (int64_t)cu_seqlens[b + 1] - cu_seqlens[b];
+        if (n < 0 || n > SPKV_MAX_TREE_NODES || (n > c->cfg.window && util_logits == nullptr)) return SPKV_E_INVAL;
+        n_max = std::max(n_max, (int)n);
+    }
+    if (n_max == 0) return SPKV_OK;
+    if (k == nullptr || v == nullptr || q == nullptr || parents == nullptr || out == nullptr) return SPKV_E_INVAL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(util_logits) || !aligned16(q) || !aligned16(parents) || !aligned16(out) ||
+        !aligned16(lse))
+        return SPKV_E_INVAL;
+    if (!(sm_scale > 0.f)) sm_scale = 1.0f / std::sqrt((float)c->cfg.head_dim);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    try {
+        if (c->bound_is_loose) {
+            const int rc = exact_lengths(c, s);
+            if (rc != SPKV_OK) return rc;
+        }
+    } catch (const std::exception&) {
+        return SPKV_E_NOMEM;
+    }
+    tighten_bound(c, s);
+    const int width = spkv_tree_width(n_max * G);
+    SpkvTree tree = {};
+    tree.k = static_cast<const uint16_t*>(k);
+    tree.v = static_cast<const uint16_t*>(v);
+    tree.f = util_logits;
+    tree.parents = parents;
+    tree.n_blocks = (n_max * G + width - 1) / width;
+    // The partial results lie in the cache's buffers of them.  What does not fit a launch (only caches of hundreds of pairs
+    // with many columns each) takes several.
+    const int64_t slots = (int64_t)c->carve.max_items * G / width;
+    int64_t per = std::min<int64_t>(kTreePairs, slots / (2 * tree.n_blocks));
+    if (per < 1) return SPKV_E_CAPACITY;
+    if (per > Hkv) per -= per % Hkv;
+    for (int p0 = 0; p0 < c->carve.n_pairs; p0 += (int)per) {
+        const int n_pairs = (int)std::min<int64_t>(per, c->carve.n_pairs - p0);
+        SpkvTreeTable table;
+        tree.pair0 = p0;
+        tree.seq0 = p0 / Hkv;
+        tree.row0 = cu_seqlens[tree.seq0];
+        const int seqs = (p0 + n_pairs - 1) / Hkv - tree.seq0 + 1;
+        if (cu_seqlens[tree.seq0 + seqs] == tree.row0) continue;
+        for (int i = 0; i <= seqs; ++i) table.cu[i] = (uint16_t)(cu_seqlens[tree.seq0 + i] - tree.row0);
+        tree.n_own = n_pairs * tree.n_blocks;
+        const int most = tree_cut(c, cu_seqlens, n_pairs, width, std::min<int64_t>(slots - tree.n_own, 32767), &tree, &table);
+        if (tree.n_units + tree.n_own > slots) return SPKV_E_CAPACITY;
+        if (spkv_launch_tree(c->view, static_cast<const uint16_t*>(q), sm_scale, width, tree, table, n_pairs, n_max * G, most,
+                             static_cast<uint16_t*>(out), lse, s) != hipSuccess)
+            return SPKV_E_HIP;
+    }
+    return SPKV_OK;
+}
+
+namespace {
 // What spkv_cache_fork makes of its sources: moves in an order in which every sequence is read before it is replaced
 // (spkv_fork_move), and the sequences that need pages of their own afterwards.
 struct ForkPlan {

@@ -357,3 +357,26 @@ hipError_t spkv_launch_gather_pairs(const SpkvView& v, const SpkvSequences& of, 
                                     hipStream_t s);
 hipError_t spkv_launch_append_rows(const SpkvView& v, const uint16_t* k, const uint16_t* vv, const float* f,
                                    const int32_t* rows, int n_rows, const SpkvCu& cu, hipStream_t s);
+
+// Attention of trees of drafts (spkv_tree.hip), at most kTreePairs (sequence, KV head) pairs to a launch: those from
+// pair0 on, sequences from seq0 on, whose first row is row0.
+constexpr int kTreePairs = 512;
+struct SpkvTree {
+    const uint16_t *k, *v;
+    const float* f;              // null: every path fits the window
+    const int32_t* parents;
+    int32_t pair0, seq0, row0;
+    int32_t n_own;               // units of the drafts themselves: a pair's blocks of columns
+    int32_t n_blocks;            // ... of the pair with the most columns
+    int32_t n_units;             // units of the lists
+};
+struct SpkvTreeTable {
+    alignas(16) uint16_t end[kTreePairs];        // units of the lists up to and with each pair's; pairs that are not there: 65535
+    uint16_t cu[kTreePairs + 1];                 // rows from row0 on
+    uint8_t ranges[kTreePairs];
+};
+int spkv_tree_width(int n_cols);         // columns of a workgroup, for the pair with the most
+int spkv_tree_waves(int width);
+hipError_t spkv_launch_tree(const SpkvView& v, const uint16_t* q, float sm_scale, int width, const SpkvTree& tree,
+                            const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, uint16_t* out, float* lse,
+                            hipStream_t s);

@@ -85,6 +85,10 @@ def _main():
         elif op == "rows":
             rc = lib.spkv_append_rows(who, ptr(a.get("k", AT)), ptr(a.get("v", AT)), ptr(a.get("f", AT)), ptr(a.get("rows", AT)),
                                       a.get("n_rows", 100), cu(a["counts"]), None)
+        elif op == "tree":
+            rc = lib.spkv_score_tree(who, ptr(a.get("k", AT)), ptr(a.get("v", AT)), ptr(a.get("f", AT)), ptr(a.get("q", AT)),
+                                     ptr(a.get("parents", AT)), cu(a["counts"]), ptr(a.get("out", AT)), ptr(a.get("lse", 0)),
+                                     C.c_float(0.0), None)
         else:
             raise ValueError(op)
         calls.append([rc, taken()])
@@ -182,6 +186,39 @@ def test_appends_of_rows_that_are_refused(bad, code):
 def test_appends_of_rows():
     got = _run([{}], FED + [["rows", dict(counts=[1, 64, 0])], ["rows", dict(counts=[0, 0, 0], k=0, rows=0)]])[2:]
     assert got == [(0, [("spkv_append_rows<128>", 24, 256)]), (0, [])]
+
+
+@pytest.mark.parametrize("bad", [
+    dict(on="none"), dict(counts=None), dict(counts=[0, 65, 0]), dict(counts=[3, -1, 1]), dict(k=0), dict(v=0), dict(q=0), dict(parents=0),
+    dict(out=0), dict(k=AT + 8), dict(v=AT + 2), dict(f=AT + 4), dict(q=AT + 8), dict(parents=AT + 4), dict(out=AT + 8), dict(lse=AT + 4),
+    dict(on="b", f=0, counts=[0, 21, 0])])
+def test_trees_that_are_refused(bad):
+    assert _run([{}, dict(window=20)], FED + [["tree", {**dict(counts=[1, 2, 0]), **bad}]])[-1] == (-1, [])
+
+
+def test_launches_of_a_tree():
+    """A workgroup as wide as the largest tree asks, the lists in one pass, and one join."""
+    for n, kernel, waves in ((1, "few<128, 1>", 4), (4, "few<128, 1>", 4), (5, "few<128, 2>", 4), (8, "few<128, 2>", 4), (9, "split<128, 2>", 2),
+                             (16, "split<128, 2>", 2), (17, "split<128, 4>", 4), (32, "split<128, 4>", 4), (33, "split<128, 8>", 8),
+                             (64, "split<128, 8>", 8)):
+        rc, got = _run([{}], FED + [["tree", dict(counts=[n, 1, 0])]])[-1]
+        assert rc == 0 and len(got) == 2 and got[1][0].startswith("spkv_tree_merge<128, ")
+        assert got[0][0] == "spkv_tree_" + kernel and got[0][2] == 64 * waves
+        assert 24 + 16 <= got[0][1] <= 24 + 16 + 512      # the drafts' units, a range for every list at least, two rounds at most
+    assert _run([{}], FED + [["tree", dict(counts=[0, 0, 0], k=0, q=0)]])[-1] == (0, [])
+    assert _run([dict(window=20)], FED + [["tree", dict(counts=[20, 0, 3], f=0)]])[-1][0] == 0
+
+
+def test_trees_of_many_pairs_take_several_launches():
+    cfg = dict(batch=200, n_q_heads=8, n_kv_heads=4, head_dim=64, max_context=500, max_total_kept_tokens=100000)
+    rc, got = _run([cfg], [["append", dict(counts=[5] * 200)], ["lengths", dict(kept=[0] * 800)], ["tree", dict(counts=[1] * 200)]])[-1]
+    assert rc == 0 and [n.split("<")[0] for n, _, _ in got] == ["spkv_tree_few", "spkv_tree_merge"] * 2
+    # as many columns as there are, on as many pairs: what does not fit the partial results' room
+    cfg = dict(batch=512, n_q_heads=512, n_kv_heads=32, head_dim=64, max_context=200, max_total_kept_tokens=1000)
+    rc, got = _run([cfg], [["tree", dict(counts=[64] * 512)]])[-1]
+    assert rc == 0 and len(got) % 2 == 0 and len(got) >= 64
+    rc, got = _run([cfg], [["tree", dict(counts=[64] + [0] * 511)]])[-1]
+    assert rc == 0 and len(got) == 2
 
 
 if __name__ == "__main__":
