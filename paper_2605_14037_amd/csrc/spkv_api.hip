@@ -2089,19 +2089,22 @@ namespace {
 // (spkv_fork_move), and the sequences that need pages of their own afterwards.
 struct ForkPlan {
     SpkvForkMoves moves;
-    SpkvSequences copies;
+    SpkvForkCopies copies;
     int n_copies;
+    bool wanted[SPKV_MAX_BATCH];         // (in the cache itself) what it held goes to another sequence
 };
 // same: the sources are sequences of the cache itself.
 void plan_fork(int B, const int32_t* source, bool same, ForkPlan* p) {
     // Sequences that hang together: each points towards the one that stands for its component.
     int16_t towards[SPKV_MAX_BATCH], next[SPKV_MAX_BATCH], first[SPKV_MAX_BATCH], readers[SPKV_MAX_BATCH];
-    bool replaced[SPKV_MAX_BATCH], made[SPKV_MAX_BATCH], taken[SPKV_MAX_BATCH], wanted[SPKV_MAX_BATCH];
+    int16_t taken_by[SPKV_MAX_BATCH];
+    bool replaced[SPKV_MAX_BATCH], made[SPKV_MAX_BATCH];
     for (int b = 0; b < B; ++b) {
         towards[b] = (int16_t)b;
         first[b] = -1;
         readers[b] = 0;
-        made[b] = taken[b] = wanted[b] = false;
+        taken_by[b] = -1;
+        made[b] = p->wanted[b] = false;
         replaced[b] = source[b] == SPKV_FORK_EMPTY || (source[b] >= 0 && !(same && source[b] == b));
     }
     auto root = [&](int b) -> int {
@@ -2111,7 +2114,7 @@ void plan_fork(int B, const int32_t* source, bool same, ForkPlan* p) {
     for (int b = 0; same && b < B; ++b) {
         const int s = source[b];
         if (!replaced[b] || s < 0 || !replaced[s]) continue;
-        wanted[s] = true;
+        p->wanted[s] = true;
         ++readers[s];
         towards[root(b)] = (int16_t)root(s);
     }
@@ -2126,12 +2129,15 @@ void plan_fork(int B, const int32_t* source, bool same, ForkPlan* p) {
     auto emit = [&](int b, int dst_flags, int src_flags) {
         const int s = source[b];
         made[b] = true;
-        if (!wanted[b]) dst_flags |= kForkFree;              // (of another cache: nothing here is read)
+        if (!p->wanted[b]) dst_flags |= kForkFree;              // (of another cache: nothing here is read)
         p->moves.dst[at] = (uint16_t)(b | dst_flags);
+        if (s >= 0 && same && replaced[s] && taken_by[s] < 0) {
+            taken_by[s] = (int16_t)b;
+        } else if (s >= 0) {
+            src_flags |= kForkCopy;
+            p->copies.dst[p->n_copies++] = (uint16_t)b;
+        }
         p->moves.src[at++] = (uint16_t)(s < 0 ? kForkNothing : s | src_flags);
-        if (s < 0) return;
-        if (same && replaced[s] && !taken[s]) taken[s] = true;
-        else p->copies.seq[p->n_copies++] = (uint16_t)b;
     };
     for (int r = 0; r < B; ++r) {
         if (first[r] < 0) continue;
@@ -2154,6 +2160,10 @@ void plan_fork(int B, const int32_t* source, bool same, ForkPlan* p) {
         }
     }
     p->moves.start[p->moves.n] = (uint16_t)at;
+    for (int i = 0; i < p->n_copies; ++i) {                  // where the pages are by the time of the copies
+        const int s = source[p->copies.dst[i]];
+        p->copies.of[i] = (uint16_t)(same && replaced[s] ? taken_by[s] : s);
+    }
 }
 SpkvForkSource fork_source(const SpkvView& v) {
     return SpkvForkSource{v.ring, v.pool, v.ring_logit, v.logit_pool, v.page_table, v.pos_pool, v.t_pair, v.kept_len, v.gate_on,
@@ -2204,10 +2214,17 @@ int spkv_cache_fork(spkv_cache_t* c, spkv_cache_t* other, const int32_t* source,
 
     const SpkvForkSource src = fork_source(from->view);
     if (spkv_launch_fork_move(c->view, src, plan.moves, s) != hipSuccess) return SPKV_E_HIP;
-    int64_t most = 0;
-    for (int i = 0; i < plan.n_copies; ++i)
-        for (int h = 0; h < Hkv; ++h) most = std::max(most, pages_for(length_after(plan.copies.seq[i], h)));
-    if (most > 0 && spkv_launch_fork_pages(c->view, src, plan.copies, plan.n_copies, (int)most, s) != hipSuccess)
+    int64_t most = 0, all = 0, fresh = 0;
+    for (int i = 0; i < plan.n_copies; ++i) {
+        const int b = plan.copies.dst[i];
+        for (int h = 0; h < Hkv; ++h) {
+            const int64_t pages = pages_for(length_after(b, h)), own = plan.wanted[b] ? 0 : pages_for(c->L_ub[b * Hkv + h]);
+            most = std::max(most, pages);
+            all += pages;
+            fresh += std::max<int64_t>(0, pages - own);
+        }
+    }
+    if (most > 0 && spkv_launch_fork_pages(c->view, src, plan.copies, plan.n_copies, most, all, fresh, s) != hipSuccess)
         return SPKV_E_HIP;
 
     int32_t len[kMaxPairs], tokens[SPKV_MAX_BATCH], since[SPKV_MAX_BATCH];

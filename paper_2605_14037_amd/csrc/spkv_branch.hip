@@ -2,12 +2,16 @@
 // dense rows, and the append of rows that lie here and there.
 #include "spkv_device.h"
 
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+
 // ---------------------------------------------------------------- sequences become others
 // All sequences of a call change at once: sequence b becomes what source[b] was.  What a sequence holds is its
-// window ring, its counters and, per head, a row of the page table.  Rows move as they are: the first sequence that
-// takes over one whose own place is taken has its pages, without a copy; further ones hold the same page ids for the
-// length of this launch and get pages of their own in the next (spkv_fork_pages).  Pages that nobody takes go back
-// onto the stack, in this launch alone, and pages are handed out in the next alone.
+// window ring, its counters and, per head, a row of the page table.  The first sequence that takes over one whose own
+// place is taken has its row of page ids, without a copy; further ones get copies of the pages in the next launch
+// (spkv_fork_pages), from wherever they are by then, into the pages that they have themselves already, unless somebody
+// takes those, and further ones from the pool.  Pages that are left over go back onto the stack, in this launch alone, and
+// pages are handed out in the next alone.  (Copies into the pages at hand: every handing out is an atomic on one address, and
+// 2600 of them -- eight copies of 32k tokens, four pages each -- were most of 148 us.)
 //
 // Order.  Sequences that hang together (one is the source of another and is itself replaced) are a component; the
 // host has put its moves into an order in which every sequence is read before it is replaced, a cycle being opened by
@@ -59,7 +63,7 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_move(SpkvView v, SpkvF
         return;
     }
     __shared__ int s_len[SPKV_MAX_BATCH], s_tokens[SPKV_MAX_BATCH], s_on[SPKV_MAX_BATCH];   // what move m brings
-    __shared__ int s_old[SPKV_MAX_BATCH], s_at[SPKV_MAX_BATCH];   // pages that move m gives back, their place on the stack
+    __shared__ int s_own[SPKV_MAX_BATCH], s_stay[SPKV_MAX_BATCH], s_at[SPKV_MAX_BATCH];     // pages of its own, those that stay, place of the others on the stack
     __shared__ int s_most;
     if (tid == 0) s_most = 0;
     __syncthreads();
@@ -70,9 +74,14 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_move(SpkvView v, SpkvF
         s_len[i] = nothing ? 0 : from.kept_len[of];
         s_tokens[i] = nothing ? 0 : from.t_pair[of];
         s_on[i] = nothing ? 0 : from.gate_on[of];
-        s_old[i] = (d & kForkFree) != 0 ? (v.kept_len[to] + kPageTokens - 1) / kPageTokens : 0;
-        s_at[i] = s_old[i] > 0 ? atomicAdd(v.free_top, s_old[i]) : 0;
-        atomicMax(&s_most, max(s_old[i], (s_len[i] + kPageTokens - 1) / kPageTokens));
+        // its own pages: those that the copy needs stay, the others go back
+        const int own = (d & kForkFree) != 0 ? (v.kept_len[to] + kPageTokens - 1) / kPageTokens : 0;
+        const int pages = (s_len[i] + kPageTokens - 1) / kPageTokens, stay = (s & kForkCopy) != 0 ? min(own, pages) : 0;
+        s_own[i] = own;
+        s_stay[i] = stay;
+        s_at[i] = own > stay ? atomicAdd(v.free_top, own - stay) : 0;
+        if ((s & kForkCopy) != 0) v.pair_items[to] = stay;    // (scratch of the decoding steps)
+        atomicMax(&s_most, max(own, pages));
     }
     __syncthreads();
     const int most = s_most;
@@ -81,12 +90,12 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_move(SpkvView v, SpkvF
         for (int m = m0; m < m1; ++m) {
             const int d = mv.dst[m], s = mv.src[m];
             int32_t* at = v.page_table + ((size_t)(d & kForkIndex) * v.Hkv + h) * v.pt_cap;
-            const int n = (s_len[m - m0] + kPageTokens - 1) / kPageTokens;
+            const int n = (s & kForkCopy) != 0 ? 0 : (s_len[m - m0] + kPageTokens - 1) / kPageTokens;
             const int old = i < v.pt_cap ? at[i] : 0;
             int x = saved;
             if ((s & (kForkSaved | kForkNothing)) == 0 && i < n)
                 x = from.page_table[((size_t)(s & kForkIndex) * v.Hkv + h) * from.pt_cap + i];
-            if (i < s_old[m - m0]) v.free_pages[s_at[m - m0] + i] = old;
+            if (i >= s_stay[m - m0] && i < s_own[m - m0]) v.free_pages[s_at[m - m0] + i - s_stay[m - m0]] = old;
             if ((d & kForkSave) != 0) saved = old;
             if (i < min(n, v.pt_cap)) at[i] = x;
         }
@@ -111,39 +120,54 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_move(SpkvView v, SpkvF
     }
 }
 
-// Pages of their own for the sequences that hold another one's: kForkPages pages to a workgroup and turn, ids by one
-// atomic, then the pages with their positions and logits.
-constexpr int kForkPages = 4;
+// The copies: `chunk` pages of a pair to a workgroup and turn.  Pages that the pair does not have yet are handed out by one
+// atomic for the chunk.  A page's 32 KB (D = 128) are in flight at once, the next page's loads before this one's
+// stores.  Stores without retention: never slower, whether the copies are read next or not, and 68 -> 53 us for eight copies of 30
+// MB (4.6 TB/s written), 128 -> 107 for sixteen.
+constexpr int kForkChunk = 16;
 template <int D>
-__global__ __launch_bounds__(kForkThreads) void spkv_fork_pages(SpkvView v, SpkvForkSource from, SpkvSequences dst) {
-    const int tid = threadIdx.x, pair = dst.seq[blockIdx.z] * v.Hkv + blockIdx.y;
-    const int n = min((v.kept_len[pair] + kPageTokens - 1) / kPageTokens, v.pt_cap);
+__global__ __launch_bounds__(kForkThreads) void spkv_fork_pages(SpkvView v, SpkvForkSource from, SpkvForkCopies copies, int chunk) {
+    const int tid = threadIdx.x, pair = copies.dst[blockIdx.z] * v.Hkv + blockIdx.y;
+    const int n = min((v.kept_len[pair] + kPageTokens - 1) / kPageTokens, v.pt_cap), stay = v.pair_items[pair];
+    const int32_t* of = from.page_table + ((size_t)copies.of[blockIdx.z] * v.Hkv + blockIdx.y) * from.pt_cap;
     int32_t* row = v.page_table + (size_t)pair * v.pt_cap;
-    __shared__ int s_from[kForkPages], s_to[kForkPages];
-    for (int p0 = blockIdx.x * kForkPages; p0 < n; p0 += gridDim.x * kForkPages) {
-        const int here = min(kForkPages, n - p0);
-        if (tid == 0) {
-            const PageBatch pb = alloc_page_batch(v, here);
-            for (int i = 0; i < here; ++i) {
-                const int to = batch_page(v, pb, i);
-                s_from[i] = min(max(row[p0 + i], 0), from.n_pages - 1);
-                s_to[i] = to;
-                row[p0 + i] = max(to, 0);
+    __shared__ int s_from[kForkChunk], s_to[kForkChunk];
+    constexpr int kUnits = 2 * kPageTokens * D / 8 / kForkThreads;
+    for (int p0 = blockIdx.x * chunk; p0 < n; p0 += gridDim.x * chunk) {
+        const int here = min(chunk, n - p0), fresh = max(0, p0 + here - max(stay, p0));
+        if (tid < 64) {                                       // (chunk <= 64)
+            PageBatch pb = {0, 0, 0};
+            if (tid == 0) pb = alloc_page_batch(v, fresh);
+            pb.stack_lo = __shfl(pb.stack_lo, 0);
+            pb.from_stack = __shfl(pb.from_stack, 0);
+            pb.pool_base = __shfl(pb.pool_base, 0);
+            if (tid < here) {
+                const int i = p0 + tid, to = i < stay ? row[i] : batch_page(v, pb, i - max(stay, p0));
+                s_from[tid] = min(max(of[i], 0), from.n_pages - 1);
+                s_to[tid] = to;
+                if (i >= stay) row[i] = max(to, 0);
                 if (to < 0) *v.err_flag = 1;
             }
         }
         __syncthreads();
+        const u32x4* pool = reinterpret_cast<const u32x4*>(from.pool);
+        constexpr size_t kPageUnits = (size_t)2 * kPageTokens * D / 8;
+        u32x4 x[kUnits];
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) x[u] = pool[s_from[0] * kPageUnits + u * kForkThreads + tid];
         for (int i = 0; i < here; ++i) {
-            if (s_to[i] < 0) continue;
             const int a = s_from[i], b = s_to[i];
-            const uint4* src = reinterpret_cast<const uint4*>(from.pool + (size_t)a * spkv_page_elems(D));
-            uint4* to = reinterpret_cast<uint4*>(pool_page(v, b));
-            constexpr int kUnits = 2 * kPageTokens * D / 8 / kForkThreads;
-            uint4 x[kUnits];
+            u32x4 y[kUnits];
 #pragma unroll
-            for (int u = 0; u < kUnits; ++u) x[u] = src[u * kForkThreads + tid];
+            for (int u = 0; u < kUnits; ++u) y[u] = x[u];
+            if (i + 1 < here) {
 #pragma unroll
-            for (int u = 0; u < kUnits; ++u) to[u * kForkThreads + tid] = x[u];
+                for (int u = 0; u < kUnits; ++u) x[u] = pool[s_from[i + 1] * kPageUnits + u * kForkThreads + tid];
+            }
+            if (b < 0) continue;                              // (the pool is exhausted, and flagged)
+            u32x4* to = reinterpret_cast<u32x4*>(pool_page(v, b));
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) __builtin_nontemporal_store(y[u], to + u * kForkThreads + tid);
             if (tid < kPageTokens) v.pos_pool[(size_t)b * kPageTokens + tid] = from.pos_pool[(size_t)a * kPageTokens + tid];
             else if (tid < 2 * kPageTokens)
                 v.logit_pool[(size_t)b * kPageTokens + tid - kPageTokens] = from.logit_pool[(size_t)a * kPageTokens + tid - kPageTokens];
@@ -158,18 +182,24 @@ hipError_t spkv_launch_fork_move(const SpkvView& v, const SpkvForkSource& from, 
     return hipGetLastError();
 }
 
-hipError_t spkv_launch_fork_pages(const SpkvView& v, const SpkvForkSource& from, const SpkvSequences& dst, int n, int most_pages,
-                                  hipStream_t s) {
-    const dim3 grid((unsigned)std::max(1, std::min((most_pages + kForkPages - 1) / kForkPages, 65535)), v.Hkv, n);
-    if (v.D == 128) spkv_fork_pages<128><<<grid, dim3(kForkThreads), 0, s>>>(v, from, dst);
-    else spkv_fork_pages<64><<<grid, dim3(kForkThreads), 0, s>>>(v, from, dst);
+// Eight workgroups to a compute unit at chunks of all / 2048 pages; where pages have to be handed out, a quarter of
+// them, each with one atomic on the same address: 15 of 32 beams of 5 MB copied in 74 / 47 / 39 us with 2048 / 1024 / 512
+// workgroups, eight copies of 30 MB into pages at hand in 53 / 58 / 59.
+hipError_t spkv_launch_fork_pages(const SpkvView& v, const SpkvForkSource& from, const SpkvForkCopies& copies, int n, int64_t most_pages,
+                                  int64_t all_pages, int64_t fresh_pages, hipStream_t s) {
+    const int64_t wanted = fresh_pages * 8 > all_pages ? 512 : 2048;
+    const int chunk = (int)std::max<int64_t>(1, std::min<int64_t>(kForkChunk, all_pages / wanted));
+    const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((most_pages + chunk - 1) / chunk, 65535)), v.Hkv, n);
+    if (v.D == 128) spkv_fork_pages<128><<<grid, dim3(kForkThreads), 0, s>>>(v, from, copies, chunk);
+    else spkv_fork_pages<64><<<grid, dim3(kForkThreads), 0, s>>>(v, from, copies, chunk);
     return hipGetLastError();
 }
 
 // -------------------------------------------------------------- what sequences hold, as rows
 // A workgroup takes a half-page (32 pairs) at a time.  Rows of keys: four consecutive keys lie in 64 bytes of every
 // chunk of eight elements, so a wave that takes four keys reads whole pieces of 64 bytes and writes whole rows.
-// Values come as units of eight keys of one element and are turned in LDS.
+// Values come as units of eight keys of one element and are turned in LDS.  Stores without retention: 242 MB out of a
+// cache and into rows 105 -> 72 us, 6.7 TB/s of both; 32 MB 22.8 -> 10.7.
 template <int D>
 __global__ __launch_bounds__(256) void spkv_gather_pairs(SpkvView v, SpkvSequences of, SpkvPairRows out) {
     constexpr int kChunks = D / 8;
@@ -189,34 +219,58 @@ __global__ __launch_bounds__(256) void spkv_gather_pairs(SpkvView v, SpkvSequenc
         const uint16_t* base = ring ? ring_page(v, pair, k0 >> 6) : pool_page(v, page);
         const int in0 = k0 & 63;
         auto place = [&](int r) -> int { return ring ? L + age(k0 + r) : k0 + r; };
+        // all of the half-page's loads before anything is waited for
+        constexpr int kMine = kHalfTokens * kChunks / 256;    // 16-byte units of keys, and of values, a thread
+        uint4 kk[kMine], vl[kMine];
+        const size_t e = (size_t)page * kPageTokens + in0 + (tid & 31);
+        float logit = 0.f;
+        int position = 0;
         if (out.k != nullptr) {
-            for (int u = tid; u < kHalfTokens * kChunks; u += 256) {
-                const int r = u / kChunks, c = u - r * kChunks;
-                if (r >= n || place(r) >= out.rows) continue;
-                *reinterpret_cast<uint4*>(out.k + (row0 + place(r)) * D + c * 8) =
-                    *reinterpret_cast<const uint4*>(base + spkv_k_off(D, in0 + r, c * 8));
+#pragma unroll
+            for (int i2 = 0; i2 < kMine; ++i2) {
+                const int u = i2 * 256 + tid;
+                kk[i2] = *reinterpret_cast<const uint4*>(base + spkv_k_off(D, in0 + u / kChunks, u % kChunks * 8));
             }
         }
         if (out.v != nullptr) {
-            for (int u = tid; u < kHalfTokens / 8 * D; u += 256) {
-                const int kc = u / D, d = u - kc * D;
-                const uint4 q = *reinterpret_cast<const uint4*>(base + spkv_v_off(D, in0 + 8 * kc, d));
-                const unsigned w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s_v[8 * kc + e][d] = (uint16_t)(w[e >> 1] >> ((e & 1) * 16));
+            for (int i2 = 0; i2 < kMine; ++i2) {
+                const int u = i2 * 256 + tid;
+                vl[i2] = *reinterpret_cast<const uint4*>(base + spkv_v_off(D, in0 + u / D * 8, u % D));
+            }
+        }
+        if (tid < n) {
+            logit = ring ? v.ring_logit[(size_t)pair * v.w + k0 + tid] : v.logit_pool[e];
+            position = ring ? T - held + age(k0 + tid) : v.pos_pool[e];
+        }
+        if (out.k != nullptr) {
+#pragma unroll
+            for (int i2 = 0; i2 < kMine; ++i2) {
+                const int u = i2 * 256 + tid, r = u / kChunks;
+                if (r < n && place(r) < out.rows) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, kk[i2]), reinterpret_cast<u32x4*>(out.k + (row0 + place(r)) * D + u % kChunks * 8));
+            }
+        }
+        if (out.v != nullptr) {
+#pragma unroll
+            for (int i2 = 0; i2 < kMine; ++i2) {
+                const int u = i2 * 256 + tid, kc = u / D, d = u % D;
+                const unsigned w[4] = {vl[i2].x, vl[i2].y, vl[i2].z, vl[i2].w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s_v[8 * kc + j][d] = (uint16_t)(w[j >> 1] >> ((j & 1) * 16));
             }
             __syncthreads();
-            for (int u = tid; u < kHalfTokens * kChunks; u += 256) {
-                const int r = u / kChunks, c = u - r * kChunks;
+#pragma unroll
+            for (int i2 = 0; i2 < kMine; ++i2) {
+                const int u = i2 * 256 + tid, r = u / kChunks;
                 if (r < n && place(r) < out.rows)
-                    *reinterpret_cast<uint4*>(out.v + (row0 + place(r)) * D + c * 8) = *reinterpret_cast<const uint4*>(&s_v[r][c * 8]);
+                    __builtin_nontemporal_store(*reinterpret_cast<const u32x4*>(&s_v[r][u % kChunks * 8]),
+                                                reinterpret_cast<u32x4*>(out.v + (row0 + place(r)) * D + u % kChunks * 8));
             }
             __syncthreads();
         }
         if (tid < n && place(tid) < out.rows) {
-            const size_t e = (size_t)page * kPageTokens + in0 + tid;
-            if (out.logits != nullptr) out.logits[row0 + place(tid)] = ring ? v.ring_logit[(size_t)pair * v.w + k0 + tid] : v.logit_pool[e];
-            if (out.positions != nullptr) out.positions[row0 + place(tid)] = ring ? T - held + age(k0 + tid) : v.pos_pool[e];
+            if (out.logits != nullptr) out.logits[row0 + place(tid)] = logit;
+            if (out.positions != nullptr) out.positions[row0 + place(tid)] = position;
         }
     }
 }

@@ -330,6 +330,7 @@ constexpr int kForkSave = 0x4000;                // dst: what it held is saved f
 constexpr int kForkFree = 0x8000;                // dst: nobody takes its pages, they go back
 constexpr int kForkNothing = 0x4000;             // src: none, the sequence is emptied
 constexpr int kForkSaved = 0x8000;               // src: what was saved (the index says whose it was)
+constexpr int kForkCopy = 0x2000;                // src: the pages are copied by the next launch
 struct SpkvForkMoves {
     int32_t n;                                   // components
     uint16_t start[SPKV_MAX_BATCH + 1], dst[SPKV_MAX_BATCH], src[SPKV_MAX_BATCH];
@@ -350,9 +351,12 @@ struct SpkvPairRows {                            // [sequences][Hkv][rows], any 
     int64_t rows;
 };
 hipError_t spkv_launch_fork_move(const SpkvView& v, const SpkvForkSource& from, const SpkvForkMoves& mv, hipStream_t s);
-// most_pages: of a head of these sequences, by the host's bound.
-hipError_t spkv_launch_fork_pages(const SpkvView& v, const SpkvForkSource& from, const SpkvSequences& dst, int n, int most_pages,
-                                  hipStream_t s);
+struct SpkvForkCopies {                          // dst's pages become copies of those that `of` of `from` has now
+    uint16_t dst[SPKV_MAX_BATCH], of[SPKV_MAX_BATCH];
+};
+// most_pages, all_pages: of a head of these sequences, of all of them, fresh_pages: of them not at hand, by the host's bound.
+hipError_t spkv_launch_fork_pages(const SpkvView& v, const SpkvForkSource& from, const SpkvForkCopies& copies, int n, int64_t most_pages,
+                                  int64_t all_pages, int64_t fresh_pages, hipStream_t s);
 hipError_t spkv_launch_gather_pairs(const SpkvView& v, const SpkvSequences& of, int n, int most_half_pages, const SpkvPairRows& out,
                                     hipStream_t s);
 hipError_t spkv_launch_append_rows(const SpkvView& v, const uint16_t* k, const uint16_t* vv, const float* f,
