@@ -1972,10 +1972,18 @@ int spkv_decode_attention_shared(spkv_cache_t* c, spkv_cache_t* pc, const int32_
 }
 
 namespace {
-// Ranges of the lists of a launch (pairs tree->pair0 .. + n_pairs - 1): about as many workgroups as the chip holds at
-// once, every list cut evenly into its share of them; a half-page of the ring counts twice (ShareList::begin).
-constexpr int kTreeMinUnit = 2, kTreeStart = 16;
-int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, int width, int64_t fit, SpkvTree* tree, SpkvTreeTable* table) {
+// Ranges of the lists of a launch (pairs tree->pair0 .. + n_pairs - 1), every list cut evenly; a half-page of the ring counts
+// twice (ShareList::begin).  As many ranges as k workgroups for every compute unit, k from 1 to 4: by what the longest takes with
+// its start, what all of them take shared among the workgroups that the chip holds at once, a rest at the end, and the join
+// of a list's ranges.  The longest ranges begin first: what is left for the last ones is short.  us, 32 heads over 8 of 128, in
+// the lists' order / longest first: 64 sequences of 1k-16k, 12 drafts 134 / 105, 64 drafts 319 / 217; 16 of 32k, 64 drafts 180 / 166;
+// with k fixed at 1, 2, 3, 4: 16 of 32k, 4 drafts 89 85 88 90, 32 drafts 138 122 132 132, 64 of 1k-16k, 4 drafts 100 101 92 89,
+// 32 drafts 175 175 153 154, one of 128k, 4 drafts 26 28 33 35.
+constexpr int kTreeMinUnit = 2, kTreeStart = 16, kTreeStartAlone = 24;
+// k above 1 has to leave ranges of so many half-pages: 32 of 500 tokens, 16 drafts 28 / 23 us, 64 short lists' 18 MB, 32 drafts 32 / 24.5.
+constexpr int kTreeMinUnitMore = 20;
+int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, SpkvTreeKernel kernel, int64_t fit, SpkvTree* tree, SpkvTreeTable* table) {
+    const int width = spkv_tree_width(kernel);
     const int Hkv = c->cfg.n_kv_heads, G = c->carve.G;
     int32_t hp[kTreePairs], copies[kTreePairs];
     int64_t work = 0, lists = 0;
@@ -1987,39 +1995,54 @@ int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, int width, int
         lists += copies[i];
     }
     const int cus = spkv_compute_units();
-    const int64_t round = cus > 0 ? cus : 256;
+    const int64_t round = cus > 0 ? cus : 256, resident = round * spkv_tree_resident(kernel);
+    const int64_t start = spkv_tree_resident(kernel) == 1 ? kTreeStartAlone : kTreeStart;
     int64_t unit = 0, best = 0;
-    for (int k = 1; k <= 2; ++k) {
+    for (int k = 1; k <= 4; ++k) {
         const int64_t target = std::min(fit, (int64_t)k * round);
-        int64_t u = std::max<int64_t>(kTreeMinUnit, (work + target - 1) / target), total = 0, longest = 0;
+        int64_t u = std::max<int64_t>(k > 1 ? kTreeMinUnitMore : kTreeMinUnit, (work + target - 1) / target), total = 0, longest = 0, most = 0;
         for (int guard = 0; guard < 64; ++guard) {
-            total = longest = 0;
+            total = longest = most = 0;
             for (int i = 0; i < n_pairs; ++i) {
+                if (copies[i] == 0) continue;
                 const int64_t r = std::min<int64_t>(255, std::max<int64_t>(1, (hp[i] + u - 1) / u));
                 total += r * copies[i];
                 longest = std::max(longest, (hp[i] + r - 1) / r);
+                most = std::max(most, r);
             }
             if (total <= target || total <= lists) break;
             u += std::max<int64_t>(1, u / 16);
         }
-        const int64_t time = (total + round - 1) / round * (longest + kTreeStart);
+        const int64_t time = std::max(longest + start, (work + total * start) / resident + (total > resident ? work / (2 * total) : 0)) + most / 2;
         if (k > 1 && time >= best) continue;
         best = time;
         unit = total > fit ? (int64_t)1 << 40 : u;           // (no room for ranges: one each)
     }
+    // The longest ranges begin first.
+    uint16_t order[kTreePairs];
+    int32_t size[kTreePairs];
+    for (int i = 0; i < n_pairs; ++i) {
+        const int64_t r = std::min<int64_t>(255, std::max<int64_t>(1, (hp[i] + unit - 1) / unit));
+        order[i] = (uint16_t)i;
+        size[i] = (int32_t)((hp[i] + r - 1) / r);
+    }
+    std::sort(order, order + n_pairs, [&](uint16_t x, uint16_t y) { return size[x] != size[y] ? size[x] > size[y] : x < y; });
     int64_t end = 0;
     int most = 1;
     for (int i = 0; i < kTreePairs; ++i) {
         if (i >= n_pairs) {
             table->end[i] = 65535;
             table->ranges[i] = 1;
+            table->pair[i] = 0;
             continue;
         }
-        const int64_t r = std::min<int64_t>(255, std::max<int64_t>(1, (hp[i] + unit - 1) / unit));
+        const int p = order[i];
+        const int64_t r = std::min<int64_t>(255, std::max<int64_t>(1, (hp[p] + unit - 1) / unit));
         most = std::max(most, (int)r);
-        end += r * copies[i];
+        end += r * copies[p];
         table->end[i] = (uint16_t)end;
         table->ranges[i] = (uint8_t)r;
+        table->pair[i] = (uint16_t)p;
     }
     tree->n_units = (int32_t)end;
     return most;
@@ -2052,7 +2075,11 @@ int spkv_score_tree(spkv_cache_t* c, const void* k, const void* v, const float* 
         return SPKV_E_NOMEM;
     }
     tighten_bound(c, s);
-    const int width = spkv_tree_width(n_max * G);
+    int64_t half_pages = 0;
+    for (int p = 0; p < c->carve.n_pairs; ++p)
+        if (cu_seqlens[p / Hkv + 1] > cu_seqlens[p / Hkv]) half_pages += (c->L_ub[p] + kHalfTokens - 1) / kHalfTokens;
+    const SpkvTreeKernel kernel = spkv_tree_kernel(n_max * G, half_pages);
+    const int width = spkv_tree_width(kernel);
     SpkvTree tree = {};
     tree.k = static_cast<const uint16_t*>(k);
     tree.v = static_cast<const uint16_t*>(v);
@@ -2074,10 +2101,10 @@ int spkv_score_tree(spkv_cache_t* c, const void* k, const void* v, const float* 
         const int seqs = (p0 + n_pairs - 1) / Hkv - tree.seq0 + 1;
         if (cu_seqlens[tree.seq0 + seqs] == tree.row0) continue;
         for (int i = 0; i <= seqs; ++i) table.cu[i] = (uint16_t)(cu_seqlens[tree.seq0 + i] - tree.row0);
-        tree.n_own = n_pairs * tree.n_blocks;
-        const int most = tree_cut(c, cu_seqlens, n_pairs, width, std::min<int64_t>(slots - tree.n_own, 32767), &tree, &table);
+        tree.n_own = kernel == kTreeOwnCopies ? 0 : n_pairs * tree.n_blocks;
+        const int most = tree_cut(c, cu_seqlens, n_pairs, kernel, std::min<int64_t>(slots - tree.n_own, 32767), &tree, &table);
         if (tree.n_units + tree.n_own > slots) return SPKV_E_CAPACITY;
-        if (spkv_launch_tree(c->view, static_cast<const uint16_t*>(q), sm_scale, width, tree, table, n_pairs, n_max * G, most,
+        if (spkv_launch_tree(c->view, static_cast<const uint16_t*>(q), sm_scale, kernel, tree, table, n_pairs, n_max * G, most,
                              static_cast<uint16_t*>(out), lse, s) != hipSuccess)
             return SPKV_E_HIP;
     }

@@ -164,6 +164,13 @@ __device__ __forceinline__ void load_row_to_lds(const char* base, unsigned voff,
                  : "m0");
 }
 
+__device__ __forceinline__ void load_row_to_lds_once(const char* base, unsigned voff, unsigned lds_row) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+                 :
+                 : "v"(voff), "s"(base), "s"(lds_row)
+                 : "m0");
+}
+
 // Waits until at most N of this wave's vector memory loads are still in flight (they
 // complete in the order issued).
 template <int N>

@@ -370,17 +370,22 @@ struct SpkvTree {
     const float* f;              // null: every path fits the window
     const int32_t* parents;
     int32_t pair0, seq0, row0;
-    int32_t n_own;               // units of the drafts themselves: a pair's blocks of columns
+    int32_t n_own;               // units of the drafts themselves, a pair's blocks of columns, behind those of the lists; 0: the first range takes them
     int32_t n_blocks;            // ... of the pair with the most columns
     int32_t n_units;             // units of the lists
 };
 struct SpkvTreeTable {
-    alignas(16) uint16_t end[kTreePairs];        // units of the lists up to and with each pair's; pairs that are not there: 65535
+    alignas(16) uint16_t end[kTreePairs];        // units of the lists, up to and with each, in the order they are begun; not there: 65535
+    uint16_t pair[kTreePairs];                   // the pair of each, from pair0 on
     uint16_t cu[kTreePairs + 1];                 // rows from row0 on
-    uint8_t ranges[kTreePairs];
+    uint8_t ranges[kTreePairs];                  // of each
 };
-int spkv_tree_width(int n_cols);         // columns of a workgroup, for the pair with the most
-int spkv_tree_waves(int width);
-hipError_t spkv_launch_tree(const SpkvView& v, const uint16_t* q, float sm_scale, int width, const SpkvTree& tree,
+// Kernels by the columns of the pair with the most: 16 or 32 (spkv_tree_few), 64 (spkv_tree_own_copies, or spkv_tree_split
+// where the lists are short), 128, 256 to a workgroup.
+enum SpkvTreeKernel { kTreeFew16, kTreeFew32, kTreeOwnCopies, kTreeSplit64, kTreeSplit128, kTreeSplit256 };
+SpkvTreeKernel spkv_tree_kernel(int n_cols, int64_t half_pages);
+int spkv_tree_width(SpkvTreeKernel kernel);       // columns of a workgroup
+int spkv_tree_resident(SpkvTreeKernel kernel);    // workgroups that a compute unit holds
+hipError_t spkv_launch_tree(const SpkvView& v, const uint16_t* q, float sm_scale, SpkvTreeKernel kernel, const SpkvTree& tree,
                             const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, uint16_t* out, float* lse,
                             hipStream_t s);

@@ -1,4 +1,6 @@
 // Attention of trees of drafted tokens over the cache on gfx950.
+#include <type_traits>
+
 #include "spkv_lists.h"
 
 // The mathematics.  Draft i of a sequence that holds T tokens hangs behind draft parent(i) < i or behind the newest
@@ -12,8 +14,10 @@
 // A lane of a wave stands for a draft: paths are words of bits, joined along the parents by doubling (log2 of the deepest
 // path's length rounds of three lane exchanges), depths their counts of bits.
 //
-// Bound: the lists are read once, 4 D bytes a key for 4 D flops a key and column: past about 300 columns a list the matrix
-// units, below the read; few columns or short lists by the start of a workgroup and the join.
+// Bound: the lists are read once, 4 D bytes a key for 4 D flops a key and column: past about 180 columns a list the matrix
+// units, below the read; few columns or short lists by the start of a workgroup and the join.  Measured, 16 sequences of 32k tokens
+// (484 MB, 32 heads over 8 of 128), a call: 4 drafts 83 us (5.9 TB/s), 8: 94, 16: 98, 32: 124, 64: 170 (2.9 TB/s, 0.73 PF/s); one
+// sequence of 128k, 16 drafts 37; of 2k, 14.
 
 // ------------------------------------------------------------------------------- paths
 struct TreePath {
@@ -62,8 +66,8 @@ __device__ __forceinline__ unsigned long long tree_seen(const SpkvView& v, const
 }
 
 // ---------------------------------------------------------------------------- the work
-// Workgroup id -> unit: the drafts of every pair's blocks of columns first, then the ranges of the lists, by the host's
-// table, the ranges of a pair's block of columns next to each other.
+// Workgroup id -> unit: the ranges of the lists, by the host's table, the ranges of a pair's block of columns next to each
+// other, then the drafts of every pair's blocks of columns (short units, beside the last ranges).
 struct TreeWork {
     const SpkvTree& tree;
     const SpkvTreeTable& table;
@@ -71,14 +75,13 @@ struct TreeWork {
     __device__ __forceinline__ TreeWork(const SpkvView& v, const SpkvTree& t, const SpkvTreeTable& tab, int id, int w)
         : tree(t), table(tab), width(w) {
         int local;
-        if (id < t.n_own) {
-            local = id / t.n_blocks;
-            block = id - local * t.n_blocks;
+        if (id >= t.n_units) {
+            local = (id - t.n_units) / t.n_blocks;
+            block = id - t.n_units - local * t.n_blocks;
             range = -1;
             ranges = 1;
-            unit = t.n_units + id;
+            unit = id;
         } else {
-            id -= t.n_own;
             const uint4 raw = reinterpret_cast<const uint4*>(tab.end)[threadIdx.x & 63];      // eight pairs a lane
             const unsigned e[4] = {raw.x, raw.y, raw.z, raw.w};
             local = 0;
@@ -93,7 +96,7 @@ struct TreeWork {
             range = id - start - block * ranges;
             unit = id;
         }
-        pair = t.pair0 + local;
+        pair = t.pair0 + tab.pair[local];
         const int b = pair / v.Hkv, at = b - t.seq0;
         h = pair - b * v.Hkv;
         row0 = t.row0 + tab.cu[at];
@@ -118,7 +121,7 @@ struct TreeWork {
 // does not see has reached it (a weight of zero times it).  The whole wave.
 template <int D>
 __device__ __attribute__((noinline)) void careful_tree_sums(const uint16_t* k, const uint16_t* vv, int stride, const uint16_t* qrow,
-                                                            unsigned long long seen, float scale_log2e, float m, float* sums) {
+                                                            unsigned long long seen, float scale_log2e, float m, bool add, float* sums) {
     const int lane = threadIdx.x & 63;
     float q[D / 64], acc[D / 64];
 #pragma unroll
@@ -138,7 +141,18 @@ __device__ __attribute__((noinline)) void careful_tree_sums(const uint16_t* k, c
         for (int e = 0; e < D / 64; ++e) acc[e] += p * bf16_at(vv + at + e * 64 + lane);
     }
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) sums[e * 64 + lane] = acc[e];
+    for (int e = 0; e < D / 64; ++e) sums[e * 64 + lane] = acc[e] + (add ? sums[e * 64 + lane] : 0.f);
+}
+// Is there a value that is not finite, in a draft that others need not see?  (The whole wave.)
+template <int D>
+__device__ __attribute__((noinline)) bool careful_tree_needed(const uint16_t* vv, int stride, int n) {
+    bool odd = false;
+    for (int i = 0; n > 1 && i < n; ++i)
+        for (int d = threadIdx.x & 63; d < D; d += 64) {
+            const float x = bf16_at(vv + (size_t)i * stride + d);
+            odd = odd || !(x - x == 0.f);
+        }
+    return __ballot(odd) != 0ull;
 }
 
 // The drafts as keys, up to 16 NQ columns (so at most 32 drafts: one half-page): every wave has all scores and a
@@ -239,7 +253,7 @@ __device__ __forceinline__ void attend_drafts_few(const SpkvView& v, const uint1
                 for (int x0 = 0; x0 < 16 && i * 16 + x0 < n_cols; ++x0) {
                     const int cc = i * 16 + x0, dd = cc / v.G;
                     careful_tree_sums<D>(kr, vr, stride, q + ((size_t)(work.row0 + dd) * v.Hq + (size_t)h * v.G + (cc - dd * v.G)) * D,
-                                         lane_word(word, dd), scale_log2e, __shfl(ref, x0), v.part_acc + (pc0 + cc) * D);
+                                         lane_word(word, dd), scale_log2e, __shfl(ref, x0), false, v.part_acc + (pc0 + cc) * D);
                 }
         }
     }
@@ -338,8 +352,353 @@ __device__ __forceinline__ void attend_drafts_split(const SpkvView& v, const uin
         for (int i = 0; i < n_here; ++i) {
             const int cc = col0 + wv * 32 + i, dd = cc / v.G;
             careful_tree_sums<D>(kr, vr, stride, q + ((size_t)(work.row0 + dd) * v.Hq + (size_t)h * v.G + (cc - dd * v.G)) * D,
-                                 lane_word(word, dd), scale_log2e, __shfl(ref, i), to + (size_t)i * D);
+                                 lane_word(word, dd), scale_log2e, __shfl(ref, i), false, to + (size_t)i * D);
         }
+    }
+}
+
+constexpr int kDraftWeight = 3;
+// 33 to 64 columns: every wave has all of them, two groups of MFMA 32x32x16, and an eighth of the workgroup's range to
+// itself.  Its half-pages go from memory into 16 KB of LDS of its own (D = 128) in operand order, keys and values in turn: while
+// the scores are weighed the next keys arrive, while these are multiplied the next values.  No wave waits for another.
+// Read once, the half-pages are loaded as such (nt: 484 MB in 98 us, 114 without; 94 MB that the caches hold 30, 29 without).
+// The queries are shared, in LDS.  The drafts are up to two half-pages more for one wave of the list's first range.
+template <int D>
+__device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e, const TreeWork& work) {
+    constexpr int NS = D / 16, NB = D / 32, kRow = D + 4, kHalfElems = 2 * kHalfTokens * D;
+    __shared__ __attribute__((aligned(16))) uint16_t s_q[2 * NS * 512];
+    __shared__ __attribute__((aligned(16))) float s_acc[4][64 * kRow];         // (half-pages before)
+    __shared__ float2 s_ml[4][64];
+    static_assert(sizeof(s_acc) >= (size_t)8 * kHalfElems * 2, "the half-pages' room");
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int pair = work.pair, h = work.h, n = work.n;
+    const FirstPages first_ids = first_pages(v, pair);
+    const ShareList list = share_list(v, pair);
+    const int n_cols = work.columns(v), c0 = work.block * 64;
+    if (c0 >= n_cols) return;
+    const int tiles = (n + kHalfTokens - 1) >> 5, nA = list.nA;
+    auto cut = [&](int j) -> int {                            // the drafts count kDraftWeight half-pages each, in the first range
+        const int x = (int)((int64_t)j * (2 * list.n_hp - nA + kDraftWeight * tiles) / work.ranges) - kDraftWeight * tiles;
+        return x <= 0 ? 0 : x <= nA ? x : nA + (x - nA + 1) / 2;
+    };
+    const int r_begin = cut(work.range), r_end = work.range + 1 == work.ranges ? list.n_hp : cut(work.range + 1);
+    const int x_begin = r_begin + (r_end - r_begin) * wv / 8, x_end = r_begin + (r_end - r_begin) * (wv + 1) / 8;
+    const bool ring = x_end > nA;
+    SharePages pages = share_pages(v, pair, first_ids, x_begin >> 1);
+
+    const unsigned k_lane = ((((col >> 3) & 1) * (D / 8) + half) * 16 + 8 * (col >> 4) + 4 * ((col >> 2) & 1) + (col & 3)) * 16;
+    const unsigned v_lane = (((col >> 4) * 4 + half) * 16 + (col & 15)) * 16 + kHalfTokens * D * 2;
+    uint16_t* const slot = reinterpret_cast<uint16_t*>(&s_acc[0][0]) + wv * kHalfElems;
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)slot;
+    auto page_of = [&](int x) -> const char* { return reinterpret_cast<const char*>(half_page_at(v, list, pages, x)); };
+    auto send_k = [&](const char* base) {
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) load_row_to_lds_once(base + sl * 512, k_lane, lds0 + sl * 1024);
+    };
+    auto send_v = [&](const char* base) {
+#pragma unroll
+        for (int j = 0; j < 2 * NB; ++j) load_row_to_lds_once(base + (j / NB) * 512 + (j % NB) * 2048, v_lane, lds0 + (NS + j) * 1024);
+    };
+    // Loads into LDS and reads of it: the compiler does not know that they belong together.
+    auto read_all = [&]() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); };           // what was read has arrived
+    const char* base = nullptr;
+    if (x_begin < x_end) {
+        base = page_of(x_begin);
+        send_k(base);
+        send_v(base);
+    }
+    int place[2], draft[2], least = 0, most = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = c0 + i * 32 + col;
+        const ShareRow sr = work.row(v, c < n_cols ? c : 0, ring);
+        place[i] = sr.place;
+        draft[i] = sr.row - work.row0;
+        const uint16_t* qrow = q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D + half * 8;
+        if ((wv & 1) == i && wv < 4) {
+#pragma unroll
+            for (int j = 0; j < NS / 2; ++j) {
+                const int sl = (wv >> 1) * (NS / 2) + j;
+                *reinterpret_cast<bf16x8*>(&s_q[(i * NS + sl) * 512 + lane * 8]) = *reinterpret_cast<const bf16x8*>(qrow + sl * 16);
+            }
+        }
+    }
+    RingGates gates = {0, 0u};
+    if (ring) {
+        gates = ring_gates(v, list, x_begin, x_end);
+        least = min(place[0], place[1]);
+        most = max(place[0], place[1]);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            least = min(least, __shfl_xor(least, o));
+            most = max(most, __shfl_xor(most, o));
+        }
+        least = __builtin_amdgcn_readfirstlane(least);
+        most = __builtin_amdgcn_readfirstlane(most);
+    }
+    __syncthreads();
+    f32x16 acc[2][NB];
+    float m[2], l[2], neg_ref[2], limit[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        m[i] = SPKV_NEG_INF;
+        l[i] = neg_ref[i] = 0.f;
+        limit[i] = -1.f;
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][db][e] = 0.f;
+    }
+    f32x16 s[2];
+    auto scores = [&]() {
+        f32x16 zero;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+#pragma unroll
+        for (int sl = 0; sl < NS; ++sl) {
+            const bf16x8 key = *reinterpret_cast<const bf16x8*>(slot + sl * 512 + lane * 8);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key, *reinterpret_cast<const bf16x8*>(&s_q[(i * NS + sl) * 512 + lane * 8]),
+                                                               sl == 0 ? zero : s[i], 0, 0, 0);
+        }
+    };
+    // weights of group i against its reference as it stands; where one is too low or not set, it is raised first
+    bf16x8 pb[2][2];
+    auto weigh = [&](int i) {
+        float psum;
+        auto weights = [&]() -> bool {
+            f32x8 p[2];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e >> 3][e & 7] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], scale_log2e, neg_ref[i]));
+            float s4[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s4[e] = (p[0][e] + p[0][4 + e]) + (p[1][e] + p[1][4 + e]);
+            psum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            pb[i][0] = __builtin_convertvector(p[0], bf16x8);
+            pb[i][1] = __builtin_convertvector(p[1], bf16x8);
+            return __builtin_amdgcn_ballot_w64(!(psum <= limit[i])) != 0ull;
+        };
+        if (__builtin_expect(weights(), 0)) {
+            float cm = s[i][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) cm = fmaxf(cm, s[i][e]);
+            cm *= scale_log2e;
+            cm = fmaxf(cm, __shfl_xor(cm, 32));
+            const float m_new = fmaxf(m[i], cm);
+            const bool unset = m_new == SPKV_NEG_INF;         // every key so far excluded
+            const float m_ref = unset ? 0.f : m_new, alpha = __builtin_amdgcn_exp2f(m[i] - m_ref);
+            l[i] *= alpha;
+#pragma unroll
+            for (int db = 0; db < NB; ++db) acc[i][db] *= alpha;
+            m[i] = m_new;
+            neg_ref[i] = -m_ref;
+            limit[i] = unset ? -1.f : kSumLimit;
+            (void)weights();
+        }
+        l[i] += psum;
+    };
+    auto accumulate = [&](unsigned seen) {                    // seen: keys that some column sees, 16 of the lane's half
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int db = 0; db < NB; ++db) {
+                bf16x8 val = *reinterpret_cast<const bf16x8*>(slot + kHalfTokens * D + (g * NB + db) * 512 + lane * 8);
+                if (seen != 0xffffu) val = keep_keys(val, seen >> (8 * g));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[i][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(val, pb[i][g], acc[i][db], 0, 0, 0);
+            }
+    };
+    const int full = min(list.L >> 5, x_end);
+    auto seen_of = [&](int x) -> unsigned {
+        asm volatile("" : "+s"(x));                           // (nothing of this is to be carried along from turn to turn)
+        unsigned seen = 0u;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int k0 = 16 * g + 8 * half, at0 = (x - nA) * kHalfTokens + k0;
+            unsigned ok[2], any;
+            if (x < nA) {
+                ok[0] = ok[1] = any = bits_below(list.L - x * kHalfTokens - k0);
+            } else {
+                const unsigned on = gates_of(v, list, gates, x - nA, k0);
+                ok[0] = ring_seen(v, list, on, at0, place[0]);
+                ok[1] = ring_seen(v, list, on, at0, place[1]);
+                any = ring_seen(v, list, on, at0, least);
+            }
+            seen |= any << (8 * g);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[i][8 * g + e] = ((ok[i] >> e) & 1u) ? s[i][8 * g + e] : SPKV_NEG_INF;
+        }
+        return seen;
+    };
+    // Loads land in the order sent: keys, values, keys, values.
+    auto turn = [&](int x, auto edge) {
+        asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * NB) : "memory");       // the keys are here
+        scores();
+        const bool more = x + 1 < x_end;
+        if (more) base = page_of(x + 1);
+        read_all();
+        if (more) send_k(base);
+        unsigned seen = 0xffffu;
+        if (decltype(edge)::value) seen = seen_of(x);
+        weigh(0);
+        weigh(1);
+        if (more) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NS) : "memory");  // the values are here
+        else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        accumulate(decltype(edge)::value ? seen : 0xffffu);
+        read_all();
+        if (more) send_v(base);
+    };
+    int x = x_begin;
+#pragma unroll 1
+    for (; x < full; ++x) turn(x, std::false_type());
+#pragma unroll 1
+    for (; x < x_end; ++x) turn(x, std::true_type());
+    const bool drafts = work.range == 0 && wv == 0;
+    unsigned long long word = 0ull;
+    const uint16_t* kr = work.tree.k + ((size_t)work.row0 * v.Hkv + h) * D;
+    const uint16_t* vr = work.tree.v + ((size_t)work.row0 * v.Hkv + h) * D;
+    const int stride = v.Hkv * D;
+    if (drafts) {
+        const TreePath path = tree_path(work.tree.parents + work.row0, n);
+        word = tree_seen(v, path, work.tree.f, h, work.row0, n, list.T);
+#pragma unroll 1
+        for (int t = 0; t < tiles; ++t) {                     // a half-page of them into the slot, then as any other
+#pragma unroll 2
+            for (int sl = 0; sl < NS; ++sl) {
+                const int key = 32 * t + 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+                uint4 u = {0u, 0u, 0u, 0u};
+                if (key < n) u = *reinterpret_cast<const uint4*>(kr + (size_t)key * stride + 16 * sl + 8 * half);
+                *reinterpret_cast<uint4*>(slot + sl * 512 + lane * 8) = u;
+            }
+#pragma unroll 2
+            for (int j = 0; j < 2 * NB; ++j) {
+                const int d = 32 * (j % NB) + col, key0 = 32 * t + 16 * (j / NB) + 8 * half;
+                unsigned y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = key0 + e < n ? vr[(size_t)(key0 + e) * stride + d] : 0u;
+                *reinterpret_cast<uint4*>(slot + kHalfTokens * D + j * 512 + lane * 8) =
+                    make_uint4(y[0] | (y[1] << 16), y[2] | (y[3] << 16), y[4] | (y[5] << 16), y[6] | (y[7] << 16));
+            }
+            read_all();
+            scores();
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const unsigned mine = (unsigned)(lane_word(word, draft[i]) >> (32 * t));
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[i][e] = ((mine >> (16 * (e >> 3) + 8 * half + (e & 7))) & 1u) ? s[i][e] : SPKV_NEG_INF;
+            }
+            weigh(0);
+            weigh(1);
+            accumulate(0xffffu);
+            read_all();
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) l[i] += __shfl_xor(l[i], 32);
+    const bool odd = odd_sums(acc[0], NB, l[0]) || odd_sums(acc[1], NB, l[1]);
+    // Sums of one column, worked out again (see careful_sums): into `to`.
+    auto careful = [&](int c, float ref, float* to) {
+        const CarefulRange range = careful_range(v, list, scale_log2e, x_begin, x_end);
+        const ShareRow sr = work.row(v, c0 + c, true);
+        const uint16_t* qrow = q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D;
+        careful_sums<D>(range, qrow, sr.place, ref, to);
+        if (drafts) {
+            __builtin_amdgcn_wave_barrier();
+            careful_tree_sums<D>(kr, vr, stride, qrow, lane_word(word, sr.row - work.row0), scale_log2e, ref, true, to);
+        }
+        read_all();
+    };
+    bool again = false;
+    if (__builtin_expect(__ballot(odd) != 0ull, 0))
+        again = (ring && least != most && careful_needed<D>(careful_range(v, list, scale_log2e, x_begin, x_end), least, most)) ||
+                (drafts && careful_tree_needed<D>(vr, stride, n));
+    // Four waves leave their sums in LDS, the other four add theirs.
+    __syncthreads();                                          // the half-pages are no longer read
+    float* mine = s_acc[wv & 3];
+    auto leave = [&]() {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float* pa = mine + (i * 32 + col) * kRow + half * 4;
+#pragma unroll
+            for (int db = 0; db < NB; ++db)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f32x4*>(pa + db * 32 + g * 8) =
+                        (f32x4){acc[i][db][4 * g], acc[i][db][4 * g + 1], acc[i][db][4 * g + 2], acc[i][db][4 * g + 3]};
+            if (half == 0) s_ml[wv & 3][i * 32 + col] = make_float2(m[i], l[i]);
+        }
+    };
+    const int n_here = min(64, n_cols - c0);
+    if (wv >= 4) {
+        leave();
+        if (__builtin_expect(again, 0)) {
+            read_all();
+            for (int c = 0; c < n_here; ++c) careful(c, s_ml[wv & 3][c].x, mine + c * kRow);
+        }
+    }
+    __syncthreads();
+    if (wv < 4) {
+        if (__builtin_expect(again, 0)) {                     // column by column: what is there, scaled, and the sums worked out again
+#pragma unroll 1
+            for (int c = 0; c < n_here; ++c) {
+                const float my_m = __shfl(c < 32 ? m[0] : m[1], c & 31), my_l = __shfl(c < 32 ? l[0] : l[1], c & 31);
+                const float2 there = s_ml[wv][c];
+                const float top = fmaxf(my_m, there.x), ref = top == SPKV_NEG_INF ? 0.f : top;
+                const float a = __builtin_amdgcn_exp2f(there.x - ref), b = __builtin_amdgcn_exp2f(my_m - ref);
+                float old[D / 64];
+#pragma unroll
+                for (int e = 0; e < D / 64; ++e) old[e] = mine[c * kRow + e * 64 + lane];
+                read_all();
+                careful(c, my_m, mine + c * kRow);
+#pragma unroll
+                for (int e = 0; e < D / 64; ++e) mine[c * kRow + e * 64 + lane] = old[e] * a + mine[c * kRow + e * 64 + lane] * b;
+                if (lane == 0) s_ml[wv][c] = make_float2(top, there.y * a + my_l * b);
+                read_all();
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float2 there = s_ml[wv][i * 32 + col];
+                const float top = fmaxf(m[i], there.x), ref = top == SPKV_NEG_INF ? 0.f : top;
+                const float a = __builtin_amdgcn_exp2f(there.x - ref), b = __builtin_amdgcn_exp2f(m[i] - ref);
+                const float* pa = mine + (i * 32 + col) * kRow + half * 4;
+#pragma unroll
+                for (int db = 0; db < NB; ++db)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x4 y = *reinterpret_cast<const f32x4*>(pa + db * 32 + g * 8);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][db][4 * g + e] = acc[i][db][4 * g + e] * b + y[e] * a;
+                    }
+                l[i] = l[i] * b + there.y * a;
+                m[i] = top;
+            }
+            read_all();
+            leave();
+        }
+    }
+    __syncthreads();
+    const size_t pc0 = work.part0(v);
+    for (int e = tid; e < n_here * (D / 4); e += 512) {
+        const int c = e / (D / 4), d = (e - c * (D / 4)) * 4;
+        float M = SPKV_NEG_INF, sum = 0.f;
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) M = fmaxf(M, s_ml[w][c].x);
+        const float m_ref = M == SPKV_NEG_INF ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float2 ml = s_ml[w][c];
+            const float sc = __builtin_amdgcn_exp2f(ml.x - m_ref);
+            a += *reinterpret_cast<const f32x4*>(s_acc[w] + c * kRow + d) * sc;
+            sum += ml.y * sc;
+        }
+        *reinterpret_cast<f32x4*>(v.part_acc + (pc0 + c0 + c) * D + d) = a;
+        if (d == 0) work.part_ml<D>(v)[pc0 + c0 + c] = make_float2(M, sum);
     }
 }
 
@@ -360,6 +719,13 @@ void spkv_tree_split(SpkvView v, const uint16_t* __restrict__ q, float scale_log
     else attend_list_split<D, NW>(v, q, scale_log2e, work, s_tile);
 }
 
+template <int D>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void spkv_tree_own_copies(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvTree tree, SpkvTreeTable table) {
+    TreeWork work(v, tree, table, (int)blockIdx.x, 64);
+    attend_own_copies<D>(v, q, scale_log2e, work);
+}
+
 // The join: D / 4 threads own a column, four consecutive elements each; S such groups share a column, each with every
 // S-th of its partial results, and meet in LDS.
 template <int D, int S>
@@ -368,7 +734,7 @@ __global__ __launch_bounds__(256, 8) void spkv_tree_merge(SpkvView v, SpkvTree t
     __shared__ f32x4 s_num[S > 1 ? CPB : 1][S > 1 ? TPC : 1];
     __shared__ float2 s_ml[S > 1 ? CPB : 1];
     const int slice = (int)threadIdx.x / TPC, share = slice % S, d = ((int)threadIdx.x % TPC) * 4;
-    const int local = blockIdx.y, pair = tree.pair0 + local, b = pair / v.Hkv, h = pair - b * v.Hkv, at = b - tree.seq0;
+    const int local = blockIdx.y, pair = tree.pair0 + table.pair[local], b = pair / v.Hkv, h = pair - b * v.Hkv, at = b - tree.seq0;
     const int n_cols = (table.cu[at + 1] - table.cu[at]) * v.G, c0 = (int)blockIdx.x * kCols;
     if (c0 >= n_cols) return;
     const bool exists = c0 + slice / S < n_cols;
@@ -379,14 +745,14 @@ __global__ __launch_bounds__(256, 8) void spkv_tree_merge(SpkvView v, SpkvTree t
     const float2* ml = reinterpret_cast<const float2*>(v.part_ml);
     float M = SPKV_NEG_INF, den = 0.f;
     f32x4 num = {0.f, 0.f, 0.f, 0.f};
-    const int parts = ranges + 1;
+    const int none = tree.n_own == 0 ? 1 : 0, parts = ranges + 1 - none;        // (the drafts' own part, and the lists')
     for (int r0 = share; r0 < parts; r0 += kFold * S) {
         float2 x[kFold];
         f32x4 a[kFold];
 #pragma unroll
         for (int u = 0; u < kFold; ++u) {
             const int r = min(r0 + u * S, parts - 1);        // past the end: re-read, ignored
-            const size_t pc = r == 0 ? own : lists + (size_t)(r - 1) * width;
+            const size_t pc = r + none == 0 ? own : lists + (size_t)(r + none - 1) * width;
             x[u] = ml[pc];
             a[u] = *reinterpret_cast<const f32x4*>(v.part_acc + pc * D + d);
         }
@@ -439,19 +805,33 @@ __global__ __launch_bounds__(256, 8) void spkv_tree_merge(SpkvView v, SpkvTree t
     if (lse != nullptr && d == 0) lse[id] = den == 0.f ? SPKV_NEG_INF : (M + log2f(den)) * 0.6931471805599453f;
 }
 
-int spkv_tree_width(int n_cols) { return n_cols <= 16 ? 16 : n_cols <= 32 ? 32 : n_cols <= 64 ? 64 : n_cols <= 128 ? 128 : 256; }
-int spkv_tree_waves(int width) { return width <= 32 ? 4 : width / 32; }
+// The kernel of own copies has the higher rate on long lists and the longer start: 33 to 64 columns, split / own copies, us: 484 MB
+// in 128 lists 116 / 98, 404 MB in 512 uneven ones 170 / 105, 120 MB in 8 38.3 / 36.5; D = 64, 94 MB 43 / 29; but 28 MB
+// in 256 26 / 30, 17 MB in 32 19.5 / 22.6, 2 MB in 8 13.9 / 19.6.
+constexpr int64_t kTreeOwnHalfPages = 4096;
+SpkvTreeKernel spkv_tree_kernel(int n_cols, int64_t half_pages) {
+    return n_cols <= 16 ? kTreeFew16 : n_cols <= 32 ? kTreeFew32 : n_cols <= 64 ? (half_pages >= kTreeOwnHalfPages ? kTreeOwnCopies : kTreeSplit64)
+                        : n_cols <= 128 ? kTreeSplit128 : kTreeSplit256;
+}
+int spkv_tree_width(SpkvTreeKernel k) {
+    return k == kTreeFew16 ? 16 : k == kTreeFew32 ? 32 : k == kTreeOwnCopies || k == kTreeSplit64 ? 64 : k == kTreeSplit128 ? 128 : 256;
+}
+int spkv_tree_resident(SpkvTreeKernel k) { return k == kTreeOwnCopies || k == kTreeSplit256 ? 1 : 2; }
 
 constexpr int kTreeMergeRound = 2048;
 template <int D>
-static hipError_t launch_tree(const SpkvView& v, const uint16_t* q, float sl, int width, const SpkvTree& tree, const SpkvTreeTable& table,
-                              int n_pairs, int most_cols, int most_ranges, uint16_t* out, float* lse, hipStream_t s) {
-    const dim3 grid((unsigned)(tree.n_own + tree.n_units)), block(64 * spkv_tree_waves(width));
-    if (width == 16) spkv_tree_few<D, 1><<<grid, block, 0, s>>>(v, q, sl, tree, table);
-    else if (width == 32) spkv_tree_few<D, 2><<<grid, block, 0, s>>>(v, q, sl, tree, table);
-    else if (width == 64) spkv_tree_split<D, 2><<<grid, block, 0, s>>>(v, q, sl, tree, table);
-    else if (width == 128) spkv_tree_split<D, 4><<<grid, block, 0, s>>>(v, q, sl, tree, table);
-    else spkv_tree_split<D, 8><<<grid, block, 0, s>>>(v, q, sl, tree, table);
+static hipError_t launch_tree(const SpkvView& v, const uint16_t* q, float sl, SpkvTreeKernel kernel, const SpkvTree& tree,
+                              const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, uint16_t* out, float* lse, hipStream_t s) {
+    const dim3 grid((unsigned)(tree.n_own + tree.n_units));
+    const int width = spkv_tree_width(kernel);
+    switch (kernel) {
+        case kTreeFew16: spkv_tree_few<D, 1><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeFew32: spkv_tree_few<D, 2><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeOwnCopies: spkv_tree_own_copies<D><<<grid, dim3(512), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeSplit64: spkv_tree_split<D, 2><<<grid, dim3(128), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeSplit128: spkv_tree_split<D, 4><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeSplit256: spkv_tree_split<D, 8><<<grid, dim3(512), 0, s>>>(v, q, sl, tree, table); break;
+    }
     constexpr int CPB = 256 / (D / 4);
     int share = std::min(8, CPB);
     while (share > 1 && (n_pairs * ((most_cols * share + CPB - 1) / CPB) > kTreeMergeRound || share > most_ranges + 1)) share >>= 1;
@@ -463,10 +843,10 @@ static hipError_t launch_tree(const SpkvView& v, const uint16_t* q, float sl, in
     return hipGetLastError();
 }
 
-hipError_t spkv_launch_tree(const SpkvView& v, const uint16_t* q, float sm_scale, int width, const SpkvTree& tree,
+hipError_t spkv_launch_tree(const SpkvView& v, const uint16_t* q, float sm_scale, SpkvTreeKernel kernel, const SpkvTree& tree,
                             const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, uint16_t* out, float* lse,
                             hipStream_t s) {
     const float sl = sm_scale * 1.4426950408889634f;
-    return v.D == 128 ? launch_tree<128>(v, q, sl, width, tree, table, n_pairs, most_cols, most_ranges, out, lse, s)
-                      : launch_tree<64>(v, q, sl, width, tree, table, n_pairs, most_cols, most_ranges, out, lse, s);
+    return v.D == 128 ? launch_tree<128>(v, q, sl, kernel, tree, table, n_pairs, most_cols, most_ranges, out, lse, s)
+                      : launch_tree<64>(v, q, sl, kernel, tree, table, n_pairs, most_cols, most_ranges, out, lse, s);
 }

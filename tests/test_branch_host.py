@@ -204,9 +204,20 @@ def test_launches_of_a_tree():
         rc, got = _run([{}], FED + [["tree", dict(counts=[n, 1, 0])]])[-1]
         assert rc == 0 and len(got) == 2 and got[1][0].startswith("spkv_tree_merge<128, ")
         assert got[0][0] == "spkv_tree_" + kernel and got[0][2] == 64 * waves
-        assert 24 + 16 <= got[0][1] <= 24 + 16 + 512      # the drafts' units, a range for every list at least, two rounds at most
+        assert 24 + 16 <= got[0][1] <= 24 + 16 + 1024     # the drafts' units, a range for every list at least, four rounds at most
     assert _run([{}], FED + [["tree", dict(counts=[0, 0, 0], k=0, q=0)]])[-1] == (0, [])
     assert _run([dict(window=20)], FED + [["tree", dict(counts=[20, 0, 3], f=0)]])[-1][0] == 0
+
+
+def test_launches_of_a_tree_over_long_lists():
+    """33 to 64 columns take another kernel where the lists are long; ranges as many as a round of the chip or more."""
+    fed = [["append", dict(counts=[60000, 3, 0])], ["lengths", dict(kept=[55000] * 8 + [0] * 16)]]
+    for n, kernel, threads, rounds in ((4, "few<128, 1>", 256, 4), (8, "few<128, 2>", 256, 4), (9, "own_copies<128>", 512, 1),
+                                       (16, "own_copies<128>", 512, 1), (17, "split<128, 4>", 256, 4), (64, "split<128, 8>", 512, 4)):
+        rc, got = _run([{}], fed + [["tree", dict(counts=[n, 1, 0])]])[-1]
+        assert rc == 0 and [g[0].split("<")[0] for g in got][1:] == ["spkv_tree_merge"]
+        assert got[0][0] == "spkv_tree_" + kernel and got[0][2] == threads
+        assert 200 <= got[0][1] <= 256 * rounds + 16 + 24
 
 
 def test_trees_of_many_pairs_take_several_launches():

@@ -144,6 +144,41 @@ def test_long_lists_in_ranges(hq, hk, d, lengths, counts):
     x.check_tree(sm_scale=0.0)
 
 
+@pytest.mark.parametrize("hq,hk,d,lengths,counts", [
+    (8, 8, 64, [9500, 10000, 500, 0, 128], [64, 40, 33, 9, 50]), (32, 8, 128, [9900, 31, 9700], [16, 16, 9]), (16, 16, 128, [9600, 1], [37, 64]),
+    (48, 16, 64, [33, 9600, 200], [21, 13, 1])])
+def test_lists_long_enough_for_copies_of_their_own(hq, hk, d, lengths, counts):
+    """33 to 64 columns over 130 thousand pairs and more; short, empty and window-only sequences among them."""
+    x = Trees(len(lengths), hq=hq, hk=hk, d=d, window=128, seed=hq + d, context=11000, keep=0.9)
+    x.append(lengths)
+    x.drafts(counts)
+    x.check_tree()
+    x.check_tree(sm_scale=0.0)
+
+
+@pytest.mark.parametrize("long", [False, True])
+@pytest.mark.parametrize("n", [40, 64])
+def test_odd_values_among_short_and_long_lists(n, long):
+    """Ring keys that some drafts see, and drafts, that are not finite, in a short list beside short and long ones."""
+    x = Trees(2, hq=8, hk=8, d=128, window=120, seed=n, keep=0.95, context=20000)
+    x.append([19000 if long else 500, 0])
+    k, v, f = x.rows(120)
+    f = f - 100                                           # these leave the ring for good
+    v[:3], v[3, 1], k[4, 2] = float("nan"), float("inf"), float("nan")
+    x.cache.append(k, v, f, [0, 0, 120])
+    k[4], v[:4] = 0, 0                                    # drafts below depth 5 do not see them
+    x.oracle.append(to_numpy_f32(k), to_numpy_f32(v), to_numpy_f32(f), [0, 0, 120])
+    x.drafts([n, n], lambda r, m: [i - 1 for i in range(m - 8)] + [10] * 8)
+    x.f -= 100
+    x.v[n - 4, :, 3], x.k[2 * n - 2], x.v[2 * n - 3, :, 64:] = float("nan"), float("nan"), float("-inf")
+    out, lse = x.score()
+    for r in (n - 4, n, n + 1, 2 * n - 2, 2 * n - 3):
+        assert not bool(torch.isfinite(out[r]).all()), r
+    x.v[n - 4], x.k[2 * n - 2], x.v[2 * n - 3] = 0, 0, 0
+    clean = [r for r in range(2 * n) if r not in (n - 4, 2 * n - 2, 2 * n - 3) and not n <= r < n + 5]
+    x.check_tree(got=(out, lse), rows=clean)
+
+
 def test_more_pairs_than_a_launch_takes():
     x = Trees(200, hq=8, hk=4, d=64, window=20, seed=8, context=200)
     x.append([b % 50 for b in range(200)])
