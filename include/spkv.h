@@ -397,9 +397,10 @@ int spkv_decode_attention_shared(spkv_cache_t* cache, spkv_cache_t* prefix, cons
  *   cu_seqlens   host int32 [batch + 1]: sequence b's drafts are rows cu[b] .. cu[b+1]-1, at most SPKV_MAX_TREE_NODES
  *   lse          device fp32 [total, n_q_heads] or NULL
  * A sequence may hold no token.  One pass over the cache serves all drafts of a sequence.  Needs no workspace (partial results
- * lie in the cache's own buffers); two launches, more for hundreds of (sequence, KV head) pairs with many columns each.  Waits
- * once for the lengths after a prompt's append, as spkv_decode_attention does.  May be captured; a replay takes the parents and
- * the lists as they are by then.  Copies of a sequence get results that agree to rounding.
+ * lie in the cache's own buffers); one launch, or two where the lists are cut into ranges, more for hundreds of (sequence, KV head)
+ * pairs with many columns each.  Waits once for the lengths after a prompt's append, as spkv_decode_attention does.  May be
+ * captured; a replay takes the parents and the lists as they are by then (the cut is made for lists that fill the pool).  Copies of
+ * a sequence get results that agree to rounding.
  * Errors: SPKV_E_INVAL for bad shapes and pointers; never SPKV_E_STATE. */
 int spkv_score_tree(spkv_cache_t* cache, const void* k, const void* v, const float* util_logits, const void* q,
                     const int32_t* parents, const int32_t* cu_seqlens, void* out, float* lse, float sm_scale,

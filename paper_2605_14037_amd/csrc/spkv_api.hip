@@ -1982,22 +1982,40 @@ namespace {
 constexpr int kTreeMinUnit = 2, kTreeStart = 16, kTreeStartAlone = 24;
 // k above 1 has to leave ranges of so many half-pages: 32 of 500 tokens, 16 drafts 28 / 23 us, 64 short lists' 18 MB, 32 drafts 32 / 24.5.
 constexpr int kTreeMinUnitMore = 20;
-int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, SpkvTreeKernel kernel, int64_t fit, SpkvTree* tree, SpkvTreeTable* table) {
+// Half-pages of a list.  A launch that is captured is cut for lists that have grown into the pool (room: a list's share of it), and does
+// without ranges only where the lists alone fill the chip.
+int64_t tree_half_pages(const spkv_cache* c, int p, int64_t room) {
+    return std::max<int64_t>((c->L_ub[p] + kHalfTokens - 1) / kHalfTokens, room);
+}
+// What a launch takes, ns: its longest unit, or all of them shared among the workgroups that the chip holds.  (D = 64 three quarters
+// of it.  From 1 to 128 sequences of 300 to 4000 tokens, 4 to 64 drafts of 4 heads; only for the choice below.)
+int64_t tree_time(SpkvTreeKernel kernel, int64_t resident, int64_t units, int64_t longest, int64_t work) {
+    static const int start[] = {8100, 8500, 13200, 10200, 10500, 14900}, half_page[] = {300, 550, 320, 700, 700, 780};
+    return std::max(start[kernel] + half_page[kernel] * longest, (start[kernel] * units + half_page[kernel] * work) / resident);
+}
+constexpr int kTreeJoin = 4000, kTreeJoinBytesPerUs = 6000000;       // the second launch, and partial results written and read
+
+// Or every list in one range, with the drafts, its results written at once (tree->whole): two to five times less to write, and one
+// launch.  us, 4 / 16 / 64 drafts, cut / whole: one sequence of 300 tokens 14 / 10, 13 / 17, 19 / 22, one of 2048 12 / 13, 14 / 30, 23 / 33,
+// 16 of 1000 15 / 12, 24 / 20, 44 / 31, 64 of 300 25 / 15, 40 / 25, 101 / 56, 64 of 1k-16k 85 / 84, 99 / 86 (12 drafts), 201 / 161.
+int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, SpkvTreeKernel* chosen, int64_t room, int64_t fit, SpkvTree* tree, SpkvTreeTable* table) {
+    const SpkvTreeKernel kernel = *chosen;
     const int width = spkv_tree_width(kernel);
     const int Hkv = c->cfg.n_kv_heads, G = c->carve.G;
     int32_t hp[kTreePairs], copies[kTreePairs];
-    int64_t work = 0, lists = 0;
+    int64_t work = 0, lists = 0, longest_list = 0;
     for (int i = 0; i < n_pairs; ++i) {
         const int p = tree->pair0 + i, b = p / Hkv;
         copies[i] = ((cu[b + 1] - cu[b]) * G + width - 1) / width;
-        hp[i] = (c->L_ub[p] + kHalfTokens - 1) / kHalfTokens + 2 * ((std::min(c->T[b], c->cfg.window) + kHalfTokens - 1) / kHalfTokens);
+        hp[i] = (int32_t)tree_half_pages(c, p, room) + 2 * ((std::min(c->T[b], c->cfg.window) + kHalfTokens - 1) / kHalfTokens);
         work += (int64_t)hp[i] * copies[i];
         lists += copies[i];
+        if (copies[i] > 0) longest_list = std::max<int64_t>(longest_list, hp[i]);
     }
     const int cus = spkv_compute_units();
     const int64_t round = cus > 0 ? cus : 256, resident = round * spkv_tree_resident(kernel);
     const int64_t start = spkv_tree_resident(kernel) == 1 ? kTreeStartAlone : kTreeStart;
-    int64_t unit = 0, best = 0;
+    int64_t unit = 0, best = 0, cut_time = 0;
     for (int k = 1; k <= 4; ++k) {
         const int64_t target = std::min(fit, (int64_t)k * round);
         int64_t u = std::max<int64_t>(k > 1 ? kTreeMinUnitMore : kTreeMinUnit, (work + target - 1) / target), total = 0, longest = 0, most = 0;
@@ -2017,6 +2035,15 @@ int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, SpkvTreeKernel
         if (k > 1 && time >= best) continue;
         best = time;
         unit = total > fit ? (int64_t)1 << 40 : u;           // (no room for ranges: one each)
+        cut_time = tree_time(kernel, resident, total, longest, work) + kTreeJoin +
+                   (total + tree->n_own) * width * c->cfg.head_dim * 8 * 1000 / kTreeJoinBytesPerUs;
+    }
+    const SpkvTreeKernel alone = spkv_tree_kernel_whole(kernel, lists, round);
+    if ((room == 0 || lists >= round) && tree_time(alone, round * spkv_tree_resident(alone), lists, longest_list, work) < cut_time) {
+        *chosen = alone;
+        tree->whole = 1;
+        tree->n_own = 0;
+        unit = (int64_t)1 << 40;
     }
     // The longest ranges begin first.
     uint16_t order[kTreePairs];
@@ -2075,9 +2102,10 @@ int spkv_score_tree(spkv_cache_t* c, const void* k, const void* v, const float* 
         return SPKV_E_NOMEM;
     }
     tighten_bound(c, s);
+    const int64_t room = being_captured(s) ? 2 * c->carve.n_pages / c->carve.n_pairs : 0;
     int64_t half_pages = 0;
     for (int p = 0; p < c->carve.n_pairs; ++p)
-        if (cu_seqlens[p / Hkv + 1] > cu_seqlens[p / Hkv]) half_pages += (c->L_ub[p] + kHalfTokens - 1) / kHalfTokens;
+        if (cu_seqlens[p / Hkv + 1] > cu_seqlens[p / Hkv]) half_pages += tree_half_pages(c, p, room);
     const SpkvTreeKernel kernel = spkv_tree_kernel(n_max * G, half_pages);
     const int width = spkv_tree_width(kernel);
     SpkvTree tree = {};
@@ -2085,6 +2113,8 @@ int spkv_score_tree(spkv_cache_t* c, const void* k, const void* v, const float* 
     tree.v = static_cast<const uint16_t*>(v);
     tree.f = util_logits;
     tree.parents = parents;
+    tree.out = static_cast<uint16_t*>(out);
+    tree.lse = lse;
     tree.n_blocks = (n_max * G + width - 1) / width;
     // The partial results lie in the cache's buffers of them.  What does not fit a launch (only caches of hundreds of pairs
     // with many columns each) takes several.
@@ -2101,11 +2131,12 @@ int spkv_score_tree(spkv_cache_t* c, const void* k, const void* v, const float* 
         const int seqs = (p0 + n_pairs - 1) / Hkv - tree.seq0 + 1;
         if (cu_seqlens[tree.seq0 + seqs] == tree.row0) continue;
         for (int i = 0; i <= seqs; ++i) table.cu[i] = (uint16_t)(cu_seqlens[tree.seq0 + i] - tree.row0);
+        tree.whole = 0;
         tree.n_own = kernel == kTreeOwnCopies ? 0 : n_pairs * tree.n_blocks;
-        const int most = tree_cut(c, cu_seqlens, n_pairs, kernel, std::min<int64_t>(slots - tree.n_own, 32767), &tree, &table);
+        SpkvTreeKernel chosen = kernel;
+        const int most = tree_cut(c, cu_seqlens, n_pairs, &chosen, room, std::min<int64_t>(slots - tree.n_own, 32767), &tree, &table);
         if (tree.n_units + tree.n_own > slots) return SPKV_E_CAPACITY;
-        if (spkv_launch_tree(c->view, static_cast<const uint16_t*>(q), sm_scale, kernel, tree, table, n_pairs, n_max * G, most,
-                             static_cast<uint16_t*>(out), lse, s) != hipSuccess)
+        if (spkv_launch_tree(c->view, static_cast<const uint16_t*>(q), sm_scale, chosen, tree, table, n_pairs, n_max * G, most, s) != hipSuccess)
             return SPKV_E_HIP;
     }
     return SPKV_OK;

@@ -369,7 +369,10 @@ struct SpkvTree {
     const uint16_t *k, *v;
     const float* f;              // null: every path fits the window
     const int32_t* parents;
+    uint16_t* out;
+    float* lse;                  // or null
     int32_t pair0, seq0, row0;
+    int32_t whole;               // every list is one range, which takes the drafts and writes the results
     int32_t n_own;               // units of the drafts themselves, a pair's blocks of columns, behind those of the lists; 0: the first range takes them
     int32_t n_blocks;            // ... of the pair with the most columns
     int32_t n_units;             // units of the lists
@@ -384,8 +387,8 @@ struct SpkvTreeTable {
 // where the lists are short), 128, 256 to a workgroup.
 enum SpkvTreeKernel { kTreeFew16, kTreeFew32, kTreeOwnCopies, kTreeSplit64, kTreeSplit128, kTreeSplit256 };
 SpkvTreeKernel spkv_tree_kernel(int n_cols, int64_t half_pages);
+SpkvTreeKernel spkv_tree_kernel_whole(SpkvTreeKernel kernel, int64_t lists, int64_t compute_units);      // ... where no list is cut
 int spkv_tree_width(SpkvTreeKernel kernel);       // columns of a workgroup
 int spkv_tree_resident(SpkvTreeKernel kernel);    // workgroups that a compute unit holds
 hipError_t spkv_launch_tree(const SpkvView& v, const uint16_t* q, float sm_scale, SpkvTreeKernel kernel, const SpkvTree& tree,
-                            const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, uint16_t* out, float* lse,
-                            hipStream_t s);
+                            const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, hipStream_t s);

@@ -205,6 +205,10 @@ __device__ __forceinline__ bool odd_sums(const Acc* acc, int n, float l) {
     return sum != 0.f && l - l == 0.f;
 }
 
+__device__ __forceinline__ unsigned long long lane_word(unsigned long long x, int lane) {
+    return (unsigned long long)(unsigned)__shfl((int)(unsigned)x, lane) | ((unsigned long long)(unsigned)__shfl((int)(x >> 32), lane) << 32);
+}
+
 // The query row of a column, its head in the group, and its token's place behind the list's newest token (looked for
 // only where the ring is read).
 struct ShareRow {
@@ -216,6 +220,8 @@ struct ShareRow {
 //   columns(v)                       columns of the list, asked once and before those that follow
 //   row(v, c, ring)                  ShareRow of column c; ring: the place is wanted.  The whole wave asks.
 //   part(v), part_ml<D>(v), part0(v) partial sums and (m, l), those of column c at part0 + c
+//   kWhole                           the range is all there is (one range, of the whole list): the workgroup takes the drafts, too,
+//                                    and writes the columns' results; see TreeWork in spkv_tree.hip for what is asked of it then
 
 // Up to 16 NQ columns.  A half-page's operands come straight from memory (1 KB a load, as in spkv_decode_split) and are
 // used for all NQ groups of 16 columns: scores of all groups -- the next half-page's keys are sent for -- then
@@ -239,7 +245,12 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
     if (n_cols <= 0) return;
     const int nA = list.nA;
     const int r_begin = list.begin(j, ranges), r_end = list.begin(j + 1, ranges);
-    const int x_begin = r_begin + (r_end - r_begin) * wv / 4, x_end = r_begin + (r_end - r_begin) * (wv + 1) / 4;
+    // the first wave's drafts count as kDrafts half-pages
+    constexpr int kDrafts = Work::kWhole ? 3 : 0;
+    auto cut = [&](int w) -> int { return r_begin + max(0, (r_end - r_begin + kDrafts) * w / 4 - kDrafts); };
+    const int x_begin = wv == 0 ? r_begin : cut(wv), x_end = cut(wv + 1);
+    const bool drafts = Work::kWhole && wv == 0;
+    const int x_first = drafts ? x_begin - 1 : x_begin;      // they come before the half-pages
 
     SharePages pages = share_pages(v, pair, first_ids, x_begin >> 1);
     bf16x8 k[2][NS], va[NB];
@@ -271,7 +282,13 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
                 *reinterpret_cast<bf16x8*>(&s_q[NQ == 1 ? 0 : i * NS + sl][lane * 8]) = *reinterpret_cast<const bf16x8*>(qrow + sl * 32);
         }
     }
-    if (x_begin < x_end) {
+    unsigned long long word = 0ull;                          // drafts that lane's draft sees
+    if (drafts) {
+        if constexpr (Work::kWhole) {
+            work.template load_few<D>(v, k, va);
+            word = work.seen(v, list.T);
+        }
+    } else if (x_begin < x_end) {
         const uint16_t* page = half_page_at(v, list, pages, x_begin);
         load_k(page);
         load_v(page);
@@ -305,7 +322,7 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
     }
     const int full = list.L >> 5;                            // half-pages that need no mask
 #pragma unroll 1
-    for (int x = x_begin; x < x_end; ++x) {
+    for (int x = x_first; x < x_end; ++x) {
         const bool more = x + 1 < x_end;
         const uint16_t* next = more ? half_page_at(v, list, pages, x + 1) : nullptr;
         f32x8 s[NQ];
@@ -326,7 +343,15 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
             }
         }
         if (more) load_k(next);
-        if (x >= full) {
+        if (Work::kWhole && drafts && x == x_first) {         // a draft: a word of the drafts that it sees
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                const int c = i * 16 + n;
+                const unsigned mine = (unsigned)(lane_word(word, (c < n_cols ? c : 0) / v.G) >> (8 * kc));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[i][e] = ((mine >> e) & 1u) ? s[i][e] : SPKV_NEG_INF;
+            }
+        } else if (x >= full) {
             unsigned any, on = 0u;
             const int at0 = (x - nA) * kHalfTokens + kc * 8;
             if (x < nA) any = bits_below(list.L - x * kHalfTokens - kc * 8);
@@ -368,7 +393,7 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
                 const float alpha = __builtin_amdgcn_exp2f(m[i] - (m_new == SPKV_NEG_INF ? 0.f : m_new));
                 m[i] = m_new;
                 l[i] *= alpha;
-                if (x > x_begin) {
+                if (x > x_first) {
 #pragma unroll
                     for (int db = 0; db < NB; ++db) acc[i][db] *= alpha;
                 }
@@ -395,23 +420,27 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
         for (int db = 0; db < NB; ++db) *reinterpret_cast<f32x4*>(pa + db * 16) = acc[i][db];
         if (kc == 0) s_ml[wv][i * 16 + n] = make_float2(m[i], l[i]);
     }
-    if (ring && least != most) {
+    if ((ring && least != most) || drafts) {
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < NQ; ++i) odd = odd || odd_sums(acc[i], NB, l[i]);
         if (__builtin_expect(__ballot(odd) != 0ull, 0)) {
             const CarefulRange range = careful_range(v, list, scale_log2e, x_begin, x_end);
-            if (careful_needed<D>(range, least, most))
+            bool again = ring && least != most && careful_needed<D>(range, least, most);
+            if constexpr (Work::kWhole) again = again || (drafts && work.template careful_needed<D>(v));
+            if (again)
                 for (int c = 0; c < min(16 * NQ, n_cols); ++c) {
                     const ShareRow sr = work.row(v, c, true);
                     __builtin_amdgcn_wave_barrier();
-                    careful_sums<D>(range, q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D, sr.place, s_ml[wv][c].x,
-                                    s_acc[wv] + c * kRow);
+                    const uint16_t* qrow = q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D;
+                    careful_sums<D>(range, qrow, sr.place, s_ml[wv][c].x, s_acc[wv] + c * kRow);
+                    if constexpr (Work::kWhole)
+                        if (drafts) work.template add_careful<D>(v, qrow, lane_word(word, sr.row - work.row0), scale_log2e, s_ml[wv][c].x, s_acc[wv] + c * kRow);
                 }
         }
     }
     __syncthreads();
-    const size_t pc0 = work.part0(v);
+    const size_t pc0 = Work::kWhole ? 0 : work.part0(v);
     float* part = work.part(v);
     float2* part_ml = work.template part_ml<D>(v);
     for (int e = tid; e < n_cols * (D / 4); e += 256) {
@@ -432,15 +461,19 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
             a += *reinterpret_cast<const f32x4*>(s_acc[w] + c * kRow + d) * sc;
             sum += ml[w].y * sc;
         }
-        *reinterpret_cast<f32x4*>(part + (pc0 + c) * D + d) = a;
-        if (d == 0) part_ml[pc0 + c] = make_float2(M, sum);
+        if constexpr (Work::kWhole) {
+            work.template store<D>(v, c, d, a, M, sum);
+        } else {
+            *reinterpret_cast<f32x4*>(part + (pc0 + c) * D + d) = a;
+            if (d == 0) part_ml[pc0 + c] = make_float2(M, sum);
+        }
     }
 }
 
 // A wave's sums of 32 columns leave through LDS, a column's row at a time (straight from the registers every store touched 32 rows,
 // 32 bytes each).  16-byte unit x of column col lies at x ^ col: no bank conflicts either way.
 template <int D>
-__device__ __forceinline__ void store_column_sums(const f32x16 (&acc)[D / 32], float* sums, float* to, int n_here) {
+__device__ __forceinline__ void column_sums_to_lds(const f32x16 (&acc)[D / 32], float* sums) {
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
@@ -449,12 +482,20 @@ __device__ __forceinline__ void store_column_sums(const f32x16 (&acc)[D / 32], f
             *reinterpret_cast<f32x4*>(sums + col * D + ((db * 8 + g * 2 + half) ^ (col & (D / 4 - 1))) * 4) =
                 (f32x4){acc[db][4 * g], acc[db][4 * g + 1], acc[db][4 * g + 2], acc[db][4 * g + 3]};
     __builtin_amdgcn_wave_barrier();
+}
+template <int D>
+__device__ __forceinline__ f32x4 column_sum_at(const float* sums, int i, int unit) {
+    return *reinterpret_cast<const f32x4*>(sums + i * D + (unit ^ (i & (D / 4 - 1))) * 4);
+}
+template <int D>
+__device__ __forceinline__ void store_column_sums(const f32x16 (&acc)[D / 32], float* sums, float* to, int n_here) {
+    column_sums_to_lds<D>(acc, sums);
+    const int lane = threadIdx.x & 63;
     constexpr int kUnits = D / 4, kColsPerPass = 64 / kUnits;
     const int unit = lane % kUnits;
 #pragma unroll 4
     for (int i = lane / kUnits; i < n_here; i += kColsPerPass)
-        *reinterpret_cast<f32x4*>(to + (size_t)i * D + unit * 4) =
-            *reinterpret_cast<const f32x4*>(sums + i * D + (unit ^ (i & (D / 4 - 1))) * 4);
+        *reinterpret_cast<f32x4*>(to + (size_t)i * D + unit * 4) = column_sum_at<D>(sums, i, unit);
 }
 
 // More columns: the copies of the range's half-pages go from memory straight into LDS, in operand order, so that
@@ -480,15 +521,15 @@ __device__ __forceinline__ void attend_list_split(const SpkvView& v, const uint1
     const int col0 = work.block * (32 * NW);
     if (col0 >= n_cols) return;
     const int nA = list.nA;
-    const int x_begin = list.begin(j, ranges), x_end = list.begin(j + 1, ranges), last = x_end - 1;
+    const int x_begin = list.begin(j, ranges), x_end = list.begin(j + 1, ranges), last = max(x_end - 1, x_begin);
 
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = col0 + wv * 32 + col;
     const bool valid = c < n_cols;
-    const size_t pc = work.part0(v) + c;                     // of the partial result
+    const size_t pc = Work::kWhole ? 0 : work.part0(v) + c;  // of the partial result
     float2* part_ml = work.template part_ml<D>(v);
-    if (x_begin >= x_end) {                                  // fewer half-pages than ranges
+    if (!Work::kWhole && x_begin >= x_end) {                 // fewer half-pages than ranges
         if (valid && half == 0) part_ml[pc] = make_float2(SPKV_NEG_INF, 0.f);
         return;
     }
@@ -700,6 +741,36 @@ __device__ __forceinline__ void attend_list_split(const SpkvView& v, const uint1
     }
     wait_loads_but<0>();
 
+    if constexpr (Work::kWhole) {
+        __syncthreads();                                     // the tiles are no longer read
+        work.template stage_split<D, NW>(v, s_tile[0]);
+        const unsigned long long word = work.seen(v, list.T), mine = lane_word(word, sr.row - work.row0);
+        __syncthreads();
+#pragma unroll 1
+        for (int t = 0; t < (work.n + kHalfTokens - 1) / kHalfTokens; ++t) {
+            load_k(s_tile[t]);
+            load_v(s_tile[t], 0);
+            load_v(s_tile[t], 1);
+            scores(s0);
+            const unsigned ok = (unsigned)(mine >> (32 * t)) >> (8 * half);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s0[e] = ((ok >> (16 * (e >> 3) + (e & 7))) & 1u) ? s0[e] : SPKV_NEG_INF;
+            if (weights(s0)) rescale(s0);
+            l += psum;
+            accumulate(0);
+            accumulate(1);
+        }
+        l += __shfl_xor(l, 32);
+        const bool odd = odd_sums(acc, NB, l);
+        bool again = false;
+        const CarefulRange range = careful_range(v, list, scale_log2e, x_begin, x_end);
+        if (__builtin_expect(__ballot(odd) != 0ull, 0))
+            again = (x_end > nA && least != most && careful_needed<D>(range, least, most)) || work.template careful_needed<D>(v);
+        __syncthreads();                                     // the drafts are no longer read
+        work.template finish_split<D>(v, q, range, word, acc, m, l, again, reinterpret_cast<float*>(&s_tile[0][0]) + wv * 32 * D, col0 + wv * 32,
+                                      min(32, n_cols - (col0 + wv * 32)));
+        return;
+    }
     l += __shfl_xor(l, 32);
     if (valid && half == 0) part_ml[pc] = make_float2(m, l);
     const bool odd = x_end > nA && least != most && odd_sums(acc, NB, l);

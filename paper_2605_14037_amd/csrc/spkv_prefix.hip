@@ -174,6 +174,7 @@ __device__ __forceinline__ ShareRow share_row(const SpkvShareRows& rows, int fir
 }
 
 struct PromptWork {
+    static constexpr bool kWhole = false;
     const SpkvShareCut& cut;
     const SpkvShareRows& rows;
     int act, h, pair, range, ranges, block, first;

@@ -9,24 +9,23 @@
 // path and d(i) - d(a) < w or a's gate is on (Eq. 3-5 for the tokens of the path alone).  All drafts of a sequence
 // and all heads of a group are columns of one product with the list, as the rows of sequences that share a prompt are
 // (spkv_lists.h), with d(i) for the place behind the list's newest token; the drafts themselves, at most 64
-// keys, are one unit of work more, whose mask is a word of 64 bits a draft.
+// keys, are one unit of work more, whose mask is a word of 64 bits a draft.  Lists of a few half-pages, or lists enough to fill
+// the chip, are taken whole: one workgroup a list, the drafts with it, its results final (32 sequences of 300 tokens, 16 drafts, 25 -> 19
+// us, 64 drafts 53 -> 29; 64 of 1k-16k, 64 drafts, 201 -> 155).
 //
 // A lane of a wave stands for a draft: paths are words of bits, joined along the parents by doubling (log2 of the deepest
 // path's length rounds of three lane exchanges), depths their counts of bits.
 //
 // Bound: the lists are read once, 4 D bytes a key for 4 D flops a key and column: past about 180 columns a list the matrix
 // units, below the read; few columns or short lists by the start of a workgroup and the join.  Measured, 16 sequences of 32k tokens
-// (484 MB, 32 heads over 8 of 128), a call: 4 drafts 83 us (5.9 TB/s), 8: 94, 16: 98, 32: 124, 64: 170 (2.9 TB/s, 0.73 PF/s); one
-// sequence of 128k, 16 drafts 37; of 2k, 14.
+// (484 MB, 32 heads over 8 of 128), a call: 4 drafts 83 us (5.8 TB/s), 8: 94, 16: 99, 32: 120, 64: 162 (3.0 TB/s, 0.76 PF/s); one
+// sequence of 128k, 16 drafts 34; of 2k, 14.
 
 // ------------------------------------------------------------------------------- paths
 struct TreePath {
     unsigned long long path;     // of lane's draft: itself and what it hangs behind
     int up, depth;
 };
-__device__ __forceinline__ unsigned long long lane_word(unsigned long long x, int lane) {
-    return (unsigned long long)(unsigned)__shfl((int)(unsigned)x, lane) | ((unsigned long long)(unsigned)__shfl((int)(x >> 32), lane) << 32);
-}
 // Any value but 0 .. i - 1 for a parent means that the draft hangs behind the newest token.
 __device__ __forceinline__ TreePath tree_path(const int32_t* __restrict__ parents, int n) {
     const int lane = threadIdx.x & 63;
@@ -64,58 +63,6 @@ __device__ __forceinline__ unsigned long long tree_seen(const SpkvView& v, const
     const unsigned long long gates = __ballot(on);
     return at >= 0 ? t.path & (~far | gates) : t.path;
 }
-
-// ---------------------------------------------------------------------------- the work
-// Workgroup id -> unit: the ranges of the lists, by the host's table, the ranges of a pair's block of columns next to each
-// other, then the drafts of every pair's blocks of columns (short units, beside the last ranges).
-struct TreeWork {
-    const SpkvTree& tree;
-    const SpkvTreeTable& table;
-    int pair, h, range, ranges, block, n, row0, unit, width;
-    __device__ __forceinline__ TreeWork(const SpkvView& v, const SpkvTree& t, const SpkvTreeTable& tab, int id, int w)
-        : tree(t), table(tab), width(w) {
-        int local;
-        if (id >= t.n_units) {
-            local = (id - t.n_units) / t.n_blocks;
-            block = id - t.n_units - local * t.n_blocks;
-            range = -1;
-            ranges = 1;
-            unit = id;
-        } else {
-            const uint4 raw = reinterpret_cast<const uint4*>(tab.end)[threadIdx.x & 63];      // eight pairs a lane
-            const unsigned e[4] = {raw.x, raw.y, raw.z, raw.w};
-            local = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                local += __popcll(__ballot((int)(e[i] & 0xffffu) <= id));
-                local += __popcll(__ballot((int)(e[i] >> 16) <= id));
-            }
-            const int start = local > 0 ? tab.end[local - 1] : 0;
-            ranges = tab.ranges[local];
-            block = (id - start) / ranges;
-            range = id - start - block * ranges;
-            unit = id;
-        }
-        pair = t.pair0 + tab.pair[local];
-        const int b = pair / v.Hkv, at = b - t.seq0;
-        h = pair - b * v.Hkv;
-        row0 = t.row0 + tab.cu[at];
-        n = tab.cu[at + 1] - tab.cu[at];
-    }
-    __device__ __forceinline__ int columns(const SpkvView& v) const { return n * v.G; }
-    __device__ __forceinline__ ShareRow row(const SpkvView& v, int c, bool ring) const {
-        ShareRow r;
-        const int i = c / v.G;
-        r.head = c - i * v.G;
-        r.row = row0 + i;
-        r.place = ring ? __shfl(tree_path(tree.parents + row0, n).depth, i) : 0;
-        return r;
-    }
-    __device__ __forceinline__ float* part(const SpkvView& v) const { return v.part_acc; }
-    template <int D>
-    __device__ __forceinline__ float2* part_ml(const SpkvView& v) const { return reinterpret_cast<float2*>(v.part_ml); }
-    __device__ __forceinline__ size_t part0(const SpkvView&) const { return (size_t)(unit - block) * width; }
-};
 
 // Sums of one column over the drafts that it sees, key by key, where an infinity or NaN among the values of a draft that it
 // does not see has reached it (a weight of zero times it).  The whole wave.
@@ -155,48 +102,201 @@ __device__ __attribute__((noinline)) bool careful_tree_needed(const uint16_t* vv
     return __ballot(odd) != 0ull;
 }
 
+__device__ __forceinline__ void store_result(uint16_t* to, f32x4 x) {
+    uint2 packed;
+    packed.x = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)x[0]) | ((unsigned)__builtin_bit_cast(uint16_t, (__bf16)x[1]) << 16);
+    packed.y = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)x[2]) | ((unsigned)__builtin_bit_cast(uint16_t, (__bf16)x[3]) << 16);
+    *reinterpret_cast<uint2*>(to) = packed;
+}
+__device__ __forceinline__ float log_of_sum(float m, float l) { return l == 0.f ? SPKV_NEG_INF : (m + log2f(l)) * 0.6931471805599453f; }
+
+// ---------------------------------------------------------------------------- the work
+// Workgroup id -> unit: the ranges of the lists, by the host's table, the ranges of a pair's block of columns next to each
+// other, then the drafts of every pair's blocks of columns (short units, beside the last ranges).  W: every list is one range, whose
+// unit takes the drafts too and writes the results; there are no others, and no join.
+template <bool W>
+struct TreeWork {
+    static constexpr bool kWhole = W;
+    const SpkvTree& tree;
+    const SpkvTreeTable& table;
+    int pair, h, range, ranges, block, n, row0, unit, width;
+    __device__ __forceinline__ TreeWork(const SpkvView& v, const SpkvTree& t, const SpkvTreeTable& tab, int id, int w)
+        : tree(t), table(tab), width(w) {
+        int local;
+        if (!W && id >= t.n_units) {
+            local = (id - t.n_units) / t.n_blocks;
+            block = id - t.n_units - local * t.n_blocks;
+            range = -1;
+            ranges = 1;
+            unit = id;
+        } else {
+            const uint4 raw = reinterpret_cast<const uint4*>(tab.end)[threadIdx.x & 63];      // eight pairs a lane
+            const unsigned e[4] = {raw.x, raw.y, raw.z, raw.w};
+            local = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                local += __popcll(__ballot((int)(e[i] & 0xffffu) <= id));
+                local += __popcll(__ballot((int)(e[i] >> 16) <= id));
+            }
+            const int start = local > 0 ? tab.end[local - 1] : 0;
+            ranges = tab.ranges[local];
+            block = (id - start) / ranges;
+            range = id - start - block * ranges;
+            unit = id;
+        }
+        pair = t.pair0 + tab.pair[local];
+        const int b = pair / v.Hkv, at = b - t.seq0;
+        h = pair - b * v.Hkv;
+        row0 = t.row0 + tab.cu[at];
+        n = tab.cu[at + 1] - tab.cu[at];
+    }
+    __device__ __forceinline__ int columns(const SpkvView& v) const { return n * v.G; }
+    __device__ __forceinline__ ShareRow row(const SpkvView& v, int c, bool ring) const {
+        ShareRow r;
+        const int i = c / v.G;
+        r.head = c - i * v.G;
+        r.row = row0 + i;
+        r.place = ring ? __shfl(tree_path(tree.parents + row0, n).depth, i) : 0;
+        return r;
+    }
+    __device__ __forceinline__ float* part(const SpkvView& v) const { return v.part_acc; }
+    template <int D>
+    __device__ __forceinline__ float2* part_ml(const SpkvView& v) const { return reinterpret_cast<float2*>(v.part_ml); }
+    __device__ __forceinline__ size_t part0(const SpkvView&) const { return (size_t)(unit - block) * width; }
+
+    // ---- the drafts
+    __device__ __forceinline__ int stride(const SpkvView& v) const { return v.Hkv * v.D; }
+    __device__ __forceinline__ const uint16_t* keys(const SpkvView& v) const { return tree.k + ((size_t)row0 * v.Hkv + h) * v.D; }
+    __device__ __forceinline__ const uint16_t* values(const SpkvView& v) const { return tree.v + ((size_t)row0 * v.Hkv + h) * v.D; }
+    __device__ __forceinline__ unsigned long long seen(const SpkvView& v, int T) const {
+        return tree_seen(v, tree_path(tree.parents + row0, n), tree.f, h, row0, n, T);
+    }
+    // Operands of attend_list_few, N groups of 16 of the values' elements from group first on.  Keys straight from their rows;
+    // values, of which an operand wants eight keys of one element, by 2-byte loads.
+    template <int D, int N>
+    __device__ __forceinline__ void load_few(const SpkvView& v, bf16x8 (&k)[2][D / 32], bf16x8 (&va)[N], int first = 0) const {
+        const int lane = threadIdx.x & 63, kc = lane >> 4, col = lane & 15, step = v.Hkv * D;
+        const uint16_t *kr = keys(v), *vr = values(v);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int sl = 0; sl < D / 32; ++sl) {            // (rows that are not there: the last one's; no column sees them)
+                const int key = min(8 * (col >> 2) + 4 * t + (col & 3), n - 1);
+                k[t][sl] = *reinterpret_cast<const bf16x8*>(kr + (size_t)key * step + sl * 32 + kc * 8);
+            }
+        uint16_t raw[N][8];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) raw[i][e] = vr[(size_t)min(8 * kc + e, n - 1) * step + (first + i) * 16 + col];
+        const unsigned there = bits_below(n - 8 * kc);       // (a weight of zero would make a NaN of an infinity)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint4 u;
+            u.x = raw[i][0] | ((unsigned)raw[i][1] << 16);
+            u.y = raw[i][2] | ((unsigned)raw[i][3] << 16);
+            u.z = raw[i][4] | ((unsigned)raw[i][5] << 16);
+            u.w = raw[i][6] | ((unsigned)raw[i][7] << 16);
+            va[i] = keep_keys(__builtin_bit_cast(bf16x8, u), there);
+        }
+    }
+    // Keys and values in LDS, in the operand order of attend_list_split, a half-page of them to a tile: rows of 1 KB, D / 16 of keys
+    // and as many of values.  Four rows of each are in flight at once: one after the other they were most of the unit's time.
+    template <int D, int NW>
+    __device__ __forceinline__ void stage_split(const SpkvView& v, uint16_t* s_tile) const {
+        constexpr int NS = D / 16, NB = D / 32, kAtOnce = 4;
+        const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        const int rows = ((n + kHalfTokens - 1) >> 5) * NS, step = v.Hkv * D;
+        const uint16_t *kr = keys(v) + 8 * half, *vr = values(v) + col;
+        const int k_key = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+        for (int r0 = wv; r0 < rows; r0 += kAtOnce * NW) {
+            uint4 k[kAtOnce];
+            unsigned x[kAtOnce][8];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {              // (rows of drafts that are not there: the last one's)
+                const int r = min(r0 + j * NW, rows - 1), t = r / NS, row = r - t * NS;
+                k[j] = *reinterpret_cast<const uint4*>(kr + (size_t)min(32 * t + k_key, n - 1) * step + 16 * row);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[j][e] = vr[(size_t)min(32 * t + 16 * (row / NB) + 8 * half + e, n - 1) * step + 32 * (row % NB)];
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                if (r0 + j * NW >= rows) break;
+                const int r = r0 + j * NW, t = r / NS, row = r - t * NS;
+                uint16_t* to = s_tile + (size_t)t * (2 * kHalfTokens * D) + row * 512 + lane * 8;
+                *reinterpret_cast<uint4*>(to) = k[j];
+                const uint4 u = make_uint4(x[j][0] | (x[j][1] << 16), x[j][2] | (x[j][3] << 16), x[j][4] | (x[j][5] << 16), x[j][6] | (x[j][7] << 16));
+                *reinterpret_cast<bf16x8*>(to + kHalfTokens * D) =          // (a weight of zero would make a NaN of an infinity)
+                    keep_keys(__builtin_bit_cast(bf16x8, u), bits_below(n - (32 * t + 16 * (row / NB) + 8 * half)));
+            }
+        }
+    }
+    template <int D>
+    __device__ __forceinline__ bool careful_needed(const SpkvView& v) const {
+        return careful_tree_needed<D>(values(v), stride(v), n);
+    }
+    template <int D>
+    __device__ __forceinline__ void add_careful(const SpkvView& v, const uint16_t* qrow, unsigned long long word, float scale_log2e, float m,
+                                                float* sums) const {
+        __builtin_amdgcn_wave_barrier();
+        careful_tree_sums<D>(keys(v), values(v), stride(v), qrow, word, scale_log2e, m, true, sums);
+    }
+
+    // ---- results
+    __device__ __forceinline__ size_t result(const SpkvView& v, int c) const {
+        const int draft = c / v.G;
+        return (size_t)(row0 + draft) * v.Hq + (size_t)h * v.G + (c - draft * v.G);
+    }
+    // four elements of column c; m, l of its sums
+    template <int D>
+    __device__ __forceinline__ void store(const SpkvView& v, int c, int d, f32x4 a, float m, float l) const {
+        const size_t id = result(v, c);
+        store_result(tree.out + id * D + d, a * (l == 0.f ? 0.f : 1.0f / l));
+        if (tree.lse != nullptr && d == 0) tree.lse[id] = log_of_sum(m, l);
+    }
+    // attend_list_split's: a wave's sums of columns c0 .. + n_here - 1, or, again, worked out key by key; sums: room in LDS
+    template <int D>
+    __device__ __forceinline__ void finish_split(const SpkvView& v, const uint16_t* q, const CarefulRange& range, unsigned long long word,
+                                                 f32x16 (&acc)[D / 32], float m, float l, bool again, float* sums, int c0, int n_here) const {
+        const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        if (tree.lse != nullptr && half == 0 && col < n_here) tree.lse[result(v, c0 + col)] = log_of_sum(m, l);
+        if (__builtin_expect(again, 0)) {
+            for (int i = 0; i < n_here; ++i) {
+                const size_t id = result(v, c0 + i);
+                const uint16_t* qrow = q + id * D;
+                const int draft = (c0 + i) / v.G;
+                const float ref = __shfl(m, i), scale = __shfl(inv, i);
+                careful_sums<D>(range, qrow, __popcll(lane_word(tree_path(tree.parents + row0, n).path, draft)) - 1, ref, sums);
+                add_careful<D>(v, qrow, lane_word(word, draft), range.scale_log2e, ref, sums);
+                for (int d = lane; d < D; d += 64) tree.out[id * D + d] = __builtin_bit_cast(uint16_t, (__bf16)(sums[d] * scale));
+            }
+            return;
+        }
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) acc[db] *= inv;
+        column_sums_to_lds<D>(acc, sums);
+        constexpr int kUnits = D / 4, kColsPerPass = 64 / kUnits;
+        const int unit = lane % kUnits;
+#pragma unroll 4
+        for (int i = lane / kUnits; i < n_here; i += kColsPerPass)
+            store_result(tree.out + result(v, c0 + i) * D + unit * 4, column_sum_at<D>(sums, i, unit));
+    }
+};
+
 // The drafts as keys, up to 16 NQ columns (so at most 32 drafts: one half-page): every wave has all scores and a
-// quarter of the values' elements.  Keys straight from their rows; values, of which an operand wants eight keys of one
-// element, by 2-byte loads: a unit of a few microseconds beside those of the lists.
+// quarter of the values' elements.
 template <int D, int NQ>
 __device__ __forceinline__ void attend_drafts_few(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e,
-                                                  const TreeWork& work) {
+                                                  const TreeWork<false>& work) {
     constexpr int NS = D / 32, NB = D / 16, kMine = NB / 4;
     const int lane = threadIdx.x & 63, kc = lane >> 4, col = lane & 15, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int n = work.n, h = work.h, stride = v.Hkv * D, n_cols = work.columns(v);
+    const int n = work.n, h = work.h, n_cols = work.columns(v);
     if (n == 0) return;
-    const uint16_t* kr = work.tree.k + ((size_t)work.row0 * v.Hkv + h) * D;
-    const uint16_t* vr = work.tree.v + ((size_t)work.row0 * v.Hkv + h) * D;
-    const uint4 zero = {0u, 0u, 0u, 0u};
-    bf16x8 k[2][NS];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int sl = 0; sl < NS; ++sl) {
-            const int key = 8 * (col >> 2) + 4 * t + (col & 3);
-            k[t][sl] = __builtin_bit_cast(bf16x8, key < n ? *reinterpret_cast<const uint4*>(kr + (size_t)key * stride + sl * 32 + kc * 8) : zero);
-        }
-    uint16_t raw[kMine][8];
-#pragma unroll
-    for (int i = 0; i < kMine; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int key = 8 * kc + e;
-            raw[i][e] = key < n ? vr[(size_t)key * stride + (wv * kMine + i) * 16 + col] : (uint16_t)0;
-        }
-    const int T = v.t_pair[work.pair];
-    const TreePath path = tree_path(work.tree.parents + work.row0, n);
-    const unsigned long long word = tree_seen(v, path, work.tree.f, h, work.row0, n, T);
-    bf16x8 va[kMine];
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        uint4 u;
-        u.x = raw[i][0] | ((unsigned)raw[i][1] << 16);
-        u.y = raw[i][2] | ((unsigned)raw[i][3] << 16);
-        u.z = raw[i][4] | ((unsigned)raw[i][5] << 16);
-        u.w = raw[i][6] | ((unsigned)raw[i][7] << 16);
-        va[i] = __builtin_bit_cast(bf16x8, u);
-    }
+    bf16x8 k[2][NS], va[kMine];
+    work.load_few<D>(v, k, va, wv * kMine);
+    const unsigned long long word = work.seen(v, v.t_pair[work.pair]);
     const size_t pc0 = work.part0(v);
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
@@ -252,8 +352,8 @@ __device__ __forceinline__ void attend_drafts_few(const SpkvView& v, const uint1
             if (wv == 0)
                 for (int x0 = 0; x0 < 16 && i * 16 + x0 < n_cols; ++x0) {
                     const int cc = i * 16 + x0, dd = cc / v.G;
-                    careful_tree_sums<D>(kr, vr, stride, q + ((size_t)(work.row0 + dd) * v.Hq + (size_t)h * v.G + (cc - dd * v.G)) * D,
-                                         lane_word(word, dd), scale_log2e, __shfl(ref, x0), false, v.part_acc + (pc0 + cc) * D);
+                    careful_tree_sums<D>(work.keys(v), work.values(v), work.stride(v), q + work.result(v, cc) * D, lane_word(word, dd), scale_log2e,
+                                         __shfl(ref, x0), false, v.part_acc + (pc0 + cc) * D);
                 }
         }
     }
@@ -262,29 +362,13 @@ __device__ __forceinline__ void attend_drafts_few(const SpkvView& v, const uint1
 // More columns: keys and values into LDS once, in the operand order of attend_list_split, then 32 columns a wave.
 template <int D, int NW>
 __device__ __forceinline__ void attend_drafts_split(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e,
-                                                    const TreeWork& work, uint16_t (&s_tile)[kSplitSlots<NW>][2 * kHalfTokens * D]) {
+                                                    const TreeWork<false>& work, uint16_t (&s_tile)[kSplitSlots<NW>][2 * kHalfTokens * D]) {
     constexpr int NS = D / 16, NB = D / 32;
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int n = work.n, h = work.h, stride = v.Hkv * D, n_cols = work.columns(v), col0 = work.block * (32 * NW);
+    const int n = work.n, h = work.h, n_cols = work.columns(v), col0 = work.block * (32 * NW);
     if (col0 >= n_cols) return;
-    const uint16_t* kr = work.tree.k + ((size_t)work.row0 * v.Hkv + h) * D;
-    const uint16_t* vr = work.tree.v + ((size_t)work.row0 * v.Hkv + h) * D;
     const int tiles = (n + kHalfTokens - 1) >> 5;
-    for (int r = wv; r < tiles * (D / 8); r += NW) {          // rows of 1 KB: D / 16 of keys, D / 16 of values
-        const int t = r / (D / 8), row = r - t * (D / 8);
-        uint4 u = {0u, 0u, 0u, 0u};
-        if (row < NS) {
-            const int key = 32 * t + 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
-            if (key < n) u = *reinterpret_cast<const uint4*>(kr + (size_t)key * stride + 16 * row + 8 * half);
-        } else {
-            const int g = (row - NS) / NB, d = 32 * ((row - NS) % NB) + col, key0 = 32 * t + 16 * g + 8 * half;
-            unsigned x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = key0 + e < n ? vr[(size_t)(key0 + e) * stride + d] : 0u;
-            u = make_uint4(x[0] | (x[1] << 16), x[2] | (x[3] << 16), x[4] | (x[5] << 16), x[6] | (x[7] << 16));
-        }
-        *reinterpret_cast<uint4*>(&s_tile[t][row * 512 + lane * 8]) = u;
-    }
+    work.stage_split<D, NW>(v, s_tile[0]);
     const int c = col0 + wv * 32 + col;
     const bool valid = c < n_cols;
     const int draft = (valid ? c : 0) / v.G;
@@ -292,9 +376,7 @@ __device__ __forceinline__ void attend_drafts_split(const SpkvView& v, const uin
     bf16x8 qb[NS];
 #pragma unroll
     for (int sl = 0; sl < NS; ++sl) qb[sl] = *reinterpret_cast<const bf16x8*>(qrow + sl * 16 + half * 8);
-    const int T = v.t_pair[work.pair];
-    const TreePath path = tree_path(work.tree.parents + work.row0, n);
-    const unsigned long long word = tree_seen(v, path, work.tree.f, h, work.row0, n, T), seen = lane_word(word, draft);
+    const unsigned long long word = work.seen(v, v.t_pair[work.pair]), seen = lane_word(word, draft);
     __syncthreads();
     f32x16 s[2], acc[NB];
 #pragma unroll
@@ -351,8 +433,8 @@ __device__ __forceinline__ void attend_drafts_split(const SpkvView& v, const uin
         __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0): the stores above come first
         for (int i = 0; i < n_here; ++i) {
             const int cc = col0 + wv * 32 + i, dd = cc / v.G;
-            careful_tree_sums<D>(kr, vr, stride, q + ((size_t)(work.row0 + dd) * v.Hq + (size_t)h * v.G + (cc - dd * v.G)) * D,
-                                 lane_word(word, dd), scale_log2e, __shfl(ref, i), false, to + (size_t)i * D);
+            careful_tree_sums<D>(work.keys(v), work.values(v), work.stride(v), q + work.result(v, cc) * D, lane_word(word, dd), scale_log2e,
+                                 __shfl(ref, i), false, to + (size_t)i * D);
         }
     }
 }
@@ -362,9 +444,9 @@ constexpr int kDraftWeight = 3;
 // itself.  Its half-pages go from memory into 16 KB of LDS of its own (D = 128) in operand order, keys and values in turn: while
 // the scores are weighed the next keys arrive, while these are multiplied the next values.  No wave waits for another.
 // Read once, the half-pages are loaded as such (nt: 484 MB in 98 us, 114 without; 94 MB that the caches hold 30, 29 without).
-// The queries are shared, in LDS.  The drafts are up to two half-pages more for one wave of the list's first range.
-template <int D>
-__device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e, const TreeWork& work) {
+// The queries are shared, in LDS.  The drafts are up to two half-pages more in the list's first range, for a wave each.
+template <int D, bool W>
+__device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e, const TreeWork<W>& work) {
     constexpr int NS = D / 16, NB = D / 32, kRow = D + 4, kHalfElems = 2 * kHalfTokens * D;
     __shared__ __attribute__((aligned(16))) uint16_t s_q[2 * NS * 512];
     __shared__ __attribute__((aligned(16))) float s_acc[4][64 * kRow];         // (half-pages before)
@@ -372,19 +454,24 @@ __device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint1
     static_assert(sizeof(s_acc) >= (size_t)8 * kHalfElems * 2, "the half-pages' room");
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int pair = work.pair, h = work.h, n = work.n;
+    const int pair = work.pair, h = work.h;
     const FirstPages first_ids = first_pages(v, pair);
     const ShareList list = share_list(v, pair);
     const int n_cols = work.columns(v), c0 = work.block * 64;
     if (c0 >= n_cols) return;
-    const int tiles = (n + kHalfTokens - 1) >> 5, nA = list.nA;
+    const int tiles = (work.n + kHalfTokens - 1) >> 5, nA = list.nA;
     auto cut = [&](int j) -> int {                            // the drafts count kDraftWeight half-pages each, in the first range
         const int x = (int)((int64_t)j * (2 * list.n_hp - nA + kDraftWeight * tiles) / work.ranges) - kDraftWeight * tiles;
         return x <= 0 ? 0 : x <= nA ? x : nA + (x - nA + 1) / 2;
     };
     const int r_begin = cut(work.range), r_end = work.range + 1 == work.ranges ? list.n_hp : cut(work.range + 1);
-    const int x_begin = r_begin + (r_end - r_begin) * wv / 8, x_end = r_begin + (r_end - r_begin) * (wv + 1) / 8;
-    const bool ring = x_end > nA;
+    const int with_drafts = work.range == 0 ? tiles : 0;      // the first waves take one half-page of them each
+    auto cut_wave = [&](int w) -> int {
+        const int all = r_end - r_begin + kDraftWeight * with_drafts;
+        return r_begin + max(0, all * w / 8 - kDraftWeight * min(w, with_drafts));
+    };
+    const int x_begin = cut_wave(wv), x_end = cut_wave(wv + 1);
+    const bool ring = x_end > nA, drafts = wv < with_drafts;
     SharePages pages = share_pages(v, pair, first_ids, x_begin >> 1);
 
     const unsigned k_lane = ((((col >> 3) & 1) * (D / 8) + half) * 16 + 8 * (col >> 4) + 4 * ((col >> 2) & 1) + (col & 3)) * 16;
@@ -403,11 +490,14 @@ __device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint1
     // Loads into LDS and reads of it: the compiler does not know that they belong together.
     auto read_all = [&]() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); };           // what was read has arrived
     const char* base = nullptr;
-    if (x_begin < x_end) {
+    auto send_first = [&]() {
+        if (x_begin >= x_end) return;
         base = page_of(x_begin);
         send_k(base);
         send_v(base);
-    }
+    };
+    if (!drafts) send_first();
+    if (with_drafts > 0) work.template stage_split<D, 8>(v, reinterpret_cast<uint16_t*>(&s_acc[0][0]));     // into the first waves' slots
     int place[2], draft[2], least = 0, most = 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -552,51 +642,27 @@ __device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint1
         read_all();
         if (more) send_v(base);
     };
+    unsigned long long word = 0ull;
+    if (drafts) {
+        word = work.seen(v, list.T);
+        scores();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const unsigned mine = (unsigned)(lane_word(word, draft[i]) >> (32 * wv));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[i][e] = ((mine >> (16 * (e >> 3) + 8 * half + (e & 7))) & 1u) ? s[i][e] : SPKV_NEG_INF;
+        }
+        weigh(0);
+        weigh(1);
+        accumulate(0xffffu);
+        read_all();
+        send_first();
+    }
     int x = x_begin;
 #pragma unroll 1
     for (; x < full; ++x) turn(x, std::false_type());
 #pragma unroll 1
     for (; x < x_end; ++x) turn(x, std::true_type());
-    const bool drafts = work.range == 0 && wv == 0;
-    unsigned long long word = 0ull;
-    const uint16_t* kr = work.tree.k + ((size_t)work.row0 * v.Hkv + h) * D;
-    const uint16_t* vr = work.tree.v + ((size_t)work.row0 * v.Hkv + h) * D;
-    const int stride = v.Hkv * D;
-    if (drafts) {
-        const TreePath path = tree_path(work.tree.parents + work.row0, n);
-        word = tree_seen(v, path, work.tree.f, h, work.row0, n, list.T);
-#pragma unroll 1
-        for (int t = 0; t < tiles; ++t) {                     // a half-page of them into the slot, then as any other
-#pragma unroll 2
-            for (int sl = 0; sl < NS; ++sl) {
-                const int key = 32 * t + 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
-                uint4 u = {0u, 0u, 0u, 0u};
-                if (key < n) u = *reinterpret_cast<const uint4*>(kr + (size_t)key * stride + 16 * sl + 8 * half);
-                *reinterpret_cast<uint4*>(slot + sl * 512 + lane * 8) = u;
-            }
-#pragma unroll 2
-            for (int j = 0; j < 2 * NB; ++j) {
-                const int d = 32 * (j % NB) + col, key0 = 32 * t + 16 * (j / NB) + 8 * half;
-                unsigned y[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = key0 + e < n ? vr[(size_t)(key0 + e) * stride + d] : 0u;
-                *reinterpret_cast<uint4*>(slot + kHalfTokens * D + j * 512 + lane * 8) =
-                    make_uint4(y[0] | (y[1] << 16), y[2] | (y[3] << 16), y[4] | (y[5] << 16), y[6] | (y[7] << 16));
-            }
-            read_all();
-            scores();
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const unsigned mine = (unsigned)(lane_word(word, draft[i]) >> (32 * t));
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[i][e] = ((mine >> (16 * (e >> 3) + 8 * half + (e & 7))) & 1u) ? s[i][e] : SPKV_NEG_INF;
-            }
-            weigh(0);
-            weigh(1);
-            accumulate(0xffffu);
-            read_all();
-        }
-    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) l[i] += __shfl_xor(l[i], 32);
     const bool odd = odd_sums(acc[0], NB, l[0]) || odd_sums(acc[1], NB, l[1]);
@@ -606,16 +672,16 @@ __device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint1
         const ShareRow sr = work.row(v, c0 + c, true);
         const uint16_t* qrow = q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D;
         careful_sums<D>(range, qrow, sr.place, ref, to);
-        if (drafts) {
-            __builtin_amdgcn_wave_barrier();
-            careful_tree_sums<D>(kr, vr, stride, qrow, lane_word(word, sr.row - work.row0), scale_log2e, ref, true, to);
+        if (drafts) {                                         // (of this wave's half-page of them)
+            const unsigned long long mine = lane_word(word, sr.row - work.row0) & (0xffffffffull << (32 * wv));
+            work.template add_careful<D>(v, qrow, mine, scale_log2e, ref, to);
         }
         read_all();
     };
     bool again = false;
     if (__builtin_expect(__ballot(odd) != 0ull, 0))
         again = (ring && least != most && careful_needed<D>(careful_range(v, list, scale_log2e, x_begin, x_end), least, most)) ||
-                (drafts && careful_tree_needed<D>(vr, stride, n));
+                (drafts && work.template careful_needed<D>(v));
     // Four waves leave their sums in LDS, the other four add theirs.
     __syncthreads();                                          // the half-pages are no longer read
     float* mine = s_acc[wv & 3];
@@ -682,7 +748,7 @@ __device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint1
         }
     }
     __syncthreads();
-    const size_t pc0 = work.part0(v);
+    const size_t pc0 = W ? 0 : work.part0(v);
     for (int e = tid; e < n_here * (D / 4); e += 512) {
         const int c = e / (D / 4), d = (e - c * (D / 4)) * 4;
         float M = SPKV_NEG_INF, sum = 0.f;
@@ -697,39 +763,45 @@ __device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint1
             a += *reinterpret_cast<const f32x4*>(s_acc[w] + c * kRow + d) * sc;
             sum += ml.y * sc;
         }
-        *reinterpret_cast<f32x4*>(v.part_acc + (pc0 + c0 + c) * D + d) = a;
-        if (d == 0) work.part_ml<D>(v)[pc0 + c0 + c] = make_float2(M, sum);
+        if constexpr (W) {
+            work.template store<D>(v, c0 + c, d, a, M, sum);
+        } else {
+            *reinterpret_cast<f32x4*>(v.part_acc + (pc0 + c0 + c) * D + d) = a;
+            if (d == 0) work.template part_ml<D>(v)[pc0 + c0 + c] = make_float2(M, sum);
+        }
     }
 }
 
-template <int D, int NQ>
+template <int D, int NQ, bool W>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, NQ == 1 ? 3 : 2)))
 void spkv_tree_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvTree tree, SpkvTreeTable table) {
-    TreeWork work(v, tree, table, (int)blockIdx.x, 16 * NQ);
-    if (work.range < 0) attend_drafts_few<D, NQ>(v, q, scale_log2e, work);
-    else attend_list_few<D, NQ>(v, q, scale_log2e, work);
+    TreeWork<W> work(v, tree, table, (int)blockIdx.x, 16 * NQ);
+    if constexpr (!W)
+        if (work.range < 0) return attend_drafts_few<D, NQ>(v, q, scale_log2e, work);
+    attend_list_few<D, NQ>(v, q, scale_log2e, work);
 }
 
-template <int D, int NW>
+template <int D, int NW, bool W>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 2 ? 1 : 2, 2)))
 void spkv_tree_split(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvTree tree, SpkvTreeTable table) {
     __shared__ __attribute__((aligned(16))) uint16_t s_tile[kSplitSlots<NW>][2 * kHalfTokens * D];
-    TreeWork work(v, tree, table, (int)blockIdx.x, 32 * NW);
-    if (work.range < 0) attend_drafts_split<D, NW>(v, q, scale_log2e, work, s_tile);
-    else attend_list_split<D, NW>(v, q, scale_log2e, work, s_tile);
+    TreeWork<W> work(v, tree, table, (int)blockIdx.x, 32 * NW);
+    if constexpr (!W)
+        if (work.range < 0) return attend_drafts_split<D, NW>(v, q, scale_log2e, work, s_tile);
+    attend_list_split<D, NW>(v, q, scale_log2e, work, s_tile);
 }
 
-template <int D>
+template <int D, bool W>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void spkv_tree_own_copies(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvTree tree, SpkvTreeTable table) {
-    TreeWork work(v, tree, table, (int)blockIdx.x, 64);
-    attend_own_copies<D>(v, q, scale_log2e, work);
+    TreeWork<W> work(v, tree, table, (int)blockIdx.x, 64);
+    attend_own_copies<D, W>(v, q, scale_log2e, work);
 }
 
 // The join: D / 4 threads own a column, four consecutive elements each; S such groups share a column, each with every
 // S-th of its partial results, and meet in LDS.
 template <int D, int S>
-__global__ __launch_bounds__(256, 8) void spkv_tree_merge(SpkvView v, SpkvTree tree, SpkvTreeTable table, int width, uint16_t* out, float* lse) {
+__global__ __launch_bounds__(256, 8) void spkv_tree_merge(SpkvView v, SpkvTree tree, SpkvTreeTable table, int width) {
     constexpr int TPC = D / 4, CPB = 256 / TPC, kFold = S > 1 ? 5 : 2, kCols = CPB / S;
     __shared__ f32x4 s_num[S > 1 ? CPB : 1][S > 1 ? TPC : 1];
     __shared__ float2 s_ml[S > 1 ? CPB : 1];
@@ -794,15 +866,10 @@ __global__ __launch_bounds__(256, 8) void spkv_tree_merge(SpkvView v, SpkvTree t
     }
     if (!exists) return;
     const float inv = den == 0.f ? 0.f : 1.0f / den;
-    uint2 packed;
-    packed.x = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)(num[0] * inv)) |
-               ((unsigned)__builtin_bit_cast(uint16_t, (__bf16)(num[1] * inv)) << 16);
-    packed.y = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)(num[2] * inv)) |
-               ((unsigned)__builtin_bit_cast(uint16_t, (__bf16)(num[3] * inv)) << 16);
     const int draft = c / v.G;
     const size_t id = (size_t)(tree.row0 + table.cu[at] + draft) * v.Hq + (size_t)h * v.G + (c - draft * v.G);
-    *reinterpret_cast<uint2*>(out + id * D + d) = packed;
-    if (lse != nullptr && d == 0) lse[id] = den == 0.f ? SPKV_NEG_INF : (M + log2f(den)) * 0.6931471805599453f;
+    store_result(tree.out + id * D + d, num * inv);
+    if (tree.lse != nullptr && d == 0) tree.lse[id] = log_of_sum(M, den);
 }
 
 // The kernel of own copies has the higher rate on long lists and the longer start: 33 to 64 columns, split / own copies, us: 484 MB
@@ -813,40 +880,53 @@ SpkvTreeKernel spkv_tree_kernel(int n_cols, int64_t half_pages) {
     return n_cols <= 16 ? kTreeFew16 : n_cols <= 32 ? kTreeFew32 : n_cols <= 64 ? (half_pages >= kTreeOwnHalfPages ? kTreeOwnCopies : kTreeSplit64)
                         : n_cols <= 128 ? kTreeSplit128 : kTreeSplit256;
 }
+// Whole lists, one to a compute unit: eight waves to a list are better than two.  us, 16 drafts of 4 heads, split / own copies: 8
+// sequences of 500 19.4 / 17.5, 32 of 1000 27 / 21.5, but 64 of 300 (512 lists) 25 / 36.6; D = 64, 8 drafts of 8 heads, 32 of 1000 18.5 / 13.4.
+SpkvTreeKernel spkv_tree_kernel_whole(SpkvTreeKernel k, int64_t lists, int64_t compute_units) {
+    return k == kTreeSplit64 && lists <= compute_units ? kTreeOwnCopies : k;
+}
 int spkv_tree_width(SpkvTreeKernel k) {
     return k == kTreeFew16 ? 16 : k == kTreeFew32 ? 32 : k == kTreeOwnCopies || k == kTreeSplit64 ? 64 : k == kTreeSplit128 ? 128 : 256;
 }
 int spkv_tree_resident(SpkvTreeKernel k) { return k == kTreeOwnCopies || k == kTreeSplit256 ? 1 : 2; }
 
 constexpr int kTreeMergeRound = 2048;
+template <int D, bool W>
+static void launch_lists(const SpkvView& v, const uint16_t* q, float sl, SpkvTreeKernel kernel, const SpkvTree& tree, const SpkvTreeTable& table,
+                         hipStream_t s) {
+    const dim3 grid((unsigned)(tree.n_own + tree.n_units));
+    switch (kernel) {
+        case kTreeFew16: spkv_tree_few<D, 1, W><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeFew32: spkv_tree_few<D, 2, W><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeOwnCopies: spkv_tree_own_copies<D, W><<<grid, dim3(512), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeSplit64: spkv_tree_split<D, 2, W><<<grid, dim3(128), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeSplit128: spkv_tree_split<D, 4, W><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeSplit256: spkv_tree_split<D, 8, W><<<grid, dim3(512), 0, s>>>(v, q, sl, tree, table); break;
+    }
+}
 template <int D>
 static hipError_t launch_tree(const SpkvView& v, const uint16_t* q, float sl, SpkvTreeKernel kernel, const SpkvTree& tree,
-                              const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, uint16_t* out, float* lse, hipStream_t s) {
-    const dim3 grid((unsigned)(tree.n_own + tree.n_units));
+                              const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, hipStream_t s) {
     const int width = spkv_tree_width(kernel);
-    switch (kernel) {
-        case kTreeFew16: spkv_tree_few<D, 1><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
-        case kTreeFew32: spkv_tree_few<D, 2><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
-        case kTreeOwnCopies: spkv_tree_own_copies<D><<<grid, dim3(512), 0, s>>>(v, q, sl, tree, table); break;
-        case kTreeSplit64: spkv_tree_split<D, 2><<<grid, dim3(128), 0, s>>>(v, q, sl, tree, table); break;
-        case kTreeSplit128: spkv_tree_split<D, 4><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
-        case kTreeSplit256: spkv_tree_split<D, 8><<<grid, dim3(512), 0, s>>>(v, q, sl, tree, table); break;
+    if (tree.whole) {
+        launch_lists<D, true>(v, q, sl, kernel, tree, table, s);
+        return hipGetLastError();
     }
+    launch_lists<D, false>(v, q, sl, kernel, tree, table, s);
     constexpr int CPB = 256 / (D / 4);
     int share = std::min(8, CPB);
     while (share > 1 && (n_pairs * ((most_cols * share + CPB - 1) / CPB) > kTreeMergeRound || share > most_ranges + 1)) share >>= 1;
     const dim3 merge((unsigned)((most_cols * share + CPB - 1) / CPB), (unsigned)n_pairs);
-    if (share == 8) spkv_tree_merge<D, 8><<<merge, dim3(256), 0, s>>>(v, tree, table, width, out, lse);
-    else if (share == 4) spkv_tree_merge<D, 4><<<merge, dim3(256), 0, s>>>(v, tree, table, width, out, lse);
-    else if (share == 2) spkv_tree_merge<D, 2><<<merge, dim3(256), 0, s>>>(v, tree, table, width, out, lse);
-    else spkv_tree_merge<D, 1><<<merge, dim3(256), 0, s>>>(v, tree, table, width, out, lse);
+    if (share == 8) spkv_tree_merge<D, 8><<<merge, dim3(256), 0, s>>>(v, tree, table, width);
+    else if (share == 4) spkv_tree_merge<D, 4><<<merge, dim3(256), 0, s>>>(v, tree, table, width);
+    else if (share == 2) spkv_tree_merge<D, 2><<<merge, dim3(256), 0, s>>>(v, tree, table, width);
+    else spkv_tree_merge<D, 1><<<merge, dim3(256), 0, s>>>(v, tree, table, width);
     return hipGetLastError();
 }
 
 hipError_t spkv_launch_tree(const SpkvView& v, const uint16_t* q, float sm_scale, SpkvTreeKernel kernel, const SpkvTree& tree,
-                            const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, uint16_t* out, float* lse,
-                            hipStream_t s) {
+                            const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, hipStream_t s) {
     const float sl = sm_scale * 1.4426950408889634f;
-    return v.D == 128 ? launch_tree<128>(v, q, sl, kernel, tree, table, n_pairs, most_cols, most_ranges, out, lse, s)
-                      : launch_tree<64>(v, q, sl, kernel, tree, table, n_pairs, most_cols, most_ranges, out, lse, s);
+    return v.D == 128 ? launch_tree<128>(v, q, sl, kernel, tree, table, n_pairs, most_cols, most_ranges, s)
+                      : launch_tree<64>(v, q, sl, kernel, tree, table, n_pairs, most_cols, most_ranges, s);
 }

@@ -156,6 +156,50 @@ def test_lists_long_enough_for_copies_of_their_own(hq, hk, d, lengths, counts):
     x.check_tree(sm_scale=0.0)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,hq,hk", [(1, 8, 2), (4, 8, 2), (8, 8, 2), (13, 8, 2), (16, 8, 2), (29, 8, 2), (32, 8, 2), (50, 8, 2), (64, 8, 2), (64, 8, 1),
+                                     (64, 2, 2)])
+def test_one_long_list_and_many_short_ones(n, hq, hk, d):
+    """A list in ranges that meet in a join; many lists that are a workgroup's each, drafts and results with them."""
+    one = Trees(1, hq=hq, hk=hk, d=d, window=77, seed=n + d, keep=0.9)
+    one.append([2900])
+    one.drafts([n], seed=n)
+    one.check_tree()
+    many = Trees(26, hq=hq, hk=hk, d=d, window=77, seed=n + d, keep=0.5, context=500)
+    many.append([0, 1, 31, 32, 33, 64, 65, 77, 78, 100, 160, 161, 200, 256, 300] + [b + 60 for b in range(11)])
+    for most in (n, max(1, n - 3)):
+        many.drafts([most if b % 3 else max(1, most - b) for b in range(26)], seed=n)
+        many.check_tree()
+    many.check_tree(sm_scale=0.0)
+
+
+@pytest.mark.parametrize("batch", [1, 26])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n", [4, 8, 12, 30, 64])
+def test_odd_values_in_ranges_and_in_whole_lists(n, d, batch):
+    """Values that are not finite, in drafts and in ring keys that only the drafts near the newest token see."""
+    x = Trees(batch, hq=8, hk=2, d=d, window=30, seed=n + d, keep=0.9)
+    lengths = [2900] if batch == 1 else [7 * b for b in range(batch)]
+    k, v, f = x.rows(sum(lengths))
+    last = sum(lengths) - 30                                  # the last sequence's window: its gates off, its oldest values odd
+    f[last:] -= 100
+    v[last], v[last + 1, :, 3], k[last + 2, 1] = float("inf"), float("nan"), float("nan")
+    x.cache.append(k, v, f, x.cu(lengths))
+    v[last:last + 2], k[last + 2] = 0, 0                      # (drafts three deep and more do not see them)
+    x.oracle.append(to_numpy_f32(k), to_numpy_f32(v), to_numpy_f32(f), x.cu(lengths))
+    counts = [n] * batch
+    x.drafts(counts, lambda r, m: [i - 1 for i in range(m - 1)] + [-1])
+    x.f -= 100
+    top = n * (batch - 1)
+    bad = top + n - 2                                         # the chain's last draft; the last draft of all hangs elsewhere
+    x.v[bad, :, 5] = float("-inf")
+    out, lse = x.score()
+    for r in (top, top + 1, bad, top + n - 1):
+        assert not bool(torch.isfinite(out[r]).all()), r
+    x.v[bad] = 0
+    x.check_tree(got=(out, lse), rows=[r for r in range(n * batch) if r not in (top, top + 1, top + 2, bad, top + n - 1)])
+
+
 @pytest.mark.parametrize("long", [False, True])
 @pytest.mark.parametrize("n", [40, 64])
 def test_odd_values_among_short_and_long_lists(n, long):
