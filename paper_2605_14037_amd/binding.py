@@ -801,12 +801,18 @@ class SPKVCache:
         qp = _dev_ptr(q, torch.bfloat16, shape, "q")
         fp = _dev_ptr(util_logits, torch.float32, kv_shape[:2], "util_logits") if util_logits is not None else None
         pp = _dev_ptr(parents, torch.int32, (total,), "parents")
-        if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
-        op = _dev_ptr(out, torch.bfloat16, shape, "out")
-        if lse is None and want_lse:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=q.device)
-        lp = _dev_ptr(lse, torch.float32, shape[:2], "lse") if lse is not None else None
+        if out is None:                       # (with strides: half a microsecond less than torch.empty)
+            out = torch.empty_strided(shape, (shape[1] * shape[2], shape[2], 1), dtype=torch.bfloat16, device=q.device)
+            op = out.data_ptr()
+        else:
+            op = _dev_ptr(out, torch.bfloat16, shape, "out")
+        if lse is not None:
+            lp = _dev_ptr(lse, torch.float32, shape[:2], "lse")
+        elif want_lse:
+            lse = torch.empty_strided(shape[:2], (shape[1], 1), dtype=torch.float32, device=q.device)
+            lp = lse.data_ptr()
+        else:
+            lp = None
         _check(self.lib.spkv_score_tree(self.handle, kp, vp, fp, qp, pp, cu, op, lp, float(sm_scale), _stream()),
                "spkv_score_tree")
         return (out, lse) if lse is not None else out
