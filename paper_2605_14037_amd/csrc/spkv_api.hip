@@ -1989,11 +1989,12 @@ int64_t tree_half_pages(const spkv_cache* c, int p, int64_t room) {
 }
 // What a launch takes, ns: its longest unit, or all of them shared among the workgroups that the chip holds.  (D = 64 three quarters
 // of it.  From 1 to 128 sequences of 300 to 4000 tokens, 4 to 64 drafts of 4 heads; only for the choice below.)
-int64_t tree_time(SpkvTreeKernel kernel, int64_t resident, int64_t units, int64_t longest, int64_t work) {
+int64_t tree_time(SpkvTreeKernel kernel, int head_dim, int64_t resident, int64_t units, int64_t longest, int64_t work) {
     static const int start[] = {8100, 8500, 13200, 10200, 10500, 14900}, half_page[] = {300, 550, 320, 700, 700, 780};
-    return std::max(start[kernel] + half_page[kernel] * longest, (start[kernel] * units + half_page[kernel] * work) / resident);
+    const int64_t t = std::max(start[kernel] + half_page[kernel] * longest, (start[kernel] * units + half_page[kernel] * work) / resident);
+    return head_dim == 64 ? t * 3 / 4 : t;
 }
-constexpr int kTreeJoin = 4000, kTreeJoinBytesPerUs = 6000000;       // the second launch, and partial results written and read
+constexpr int kTreeJoin = 5500, kTreeJoinBytesPerUs = 6000000;       // the second launch, and partial results written and read
 
 // Or every list in one range, with the drafts, its results written at once (tree->whole): two to five times less to write, and one
 // launch.  us, 4 / 16 / 64 drafts, cut / whole: one sequence of 300 tokens 14 / 10, 13 / 17, 19 / 22, one of 2048 12 / 13, 14 / 30, 23 / 33,
@@ -2003,27 +2004,34 @@ int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, SpkvTreeKernel
     const int width = spkv_tree_width(kernel);
     const int Hkv = c->cfg.n_kv_heads, G = c->carve.G;
     int32_t hp[kTreePairs], copies[kTreePairs];
-    int64_t work = 0, lists = 0, longest_list = 0;
+    int64_t work = 0, lists = 0, longest_list = 0, drafts = 0;
+    const int alone = tree->alone = spkv_tree_few_columns(kernel) ? 1 : 0;
+    tree->whole = 0;
     for (int i = 0; i < n_pairs; ++i) {
-        const int p = tree->pair0 + i, b = p / Hkv;
+        const int p = tree->pair0 + i, b = p / Hkv, weight = alone ? 0 : spkv_tree_draft_weight(kernel, cu[b + 1] - cu[b]);
         copies[i] = ((cu[b + 1] - cu[b]) * G + width - 1) / width;
         hp[i] = (int32_t)tree_half_pages(c, p, room) + 2 * ((std::min(c->T[b], c->cfg.window) + kHalfTokens - 1) / kHalfTokens);
-        work += (int64_t)hp[i] * copies[i];
-        lists += copies[i];
         if (copies[i] > 0) longest_list = std::max<int64_t>(longest_list, hp[i]);
+        hp[i] += weight;
+        work += (int64_t)hp[i] * copies[i];
+        drafts = std::max<int64_t>(drafts, weight);
+        lists += copies[i];
     }
     const int cus = spkv_compute_units();
     const int64_t round = cus > 0 ? cus : 256, resident = round * spkv_tree_resident(kernel);
     const int64_t start = spkv_tree_resident(kernel) == 1 ? kTreeStartAlone : kTreeStart;
-    int64_t unit = 0, best = 0, cut_time = 0;
+    fit -= alone * n_pairs;
+    auto ranges_of = [&](int i, int64_t unit) -> int64_t { return std::min<int64_t>(255, std::max<int64_t>(1, (hp[i] + unit - 1) / unit)); };
+    int64_t unit = (int64_t)1 << 40, best = 0, cut_time = 0;
     for (int k = 1; k <= 4; ++k) {
         const int64_t target = std::min(fit, (int64_t)k * round);
-        int64_t u = std::max<int64_t>(k > 1 ? kTreeMinUnitMore : kTreeMinUnit, (work + target - 1) / target), total = 0, longest = 0, most = 0;
+        int64_t u = std::max<int64_t>(k > 1 ? kTreeMinUnitMore : kTreeMinUnit, (work + target - 1) / std::max<int64_t>(target, 1));
+        int64_t total = 0, longest = 0, most = 0;
         for (int guard = 0; guard < 64; ++guard) {
             total = longest = most = 0;
             for (int i = 0; i < n_pairs; ++i) {
                 if (copies[i] == 0) continue;
-                const int64_t r = std::min<int64_t>(255, std::max<int64_t>(1, (hp[i] + u - 1) / u));
+                const int64_t r = ranges_of(i, u);
                 total += r * copies[i];
                 longest = std::max(longest, (hp[i] + r - 1) / r);
                 most = std::max(most, r);
@@ -2035,21 +2043,22 @@ int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, SpkvTreeKernel
         if (k > 1 && time >= best) continue;
         best = time;
         unit = total > fit ? (int64_t)1 << 40 : u;           // (no room for ranges: one each)
-        cut_time = tree_time(kernel, resident, total, longest, work) + kTreeJoin +
-                   (total + tree->n_own) * width * c->cfg.head_dim * 8 * 1000 / kTreeJoinBytesPerUs;
+        cut_time = tree_time(kernel, c->cfg.head_dim, resident, total, std::max<int64_t>(0, longest - drafts), work - drafts * lists) + kTreeJoin +
+                   (total + alone * n_pairs) * width * c->cfg.head_dim * 8 * 1000 / kTreeJoinBytesPerUs;
     }
-    const SpkvTreeKernel alone = spkv_tree_kernel_whole(kernel, lists, round);
-    if ((room == 0 || lists >= round) && tree_time(alone, round * spkv_tree_resident(alone), lists, longest_list, work) < cut_time) {
-        *chosen = alone;
+    const SpkvTreeKernel uncut = spkv_tree_kernel_whole(kernel, lists, round);
+    if ((room == 0 || lists >= round) &&
+        tree_time(uncut, c->cfg.head_dim, round * spkv_tree_resident(uncut), lists, longest_list, work - drafts * lists) < cut_time) {
+        *chosen = uncut;
         tree->whole = 1;
-        tree->n_own = 0;
         unit = (int64_t)1 << 40;
+        tree->alone = 0;
     }
     // The longest ranges begin first.
     uint16_t order[kTreePairs];
     int32_t size[kTreePairs];
     for (int i = 0; i < n_pairs; ++i) {
-        const int64_t r = std::min<int64_t>(255, std::max<int64_t>(1, (hp[i] + unit - 1) / unit));
+        const int64_t r = ranges_of(i, unit);
         order[i] = (uint16_t)i;
         size[i] = (int32_t)((hp[i] + r - 1) / r);
     }
@@ -2064,7 +2073,7 @@ int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, SpkvTreeKernel
             continue;
         }
         const int p = order[i];
-        const int64_t r = std::min<int64_t>(255, std::max<int64_t>(1, (hp[p] + unit - 1) / unit));
+        const int64_t r = ranges_of(p, unit);
         most = std::max(most, (int)r);
         end += r * copies[p];
         table->end[i] = (uint16_t)end;
@@ -2115,11 +2124,11 @@ int spkv_score_tree(spkv_cache_t* c, const void* k, const void* v, const float* 
     tree.parents = parents;
     tree.out = static_cast<uint16_t*>(out);
     tree.lse = lse;
-    tree.n_blocks = (n_max * G + width - 1) / width;
+    const int n_blocks = (n_max * G + width - 1) / width;    // of the pair with the most columns
     // The partial results lie in the cache's buffers of them.  What does not fit a launch (only caches of hundreds of pairs
     // with many columns each) takes several.
     const int64_t slots = (int64_t)c->carve.max_items * G / width;
-    int64_t per = std::min<int64_t>(kTreePairs, slots / (2 * tree.n_blocks));
+    int64_t per = std::min<int64_t>(kTreePairs, slots / (2 * n_blocks));
     if (per < 1) return SPKV_E_CAPACITY;
     if (per > Hkv) per -= per % Hkv;
     for (int p0 = 0; p0 < c->carve.n_pairs; p0 += (int)per) {
@@ -2131,11 +2140,9 @@ int spkv_score_tree(spkv_cache_t* c, const void* k, const void* v, const float* 
         const int seqs = (p0 + n_pairs - 1) / Hkv - tree.seq0 + 1;
         if (cu_seqlens[tree.seq0 + seqs] == tree.row0) continue;
         for (int i = 0; i <= seqs; ++i) table.cu[i] = (uint16_t)(cu_seqlens[tree.seq0 + i] - tree.row0);
-        tree.whole = 0;
-        tree.n_own = kernel == kTreeOwnCopies ? 0 : n_pairs * tree.n_blocks;
         SpkvTreeKernel chosen = kernel;
-        const int most = tree_cut(c, cu_seqlens, n_pairs, &chosen, room, std::min<int64_t>(slots - tree.n_own, 32767), &tree, &table);
-        if (tree.n_units + tree.n_own > slots) return SPKV_E_CAPACITY;
+        const int most = tree_cut(c, cu_seqlens, n_pairs, &chosen, room, std::min<int64_t>(slots, 32767), &tree, &table);
+        if (tree.n_units + tree.alone * n_pairs > slots) return SPKV_E_CAPACITY;
         if (spkv_launch_tree(c->view, static_cast<const uint16_t*>(q), sm_scale, chosen, tree, table, n_pairs, n_max * G, most, s) != hipSuccess)
             return SPKV_E_HIP;
     }

@@ -373,8 +373,7 @@ struct SpkvTree {
     float* lse;                  // or null
     int32_t pair0, seq0, row0;
     int32_t whole;               // every list is one range, which takes the drafts and writes the results
-    int32_t n_own;               // units of the drafts themselves, a pair's blocks of columns, behind those of the lists; 0: the first range takes them
-    int32_t n_blocks;            // ... of the pair with the most columns
+    int32_t alone;               // 1: the drafts are units of their own, a pair's each, behind the lists'
     int32_t n_units;             // units of the lists
 };
 struct SpkvTreeTable {
@@ -388,7 +387,17 @@ struct SpkvTreeTable {
 enum SpkvTreeKernel { kTreeFew16, kTreeFew32, kTreeOwnCopies, kTreeSplit64, kTreeSplit128, kTreeSplit256 };
 SpkvTreeKernel spkv_tree_kernel(int n_cols, int64_t half_pages);
 SpkvTreeKernel spkv_tree_kernel_whole(SpkvTreeKernel kernel, int64_t lists, int64_t compute_units);      // ... where no list is cut
-int spkv_tree_width(SpkvTreeKernel kernel);       // columns of a workgroup
+constexpr __host__ __device__ int spkv_tree_width(SpkvTreeKernel k) {         // columns of a workgroup
+    return k == kTreeFew16 ? 16 : k == kTreeFew32 ? 32 : k == kTreeOwnCopies || k == kTreeSplit64 ? 64 : k == kTreeSplit128 ? 128 : 256;
+}
+// Few columns: the drafts are units of their own.
+constexpr __host__ __device__ bool spkv_tree_few_columns(SpkvTreeKernel k) { return k == kTreeFew16 || k == kTreeFew32; }
+// Half-pages of 32 keys that n drafts count for where they go with a range.
+constexpr int kOwnDrafts = 3;
+constexpr __host__ __device__ int spkv_tree_draft_weight(SpkvTreeKernel k, int n) {
+    const int tiles = (n + 31) / 32;
+    return k == kTreeOwnCopies ? kOwnDrafts * tiles : spkv_tree_few_columns(k) ? 6 * tiles : (4 + tiles) * (tiles > 0);
+}
 int spkv_tree_resident(SpkvTreeKernel kernel);    // workgroups that a compute unit holds
 hipError_t spkv_launch_tree(const SpkvView& v, const uint16_t* q, float sm_scale, SpkvTreeKernel kernel, const SpkvTree& tree,
                             const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, hipStream_t s);

@@ -220,8 +220,10 @@ struct ShareRow {
 //   columns(v)                       columns of the list, asked once and before those that follow
 //   row(v, c, ring)                  ShareRow of column c; ring: the place is wanted.  The whole wave asks.
 //   part(v), part_ml<D>(v), part0(v) partial sums and (m, l), those of column c at part0 + c
-//   kWhole                           the range is all there is (one range, of the whole list): the workgroup takes the drafts, too,
-//                                    and writes the columns' results; see TreeWork in spkv_tree.hip for what is asked of it then
+//   begin(list, j)                   first half-page of the list's range j
+//   kTree                            there are drafts, too: keys that every column sees some of, which the workgroup of a list's first
+//                                    range takes (drafts()); see TreeWork in spkv_tree.hip for what is asked of it then
+//   kWhole                           the range is the whole list, and what the workgroup has at the end is the columns' result
 
 // Up to 16 NQ columns.  A half-page's operands come straight from memory (1 KB a load, as in spkv_decode_split) and are
 // used for all NQ groups of 16 columns: scores of all groups -- the next half-page's keys are sent for -- then
@@ -238,18 +240,17 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
     __shared__ __attribute__((aligned(16))) uint16_t s_q[NQ == 1 ? 1 : NQ * NS][512];
     const int tid = threadIdx.x, lane = tid & 63, kc = lane >> 4, n = lane & 15;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int pair = work.pair, h = work.h, j = work.range, ranges = work.ranges;
+    const int pair = work.pair, h = work.h, j = work.range;
     const FirstPages first_ids = first_pages(v, pair);
     const ShareList list = share_list(v, pair);
     const int n_cols = work.columns(v);
     if (n_cols <= 0) return;
     const int nA = list.nA;
-    const int r_begin = list.begin(j, ranges), r_end = list.begin(j + 1, ranges);
-    // the first wave's drafts count as kDrafts half-pages
-    constexpr int kDrafts = Work::kWhole ? 3 : 0;
-    auto cut = [&](int w) -> int { return r_begin + max(0, (r_end - r_begin + kDrafts) * w / 4 - kDrafts); };
+    const int r_begin = work.begin(list, j), r_end = work.begin(list, j + 1);
+    const bool drafts = work.drafts() && wv == 0;            // they are the first wave's, and count as some half-pages
+    const int n_drafts = work.drafts() ? work.draft_weight() : 0;
+    auto cut = [&](int w) -> int { return r_begin + max(0, (r_end - r_begin + n_drafts) * w / 4 - n_drafts); };
     const int x_begin = wv == 0 ? r_begin : cut(wv), x_end = cut(wv + 1);
-    const bool drafts = Work::kWhole && wv == 0;
     const int x_first = drafts ? x_begin - 1 : x_begin;      // they come before the half-pages
 
     SharePages pages = share_pages(v, pair, first_ids, x_begin >> 1);
@@ -284,7 +285,7 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
     }
     unsigned long long word = 0ull;                          // drafts that lane's draft sees
     if (drafts) {
-        if constexpr (Work::kWhole) {
+        if constexpr (Work::kTree) {
             work.template load_few<D>(v, k, va);
             word = work.seen(v, list.T);
         }
@@ -343,7 +344,7 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
             }
         }
         if (more) load_k(next);
-        if (Work::kWhole && drafts && x == x_first) {         // a draft: a word of the drafts that it sees
+        if (Work::kTree && drafts && x == x_first) {          // a draft: a word of the drafts that it sees
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
                 const int c = i * 16 + n;
@@ -427,14 +428,14 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
         if (__builtin_expect(__ballot(odd) != 0ull, 0)) {
             const CarefulRange range = careful_range(v, list, scale_log2e, x_begin, x_end);
             bool again = ring && least != most && careful_needed<D>(range, least, most);
-            if constexpr (Work::kWhole) again = again || (drafts && work.template careful_needed<D>(v));
+            if constexpr (Work::kTree) again = again || (drafts && work.template careful_needed<D>(v));
             if (again)
                 for (int c = 0; c < min(16 * NQ, n_cols); ++c) {
                     const ShareRow sr = work.row(v, c, true);
                     __builtin_amdgcn_wave_barrier();
                     const uint16_t* qrow = q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D;
                     careful_sums<D>(range, qrow, sr.place, s_ml[wv][c].x, s_acc[wv] + c * kRow);
-                    if constexpr (Work::kWhole)
+                    if constexpr (Work::kTree)
                         if (drafts) work.template add_careful<D>(v, qrow, lane_word(word, sr.row - work.row0), scale_log2e, s_ml[wv][c].x, s_acc[wv] + c * kRow);
                 }
         }
@@ -514,14 +515,14 @@ __device__ __forceinline__ void attend_list_split(const SpkvView& v, const uint1
     constexpr int kHps = NW == 8 ? 2 : 1;                    // half-pages to a step
     constexpr int kSlots = kSplitSlots<NW>;
     constexpr int kRowsPerWave = kHps * (D / 8) / NW;        // 1 KB rows of a step that a wave copies
-    const int pair = work.pair, h = work.h, j = work.range, ranges = work.ranges;
+    const int pair = work.pair, h = work.h, j = work.range;
     const FirstPages first_ids = first_pages(v, pair);
     const ShareList list = share_list(v, pair);
     const int n_cols = work.columns(v);
     const int col0 = work.block * (32 * NW);
     if (col0 >= n_cols) return;
     const int nA = list.nA;
-    const int x_begin = list.begin(j, ranges), x_end = list.begin(j + 1, ranges), last = max(x_end - 1, x_begin);
+    const int x_begin = work.begin(list, j), x_end = work.begin(list, j + 1), last = max(x_end - 1, x_begin);
 
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -529,7 +530,7 @@ __device__ __forceinline__ void attend_list_split(const SpkvView& v, const uint1
     const bool valid = c < n_cols;
     const size_t pc = Work::kWhole ? 0 : work.part0(v) + c;  // of the partial result
     float2* part_ml = work.template part_ml<D>(v);
-    if (!Work::kWhole && x_begin >= x_end) {                 // fewer half-pages than ranges
+    if (x_begin >= x_end && !work.drafts()) {                // fewer half-pages than ranges
         if (valid && half == 0) part_ml[pc] = make_float2(SPKV_NEG_INF, 0.f);
         return;
     }
@@ -741,52 +742,59 @@ __device__ __forceinline__ void attend_list_split(const SpkvView& v, const uint1
     }
     wait_loads_but<0>();
 
-    if constexpr (Work::kWhole) {
-        __syncthreads();                                     // the tiles are no longer read
-        work.template stage_split<D, NW>(v, s_tile[0]);
-        const unsigned long long word = work.seen(v, list.T), mine = lane_word(word, sr.row - work.row0);
-        __syncthreads();
+    unsigned long long word = 0ull;                          // drafts that lane's draft sees
+    if constexpr (Work::kTree) {
+        if (work.drafts()) {
+            __syncthreads();                                 // the tiles are no longer read
+            work.template stage_split<D, NW>(v, s_tile[0]);
+            word = work.seen(v, list.T);
+            const unsigned long long mine = lane_word(word, sr.row - work.row0);
+            __syncthreads();
 #pragma unroll 1
-        for (int t = 0; t < (work.n + kHalfTokens - 1) / kHalfTokens; ++t) {
-            load_k(s_tile[t]);
-            load_v(s_tile[t], 0);
-            load_v(s_tile[t], 1);
-            scores(s0);
-            const unsigned ok = (unsigned)(mine >> (32 * t)) >> (8 * half);
+            for (int t = 0; t < (work.n + kHalfTokens - 1) / kHalfTokens; ++t) {
+                load_k(s_tile[t]);
+                load_v(s_tile[t], 0);
+                load_v(s_tile[t], 1);
+                scores(s0);
+                const unsigned ok = (unsigned)(mine >> (32 * t)) >> (8 * half);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s0[e] = ((ok >> (16 * (e >> 3) + (e & 7))) & 1u) ? s0[e] : SPKV_NEG_INF;
-            if (weights(s0)) rescale(s0);
-            l += psum;
-            accumulate(0);
-            accumulate(1);
+                for (int e = 0; e < 16; ++e) s0[e] = ((ok >> (16 * (e >> 3) + (e & 7))) & 1u) ? s0[e] : SPKV_NEG_INF;
+                if (weights(s0)) rescale(s0);
+                l += psum;
+                accumulate(0);
+                accumulate(1);
+            }
         }
-        l += __shfl_xor(l, 32);
-        const bool odd = odd_sums(acc, NB, l);
-        bool again = false;
-        const CarefulRange range = careful_range(v, list, scale_log2e, x_begin, x_end);
-        if (__builtin_expect(__ballot(odd) != 0ull, 0))
-            again = (x_end > nA && least != most && careful_needed<D>(range, least, most)) || work.template careful_needed<D>(v);
-        __syncthreads();                                     // the drafts are no longer read
-        work.template finish_split<D>(v, q, range, word, acc, m, l, again, reinterpret_cast<float*>(&s_tile[0][0]) + wv * 32 * D, col0 + wv * 32,
-                                      min(32, n_cols - (col0 + wv * 32)));
-        return;
     }
     l += __shfl_xor(l, 32);
-    if (valid && half == 0) part_ml[pc] = make_float2(m, l);
-    const bool odd = x_end > nA && least != most && odd_sums(acc, NB, l);
+    const bool ring = x_end > nA && least != most;
+    const bool odd = (ring || work.drafts()) && odd_sums(acc, NB, l);
     __syncthreads();                                         // the tiles are no longer read
     const int n_here = min(32, n_cols - (col0 + wv * 32));
-    float* to = work.part(v) + (work.part0(v) + col0 + wv * 32) * D;
-    store_column_sums<D>(acc, reinterpret_cast<float*>(&s_tile[0][0]) + wv * 32 * D, to, n_here);
+    float* sums = reinterpret_cast<float*>(&s_tile[0][0]) + wv * 32 * D;
+    bool again = false;
+    const CarefulRange range = careful_range(v, list, scale_log2e, x_begin, x_end);
     if (__builtin_expect(__ballot(odd) != 0ull, 0)) {
-        const CarefulRange range = careful_range(v, list, scale_log2e, x_begin, x_end);
-        if (careful_needed<D>(range, least, most)) {
+        again = ring && careful_needed<D>(range, least, most);
+        if constexpr (Work::kTree) again = again || (work.drafts() && work.template careful_needed<D>(v));
+    }
+    auto careful = [&](int i, float* to) {                   // column i's sums, key by key
+        const ShareRow at = work.row(v, col0 + wv * 32 + i, true);
+        const uint16_t* qrow = q + ((size_t)at.row * v.Hq + (size_t)h * v.G + at.head) * D;
+        const float ref = __shfl(m, i);
+        careful_sums<D>(range, qrow, at.place, ref, to);
+        if constexpr (Work::kTree)
+            if (work.drafts()) work.template add_careful<D>(v, qrow, lane_word(word, at.row - work.row0), scale_log2e, ref, to);
+    };
+    if constexpr (Work::kWhole) {
+        work.template finish_split<D>(v, acc, m, l, sums, col0 + wv * 32, n_here, again, careful);
+    } else {
+        if (valid && half == 0) part_ml[pc] = make_float2(m, l);
+        float* to = work.part(v) + (work.part0(v) + col0 + wv * 32) * D;
+        store_column_sums<D>(acc, sums, to, n_here);
+        if (__builtin_expect(again, 0)) {
             __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0): the stores above come first
-            for (int i = 0; i < n_here; ++i) {
-                const ShareRow at = work.row(v, col0 + wv * 32 + i, true);
-                careful_sums<D>(range, q + ((size_t)at.row * v.Hq + (size_t)h * v.G + at.head) * D, at.place, __shfl(m, i),
-                                to + (size_t)i * D);
-            }
+            for (int i = 0; i < n_here; ++i) careful(i, to + (size_t)i * D);
         }
     }
 }

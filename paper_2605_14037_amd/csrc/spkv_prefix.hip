@@ -174,7 +174,9 @@ __device__ __forceinline__ ShareRow share_row(const SpkvShareRows& rows, int fir
 }
 
 struct PromptWork {
-    static constexpr bool kWhole = false;
+    static constexpr bool kTree = false, kWhole = false;
+    static constexpr bool drafts() { return false; }
+    static constexpr int draft_weight() { return 0; }
     const SpkvShareCut& cut;
     const SpkvShareRows& rows;
     int act, h, pair, range, ranges, block, first;
@@ -189,6 +191,7 @@ struct PromptWork {
         block = u.block;
         pair = (int)rows.prefix[act] * v.Hkv + h;
     }
+    __device__ __forceinline__ int begin(const ShareList& list, int i) const { return list.begin(i, ranges); }
     __device__ __forceinline__ int columns(const SpkvView& v) {
         first = share_first(rows, act);
         return (share_first(rows, act + 1) - first) * v.G;

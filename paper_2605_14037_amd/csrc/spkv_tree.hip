@@ -112,27 +112,25 @@ __device__ __forceinline__ float log_of_sum(float m, float l) { return l == 0.f 
 
 // ---------------------------------------------------------------------------- the work
 // Workgroup id -> unit: the ranges of the lists, by the host's table, the ranges of a pair's block of columns next to each
-// other, then the drafts of every pair's blocks of columns (short units, beside the last ranges).  W: every list is one range, whose
-// unit takes the drafts too and writes the results; there are no others, and no join.
-template <bool W>
+// other.  W: every list is one range, whose unit writes the results, and there is no join.  With: the drafts go with a list's first range,
+// where they count for `weight` half-pages (of a short list it has little else); without, they are units of their own, behind the lists'.
+template <bool W, bool With>
 struct TreeWork {
-    static constexpr bool kWhole = W;
+    static constexpr bool kTree = With, kWhole = W;
     const SpkvTree& tree;
     const SpkvTreeTable& table;
-    int pair, h, range, ranges, block, n, row0, unit, width;
-    __device__ __forceinline__ TreeWork(const SpkvView& v, const SpkvTree& t, const SpkvTreeTable& tab, int id, int w)
-        : tree(t), table(tab), width(w) {
-        int local;
-        if (!W && id >= t.n_units) {
-            local = (id - t.n_units) / t.n_blocks;
-            block = id - t.n_units - local * t.n_blocks;
-            range = -1;
+    int pair, h, range, ranges, block, n, row0, unit, width, weight;
+    __device__ __forceinline__ TreeWork(const SpkvView& v, const SpkvTree& t, const SpkvTreeTable& tab, int id, SpkvTreeKernel kernel)
+        : tree(t), table(tab), width(spkv_tree_width(kernel)) {
+        int local = 0;
+        if (!With && id >= t.n_units) {
+            local = id - t.n_units;
             ranges = 1;
-            unit = id;
+            block = 0;
+            range = -1;
         } else {
             const uint4 raw = reinterpret_cast<const uint4*>(tab.end)[threadIdx.x & 63];      // eight pairs a lane
             const unsigned e[4] = {raw.x, raw.y, raw.z, raw.w};
-            local = 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 local += __popcll(__ballot((int)(e[i] & 0xffffu) <= id));
@@ -142,13 +140,21 @@ struct TreeWork {
             ranges = tab.ranges[local];
             block = (id - start) / ranges;
             range = id - start - block * ranges;
-            unit = id;
         }
+        unit = id;
         pair = t.pair0 + tab.pair[local];
         const int b = pair / v.Hkv, at = b - t.seq0;
         h = pair - b * v.Hkv;
         row0 = t.row0 + tab.cu[at];
         n = tab.cu[at + 1] - tab.cu[at];
+        weight = spkv_tree_draft_weight(kernel, n);
+    }
+    __device__ __forceinline__ bool drafts() const { return With && (W || range == 0); }
+    __device__ __forceinline__ int draft_weight() const { return weight; }
+    __device__ __forceinline__ int begin(const ShareList& list, int j) const {
+        if (!With) return list.begin(j, ranges);
+        const int x = (int)((int64_t)j * (2 * list.n_hp - list.nA + weight) / ranges) - weight;
+        return x <= 0 ? 0 : x <= list.nA ? x : list.nA + (x - list.nA + 1) / 2;
     }
     __device__ __forceinline__ int columns(const SpkvView& v) const { return n * v.G; }
     __device__ __forceinline__ ShareRow row(const SpkvView& v, int c, bool ring) const {
@@ -255,22 +261,18 @@ struct TreeWork {
         store_result(tree.out + id * D + d, a * (l == 0.f ? 0.f : 1.0f / l));
         if (tree.lse != nullptr && d == 0) tree.lse[id] = log_of_sum(m, l);
     }
-    // attend_list_split's: a wave's sums of columns c0 .. + n_here - 1, or, again, worked out key by key; sums: room in LDS
-    template <int D>
-    __device__ __forceinline__ void finish_split(const SpkvView& v, const uint16_t* q, const CarefulRange& range, unsigned long long word,
-                                                 f32x16 (&acc)[D / 32], float m, float l, bool again, float* sums, int c0, int n_here) const {
+    // attend_list_split's: a wave's sums of columns c0 .. + n_here - 1, or, again, each worked out by careful; sums: room in LDS
+    template <int D, class Careful>
+    __device__ __forceinline__ void finish_split(const SpkvView& v, f32x16 (&acc)[D / 32], float m, float l, float* sums, int c0, int n_here,
+                                                 bool again, Careful&& careful) const {
         const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
         const float inv = l == 0.f ? 0.f : 1.0f / l;
         if (tree.lse != nullptr && half == 0 && col < n_here) tree.lse[result(v, c0 + col)] = log_of_sum(m, l);
         if (__builtin_expect(again, 0)) {
             for (int i = 0; i < n_here; ++i) {
-                const size_t id = result(v, c0 + i);
-                const uint16_t* qrow = q + id * D;
-                const int draft = (c0 + i) / v.G;
-                const float ref = __shfl(m, i), scale = __shfl(inv, i);
-                careful_sums<D>(range, qrow, __popcll(lane_word(tree_path(tree.parents + row0, n).path, draft)) - 1, ref, sums);
-                add_careful<D>(v, qrow, lane_word(word, draft), range.scale_log2e, ref, sums);
-                for (int d = lane; d < D; d += 64) tree.out[id * D + d] = __builtin_bit_cast(uint16_t, (__bf16)(sums[d] * scale));
+                const float scale = __shfl(inv, i);
+                careful(i, sums);
+                for (int d = lane; d < D; d += 64) tree.out[result(v, c0 + i) * D + d] = __builtin_bit_cast(uint16_t, (__bf16)(sums[d] * scale));
             }
             return;
         }
@@ -289,7 +291,7 @@ struct TreeWork {
 // quarter of the values' elements.
 template <int D, int NQ>
 __device__ __forceinline__ void attend_drafts_few(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e,
-                                                  const TreeWork<false>& work) {
+                                                  const TreeWork<false, false>& work) {
     constexpr int NS = D / 32, NB = D / 16, kMine = NB / 4;
     const int lane = threadIdx.x & 63, kc = lane >> 4, col = lane & 15, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n = work.n, h = work.h, n_cols = work.columns(v);
@@ -359,94 +361,14 @@ __device__ __forceinline__ void attend_drafts_few(const SpkvView& v, const uint1
     }
 }
 
-// More columns: keys and values into LDS once, in the operand order of attend_list_split, then 32 columns a wave.
-template <int D, int NW>
-__device__ __forceinline__ void attend_drafts_split(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e,
-                                                    const TreeWork<false>& work, uint16_t (&s_tile)[kSplitSlots<NW>][2 * kHalfTokens * D]) {
-    constexpr int NS = D / 16, NB = D / 32;
-    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int n = work.n, h = work.h, n_cols = work.columns(v), col0 = work.block * (32 * NW);
-    if (col0 >= n_cols) return;
-    const int tiles = (n + kHalfTokens - 1) >> 5;
-    work.stage_split<D, NW>(v, s_tile[0]);
-    const int c = col0 + wv * 32 + col;
-    const bool valid = c < n_cols;
-    const int draft = (valid ? c : 0) / v.G;
-    const uint16_t* qrow = q + ((size_t)(work.row0 + draft) * v.Hq + (size_t)h * v.G + ((valid ? c : 0) - draft * v.G)) * D;
-    bf16x8 qb[NS];
-#pragma unroll
-    for (int sl = 0; sl < NS; ++sl) qb[sl] = *reinterpret_cast<const bf16x8*>(qrow + sl * 16 + half * 8);
-    const unsigned long long word = work.seen(v, v.t_pair[work.pair]), seen = lane_word(word, draft);
-    __syncthreads();
-    f32x16 s[2], acc[NB];
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
-    float m = SPKV_NEG_INF;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
-        if (t < tiles) {
-#pragma unroll
-            for (int sl = 0; sl < NS; ++sl)
-                s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(&s_tile[t][sl * 512 + lane * 8]), qb[sl], s[t], 0, 0, 0);
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int key = 32 * t + 16 * (e >> 3) + 8 * half + (e & 7);
-            s[t][e] = ((seen >> key) & 1ull) ? s[t][e] * scale_log2e : SPKV_NEG_INF;
-            m = fmaxf(m, s[t][e]);
-        }
-    }
-    m = fmaxf(m, __shfl_xor(m, 32));
-    const float ref = m == SPKV_NEG_INF ? 0.f : m;
-    float l = 0.f;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        if (t >= tiles) break;
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            f32x8 p;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                p[e] = __builtin_amdgcn_exp2f(s[t][8 * g + e] - ref);
-                l += p[e];
-            }
-            const bf16x8 pb = __builtin_convertvector(p, bf16x8);
-#pragma unroll
-            for (int db = 0; db < NB; ++db)
-                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    *reinterpret_cast<const bf16x8*>(&s_tile[t][kHalfTokens * D + (g * NB + db) * 512 + lane * 8]), pb, acc[db], 0, 0, 0);
-        }
-    }
-    l += __shfl_xor(l, 32);
-    const size_t pc0 = work.part0(v);
-    if (valid && half == 0) work.part_ml<D>(v)[pc0 + c] = make_float2(m, l);
-    const bool odd = valid && odd_sums(acc, NB, l);
-    __syncthreads();                                         // the tiles are no longer read
-    const int n_here = min(32, n_cols - (col0 + wv * 32));
-    float* to = v.part_acc + (pc0 + col0 + wv * 32) * D;
-    store_column_sums<D>(acc, reinterpret_cast<float*>(&s_tile[0][0]) + wv * 32 * D, to, n_here);
-    if (__builtin_expect(__ballot(odd) != 0ull, 0)) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);                  // vmcnt(0): the stores above come first
-        for (int i = 0; i < n_here; ++i) {
-            const int cc = col0 + wv * 32 + i, dd = cc / v.G;
-            careful_tree_sums<D>(work.keys(v), work.values(v), work.stride(v), q + work.result(v, cc) * D, lane_word(word, dd), scale_log2e,
-                                 __shfl(ref, i), false, to + (size_t)i * D);
-        }
-    }
-}
-
-constexpr int kDraftWeight = 3;
 // 33 to 64 columns: every wave has all of them, two groups of MFMA 32x32x16, and an eighth of the workgroup's range to
 // itself.  Its half-pages go from memory into 16 KB of LDS of its own (D = 128) in operand order, keys and values in turn: while
 // the scores are weighed the next keys arrive, while these are multiplied the next values.  No wave waits for another.
 // Read once, the half-pages are loaded as such (nt: 484 MB in 98 us, 114 without; 94 MB that the caches hold 30, 29 without).
 // The queries are shared, in LDS.  The drafts are up to two half-pages more in the list's first range, for a wave each.
 template <int D, bool W>
-__device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e, const TreeWork<W>& work) {
+__device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e,
+                                                  const TreeWork<W, true>& work) {
     constexpr int NS = D / 16, NB = D / 32, kRow = D + 4, kHalfElems = 2 * kHalfTokens * D;
     __shared__ __attribute__((aligned(16))) uint16_t s_q[2 * NS * 512];
     __shared__ __attribute__((aligned(16))) float s_acc[4][64 * kRow];         // (half-pages before)
@@ -460,15 +382,11 @@ __device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint1
     const int n_cols = work.columns(v), c0 = work.block * 64;
     if (c0 >= n_cols) return;
     const int tiles = (work.n + kHalfTokens - 1) >> 5, nA = list.nA;
-    auto cut = [&](int j) -> int {                            // the drafts count kDraftWeight half-pages each, in the first range
-        const int x = (int)((int64_t)j * (2 * list.n_hp - nA + kDraftWeight * tiles) / work.ranges) - kDraftWeight * tiles;
-        return x <= 0 ? 0 : x <= nA ? x : nA + (x - nA + 1) / 2;
-    };
-    const int r_begin = cut(work.range), r_end = work.range + 1 == work.ranges ? list.n_hp : cut(work.range + 1);
-    const int with_drafts = work.range == 0 ? tiles : 0;      // the first waves take one half-page of them each
+    const int r_begin = work.begin(list, work.range), r_end = work.begin(list, work.range + 1);
+    const int with_drafts = work.drafts() ? tiles : 0;       // the first waves take one half-page of them each
     auto cut_wave = [&](int w) -> int {
-        const int all = r_end - r_begin + kDraftWeight * with_drafts;
-        return r_begin + max(0, all * w / 8 - kDraftWeight * min(w, with_drafts));
+        const int all = r_end - r_begin + kOwnDrafts * with_drafts;
+        return r_begin + max(0, all * w / 8 - kOwnDrafts * min(w, with_drafts));
     };
     const int x_begin = cut_wave(wv), x_end = cut_wave(wv + 1);
     const bool ring = x_end > nA, drafts = wv < with_drafts;
@@ -775,7 +693,7 @@ __device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint1
 template <int D, int NQ, bool W>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, NQ == 1 ? 3 : 2)))
 void spkv_tree_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvTree tree, SpkvTreeTable table) {
-    TreeWork<W> work(v, tree, table, (int)blockIdx.x, 16 * NQ);
+    TreeWork<W, W> work(v, tree, table, (int)blockIdx.x, NQ == 1 ? kTreeFew16 : kTreeFew32);
     if constexpr (!W)
         if (work.range < 0) return attend_drafts_few<D, NQ>(v, q, scale_log2e, work);
     attend_list_few<D, NQ>(v, q, scale_log2e, work);
@@ -785,16 +703,14 @@ template <int D, int NW, bool W>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 2 ? 1 : 2, 2)))
 void spkv_tree_split(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvTree tree, SpkvTreeTable table) {
     __shared__ __attribute__((aligned(16))) uint16_t s_tile[kSplitSlots<NW>][2 * kHalfTokens * D];
-    TreeWork<W> work(v, tree, table, (int)blockIdx.x, 32 * NW);
-    if constexpr (!W)
-        if (work.range < 0) return attend_drafts_split<D, NW>(v, q, scale_log2e, work, s_tile);
+    TreeWork<W, true> work(v, tree, table, (int)blockIdx.x, NW == 2 ? kTreeSplit64 : NW == 4 ? kTreeSplit128 : kTreeSplit256);
     attend_list_split<D, NW>(v, q, scale_log2e, work, s_tile);
 }
 
 template <int D, bool W>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void spkv_tree_own_copies(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvTree tree, SpkvTreeTable table) {
-    TreeWork<W> work(v, tree, table, (int)blockIdx.x, 64);
+    TreeWork<W, true> work(v, tree, table, (int)blockIdx.x, kTreeOwnCopies);
     attend_own_copies<D, W>(v, q, scale_log2e, work);
 }
 
@@ -812,19 +728,18 @@ __global__ __launch_bounds__(256, 8) void spkv_tree_merge(SpkvView v, SpkvTree t
     const bool exists = c0 + slice / S < n_cols;
     const int c = exists ? c0 + slice / S : c0, block = c / width, in = c - block * width;
     const int ranges = table.ranges[local], start = local > 0 ? table.end[local - 1] : 0;
-    const size_t own = (size_t)(tree.n_units + local * tree.n_blocks + block) * width + in;
     const size_t lists = (size_t)(start + block * ranges) * width + in;
     const float2* ml = reinterpret_cast<const float2*>(v.part_ml);
     float M = SPKV_NEG_INF, den = 0.f;
     f32x4 num = {0.f, 0.f, 0.f, 0.f};
-    const int none = tree.n_own == 0 ? 1 : 0, parts = ranges + 1 - none;        // (the drafts' own part, and the lists')
+    const int parts = ranges + tree.alone;                   // (the drafts', where they are units of their own)
     for (int r0 = share; r0 < parts; r0 += kFold * S) {
         float2 x[kFold];
         f32x4 a[kFold];
 #pragma unroll
         for (int u = 0; u < kFold; ++u) {
             const int r = min(r0 + u * S, parts - 1);        // past the end: re-read, ignored
-            const size_t pc = r + none == 0 ? own : lists + (size_t)(r + none - 1) * width;
+            const size_t pc = r == ranges ? (size_t)(tree.n_units + local) * width + in : lists + (size_t)r * width;
             x[u] = ml[pc];
             a[u] = *reinterpret_cast<const f32x4*>(v.part_acc + pc * D + d);
         }
@@ -885,16 +800,13 @@ SpkvTreeKernel spkv_tree_kernel(int n_cols, int64_t half_pages) {
 SpkvTreeKernel spkv_tree_kernel_whole(SpkvTreeKernel k, int64_t lists, int64_t compute_units) {
     return k == kTreeSplit64 && lists <= compute_units ? kTreeOwnCopies : k;
 }
-int spkv_tree_width(SpkvTreeKernel k) {
-    return k == kTreeFew16 ? 16 : k == kTreeFew32 ? 32 : k == kTreeOwnCopies || k == kTreeSplit64 ? 64 : k == kTreeSplit128 ? 128 : 256;
-}
 int spkv_tree_resident(SpkvTreeKernel k) { return k == kTreeOwnCopies || k == kTreeSplit256 ? 1 : 2; }
 
 constexpr int kTreeMergeRound = 2048;
 template <int D, bool W>
 static void launch_lists(const SpkvView& v, const uint16_t* q, float sl, SpkvTreeKernel kernel, const SpkvTree& tree, const SpkvTreeTable& table,
-                         hipStream_t s) {
-    const dim3 grid((unsigned)(tree.n_own + tree.n_units));
+                         int n_pairs, hipStream_t s) {
+    const dim3 grid((unsigned)(tree.n_units + tree.alone * n_pairs));
     switch (kernel) {
         case kTreeFew16: spkv_tree_few<D, 1, W><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
         case kTreeFew32: spkv_tree_few<D, 2, W><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
@@ -909,13 +821,13 @@ static hipError_t launch_tree(const SpkvView& v, const uint16_t* q, float sl, Sp
                               const SpkvTreeTable& table, int n_pairs, int most_cols, int most_ranges, hipStream_t s) {
     const int width = spkv_tree_width(kernel);
     if (tree.whole) {
-        launch_lists<D, true>(v, q, sl, kernel, tree, table, s);
+        launch_lists<D, true>(v, q, sl, kernel, tree, table, n_pairs, s);
         return hipGetLastError();
     }
-    launch_lists<D, false>(v, q, sl, kernel, tree, table, s);
+    launch_lists<D, false>(v, q, sl, kernel, tree, table, n_pairs, s);
     constexpr int CPB = 256 / (D / 4);
     int share = std::min(8, CPB);
-    while (share > 1 && (n_pairs * ((most_cols * share + CPB - 1) / CPB) > kTreeMergeRound || share > most_ranges + 1)) share >>= 1;
+    while (share > 1 && (n_pairs * ((most_cols * share + CPB - 1) / CPB) > kTreeMergeRound || share > most_ranges + tree.alone)) share >>= 1;
     const dim3 merge((unsigned)((most_cols * share + CPB - 1) / CPB), (unsigned)n_pairs);
     if (share == 8) spkv_tree_merge<D, 8><<<merge, dim3(256), 0, s>>>(v, tree, table, width);
     else if (share == 4) spkv_tree_merge<D, 4><<<merge, dim3(256), 0, s>>>(v, tree, table, width);
