@@ -400,7 +400,8 @@ int spkv_decode_attention_shared(spkv_cache_t* cache, spkv_cache_t* prefix, cons
  * lie in the cache's own buffers); one launch, or two where the lists are cut into ranges, more for hundreds of (sequence, KV head)
  * pairs with many columns each.  Waits once for the lengths after a prompt's append, as spkv_decode_attention does.  May be
  * captured; a replay takes the parents and the lists as they are by then (the cut is made for lists that fill the pool).  Copies of
- * a sequence get results that agree to rounding.
+ * a sequence get results that agree to rounding.  spkv_prefix_attention places the rows of a call as a chain: joined with a tree's
+ * results it is right for sequences that hold `window` tokens of their own or more.
  * Errors: SPKV_E_INVAL for bad shapes and pointers; never SPKV_E_STATE. */
 int spkv_score_tree(spkv_cache_t* cache, const void* k, const void* v, const float* util_logits, const void* q,
                     const int32_t* parents, const int32_t* cu_seqlens, void* out, float* lse, float sm_scale,

@@ -493,6 +493,7 @@ class SPKVCache:
             raise SPKVError(E_INVAL, "spkv_cache_required_bytes")
         self.device = torch.device(device)
         self.arena = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self.index = self.arena.get_device()
         self.handle = C.c_void_p()
         _check(self.lib.spkv_cache_create(C.byref(self.cfg), C.c_void_p(self.arena.data_ptr()),
                                           nbytes, _stream(), C.byref(self.handle)),
@@ -783,6 +784,20 @@ class SPKVCache:
         return out, lse
 
     # ---- sequences that branch
+    # ---- sequences that branch
+    def _ptr(self, t, dtype, shape, name):
+        """_dev_ptr, of a tensor on the cache's own device."""
+        if t.get_device() != self.index or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{self.index}, "
+                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _stream(self):
+        current = torch.cuda.current_device()
+        if current != self.index:
+            raise ValueError(f"the cache is on cuda:{self.index}, the current device is cuda:{current}")
+        return _stream() if _raw_stream is None else _raw_stream(current)
+
     def score_tree(self, k, v, q, parents, cu_seqlens, util_logits=None, out=None, lse=None, sm_scale=0.0, want_lse=False):
         """Attention outputs of a tree of up to 64 drafts per sequence, the cache left unchanged (spkv_score_tree).
         parents: int32 [total] on the device, the index of an earlier draft of the same sequence or -1.  util_logits: the
@@ -792,28 +807,28 @@ class SPKVCache:
         total = cu[cfg.batch]
         if total == 0:
             _check(self.lib.spkv_score_tree(self.handle, None, None, None, None, None, cu, None, None, float(sm_scale),
-                                            _stream()), "spkv_score_tree")
+                                            self._stream()), "spkv_score_tree")
             return None
         kv_shape = (total, cfg.n_kv_heads, cfg.head_dim)
         shape = (total, cfg.n_q_heads, cfg.head_dim)
-        kp = _dev_ptr(k, torch.bfloat16, kv_shape, "k")
-        vp = _dev_ptr(v, torch.bfloat16, kv_shape, "v")
-        qp = _dev_ptr(q, torch.bfloat16, shape, "q")
-        fp = _dev_ptr(util_logits, torch.float32, kv_shape[:2], "util_logits") if util_logits is not None else None
-        pp = _dev_ptr(parents, torch.int32, (total,), "parents")
+        kp = self._ptr(k, torch.bfloat16, kv_shape, "k")
+        vp = self._ptr(v, torch.bfloat16, kv_shape, "v")
+        qp = self._ptr(q, torch.bfloat16, shape, "q")
+        fp = self._ptr(util_logits, torch.float32, kv_shape[:2], "util_logits") if util_logits is not None else None
+        pp = self._ptr(parents, torch.int32, (total,), "parents")
         if out is None:                       # (with strides: half a microsecond less than torch.empty)
             out = torch.empty_strided(shape, (shape[1] * shape[2], shape[2], 1), dtype=torch.bfloat16, device=q.device)
             op = out.data_ptr()
         else:
-            op = _dev_ptr(out, torch.bfloat16, shape, "out")
+            op = self._ptr(out, torch.bfloat16, shape, "out")
         if lse is not None:
-            lp = _dev_ptr(lse, torch.float32, shape[:2], "lse")
+            lp = self._ptr(lse, torch.float32, shape[:2], "lse")
         elif want_lse:
             lse = torch.empty_strided(shape[:2], (shape[1], 1), dtype=torch.float32, device=q.device)
             lp = lse.data_ptr()
         else:
             lp = None
-        _check(self.lib.spkv_score_tree(self.handle, kp, vp, fp, qp, pp, cu, op, lp, float(sm_scale), _stream()),
+        _check(self.lib.spkv_score_tree(self.handle, kp, vp, fp, qp, pp, cu, op, lp, float(sm_scale), self._stream()),
                "spkv_score_tree")
         return (out, lse) if lse is not None else out
 
@@ -824,11 +839,11 @@ class SPKVCache:
         cu = cu_seqlens if isinstance(cu_seqlens, C.Array) else self.make_cu(cu_seqlens)
         total, n = cu[cfg.batch], k.shape[0]
         kv_shape = (n, cfg.n_kv_heads, cfg.head_dim)
-        kp = _dev_ptr(k, torch.bfloat16, kv_shape, "k")
-        vp = _dev_ptr(v, torch.bfloat16, kv_shape, "v")
-        fp = _dev_ptr(util_logits, torch.float32, kv_shape[:2], "util_logits")
-        rp = _dev_ptr(rows, torch.int32, (total,), "rows")
-        _check(self.lib.spkv_append_rows(self.handle, kp, vp, fp, rp, n, cu, _stream()), "spkv_append_rows")
+        kp = self._ptr(k, torch.bfloat16, kv_shape, "k")
+        vp = self._ptr(v, torch.bfloat16, kv_shape, "v")
+        fp = self._ptr(util_logits, torch.float32, kv_shape[:2], "util_logits")
+        rp = self._ptr(rows, torch.int32, (total,), "rows")
+        _check(self.lib.spkv_append_rows(self.handle, kp, vp, fp, rp, n, cu, self._stream()), "spkv_append_rows")
 
     def fork(self, source, other=None):
         """Sequence b becomes what sequence source[b] -- of `other`, or of this cache -- was before the call; FORK_KEEP
@@ -837,8 +852,10 @@ class SPKVCache:
             source = (C.c_int32 * len(source))(*[int(x) for x in source])
         if len(source) != self.cfg.batch:
             raise ValueError(f"source: need one entry for each of {self.cfg.batch} sequences, got {len(source)}")
-        _check(self.lib.spkv_cache_fork(self.handle, other.handle if other is not None else None, source, _stream()),
-               "spkv_cache_fork")
+        if other is not None and other.index != self.index:
+            raise ValueError(f"other: on cuda:{other.index}, this cache is on cuda:{self.index}")
+        _check(self.lib.spkv_cache_fork(self.handle, other.handle if other is not None else None, source,
+                                        self._stream()), "spkv_cache_fork")
 
     def gather(self, sequences=None, rows=None, out=None):
         """The pairs that sequences hold (all of them by default), kept ones and then the window's, positions ascending, as
@@ -853,8 +870,8 @@ class SPKVCache:
         if out is None:
             if rows is None:
                 counts = torch.zeros(n, cfg.n_kv_heads, dtype=torch.int32, device=self.device)
-                _check(self.lib.spkv_cache_gather(self.handle, which, n, 0, None, None, None, None, counts.data_ptr(), _stream()),
-                       "spkv_cache_gather")
+                _check(self.lib.spkv_cache_gather(self.handle, which, n, 0, None, None, None, None, counts.data_ptr(),
+                                                  self._stream()), "spkv_cache_gather")
                 rows = int(counts.max()) if n > 0 else 0
             shape = (n, cfg.n_kv_heads, int(rows))
             k, v = (torch.empty(*shape, cfg.head_dim, dtype=torch.bfloat16, device=self.device) for _ in range(2))
@@ -863,12 +880,13 @@ class SPKVCache:
                    torch.empty(shape[:2], dtype=torch.int32, device=self.device))
         k, v, f, positions, counts = out
         shape = (n, cfg.n_kv_heads, k.shape[2] if k.dim() == 4 else -1)
-        kp = _dev_ptr(k, torch.bfloat16, (*shape, cfg.head_dim), "out[0]")
-        vp = _dev_ptr(v, torch.bfloat16, (*shape, cfg.head_dim), "out[1]")
-        fp = _dev_ptr(f, torch.float32, shape, "out[2]")
-        pp = _dev_ptr(positions, torch.int32, shape, "out[3]")
-        cp = _dev_ptr(counts, torch.int32, shape[:2], "out[4]")
-        _check(self.lib.spkv_cache_gather(self.handle, which, n, shape[2], kp, vp, fp, pp, cp, _stream()), "spkv_cache_gather")
+        kp = self._ptr(k, torch.bfloat16, (*shape, cfg.head_dim), "out[0]")
+        vp = self._ptr(v, torch.bfloat16, (*shape, cfg.head_dim), "out[1]")
+        fp = self._ptr(f, torch.float32, shape, "out[2]")
+        pp = self._ptr(positions, torch.int32, shape, "out[3]")
+        cp = self._ptr(counts, torch.int32, shape[:2], "out[4]")
+        _check(self.lib.spkv_cache_gather(self.handle, which, n, shape[2], kp, vp, fp, pp, cp, self._stream()),
+               "spkv_cache_gather")
         return k, v, f, positions, counts
 
     # ---- bookkeeping

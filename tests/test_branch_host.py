@@ -249,5 +249,26 @@ def test_trees_of_many_pairs_take_several_launches():
     assert rc == 0 and len(got) in (1, 2)
 
 
+def test_another_device(monkeypatch):
+    """Calls while another device than the cache's is the current one, caches of two devices, tensors that lie elsewhere."""
+    import torch
+
+    import paper_2605_14037_amd as spkv
+    a, b = (object.__new__(spkv.SPKVCache) for _ in range(2))
+    a.index, b.index = 1, 0
+    a.cfg = b.cfg = spkv.SPKVConfig(1, 2, 1, 64, 128, 0, 0.5, 100, 100)
+    a.lib = b.lib = None
+    a.handle = b.handle = None
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="cuda:1"):
+        a._stream()
+    with pytest.raises(ValueError, match="other: on cuda:0"):
+        a.fork([0], b)
+    with pytest.raises(ValueError, match="on cuda:1"):
+        a.score_tree(*(torch.zeros(1, h, 64, dtype=torch.bfloat16) for h in (1, 1, 2)), torch.zeros(1, dtype=torch.int32), (C.c_int32 * 2)(0, 1))
+    with pytest.raises(ValueError, match="out.0.*on cuda:1"):
+        a.gather(out=[torch.zeros(1, 1, 3, 64)] * 2 + [torch.zeros(1, 1, 3)] * 2 + [torch.zeros(1, 1)])
+
+
 if __name__ == "__main__":
     _main()

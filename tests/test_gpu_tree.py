@@ -343,6 +343,72 @@ def test_trees_in_a_graph():
         x.fork([-1, -1, 0 if turn == 2 else -1])
 
 
+@pytest.mark.parametrize("n", [4, 8, 16, 40])
+def test_windows_of_thousands(n):
+    """Rings of more half-pages than a wave's lanes hold gates of; long paths past none of it."""
+    x = Trees(3, hq=8, hk=2, d=64, window=2600, seed=n, keep=0.3, context=6000)
+    x.append([5000, 2599, 100])
+    for shape in (random_tree, CHAIN):
+        x.drafts([n, n, max(1, n // 2)], shape, seed=n)
+        x.check_tree()
+
+
+def test_trees_behind_shared_prompts():
+    """Joined with the attention over a shared prompt, for sequences that hold a window of their own tokens or more."""
+    shape = dict(d=128, window=40, keep=0.4, seed=30)
+    prompts, own, all_of_it = Trees(2, **shape), Trees(3, **shape), Trees(3, **shape)
+    prompts.append([500, 90])
+    continues = [1, 0, 0]
+    all_of_it.fork(continues, prompts)
+    lengths = [40, 41, 200]
+    k, v, f = own.rows(sum(lengths))
+    for x in (own, all_of_it):
+        x.cache.append(k, v, f, x.cu(lengths))
+        x.oracle.append(to_numpy_f32(k), to_numpy_f32(v), to_numpy_f32(f), x.cu(lengths))
+    own.drafts([30, 12, 1])
+    for name in ("k", "v", "f", "q", "parents", "counts"):
+        setattr(all_of_it, name, getattr(own, name))
+    all_of_it.check_tree()
+    out, lse = own.score()
+    sharing = spkv.PrefixSharing(prompts.cache, continues)
+    out, lse = own.cache.prefix_attention(sharing, own.q, own.cu([30, 12, 1]), out, lse, appended=False)
+    ref, ref_lse, size = all_of_it.reference()
+    # (what is joined has been rounded once already)
+    assert (np.abs(out.double().cpu().numpy() - ref) <= 2 * (2.0 ** -8 * (np.abs(ref) + size) + 1e-4 * size)).all()
+    assert (np.abs(lse.double().cpu().numpy() - ref_lse) <= 2e-4).all()
+
+
+def test_turns_of_drafts_and_beams():
+    """As they are used together: sequences taken over from where their prompts were fed, trees scored, paths accepted, beams that
+    take each other's places, a slot given back and taken again."""
+    rng = np.random.default_rng(31)
+    shape = dict(d=64, window=50, keep=0.4, sinks=2, seed=31)
+    prompts, x = Trees(2, **shape), Trees(6, **shape)
+    prompts.append([333, 40])
+    x.fork([0, 0, 0, 1, 1, 1], prompts)
+    beams = [[0, 0, 2, 4, 4, 4], [1, 0, 2, 3, 5, 3], [-1, 2, 1, -2, 3, -1], [0, 0, 0, 0, 4, 5], [5, 4, 3, 2, 1, 0]]
+    for turn, after in enumerate(beams):
+        counts = [int(c) for c in rng.integers(1, 30, 6)]
+        x.drafts(counts, seed=turn)
+        x.check_tree()
+        parents, rows, accepted, at = x.parents.tolist(), [], [], 0
+        for n in counts:
+            i, path = int(rng.integers(0, n)), []
+            while i >= 0:
+                path.insert(0, at + i)
+                i = parents[at + i]
+            accepted.append(len(path))
+            rows += path
+            at += n
+        x.cache.append_rows(x.k, x.v, x.f, torch.tensor(rows, dtype=torch.int32, device="cuda"), x.cu(accepted))
+        x.oracle.append(to_numpy_f32(x.k)[rows], to_numpy_f32(x.v)[rows], to_numpy_f32(x.f)[rows], x.cu(accepted))
+        x.fork(after)
+        x.check(attend=turn != 2)
+        if turn == 2:                                     # the slot that was given back
+            x.fork([-1, -1, -1, 0, -1, -1], prompts)
+            x.check()
+
+
 def test_two_caches_on_two_streams():
     xs = [Trees(2, d=64, seed=20 + i) for i in range(2)]
     for x in xs:
