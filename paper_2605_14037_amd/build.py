@@ -25,7 +25,8 @@ FLAGS = [
 EXPECTED_OCCUPANCY = {"spkv_decode_splitILi128E": 3,      # every mode and merge width at head_dim 128
                       "spkv_decode_split_compactILi128E": 3,
                       "spkv_prefix_fewILi128E": 2, "spkv_prefix_splitILi128ELi4E": 2, "spkv_prefix_splitILi128ELi8E": 2,
-                      "spkv_rope_forwardItLi128E": 7, "spkv_rope_backwardItLi128E": 4}
+                      "spkv_tree_fewILi128E": 2, "spkv_tree_own_copiesILi128E": 2, "spkv_tree_splitILi128ELi4E": 2,
+                      "spkv_tree_splitILi128ELi8E": 2, "spkv_rope_forwardItLi128E": 7, "spkv_rope_backwardItLi128E": 4}
 
 
 def _check_occupancy(remarks: str) -> list:
