@@ -120,19 +120,48 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_move(SpkvView v, SpkvF
     }
 }
 
-// The copies: `chunk` pages of a pair to a workgroup and turn.  Pages that the pair does not have yet are handed out by one
-// atomic for the chunk.  A page's 32 KB (D = 128) are in flight at once, the next page's loads before this one's
+// Many pages to hand out: every copied pair is given the ids that it lacks, off the stack and then out of the pool, by its place among the
+// pairs -- no atomic, of which all go to one address and are served one after the other.  Every workgroup, four pairs', adds up what
+// the pairs before them lack.  The counters stand still meanwhile: the copies' launch moves them on, by the sum in pos_scratch[0].
+constexpr int kAssignPairs = 1;
+__global__ __launch_bounds__(256) void spkv_fork_assign(SpkvView v, SpkvForkCopies copies) {
+    __shared__ int s_sum[4];
+    auto lacks = [&](int p) -> int { return max(0, min((v.kept_len[p] + kPageTokens - 1) / kPageTokens, v.pt_cap) - v.pair_items[p]); };
+    const int tid = threadIdx.x, here = blockIdx.x, p = copies.dst[here / v.Hkv] * v.Hkv + here % v.Hkv;
+    const int top = *v.free_top, next = *v.pool_next, mine = lacks(p);
+    int32_t* row = v.page_table + (size_t)p * v.pt_cap + v.pair_items[p];
+    int before = 0;
+    for (int i = tid; i < here; i += 256) before += lacks(copies.dst[i / v.Hkv] * v.Hkv + i % v.Hkv);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) before += __shfl_xor(before, o);
+    if ((tid & 63) == 0) s_sum[tid >> 6] = before;
+    __syncthreads();
+    const int id0 = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+    for (int e = tid; e < mine; e += 256) {
+        const int id = id0 + e, page = id < top ? v.free_pages[top - 1 - id] : next + id - max(top, 0);
+        row[e] = page < v.n_pages ? page : -1;
+    }
+    if (tid == 0 && here == (int)gridDim.x - 1) v.pos_scratch[0] = id0 + mine;
+}
+
+// The copies: `chunk` pages of a pair to a workgroup and turn.  Pages that the pair does not have yet have been assigned, or are
+// handed out by one atomic for the chunk.  A page's 32 KB (D = 128) are in flight at once, the next page's loads before this one's
 // stores.  Stores without retention: never slower, whether the copies are read next or not, and 68 -> 53 us for eight copies of 30
 // MB (4.6 TB/s written), 128 -> 107 for sixteen.
 constexpr int kForkChunk = 16;
 template <int D>
-__global__ __launch_bounds__(kForkThreads) void spkv_fork_pages(SpkvView v, SpkvForkSource from, SpkvForkCopies copies, int chunk) {
+__global__ __launch_bounds__(kForkThreads) void spkv_fork_pages(SpkvView v, SpkvForkSource from, SpkvForkCopies copies, int chunk, int assigned) {
     const int tid = threadIdx.x, pair = copies.dst[blockIdx.z] * v.Hkv + blockIdx.y;
-    const int n = min((v.kept_len[pair] + kPageTokens - 1) / kPageTokens, v.pt_cap), stay = v.pair_items[pair];
+    const int n = min((v.kept_len[pair] + kPageTokens - 1) / kPageTokens, v.pt_cap), stay = assigned != 0 ? n : v.pair_items[pair];
     const int32_t* of = from.page_table + ((size_t)copies.of[blockIdx.z] * v.Hkv + blockIdx.y) * from.pt_cap;
     int32_t* row = v.page_table + (size_t)pair * v.pt_cap;
     __shared__ int s_from[kForkChunk], s_to[kForkChunk];
     constexpr int kUnits = 2 * kPageTokens * D / 8 / kForkThreads;
+    if (assigned != 0 && tid == 0 && blockIdx.x + blockIdx.y + blockIdx.z == 0) {
+        const int all = v.pos_scratch[0], top = *v.free_top, off_stack = min(max(top, 0), all);
+        *v.free_top = top - off_stack;
+        *v.pool_next += all - off_stack;
+    }
     for (int p0 = blockIdx.x * chunk; p0 < n; p0 += gridDim.x * chunk) {
         const int here = min(chunk, n - p0), fresh = max(0, p0 + here - max(stay, p0));
         if (tid < 64) {                                       // (chunk <= 64)
@@ -145,7 +174,7 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_pages(SpkvView v, Spkv
                 const int i = p0 + tid, to = i < stay ? row[i] : batch_page(v, pb, i - max(stay, p0));
                 s_from[tid] = min(max(of[i], 0), from.n_pages - 1);
                 s_to[tid] = to;
-                if (i >= stay) row[i] = max(to, 0);
+                if (i >= stay || to < 0) row[i] = max(to, 0);
                 if (to < 0) *v.err_flag = 1;
             }
         }
@@ -182,16 +211,18 @@ hipError_t spkv_launch_fork_move(const SpkvView& v, const SpkvForkSource& from, 
     return hipGetLastError();
 }
 
-// Eight workgroups to a compute unit at chunks of all / 2048 pages; where pages have to be handed out, a quarter of
-// them, each with one atomic on the same address: 15 of 32 beams of 5 MB copied in 74 / 47 / 39 us with 2048 / 1024 / 512
-// workgroups, eight copies of 30 MB into pages at hand in 53 / 58 / 59.
+// Eight workgroups to a compute unit at chunks of all / 2048 pages; where a few pages have to be handed out, a quarter of them, each with
+// an atomic on the same address (15 of 32 beams of 5 MB, 2048 / 1024 / 512 / 256 workgroups 74 / 47 / 39 / 46 us, assigned 29).
+constexpr int64_t kForkAssign = 256;
 hipError_t spkv_launch_fork_pages(const SpkvView& v, const SpkvForkSource& from, const SpkvForkCopies& copies, int n, int64_t most_pages,
                                   int64_t all_pages, int64_t fresh_pages, hipStream_t s) {
-    const int64_t wanted = fresh_pages * 8 > all_pages ? 512 : 2048;
+    const int assigned = fresh_pages >= kForkAssign;
+    if (assigned) spkv_fork_assign<<<dim3(n * v.Hkv), dim3(256), 0, s>>>(v, copies);
+    const int64_t wanted = !assigned && fresh_pages * 8 > all_pages ? 512 : 2048;
     const int chunk = (int)std::max<int64_t>(1, std::min<int64_t>(kForkChunk, all_pages / wanted));
     const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((most_pages + chunk - 1) / chunk, 65535)), v.Hkv, n);
-    if (v.D == 128) spkv_fork_pages<128><<<grid, dim3(kForkThreads), 0, s>>>(v, from, copies, chunk);
-    else spkv_fork_pages<64><<<grid, dim3(kForkThreads), 0, s>>>(v, from, copies, chunk);
+    if (v.D == 128) spkv_fork_pages<128><<<grid, dim3(kForkThreads), 0, s>>>(v, from, copies, chunk, assigned);
+    else spkv_fork_pages<64><<<grid, dim3(kForkThreads), 0, s>>>(v, from, copies, chunk, assigned);
     return hipGetLastError();
 }
 

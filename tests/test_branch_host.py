@@ -115,16 +115,24 @@ def test_launches_of_a_fork():
         assert rc == 0
         return [n for n, _, _ in got]
 
-    move, pages = "spkv_fork_move", "spkv_fork_pages<128>"
+    move, pages, assign = "spkv_fork_move", "spkv_fork_pages<128>", "spkv_fork_assign"
     assert launches([KEEP, 1, KEEP]) == []                   # nothing to do
     assert launches([1, 0, KEEP]) == [move]                  # pages change hands
     assert launches([EMPTY, EMPTY, 0]) == [move]
-    assert launches([KEEP, KEEP, 0]) == [move, pages]        # a copy
+    assert launches([KEEP, KEEP, 0]) == [move, assign, pages]         # a copy, of many pages
     assert launches([KEEP, KEEP, 1]) == [move]               # of a sequence that is all window
-    assert launches([2, 0, 0]) == [move, pages]              # one takes the pages, one has copies
-    assert launches([0, 1, 2], of="b") == [move, pages]      # of another cache always
-    assert launches([KEEP, KEEP, 0], of="b") == [move, pages]
+    assert launches([2, 0, 0]) == [move, assign, pages]      # one takes the pages, one has copies
+    assert launches([0, 1, 2], of="b") == [move, pages]      # of another cache always; into the pages at hand
+    assert launches([KEEP, KEEP, 0], of="b") == [move, assign, pages]
     assert launches([1, EMPTY, 2], of="b") == [move]
+
+
+def test_a_few_pages_are_handed_out_by_the_copies():
+    def launches(kept):
+        return [n for n, _, _ in _run([{}], [["append", dict(counts=[9000, 50, 0])], ["lengths", dict(kept=[kept] * 8 + [0] * 16)],
+                                             ["fork", dict(source=[KEEP, KEEP, 0])]])[-1][1]]
+    assert launches(31 * 64) == ["spkv_fork_move", "spkv_fork_pages<128>"]
+    assert launches(31 * 64 + 1) == ["spkv_fork_move", "spkv_fork_assign", "spkv_fork_pages<128>"]
 
 
 def test_components_are_moved_side_by_side():

@@ -253,6 +253,28 @@ def test_what_a_window_held_does_not_show():
     x.check()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_copies_of_many_pages(d):
+    """Hundreds of pages handed out in a call: out of the pool, off the stack, of both, beside pages that stay; lists of any length."""
+    x = Both(7, hq=16, hk=16, d=d, window=40, seed=d, context=3000, keep=0.9, kept=7 * 16 * 2200)
+    x.append([2000, 300, 1, 0, 700, 90, 1300])
+    for source in ([0, 0, 0, -1, 0, -1, -1],              # out of the pool
+                   [-2, -2, -1, -1, -2, -1, -1],          # much goes back
+                   [6, 2, 2, 2, 6, 6, -1],                # off the stack, into fewer and more pages than there were
+                   [1, 0, 0, 4, 4, 4, 0],                 # trades places; some pages stay, others are new
+                   [2, 2, 2, 2, 2, 2, 2], [-2, 3, 3, -2, 3, 3, 3], [1, -1, -1, 2, -1, -1, -1]):
+        x.fork(source)
+        x.check(attend=False)
+        x.append([3, 0, 1, 70, 0, 1, 33])
+    x.check(attend=False)
+    y = Both(7, hq=16, hk=16, d=d, window=40, seed=d + 1, context=3000, keep=0.9, kept=7 * 16 * 2200)
+    y.fork([0, 1, 2, 3, 4, 5, 6], x)
+    y.check()
+    y.append([100] * 7)
+    y.fork([6, 6, -1, 0, 0, -1, 1], x)
+    y.check()
+
+
 def test_beams_of_a_wide_batch():
     """As many sequences as a cache has; groups that trade places among themselves."""
     x = Both(512, hq=2, hk=1, window=20, seed=8, context=300, keep=0.5)
