@@ -1990,15 +1990,16 @@ int64_t tree_half_pages(const spkv_cache* c, int p, int64_t room) {
 // What a launch takes, ns: its longest unit, or all of them shared among the workgroups that the chip holds.  (D = 64 three quarters
 // of it.  From 1 to 128 sequences of 300 to 4000 tokens, 4 to 64 drafts of 4 heads; only for the choice below.)
 int64_t tree_time(SpkvTreeKernel kernel, int head_dim, int64_t resident, int64_t units, int64_t longest, int64_t work) {
-    static const int start[] = {8100, 8500, 13200, 10200, 10500, 14900}, half_page[] = {300, 550, 320, 700, 700, 780};
+    static const int start[] = {8100, 8500, 13200, 10200, 10500, 14900, 8500, 9000},
+                     half_page[] = {300, 550, 320, 700, 700, 780, 160, 300};
     const int64_t t = std::max(start[kernel] + half_page[kernel] * longest, (start[kernel] * units + half_page[kernel] * work) / resident);
     return head_dim == 64 ? t * 3 / 4 : t;
 }
 constexpr int kTreeJoin = 5500, kTreeJoinBytesPerUs = 6000000;       // the second launch, and partial results written and read
 
 // Or every list in one range, with the drafts, its results written at once (tree->whole): two to five times less to write, and one
-// launch.  us, 4 / 16 / 64 drafts, cut / whole: one sequence of 300 tokens 14 / 10, 13 / 17, 19 / 22, one of 2048 12 / 13, 14 / 30, 23 / 33,
-// 16 of 1000 15 / 12, 24 / 20, 44 / 31, 64 of 300 25 / 15, 40 / 25, 101 / 56, 64 of 1k-16k 85 / 84, 99 / 86 (12 drafts), 201 / 161.
+// launch.  us, 4 / 16 / 64 drafts, cut / whole: one sequence of 300 tokens 12 / 8, 13 / 17, 19 / 22, one of 2048 12 / 12, 14 / 21, 23 / 33,
+// 16 of 1000 15 / 12, 24 / 20, 44 / 31, 64 of 300 25 / 20, 40 / 25, 101 / 56, 64 of 1k-16k 85 / 84, 99 / 86 (12 drafts), 201 / 161.
 int tree_cut(const spkv_cache* c, const int32_t* cu, int n_pairs, SpkvTreeKernel* chosen, int64_t room, int64_t fit, SpkvTree* tree, SpkvTreeTable* table) {
     const SpkvTreeKernel kernel = *chosen;
     const int width = spkv_tree_width(kernel);

@@ -123,7 +123,6 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_move(SpkvView v, SpkvF
 // Many pages to hand out: every copied pair is given the ids that it lacks, off the stack and then out of the pool, by its place among the
 // pairs -- no atomic, of which all go to one address and are served one after the other.  Every workgroup, four pairs', adds up what
 // the pairs before them lack.  The counters stand still meanwhile: the copies' launch moves them on, by the sum in pos_scratch[0].
-constexpr int kAssignPairs = 1;
 __global__ __launch_bounds__(256) void spkv_fork_assign(SpkvView v, SpkvForkCopies copies) {
     __shared__ int s_sum[4];
     auto lacks = [&](int p) -> int { return max(0, min((v.kept_len[p] + kPageTokens - 1) / kPageTokens, v.pt_cap) - v.pair_items[p]); };

@@ -384,11 +384,11 @@ struct SpkvTreeTable {
 };
 // Kernels by the columns of the pair with the most: 16 or 32 (spkv_tree_few), 64 (spkv_tree_own_copies, or spkv_tree_split
 // where the lists are short), 128, 256 to a workgroup.
-enum SpkvTreeKernel { kTreeFew16, kTreeFew32, kTreeOwnCopies, kTreeSplit64, kTreeSplit128, kTreeSplit256 };
+enum SpkvTreeKernel { kTreeFew16, kTreeFew32, kTreeOwnCopies, kTreeSplit64, kTreeSplit128, kTreeSplit256, kTreeFew16Eight, kTreeFew32Eight };
 SpkvTreeKernel spkv_tree_kernel(int n_cols, int64_t half_pages);
 SpkvTreeKernel spkv_tree_kernel_whole(SpkvTreeKernel kernel, int64_t lists, int64_t compute_units);      // ... where no list is cut
 constexpr __host__ __device__ int spkv_tree_width(SpkvTreeKernel k) {         // columns of a workgroup
-    return k == kTreeFew16 ? 16 : k == kTreeFew32 ? 32 : k == kTreeOwnCopies || k == kTreeSplit64 ? 64 : k == kTreeSplit128 ? 128 : 256;
+    return k == kTreeFew16 || k == kTreeFew16Eight ? 16 : k == kTreeFew32 || k == kTreeFew32Eight ? 32 : k == kTreeOwnCopies || k == kTreeSplit64 ? 64 : k == kTreeSplit128 ? 128 : 256;
 }
 // Few columns: the drafts are units of their own.
 constexpr __host__ __device__ bool spkv_tree_few_columns(SpkvTreeKernel k) { return k == kTreeFew16 || k == kTreeFew32; }

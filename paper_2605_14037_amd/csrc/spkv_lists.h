@@ -230,13 +230,13 @@ struct ShareRow {
 // weights against the references as they stand -- raised, and sums and accumulators rescaled, only where some lane's
 // eight weights add up to more than kSumLimit -- then the products with V, the weights as two bf16 parts (16 bits: the
 // lists' read takes the time, not these products) -- and the next values are sent for.  One body for every half-page:
-// two of them in turn on two sets of operands were slower where a wave has only a few (cold instructions).  The four
-// waves take a quarter of the range each and meet in LDS.
-template <int D, int NQ, class Work>
+// two of them in turn on two sets of operands were slower where a wave has only a few (cold instructions).  The NV
+// waves, four or eight, take an equal part of the range each and meet in LDS.
+template <int D, int NQ, int NV, class Work>
 __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_t* __restrict__ q, float scale_log2e, Work& work) {
     constexpr int NS = D / 32, NB = D / 16, kRow = D + 4;
-    __shared__ __attribute__((aligned(16))) float s_acc[4][16 * NQ * kRow];
-    __shared__ float2 s_ml[4][16 * NQ];
+    __shared__ __attribute__((aligned(16))) float s_acc[NV][16 * NQ * kRow];
+    __shared__ float2 s_ml[NV][16 * NQ];
     __shared__ __attribute__((aligned(16))) uint16_t s_q[NQ == 1 ? 1 : NQ * NS][512];
     const int tid = threadIdx.x, lane = tid & 63, kc = lane >> 4, n = lane & 15;
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -249,7 +249,7 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
     const int r_begin = work.begin(list, j), r_end = work.begin(list, j + 1);
     const bool drafts = work.drafts() && wv == 0;            // they are the first wave's, and count as some half-pages
     const int n_drafts = work.drafts() ? work.draft_weight() : 0;
-    auto cut = [&](int w) -> int { return r_begin + max(0, (r_end - r_begin + n_drafts) * w / 4 - n_drafts); };
+    auto cut = [&](int w) -> int { return r_begin + max(0, (r_end - r_begin + n_drafts) * w / NV - n_drafts); };
     const int x_begin = wv == 0 ? r_begin : cut(wv), x_end = cut(wv + 1);
     const int x_first = drafts ? x_begin - 1 : x_begin;      // they come before the half-pages
 
@@ -444,12 +444,12 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
     const size_t pc0 = Work::kWhole ? 0 : work.part0(v);
     float* part = work.part(v);
     float2* part_ml = work.template part_ml<D>(v);
-    for (int e = tid; e < n_cols * (D / 4); e += 256) {
+    for (int e = tid; e < n_cols * (D / 4); e += 64 * NV) {
         const int c = e / (D / 4), d = (e - c * (D / 4)) * 4;
-        float2 ml[4];
+        float2 ml[NV];
         float M = SPKV_NEG_INF;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NV; ++w) {
             ml[w] = s_ml[w][c];
             M = fmaxf(M, ml[w].x);
         }
@@ -457,7 +457,7 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
         f32x4 a = {0.f, 0.f, 0.f, 0.f};
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NV; ++w) {
             const float sc = __builtin_amdgcn_exp2f(ml[w].x - m_ref);
             a += *reinterpret_cast<const f32x4*>(s_acc[w] + c * kRow + d) * sc;
             sum += ml[w].y * sc;

@@ -219,7 +219,7 @@ void spkv_prefix_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log
         return;
     }
     PromptWork work(v, cut, table, rows, (int)blockIdx.x - own.n_blocks);
-    attend_list_few<D, NQ>(v, q, scale_log2e, work);
+    attend_list_few<D, NQ, 4>(v, q, scale_log2e, work);
 }
 
 template <int D, int NW>

@@ -690,13 +690,13 @@ __device__ __forceinline__ void attend_own_copies(const SpkvView& v, const uint1
     }
 }
 
-template <int D, int NQ, bool W>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, NQ == 1 ? 3 : 2)))
+template <int D, int NQ, int NV, bool W>
+__global__ __launch_bounds__(64 * NV) __attribute__((amdgpu_waves_per_eu(2, NQ == 1 && NV == 4 ? 3 : 2)))
 void spkv_tree_few(SpkvView v, const uint16_t* __restrict__ q, float scale_log2e, SpkvTree tree, SpkvTreeTable table) {
     TreeWork<W, W> work(v, tree, table, (int)blockIdx.x, NQ == 1 ? kTreeFew16 : kTreeFew32);
     if constexpr (!W)
         if (work.range < 0) return attend_drafts_few<D, NQ>(v, q, scale_log2e, work);
-    attend_list_few<D, NQ>(v, q, scale_log2e, work);
+    attend_list_few<D, NQ, NV>(v, q, scale_log2e, work);
 }
 
 template <int D, int NW, bool W>
@@ -795,10 +795,12 @@ SpkvTreeKernel spkv_tree_kernel(int n_cols, int64_t half_pages) {
     return n_cols <= 16 ? kTreeFew16 : n_cols <= 32 ? kTreeFew32 : n_cols <= 64 ? (half_pages >= kTreeOwnHalfPages ? kTreeOwnCopies : kTreeSplit64)
                         : n_cols <= 128 ? kTreeSplit128 : kTreeSplit256;
 }
-// Whole lists, one to a compute unit: eight waves to a list are better than two.  us, 16 drafts of 4 heads, split / own copies: 8
-// sequences of 500 19.4 / 17.5, 32 of 1000 27 / 21.5, but 64 of 300 (512 lists) 25 / 36.6; D = 64, 8 drafts of 8 heads, 32 of 1000 18.5 / 13.4.
+// Whole lists, one to a compute unit: eight waves to a list are better than two or four.  us, 16 drafts of 4 heads, split / own copies: 8
+// sequences of 500 19.4 / 17.5, 32 of 1000 27 / 21.5, but 64 of 300 (512 lists) 25 / 36.6; D = 64, 8 drafts of 8 heads, 32 of 1000 18.5 / 13.4;
+// 8 drafts of 4 heads, four / eight waves: 8 of 500 14.8 / 12.9, 32 of 1000 20.4 / 18.2; 4 drafts, one of 300 10 / 8.2.
 SpkvTreeKernel spkv_tree_kernel_whole(SpkvTreeKernel k, int64_t lists, int64_t compute_units) {
-    return k == kTreeSplit64 && lists <= compute_units ? kTreeOwnCopies : k;
+    if (lists > compute_units) return k;
+    return k == kTreeSplit64 ? kTreeOwnCopies : k == kTreeFew16 ? kTreeFew16Eight : k == kTreeFew32 ? kTreeFew32Eight : k;
 }
 int spkv_tree_resident(SpkvTreeKernel k) { return k == kTreeOwnCopies || k == kTreeSplit256 ? 1 : 2; }
 
@@ -808,8 +810,14 @@ static void launch_lists(const SpkvView& v, const uint16_t* q, float sl, SpkvTre
                          int n_pairs, hipStream_t s) {
     const dim3 grid((unsigned)(tree.n_units + tree.alone * n_pairs));
     switch (kernel) {
-        case kTreeFew16: spkv_tree_few<D, 1, W><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
-        case kTreeFew32: spkv_tree_few<D, 2, W><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeFew16: spkv_tree_few<D, 1, 4, W><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeFew32: spkv_tree_few<D, 2, 4, W><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;
+        case kTreeFew16Eight:
+            if constexpr (W) spkv_tree_few<D, 1, 8, W><<<grid, dim3(512), 0, s>>>(v, q, sl, tree, table);
+            break;
+        case kTreeFew32Eight:
+            if constexpr (W) spkv_tree_few<D, 2, 8, W><<<grid, dim3(512), 0, s>>>(v, q, sl, tree, table);
+            break;
         case kTreeOwnCopies: spkv_tree_own_copies<D, W><<<grid, dim3(512), 0, s>>>(v, q, sl, tree, table); break;
         case kTreeSplit64: spkv_tree_split<D, 2, W><<<grid, dim3(128), 0, s>>>(v, q, sl, tree, table); break;
         case kTreeSplit128: spkv_tree_split<D, 4, W><<<grid, dim3(256), 0, s>>>(v, q, sl, tree, table); break;

@@ -210,7 +210,7 @@ def _tree(kept, n, batch=3, **kw):
     return _run([dict(batch=batch, **kw)], fed + [["tree", dict(counts=[n] + [1] * (batch - 1))]])[-1]
 
 
-@pytest.mark.parametrize("n,kernel,threads", [(1, "few<128, 1", 256), (4, "few<128, 1", 256), (5, "few<128, 2", 256), (8, "few<128, 2", 256),
+@pytest.mark.parametrize("n,kernel,threads", [(1, "few<128, 1, 4", 256), (4, "few<128, 1, 4", 256), (5, "few<128, 2, 4", 256), (8, "few<128, 2, 4", 256),
                                               (9, "split<128, 2", 128), (16, "split<128, 2", 128), (17, "split<128, 4", 256),
                                               (32, "split<128, 4", 256), (33, "split<128, 8", 512), (64, "split<128, 8", 512)])
 def test_launches_of_a_tree(n, kernel, threads):
@@ -221,18 +221,19 @@ def test_launches_of_a_tree(n, kernel, threads):
     assert 200 <= got[0][1] <= 24 + 1024                  # ranges as many as a round of the chip, four at most
 
 
-@pytest.mark.parametrize("n,kernel,threads", [(4, "few<128, 1", 256), (8, "few<128, 2", 256), (16, "own_copies<128", 512), (32, "split<128, 4", 256),
-                                              (64, "split<128, 8", 512)])
-def test_short_lists_take_one_launch(n, kernel, threads):
-    """Where whole lists take no longer than ranges of them and a join: one workgroup a list, whose results are final."""
+@pytest.mark.parametrize("n,kernel,threads,many,many_threads", [
+    (4, "few<128, 1, 8", 512, "few<128, 1, 4", 256), (8, "few<128, 2, 8", 512, "few<128, 2, 4", 256),
+    (16, "own_copies<128", 512, "split<128, 2", 128), (32, "split<128, 4", 256, "split<128, 4", 256), (64, "split<128, 8", 512, "split<128, 8", 512)])
+def test_short_lists_take_one_launch(n, kernel, threads, many, many_threads):
+    """Where whole lists take no longer than ranges of them and a join: one workgroup a list, whose results are final; of eight
+    waves while there is one to a compute unit."""
     assert _tree(40, n, batch=24) == (0, [(f"spkv_tree_{kernel}, 1>", 192, threads)])
-    rc, got = _tree(40, n, batch=64, max_total_kept_tokens=1 << 22)
-    assert rc == 0 and got[0][:2] == (f"spkv_tree_{kernel.replace('own_copies<128', 'split<128, 2')}, 1>", 512) and len(got) == 1
+    assert _tree(40, n, batch=64, max_total_kept_tokens=1 << 22) == (0, [(f"spkv_tree_{many}, 1>", 512, many_threads)])
 
 
 def test_launches_of_a_tree_over_long_lists():
     """33 to 64 columns take another kernel where the lists are long."""
-    for n, kernel, threads, rounds in ((4, "few<128, 1", 256, 4), (8, "few<128, 2", 256, 4), (9, "own_copies<128", 512, 1),
+    for n, kernel, threads, rounds in ((4, "few<128, 1, 4", 256, 4), (8, "few<128, 2, 4", 256, 4), (9, "own_copies<128", 512, 1),
                                        (16, "own_copies<128", 512, 1), (17, "split<128, 4", 256, 4), (64, "split<128, 8", 512, 4)):
         rc, got = _tree(20000, n)
         assert rc == 0 and [g[0].split("<")[0] for g in got][1:] == ["spkv_tree_merge"]
