@@ -223,6 +223,7 @@ struct ShareRow {
 //   begin(list, j)                   first half-page of the list's range j
 //   kTree                            there are drafts, too: keys that every column sees some of, which the workgroup of a list's first
 //                                    range takes (drafts()); see TreeWork in spkv_tree.hip for what is asked of it then
+//   kPaths, parent(), place(v, c, path(parent()))            places by themselves, for who has other loads to send first
 //   kWhole                           the range is the whole list, and what the workgroup has at the end is the columns' result
 
 // Up to 16 NQ columns.  A half-page's operands come straight from memory (1 KB a load, as in spkv_decode_split) and are
@@ -268,10 +269,11 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
     bf16x8 q1[NQ == 1 ? NS : 1];                             // the query operands of one group; of several they lie in LDS
     int place[NQ], least = 0, most = 0;                      // of the wave's columns, the smallest sees most of the ring
     const bool ring = x_end > nA;
+    const int parent = work.parent();                        // (of trees; sent for before what waits longer)
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
         const int c = i * 16 + n;
-        const ShareRow sr = work.row(v, c < n_cols ? c : 0, ring);
+        const ShareRow sr = work.row(v, c < n_cols ? c : 0, ring && !Work::kPaths);
         place[i] = sr.place;
         const uint16_t* qrow = q + ((size_t)sr.row * v.Hq + (size_t)h * v.G + sr.head) * D + kc * 8;
         if (NQ == 1) {
@@ -285,14 +287,19 @@ __device__ __forceinline__ void attend_list_few(const SpkvView& v, const uint16_
     }
     unsigned long long word = 0ull;                          // drafts that lane's draft sees
     if (drafts) {
-        if constexpr (Work::kTree) {
-            work.template load_few<D>(v, k, va);
-            word = work.seen(v, list.T);
-        }
+        if constexpr (Work::kTree) work.template load_few<D>(v, k, va);
     } else if (x_begin < x_end) {
         const uint16_t* page = half_page_at(v, list, pages, x_begin);
         load_k(page);
         load_v(page);
+    }
+    if constexpr (Work::kPaths) {
+        if (ring || drafts) {
+            const auto path = work.path(parent);
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) place[i] = work.place(v, i * 16 + n < n_cols ? i * 16 + n : 0, path);
+            if (drafts) word = work.seen(v, list.T, path);
+        }
     }
     if (NQ > 1) __syncthreads();
     RingGates gates = {0, 0u};

@@ -174,7 +174,8 @@ __device__ __forceinline__ ShareRow share_row(const SpkvShareRows& rows, int fir
 }
 
 struct PromptWork {
-    static constexpr bool kTree = false, kWhole = false;
+    static constexpr bool kTree = false, kPaths = false, kWhole = false;
+    static constexpr int parent() { return 0; }
     static constexpr bool drafts() { return false; }
     static constexpr int draft_weight() { return 0; }
     const SpkvShareCut& cut;

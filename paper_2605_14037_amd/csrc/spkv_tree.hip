@@ -27,10 +27,13 @@ struct TreePath {
     int up, depth;
 };
 // Any value but 0 .. i - 1 for a parent means that the draft hangs behind the newest token.
-__device__ __forceinline__ TreePath tree_path(const int32_t* __restrict__ parents, int n) {
+__device__ __forceinline__ int tree_parent(const int32_t* __restrict__ parents, int n) {      // of lane's draft
+    const int lane = threadIdx.x & 63;
+    return lane < n ? parents[lane] : -1;
+}
+__device__ __forceinline__ TreePath tree_path(int p) {
     const int lane = threadIdx.x & 63;
     TreePath t;
-    const int p = lane < n ? parents[lane] : -1;
     t.up = p >= 0 && p < lane ? p : -1;
     t.path = 1ull << lane;
     int up = t.up;
@@ -116,7 +119,7 @@ __device__ __forceinline__ float log_of_sum(float m, float l) { return l == 0.f 
 // where they count for `weight` half-pages (of a short list it has little else); without, they are units of their own, behind the lists'.
 template <bool W, bool With>
 struct TreeWork {
-    static constexpr bool kTree = With, kWhole = W;
+    static constexpr bool kTree = With, kPaths = true, kWhole = W;
     const SpkvTree& tree;
     const SpkvTreeTable& table;
     int pair, h, range, ranges, block, n, row0, unit, width, weight;
@@ -162,9 +165,12 @@ struct TreeWork {
         const int i = c / v.G;
         r.head = c - i * v.G;
         r.row = row0 + i;
-        r.place = ring ? __shfl(tree_path(tree.parents + row0, n).depth, i) : 0;
+        r.place = ring ? place(v, c, tree_path(parent())) : 0;
         return r;
     }
+    __device__ __forceinline__ int parent() const { return tree_parent(tree.parents + row0, n); }
+    __device__ __forceinline__ TreePath path(int p) const { return tree_path(p); }
+    __device__ __forceinline__ int place(const SpkvView& v, int c, const TreePath& path) const { return __shfl(path.depth, c / v.G); }
     __device__ __forceinline__ float* part(const SpkvView& v) const { return v.part_acc; }
     template <int D>
     __device__ __forceinline__ float2* part_ml(const SpkvView& v) const { return reinterpret_cast<float2*>(v.part_ml); }
@@ -174,8 +180,9 @@ struct TreeWork {
     __device__ __forceinline__ int stride(const SpkvView& v) const { return v.Hkv * v.D; }
     __device__ __forceinline__ const uint16_t* keys(const SpkvView& v) const { return tree.k + ((size_t)row0 * v.Hkv + h) * v.D; }
     __device__ __forceinline__ const uint16_t* values(const SpkvView& v) const { return tree.v + ((size_t)row0 * v.Hkv + h) * v.D; }
-    __device__ __forceinline__ unsigned long long seen(const SpkvView& v, int T) const {
-        return tree_seen(v, tree_path(tree.parents + row0, n), tree.f, h, row0, n, T);
+    __device__ __forceinline__ unsigned long long seen(const SpkvView& v, int T) const { return seen(v, T, tree_path(parent())); }
+    __device__ __forceinline__ unsigned long long seen(const SpkvView& v, int T, const TreePath& path) const {
+        return tree_seen(v, path, tree.f, h, row0, n, T);
     }
     // Operands of attend_list_few, N groups of 16 of the values' elements from group first on.  Keys straight from their rows;
     // values, of which an operand wants eight keys of one element, by 2-byte loads.
