@@ -18,7 +18,7 @@
 //
 // Bound: the lists are read once, 4 D bytes a key for 4 D flops a key and column: past about 180 columns a list the matrix
 // units, below the read; few columns or short lists by the start of a workgroup and the join.  Measured, 16 sequences of 32k tokens
-// (484 MB, 32 heads over 8 of 128), a call: 4 drafts 83 us (5.8 TB/s), 8: 94, 16: 99, 32: 120, 64: 162 (3.0 TB/s, 0.76 PF/s); one
+// (484 MB, 32 heads over 8 of 128), a call: 4 drafts 83 us (5.8 TB/s), 8: 91, 16: 98, 32: 119, 64: 165 (2.9 TB/s, 0.75 PF/s); one
 // sequence of 128k, 16 drafts 34; of 2k, 14.
 
 // ------------------------------------------------------------------------------- paths
