@@ -428,7 +428,7 @@ int spkv_append_rows(spkv_cache_t* cache, const void* k, const void* v, const fl
  * Within a cache the first sequence that takes the contents of one that is itself replaced or emptied has its pages;
  * only further ones are copied, so beams that trade places move page ids and windows.  The same sequence may be taken by any
  * number of others.  Copies are the same to the last bit, and independent of each other from then on.
- * Three launches at most.  Waits once for the lengths after a prompt's append to `from`, as spkv_decode_attention does, and
+ * One launch for a few short sequences, else three at most.  Waits once for the lengths after a prompt's append to `from`, as spkv_decode_attention does, and
  * where the pool might not hold the copies; else it does not synchronise (a sequence is given back without waiting, too).
  * Errors: SPKV_E_INVAL for shapes that differ and sources out of range; SPKV_E_CAPACITY if the pool or max_context cannot hold
  * the result (nothing is changed); SPKV_E_STATE under stream capture -- a replay would move sequences that the

@@ -2279,7 +2279,6 @@ int spkv_cache_fork(spkv_cache_t* c, spkv_cache_t* other, const int32_t* source,
     if (pages_after() > c->carve.n_pages) return SPKV_E_CAPACITY;
 
     const SpkvForkSource src = fork_source(from->view);
-    if (spkv_launch_fork_move(c->view, src, plan.moves, s) != hipSuccess) return SPKV_E_HIP;
     int64_t most = 0, all = 0, fresh = 0;
     for (int i = 0; i < plan.n_copies; ++i) {
         const int b = plan.copies.dst[i];
@@ -2290,8 +2289,13 @@ int spkv_cache_fork(spkv_cache_t* c, spkv_cache_t* other, const int32_t* source,
             fresh += std::max<int64_t>(0, pages - own);
         }
     }
-    if (most > 0 && spkv_launch_fork_pages(c->view, src, plan.copies, plan.n_copies, most, all, fresh, s) != hipSuccess)
-        return SPKV_E_HIP;
+    const bool apart = plan.moves.start[plan.moves.n] == plan.moves.n;       // no sequence that is replaced is a source
+    hipError_t e = hipSuccess;
+    if (!(apart && most > 0 && spkv_launch_fork_few(c->view, src, plan.moves, most, s, &e))) {
+        e = spkv_launch_fork_move(c->view, src, plan.moves, s);
+        if (e == hipSuccess && most > 0) e = spkv_launch_fork_pages(c->view, src, plan.copies, plan.n_copies, most, all, fresh, s);
+    }
+    if (e != hipSuccess) return SPKV_E_HIP;
 
     int32_t len[kMaxPairs], tokens[SPKV_MAX_BATCH], since[SPKV_MAX_BATCH];
     c->slack = 0;

@@ -127,6 +127,22 @@ def test_launches_of_a_fork():
     assert launches([1, EMPTY, 2], of="b") == [move]
 
 
+def test_short_sequences_are_copied_in_one_launch():
+    """Up to 64 workgroups of 128 KB each; not where a sequence that is replaced is a source, nor where only windows are copied."""
+    def launches(kept, source, batch=3, **cfg):
+        fed = [["append", dict(counts=[9000, 50] + [0] * (batch - 2))], ["lengths", dict(kept=[kept] * 8 + [0] * 8 * (batch - 1))]]
+        return _run([dict(batch=batch, **cfg)], fed + [["fork", dict(source=source)]])[-1][1]
+    few = lambda wide: [("spkv_fork_few<128>", wide, 256)]                    # noqa: E731
+    assert launches(300, [KEEP, KEEP, 0]) == few(8)                           # 7 pages of 32 KB: 5, and 2 of the window
+    assert launches(300, [KEEP, 0, EMPTY]) == few(4)
+    assert launches(30 * 64, [KEEP, KEEP, 0]) == few(8)                       # 32 pages: four a workgroup
+    assert [n for n, _, _ in launches(30 * 64 + 1, [KEEP, KEEP, 0])] == ["spkv_fork_move", "spkv_fork_pages<128>"]
+    assert [n for n, _, _ in launches(300, [1, 0, 0])] == ["spkv_fork_move", "spkv_fork_pages<128>"]
+    assert [n for n, _, _ in launches(300, [KEEP, KEEP, 1])] == ["spkv_fork_move"]
+    assert launches(100, [KEEP] + [0] * 8, batch=9) == few(1)
+    assert [n for n, _, _ in launches(100, [KEEP] + [0] * 9, batch=10)] == ["spkv_fork_move", "spkv_fork_pages<128>"]
+
+
 def test_a_few_pages_are_handed_out_by_the_copies():
     def launches(kept):
         return [n for n, _, _ in _run([{}], [["append", dict(counts=[9000, 50, 0])], ["lengths", dict(kept=[kept] * 8 + [0] * 16)],

@@ -254,6 +254,31 @@ def test_what_a_window_held_does_not_show():
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hk", [1, 3])
+def test_short_sequences_in_one_launch(hk, d):
+    """Pages handed out and given back in the same call, by sequences that grow and shrink; many times over."""
+    x = Both(6, hq=4 * hk, hk=hk, d=d, window=70, seed=d + hk, context=2000, keep=0.8, kept=6 * hk * 700)
+    x.append([600, 0, 1, 70, 150, 380])
+    for turn in range(4):
+        for source in ([-1, 0, -1, 0, -1, -1],            # pages for two
+                       [-1, -1, -1, 4, 2, 2],             # some more, and many back
+                       [-1, -2, 0, -1, -2, 0], [3, -1, -1, -1, 3, 3]):
+            x.fork(source)
+            x.check(attend=False)
+            x.append([30 * turn + 1, 70, 0, 5, 1, 129])
+        x.fork([0, 0, 0, 0, 0, 5])                        # (everything from one)
+        x.fork([5, -2, -2, -2, -2, -2])
+        x.append([100, 0, 200, 71, 1, 0])
+        x.check(attend=False)
+    y = Both(6, hq=4 * hk, hk=hk, d=d, window=70, seed=d + 9, context=2000, keep=0.8, kept=6 * hk * 700)
+    for source in ([0, 2, 3, -1, -2, 5], [3, 0, -1, 2, 0, 0], [-2, -2, 1, -2, -2, 1], [5, 4, 3, 2, 1, 0]):
+        y.fork(source, x)
+        y.check(attend=False)
+        y.append([1, 200, 70, 0, 3, 10])
+    y.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
 def test_copies_of_many_pages(d):
     """Hundreds of pages handed out in a call: out of the pool, off the stack, of both, beside pages that stay; lists of any length."""
     x = Both(7, hq=16, hk=16, d=d, window=40, seed=d, context=3000, keep=0.9, kept=7 * 16 * 2200)
