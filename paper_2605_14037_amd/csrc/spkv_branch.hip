@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_pages(SpkvView v, Spkv
 // One sequence of 500 tokens, D = 64, two KV heads: 5.4 us, both launches 3.4 and 3.2, and 2.4 us less of the host; seven of up to 2000, three
 // heads, 63 workgroups: 9.1, 4.3 and 4.1 before.
 template <int D>
-__global__ __launch_bounds__(kForkThreads) void spkv_fork_few(SpkvView v, SpkvForkSource from, SpkvForkMoves mv) {
+__global__ __launch_bounds__(kForkThreads) void spkv_fork_few(SpkvView v, SpkvForkSource from, SpkvForkMoves mv, int chunk) {
     const int tid = threadIdx.x;
     struct Move {
         int to, of, len, pages, own;
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_few(SpkvView v, SpkvFo
         for (int i = tid; i < v.w; i += kForkThreads)
             v.ring_logit[(size_t)x.to * v.w + i] = x.of < 0 ? 0.f : from.ring_logit[(size_t)x.of * v.w + i];
     copy_pages<D>(v, from, v.page_table + (size_t)x.to * v.pt_cap, from.page_table + (size_t)max(x.of, 0) * from.pt_cap, x.pages, min(x.own, x.pages),
-                  blockIdx.x, gridDim.x, 1);
+                  blockIdx.x * chunk, gridDim.x * chunk, chunk);
     __shared__ int s_last;
     __syncthreads();
     if (tid == 0) {
@@ -304,8 +304,9 @@ bool spkv_launch_fork_few(const SpkvView& v, const SpkvForkSource& from, const S
     const int64_t wide = std::min<int64_t>(64 / pairs, std::max<int64_t>(most_pages, (bytes + 16383) / 16384));
     if (bytes > wide * (128 << 10)) return false;
     const dim3 grid((unsigned)wide, v.Hkv, mv.n);
-    if (v.D == 128) spkv_fork_few<128><<<grid, dim3(kForkThreads), 0, s>>>(v, from, mv);
-    else spkv_fork_few<64><<<grid, dim3(kForkThreads), 0, s>>>(v, from, mv);
+    const int chunk = (int)std::max<int64_t>(1, std::min<int64_t>(kForkChunk, (most_pages + wide - 1) / wide));
+    if (v.D == 128) spkv_fork_few<128><<<grid, dim3(kForkThreads), 0, s>>>(v, from, mv, chunk);
+    else spkv_fork_few<64><<<grid, dim3(kForkThreads), 0, s>>>(v, from, mv, chunk);
     *e = hipGetLastError();
     return true;
 }
