@@ -363,6 +363,18 @@ def test_chosen_rows_are_appended(window, d):
         x.check()
 
 
+@pytest.mark.parametrize("keep", [0.0, 0.5, 1.0])
+@pytest.mark.parametrize("window", [1, 7, 16, 40, 63, 64, 65])
+def test_many_rows_through_short_windows(window, keep):
+    """Rows that enter the window and leave it in the same call, lists that end anywhere in a page."""
+    rng = np.random.default_rng(window)
+    x = Both(5, d=64, hk=3, hq=3, window=window, seed=window, keep=keep if 0 < keep < 1 else 0.5, tau={0.0: 1.0, 0.5: 0.5, 1.0: 0.0}[keep], sinks=3)
+    x.append([0, 5, window, window + 60, 3 * window + 131])
+    for counts in ([64, 64, 64, 64, 64], [17, 33, 1, 48, 63], [0, 64, 18, 64, 64], [64, 2, 47, 32, 64], [1] * 5):
+        x.append_rows(70, rng.integers(0, 70, sum(counts)), counts)
+        x.check()
+
+
 def test_rows_that_are_not_there_are_flagged():
     x = Both(2, window=20, seed=11)
     x.append([30, 30])
@@ -372,6 +384,10 @@ def test_rows_that_are_not_there_are_flagged():
         x.cache.stats()
     x.cache.reset()
     x.cache.append_rows(k, v, f, torch.tensor([-1], dtype=torch.int32, device="cuda"), [0, 0, 1])
+    with pytest.raises(spkv.SPKVError, match="inconsistent"):
+        x.cache.stats()
+    x.cache.reset()
+    x.cache.append_rows(k, v, f, torch.tensor([3] * 20 + [10], dtype=torch.int32, device="cuda"), [0, 21, 21])
     with pytest.raises(spkv.SPKVError, match="inconsistent"):
         x.cache.stats()
     x.cache.reset()
