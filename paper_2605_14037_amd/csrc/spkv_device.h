@@ -67,7 +67,8 @@ __device__ __forceinline__ bool gate_passes(const SpkvView& v, float f, int pos)
 
 // One pool page for the caller: a recycled one if the stack of released pages has any,
 // else the next never-used one; -1 if the pool is exhausted.  Pushes onto the stack happen
-// only in spkv_release_sequence, never in the same launch as pops, and a failed pop puts
+// only where sequences are released, pruned or replaced, never while a launch still pops
+// (spkv_fork_few pushes once its last workgroup is done with that), and a failed pop puts
 // its decrement back, so the counter is exact between launches.
 __device__ __forceinline__ int alloc_page(const SpkvView& v) {
     const int idx = atomicSub(v.free_top, 1) - 1;
@@ -88,7 +89,7 @@ struct PageBatch {
 __device__ __forceinline__ PageBatch alloc_page_batch(const SpkvView& v, int need, int recycled) {
     PageBatch pb = {0, 0, 0};
     if (need <= 0) return pb;
-    // no page is pushed in a launch that pops, so a stack seen empty stays empty
+    // no page is pushed while a launch pops, so a stack seen empty stays empty
     if (recycled > 0) {
         const int top = atomicSub(v.free_top, need);
         const int take = min(max(top, 0), need);
