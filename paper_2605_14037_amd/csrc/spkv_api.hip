@@ -2290,8 +2290,11 @@ int spkv_cache_fork(spkv_cache_t* c, spkv_cache_t* other, const int32_t* source,
         }
     }
     const bool apart = plan.moves.start[plan.moves.n] == plan.moves.n;       // no sequence that is replaced is a source
+    // The one launch gives pages back when the copies have theirs: the pool has to hold what goes beside what comes.  (Of each sequence
+    // the larger of both, by bounds from above of either; the two launches need no more than the result.)
+    const bool both_fit = c->pages_ub + fresh <= c->carve.n_pages;
     hipError_t e = hipSuccess;
-    if (!(apart && most > 0 && spkv_launch_fork_few(c->view, src, plan.moves, most, s, &e))) {
+    if (!(apart && both_fit && most > 0 && spkv_launch_fork_few(c->view, src, plan.moves, most, s, &e))) {
         e = spkv_launch_fork_move(c->view, src, plan.moves, s);
         if (e == hipSuccess && most > 0) e = spkv_launch_fork_pages(c->view, src, plan.copies, plan.n_copies, most, all, fresh, s);
     }

@@ -211,7 +211,8 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_pages(SpkvView v, Spkv
 }
 
 // A few short sequences, none of which is a source itself: all in one launch.  Nothing that a workgroup reads is written but by the
-// last one to be done, which writes the counters and gives back the pages left over (no page is handed out any more by then).
+// last one to be done, which writes the counters and gives back the pages left over (no page is handed out any more by then: the
+// pool has to hold what goes beside what comes, which spkv_cache_fork sees to).
 // One sequence of 500 tokens, D = 64, two KV heads: 5.4 us, both launches 3.4 and 3.2, and 2.4 us less of the host; seven of up to 2000, three
 // heads, 63 workgroups: 9.1, 4.3 and 4.1 before.
 template <int D>

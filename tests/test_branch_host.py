@@ -143,6 +143,37 @@ def test_short_sequences_are_copied_in_one_launch():
     assert [n for n, _, _ in launches(100, [KEEP] + [0] * 9, batch=10)] == ["spkv_fork_move", "spkv_fork_pages<128>"]
 
 
+def test_one_launch_only_where_the_pool_holds_what_goes_beside_what_comes():
+    """The one launch gives pages back when the copies have theirs; a pool that holds the result, but not both at once, takes two."""
+    move, pages, few = "spkv_fork_move", "spkv_fork_pages<128>", "spkv_fork_few<128>"
+
+    def launches(cfg, kept, fork, other=None, other_kept=None):
+        def fed(on, lengths):
+            return [["append", dict(on=on, counts=[max(row) + 128 for row in lengths])],
+                    ["lengths", dict(on=on, kept=[n for row in lengths for n in row])]]
+        script = fed("a", kept) + (fed("b", other_kept) if other is not None else [])
+        rc, got = _run([cfg] + ([other] if other is not None else []), script + [["fork", fork]])[-1]
+        return rc, [n for n, _, _ in got]
+
+    # one sequence ends, a short one is taken twice: 80 pages are in use in the end, 160 at once
+    kept = [[300] * 8, [640] * 8, [0] * 8]                   # 5 and 10 pages a head, 120 in all; 40 are copied
+    turn = dict(source=[KEEP, EMPTY, 0])
+    assert launches(dict(max_total_kept_tokens=7520), kept, turn) == (0, [move, pages])            # 118 + 24 pages
+    assert launches(dict(max_total_kept_tokens=64 * (159 - 24)), kept, turn) == (0, [move, pages])
+    assert launches(dict(max_total_kept_tokens=64 * (160 - 24)), kept, turn) == (0, [few])
+    # two sequences that become others of another cache: one grows by as much as the other shrinks
+    heads = dict(batch=2, n_q_heads=8, n_kv_heads=2, head_dim=64)
+    two = [[300] * 2, [900] * 2]                             # 5 and 15 pages a head, 40 in all
+    swap = dict(source=[1, 0], of="b")
+    move, pages, few = "spkv_fork_move", "spkv_fork_pages<64>", "spkv_fork_few<64>"
+    assert launches(dict(heads, max_total_kept_tokens=64 * 38), two, swap, heads, two) == (0, [move, pages])      # 42 pages; 60 at once
+    assert launches(dict(heads, max_total_kept_tokens=64 * 55), two, swap, heads, two) == (0, [move, pages])
+    assert launches(dict(heads, max_total_kept_tokens=64 * 56), two, swap, heads, two) == (0, [few])
+    # a slot given up for a sequence of as many pages
+    one = dict(heads, n_q_heads=4, n_kv_heads=1)
+    assert launches(dict(one, max_total_kept_tokens=640), [[700], [0]], dict(source=[EMPTY, 0], of="b"), one, [[700], [0]]) == (0, [move, pages])
+
+
 def test_a_few_pages_are_handed_out_by_the_copies():
     def launches(kept):
         return [n for n, _, _ in _run([{}], [["append", dict(counts=[9000, 50, 0])], ["lengths", dict(kept=[kept] * 8 + [0] * 16)],

@@ -234,6 +234,44 @@ def test_a_pool_of_just_the_pages_that_are_needed():
     tight.check(attend=False)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_short_sequences_in_a_pool_that_does_not_hold_both_at_once(d):
+    """Pages of what goes are needed for what comes: a slot given up while a prompt is taken over, one sequence that grows as another
+    shrinks.  Everything that leaves a window is kept."""
+    def fed(counts, pages, **kw):
+        n_pairs = len(counts) * kw.get("hk", 2)
+        x = Both(len(counts), d=d, window=128, tau=0.0, seed=d + pages, context=4000, kept=64 * (pages - n_pairs), **kw)
+        x.append(counts)
+        x.check(attend=False)                            # (the host knows the lengths from here on)
+        return x
+
+    def pages(x):
+        return x.cache.stats().pool_pages_used
+
+    x = fed([428, 768, 0], 142, hq=8, hk=8)              # 5 and 10 pages a head
+    for source, n in (([KEEP, EMPTY, 0], 80), ([KEEP, 0, EMPTY], 80), ([KEEP, 0, 0], 120)):
+        x.fork(source)
+        x.check(attend=False)
+        assert pages(x) == n
+    x.append([10, 100, 1])
+    x.check()
+    y, other = fed([428, 1028], 42), fed([428, 1028], 42)
+    for source in ([1, 0], [0, 1], [1, 0]):              # 5 and 15 pages a head
+        y.fork(source, other)
+        y.check()
+        assert pages(y) == 40
+    y.append([1, 20])
+    y.check()
+    z, other = fed([828, 0], 12, hq=4, hk=1), fed([828, 0], 12, hq=4, hk=1)
+    for source in ([EMPTY, 0], [0, EMPTY], [EMPTY, 0]):  # 11 of 12 pages
+        z.fork(source, other)
+        z.check(attend=False)
+        assert pages(z) == 11
+    z.append([100, 50])
+    z.check()
+    other.check(attend=False)
+
+
 def test_what_a_window_held_does_not_show():
     """Infinities and NaN of a sequence that is replaced or emptied, in the ring and in pages given back."""
     x = Both(4, window=40, seed=7, keep=0.9)
