@@ -2279,7 +2279,10 @@ int spkv_cache_fork(spkv_cache_t* c, spkv_cache_t* other, const int32_t* source,
     if (pages_after() > c->carve.n_pages) return SPKV_E_CAPACITY;
 
     const SpkvForkSource src = fork_source(from->view);
-    int64_t most = 0, all = 0, fresh = 0;
+    int64_t most = 0, all = 0, fresh = 0, back = 0;
+    for (int b = 0; b < B; ++b)
+        for (int h = 0; source[b] != SPKV_FORK_KEEP && h < Hkv; ++h)
+            back = std::max(back, pages_for(c->L_ub[b * Hkv + h]) - pages_for(length_after(b, h)));
     for (int i = 0; i < plan.n_copies; ++i) {
         const int b = plan.copies.dst[i];
         for (int h = 0; h < Hkv; ++h) {
@@ -2294,7 +2297,7 @@ int spkv_cache_fork(spkv_cache_t* c, spkv_cache_t* other, const int32_t* source,
     // the larger of both, by bounds from above of either; the two launches need no more than the result.)
     const bool both_fit = c->pages_ub + fresh <= c->carve.n_pages;
     hipError_t e = hipSuccess;
-    if (!(apart && both_fit && most > 0 && spkv_launch_fork_few(c->view, src, plan.moves, most, s, &e))) {
+    if (!(apart && both_fit && most > 0 && spkv_launch_fork_few(c->view, src, plan.moves, most, back, s, &e))) {
         e = spkv_launch_fork_move(c->view, src, plan.moves, s);
         if (e == hipSuccess && most > 0) e = spkv_launch_fork_pages(c->view, src, plan.copies, plan.n_copies, most, all, fresh, s);
     }

@@ -298,8 +298,14 @@ hipError_t spkv_launch_fork_pages(const SpkvView& v, const SpkvForkSource& from,
     return hipGetLastError();
 }
 
-// Up to 64 workgroups -- they take a ticket each, one after the other -- of up to 128 KB to copy.  False: it takes the other way.
-bool spkv_launch_fork_few(const SpkvView& v, const SpkvForkSource& from, const SpkvForkMoves& mv, int64_t most_pages, hipStream_t s, hipError_t* e) {
+// Up to 64 workgroups -- they take a ticket each, one after the other -- of up to 128 KB to copy, and few pages to give back, with one thread
+// a head: one sequence of P pages a head emptied and one of five copied, one launch / two, us of a call that is waited for: two
+// heads of 64, P = 5 19.3 / 19.4, 8 19.5 / 19.4, 16 20.6 / 19.3, 64 26 / 19, 917 120 / 21; eight heads of 128, P = 5 20.4 / 20.2, 8 20.8 / 20.4,
+// 16 21.9 / 20.5, 64 29 / 21, 917 155 / 23.  False: it takes the other way.
+constexpr int64_t kForkFewBack = 8;
+bool spkv_launch_fork_few(const SpkvView& v, const SpkvForkSource& from, const SpkvForkMoves& mv, int64_t most_pages, int64_t most_back,
+                          hipStream_t s, hipError_t* e) {
+    if (most_back > kForkFewBack) return false;
     const int64_t pairs = (int64_t)mv.n * v.Hkv, bytes = (most_pages + v.n_ring_pages) * spkv_page_elems(v.D) * 2;
     if (pairs > 64) return false;
     const int64_t wide = std::min<int64_t>(64 / pairs, std::max<int64_t>(most_pages, (bytes + 16383) / 16384));

@@ -359,8 +359,9 @@ hipError_t spkv_launch_fork_pages(const SpkvView& v, const SpkvForkSource& from,
                                   int64_t all_pages, int64_t fresh_pages, hipStream_t s);
 // Both launches in one, where they are small and every move is a copy or empties; false if it is not for that.  Pages go back when the copies
 // have theirs: the pool has to hold both at once.
-bool spkv_launch_fork_few(const SpkvView& v, const SpkvForkSource& from, const SpkvForkMoves& mv, int64_t most_pages, hipStream_t s,
-                          hipError_t* e);
+// most_back: most pages that a head gives back.
+bool spkv_launch_fork_few(const SpkvView& v, const SpkvForkSource& from, const SpkvForkMoves& mv, int64_t most_pages, int64_t most_back,
+                          hipStream_t s, hipError_t* e);
 hipError_t spkv_launch_gather_pairs(const SpkvView& v, const SpkvSequences& of, int n, int most_half_pages, const SpkvPairRows& out,
                                     hipStream_t s);
 hipError_t spkv_launch_append_rows(const SpkvView& v, const uint16_t* k, const uint16_t* vv, const float* f,

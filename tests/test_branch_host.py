@@ -16,6 +16,11 @@ AT = 1 << 40                                             # an aligned address th
 KEEP, EMPTY = -1, -2
 
 
+def _fed(on, kept):
+    """Every head of a sequence holds as many kept pairs, and the host knows it."""
+    return [["append", dict(on=on, counts=[max(row) + 128 for row in kept])], ["lengths", dict(on=on, kept=[n for row in kept for n in row])]]
+
+
 def _run(configs, script):
     from tests import recorder
     out = subprocess.run([sys.executable, os.path.abspath(__file__), recorder._runtime(), recorder.LIB],
@@ -148,30 +153,50 @@ def test_one_launch_only_where_the_pool_holds_what_goes_beside_what_comes():
     move, pages, few = "spkv_fork_move", "spkv_fork_pages<128>", "spkv_fork_few<128>"
 
     def launches(cfg, kept, fork, other=None, other_kept=None):
-        def fed(on, lengths):
-            return [["append", dict(on=on, counts=[max(row) + 128 for row in lengths])],
-                    ["lengths", dict(on=on, kept=[n for row in lengths for n in row])]]
-        script = fed("a", kept) + (fed("b", other_kept) if other is not None else [])
+        script = _fed("a", kept) + (_fed("b", other_kept) if other is not None else [])
         rc, got = _run([cfg] + ([other] if other is not None else []), script + [["fork", fork]])[-1]
         return rc, [n for n, _, _ in got]
 
     # one sequence ends, a short one is taken twice: 80 pages are in use in the end, 160 at once
     kept = [[300] * 8, [640] * 8, [0] * 8]                   # 5 and 10 pages a head, 120 in all; 40 are copied
+    less = [[300] * 8, [500] * 8, [0] * 8]                   # (8 instead of 10: as many as the one launch gives back)
     turn = dict(source=[KEEP, EMPTY, 0])
     assert launches(dict(max_total_kept_tokens=7520), kept, turn) == (0, [move, pages])            # 118 + 24 pages
     assert launches(dict(max_total_kept_tokens=64 * (159 - 24)), kept, turn) == (0, [move, pages])
-    assert launches(dict(max_total_kept_tokens=64 * (160 - 24)), kept, turn) == (0, [few])
+    assert launches(dict(max_total_kept_tokens=64 * (143 - 24)), less, turn) == (0, [move, pages])
+    assert launches(dict(max_total_kept_tokens=64 * (144 - 24)), less, turn) == (0, [few])
     # two sequences that become others of another cache: one grows by as much as the other shrinks
     heads = dict(batch=2, n_q_heads=8, n_kv_heads=2, head_dim=64)
     two = [[300] * 2, [900] * 2]                             # 5 and 15 pages a head, 40 in all
+    near = [[300] * 2, [832] * 2]                            # 5 and 13
     swap = dict(source=[1, 0], of="b")
     move, pages, few = "spkv_fork_move", "spkv_fork_pages<64>", "spkv_fork_few<64>"
     assert launches(dict(heads, max_total_kept_tokens=64 * 38), two, swap, heads, two) == (0, [move, pages])      # 42 pages; 60 at once
     assert launches(dict(heads, max_total_kept_tokens=64 * 55), two, swap, heads, two) == (0, [move, pages])
-    assert launches(dict(heads, max_total_kept_tokens=64 * 56), two, swap, heads, two) == (0, [few])
+    assert launches(dict(heads, max_total_kept_tokens=64 * 47), near, swap, heads, near) == (0, [move, pages])
+    assert launches(dict(heads, max_total_kept_tokens=64 * 48), near, swap, heads, near) == (0, [few])
     # a slot given up for a sequence of as many pages
     one = dict(heads, n_q_heads=4, n_kv_heads=1)
     assert launches(dict(one, max_total_kept_tokens=640), [[700], [0]], dict(source=[EMPTY, 0], of="b"), one, [[700], [0]]) == (0, [move, pages])
+
+
+def test_one_launch_only_where_it_gives_few_pages_back():
+    """It does so with one thread a head; a head that gives up more than eight pages takes the two launches."""
+    heads = dict(batch=2, n_q_heads=8, n_kv_heads=2, head_dim=64)
+    two, few = ["spkv_fork_move", "spkv_fork_pages<64>"], ["spkv_fork_few<64>"]
+
+    def launches(kept, source):
+        rc, got = _run([heads, heads], _fed("a", kept) + _fed("b", [[300] * 2, [0] * 2]) + [["fork", dict(source=source, of="b")]])[-1]
+        assert rc == 0
+        return [n for n, _, _ in got]
+
+    assert launches([[59000] * 2, [0] * 2], [0, KEEP]) == two            # a short prompt in the place of a long conversation
+    assert launches([[59000] * 2, [0] * 2], [EMPTY, 0]) == two           # or beside it
+    assert launches([[59000] * 2, [0] * 2], [KEEP, 0]) == few            # nothing goes back
+    assert launches([[13 * 64] * 2, [0] * 2], [0, KEEP]) == few          # 13 pages for 5
+    assert launches([[0] * 2, [64, 13 * 64 + 1]], [KEEP, 0]) == two
+    assert launches([[8 * 64] * 2, [0] * 2], [EMPTY, 0]) == few
+    assert launches([[8 * 64, 8 * 64 + 1], [0] * 2], [EMPTY, 0]) == two
 
 
 def test_a_few_pages_are_handed_out_by_the_copies():
