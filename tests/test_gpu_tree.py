@@ -173,6 +173,21 @@ def test_one_long_list_and_many_short_ones(n, hq, hk, d):
     many.check_tree(sm_scale=0.0)
 
 
+@pytest.mark.parametrize("n,hq,hk,d,lengths", [
+    (n, 8, 2, d, lengths) for n in (4, 8, 13, 29, 64) for d, lengths in ((64, [2900]), (128, [25 * b for b in range(26)]))
+] + [(13, 8, 2, 128, [2900]), (33, 16, 16, 64, [9600, 1])])
+def test_scales_that_the_caller_chooses(n, hq, hk, d, lengths):
+    """Every width, in ranges and whole, and long lists."""
+    x = Trees(len(lengths), hq=hq, hk=hk, d=d, window=77, seed=n + d, keep=0.9, context=11000)
+    x.append(lengths)
+    x.drafts([n if b % 5 == 0 else 1 for b in range(len(lengths))], seed=n)
+    scale = float(np.float32(0.3 * d ** -0.5))
+    default, x.oracle.scale = x.oracle.scale, scale
+    x.check_tree(sm_scale=scale)
+    x.oracle.scale = default                              # (none, and what is none: the default)
+    x.check_tree(sm_scale=-scale)
+
+
 @pytest.mark.parametrize("batch", [1, 26])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n", [4, 8, 12, 30, 64])
