@@ -272,6 +272,45 @@ def test_short_sequences_in_a_pool_that_does_not_hold_both_at_once(d):
     other.check(attend=False)
 
 
+@pytest.mark.parametrize("seed", range(12))
+def test_forks_in_pools_that_are_nearly_full(seed):
+    """Random forks within two caches and out of each other, with appends between them: a fork is refused exactly where the pages of
+    its result do not fit, and changes nothing then."""
+    rng = np.random.default_rng(seed)
+    hk, d, window = int(rng.choice([1, 2, 8])), int(rng.choice([64, 128])), int(rng.choice([1, 16, 100, 128]))
+    both, pools = [], []
+    for i in range(2):
+        batch, room = int(rng.choice([1, 2, 3, 6])), int(rng.integers(4, 24))
+        both.append(Both(batch, hq=hk, hk=hk, d=d, window=window, tau=float(rng.choice([0.0, 0.5])), seed=2 * seed + i, context=1600,
+                         kept=64 * room * hk, keep=0.7))
+        pools.append(room * hk + batch * hk)
+
+    def pages(oracle, b):
+        return sum((n + 63) // 64 for n in oracle.kept_len()[b])
+
+    for turn in range(24):
+        x, other = both[turn % 2], both[1 - turn % 2]
+        batch = x.shape[0]
+        if rng.random() < 0.4:
+            counts = [int(rng.choice([0, 1, 70, rng.integers(0, 600)])) for _ in range(batch)]
+            if max(n + c for n, c in zip(x.oracle._len, counts)) <= 1600 and sum(counts) > 0:
+                worst = sum(hk * ((max(0, n + c - window) + 63) // 64) for n, c in zip(x.oracle._len, counts))
+                if worst <= pools[turn % 2]:                  # (what an append asks for)
+                    x.append(counts)
+            continue
+        of = other if rng.random() < 0.6 else x
+        source = [int(rng.choice([KEEP, EMPTY, rng.integers(0, of.shape[0]), rng.integers(0, of.shape[0])])) for _ in range(batch)]
+        after = sum(pages(x.oracle, b) if s == KEEP else 0 if s == EMPTY else pages(of.oracle, s) for b, s in enumerate(source))
+        if after <= pools[turn % 2]:
+            x.fork(source, of if of is not x else None)
+        else:
+            with pytest.raises(spkv.SPKVError, match="capacity"):
+                x.cache.fork(source, of.cache if of is not x else None)
+        x.check(attend=False)
+    for x in both:
+        x.check()
+
+
 def test_what_a_window_held_does_not_show():
     """Infinities and NaN of a sequence that is replaced or emptied, in the ring and in pages given back."""
     x = Both(4, window=40, seed=7, keep=0.9)
