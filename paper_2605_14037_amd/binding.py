@@ -784,7 +784,6 @@ class SPKVCache:
         return out, lse
 
     # ---- sequences that branch
-    # ---- sequences that branch
     def _ptr(self, t, dtype, shape, name):
         """_dev_ptr, of a tensor on the cache's own device."""
         if t.get_device() != self.index or t.dtype != dtype or t.shape != shape or not t.is_contiguous():

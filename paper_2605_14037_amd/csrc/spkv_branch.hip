@@ -121,8 +121,8 @@ __global__ __launch_bounds__(kForkThreads) void spkv_fork_move(SpkvView v, SpkvF
 }
 
 // Many pages to hand out: every copied pair is given the ids that it lacks, off the stack and then out of the pool, by its place among the
-// pairs -- no atomic, of which all go to one address and are served one after the other.  Every workgroup, four pairs', adds up what
-// the pairs before them lack.  The counters stand still meanwhile: the copies' launch moves them on, by the sum in pos_scratch[0].
+// pairs -- no atomic, of which all go to one address and are served one after the other.  Every workgroup, a pair's, adds up what
+// the pairs before it lack.  The counters stand still meanwhile: the copies' launch moves them on, by the sum in pos_scratch[0].
 __global__ __launch_bounds__(256) void spkv_fork_assign(SpkvView v, SpkvForkCopies copies) {
     __shared__ int s_sum[4];
     auto lacks = [&](int p) -> int { return max(0, min((v.kept_len[p] + kPageTokens - 1) / kPageTokens, v.pt_cap) - v.pair_items[p]); };
@@ -503,8 +503,7 @@ __global__ __launch_bounds__(256) void spkv_append_rows(SpkvView v, const uint16
     const int row0 = cu.v[b], n = cu.v[b + 1] - row0;
     if (n == 0) return;
     if (n > min(kFewTokens, v.w)) return append_many_rows<D>(v, pair, h, n, k, vv, f, rows + row0, n_rows);
-    int T = v.t_pair[pair], L = v.kept_len[pair];
-    append_few_rows<D>(v, pair, h, n, T, L, k, vv, f, [&](int i) -> int {
+    append_few_rows<D>(v, pair, h, n, v.t_pair[pair], v.kept_len[pair], k, vv, f, [&](int i) -> int {
         const int r = rows[row0 + i];
         if (r < 0 || r >= n_rows) *v.err_flag = 1;
         return min(max(r, 0), n_rows - 1);

@@ -336,14 +336,13 @@ __device__ __forceinline__ void store_row_chunk(uint16_t* dp, int dk, int c, uin
 // between reading the ring and writing it and the one that hands out a page.  Bound by dependent round
 // trips, three of them: counters (the new rows travel beside), ring rows, logits and page id, stores.
 constexpr int kFewTokens = 16;
-// Token i is row row_of(i) of k, vv and f.  T and L: the pair's counters before, and on return those after.
+// Token i is row row_of(i) of k, vv and f.  T and L: the pair's counters.
 template <int D, class RowOf>
-__device__ __forceinline__ void append_few_rows(const SpkvView& v, int pair, int h, int n, int& T_io, int& L_io,
+__device__ __forceinline__ void append_few_rows(const SpkvView& v, int pair, int h, int n, int T, int L,
                                                 const uint16_t* __restrict__ k, const uint16_t* __restrict__ vv,
                                                 const float* __restrict__ f, RowOf row_of) {
     __shared__ int s_few_page;
     const int tid = threadIdx.x, lane = tid & 63, r = tid >> 4, c = tid & 15;
-    const int T = T_io, L = L_io;
     const bool mover = c < D / 8;
     uint4 k_new = {0u, 0u, 0u, 0u}, v_new = k_new, k_old = k_new, v_old = k_new;
     if (r < n && mover) {
@@ -379,8 +378,6 @@ __device__ __forceinline__ void append_few_rows(const SpkvView& v, int pair, int
     }
     __syncthreads();                                     // the leaving rows have been read
     const int new_page = last > first ? s_few_page : 0;
-    T_io = T + n;
-    if (new_page >= 0) L_io = L + kept;
     if (tid == 0) {
         if (new_page >= 0) v.kept_len[pair] = L + kept;
         v.t_pair[pair] = T + n;
@@ -411,8 +408,7 @@ __device__ __forceinline__ void append_few(const SpkvView& v, int pair, const ui
                                            const SpkvCu& cu) {
     const int b = pair / v.Hkv, h = pair - b * v.Hkv, row0 = cu.v[b], n = cu.v[b + 1] - row0;
     if (n == 0) return;
-    int T = v.t_pair[pair], L = v.kept_len[pair];
-    append_few_rows<D>(v, pair, h, n, T, L, k, vv, f, [row0](int i) -> int { return row0 + i; });
+    append_few_rows<D>(v, pair, h, n, v.t_pair[pair], v.kept_len[pair], k, vv, f, [row0](int i) -> int { return row0 + i; });
 }
 
 // ------------------------------------------------------------------ work partition
