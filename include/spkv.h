@@ -395,14 +395,19 @@ int spkv_decode_attention_shared(spkv_cache_t* cache, spkv_cache_t* prefix, cons
  *   parents      device int32 [total]: -1 (or anything that is not 0 .. i - 1): the draft hangs behind the newest token,
  *                else the index, within its sequence's drafts, of an earlier one
  *   cu_seqlens   host int32 [batch + 1]: sequence b's drafts are rows cu[b] .. cu[b+1]-1, at most SPKV_MAX_TREE_NODES
- *   lse          device fp32 [total, n_q_heads] or NULL
+ *   lse          device fp32 [total, n_q_heads] or NULL       sm_scale as for spkv_decode_attention
  * A sequence may hold no token.  One pass over the cache serves all drafts of a sequence.  Needs no workspace (partial results
  * lie in the cache's own buffers); one launch, or two where the lists are cut into ranges, more for hundreds of (sequence, KV head)
  * pairs with many columns each.  Waits once for the lengths after a prompt's append, as spkv_decode_attention does.  May be
- * captured; a replay takes the parents and the lists as they are by then (the cut is made for lists that fill the pool).  Copies of
- * a sequence get results that agree to rounding.  spkv_prefix_attention places the rows of a call as a chain: joined with a tree's
- * results it is right for sequences that hold `window` tokens of their own or more.
- * Errors: SPKV_E_INVAL for bad shapes and pointers; never SPKV_E_STATE. */
+ * captured, once those lengths have been read (by a first call, or spkv_cache_stats: a capture refuses the wait); a replay takes the
+ * parents and the lists as they are by then (the cut is made for lists that fill the pool).
+ * Copies of a sequence get results that agree to rounding, and so do a sequence's results in calls with other trees: the largest one
+ * of a call decides how all are worked out.  Up to 32 query columns (drafts x group size) the softmax weights are multiplied with V
+ * as two bf16 parts, from 33 on as one, half a step (2^-8 of a weight) off at most each; their sums keep 32 bits.
+ * spkv_prefix_attention places the rows of a call as a chain: joined with a tree's results it is right for sequences that hold `window`
+ * tokens of their own or more.
+ * Errors: SPKV_E_INVAL for bad shapes and pointers; SPKV_E_HIP and SPKV_E_NOMEM, the latter from the wait for the lengths; never
+ * SPKV_E_STATE. */
 int spkv_score_tree(spkv_cache_t* cache, const void* k, const void* v, const float* util_logits, const void* q,
                     const int32_t* parents, const int32_t* cu_seqlens, void* out, float* lse, float sm_scale,
                     void* stream);
@@ -414,7 +419,8 @@ int spkv_score_tree(spkv_cache_t* cache, const void* k, const void* v, const flo
  *                rows[cu_seqlens[b]] .. rows[cu_seqlens[b + 1] - 1]; any order, the same row more than once
  *   cu_seqlens   host int32 [batch + 1], at most SPKV_MAX_TREE_NODES tokens a sequence
  * A row that is not in 0 .. n_rows - 1 makes the cache's state an error (spkv_cache_stats: SPKV_E_DEVICE); no memory
- * outside the rows is read.  One launch.  Errors as for spkv_append; SPKV_E_INVAL if a sequence has more tokens. */
+ * outside the rows is read.  One launch.  May be captured as spkv_append may: with one token for every sequence, by rows as they are at
+ * the replay.  Errors as for spkv_append; SPKV_E_INVAL if a sequence has more tokens. */
 int spkv_append_rows(spkv_cache_t* cache, const void* k, const void* v, const float* util_logits,
                      const int32_t* rows, int32_t n_rows, const int32_t* cu_seqlens, void* stream);
 
@@ -428,7 +434,8 @@ int spkv_append_rows(spkv_cache_t* cache, const void* k, const void* v, const fl
  * Within a cache the first sequence that takes the contents of one that is itself replaced or emptied has its pages;
  * only further ones are copied, so beams that trade places move page ids and windows.  The same sequence may be taken by any
  * number of others.  Copies are the same to the last bit, and independent of each other from then on.
- * One launch for a few short sequences, else three at most.  Waits once for the lengths after a prompt's append to `from`, as spkv_decode_attention does, and
+ * One launch for a few short sequences that give up few pages, where the pool holds, at once, the pages that go and those that come;
+ * else three at most, which need no more pages than the result.  Waits once for the lengths after a prompt's append to `from`, as spkv_decode_attention does, and
  * where the pool might not hold the copies; else it does not synchronise (a sequence is given back without waiting, too).
  * Errors: SPKV_E_INVAL for shapes that differ and sources out of range; SPKV_E_CAPACITY if the pool or max_context cannot hold
  * the result (nothing is changed); SPKV_E_STATE under stream capture -- a replay would move sequences that the
@@ -439,7 +446,7 @@ int spkv_cache_fork(spkv_cache_t* cache, spkv_cache_t* from, const int32_t* sour
 
 /* What sequences hold, as dense rows: for every KV head the pairs of its long-term list and then those of the window,
  * positions ascending -- what attention reads, for a host store, another kernel, a test.
- *   sequences    host int32 [n], any of them more than once, n * n_kv_heads <= 65535; NULL: the first n
+ *   sequences    host int32 [n], any of them more than once, n <= SPKV_MAX_BATCH, n * n_kv_heads <= 65535; NULL: the first n
  *   k, v         device bf16 [n, n_kv_heads, rows, head_dim]
  *   util_logits  device fp32 [n, n_kv_heads, rows]     positions  device int32 [n, n_kv_heads, rows]
  *   counts       device int32 [n, n_kv_heads]: pairs held
@@ -572,7 +579,7 @@ int spkv_qk_norm_rope_backward(const spkv_heads_t* dq, const spkv_heads_t* dk, c
  *                          SPKV_E_CAPACITY (nothing changed) if n exceeds what was safe.
  * The work partition frozen in a captured launch stays valid as the lists grow (work items
  * get longer, never out of bounds); re-capture now and then to rebalance it.  The threshold
- * and the sink count are frozen with the launch too.  spkv_decode_attention_shared and spkv_prefix_attention
+ * and the sink count are frozen with the launch too, also of a captured spkv_score_tree and spkv_append_rows.  spkv_decode_attention_shared and spkv_prefix_attention
  * may be captured as well once the prompts' lengths have been read (by a first call, or spkv_cache_stats): a
  * replay attends to what the prompts and the sequences hold by then, with the prefix_of and the cut of the capture
  * (16 sequences behind 32k, captured at 40 tokens of their own and replayed at 2000: 33 us, captured there 25). */

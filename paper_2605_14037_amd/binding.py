@@ -857,7 +857,7 @@ class SPKVCache:
                                         self._stream()), "spkv_cache_fork")
 
     def gather(self, sequences=None, rows=None, out=None):
-        """The pairs that sequences hold (all of them by default), kept ones and then the window's, positions ascending, as
+        """The pairs that sequences hold (all of them by default; up to 512, also repeated), kept ones and then the window's, positions ascending, as
         (k, v, util_logits, positions, counts): bf16 [n, H_kv, rows, D] twice, fp32 and int32 [n, H_kv, rows], int32
         [n, H_kv] (spkv_cache_gather).  rows None: as many as the longest head holds (synchronises).  out: those five
         tensors, to write; rows behind a head's last pair are left as they were (undefined in new tensors)."""

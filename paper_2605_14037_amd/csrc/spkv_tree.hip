@@ -797,6 +797,10 @@ __global__ __launch_bounds__(256, 8) void spkv_tree_merge(SpkvView v, SpkvTree t
 // The kernel of own copies has the higher rate on long lists and the longer start: 33 to 64 columns, split / own copies, us: 484 MB
 // in 128 lists 116 / 98, 404 MB in 512 uneven ones 170 / 105, 120 MB in 8 38.3 / 36.5; D = 64, 94 MB 43 / 29; but 28 MB
 // in 256 26 / 30, 17 MB in 32 19.5 / 22.6, 2 MB in 8 13.9 / 19.6.
+// 129 columns and more: 256 to a workgroup, whose eight waves read a half-page once, or blocks of 128 on four waves, two workgroups to a
+// compute unit.  256 / blocks of 128, us, 4 heads a group: 16 sequences of 32k, 33, 48, 64 drafts 158 / 180, 152 / 170, 155 / 176 (D = 64 88 / 104,
+// 93 / 107 with 33, 64); 64 of 1k-16k 173 / 200, 174 / 199, 180 / 203; 32 of 300 25.4 / 30, 27.6 / 30, 28.2 / 30; one of 128k, 64 drafts
+// 49.6 / 51; 16 heads a group, 16 of 8k, 1024 columns 56 / 58.  A few short lists alone are the other way: 4 of 4k 27.2 / 26.0, one of 2k 22.3 / 20.4.
 constexpr int64_t kTreeOwnHalfPages = 4096;
 SpkvTreeKernel spkv_tree_kernel(int n_cols, int64_t half_pages) {
     return n_cols <= 16 ? kTreeFew16 : n_cols <= 32 ? kTreeFew32 : n_cols <= 64 ? (half_pages >= kTreeOwnHalfPages ? kTreeOwnCopies : kTreeSplit64)

@@ -78,6 +78,9 @@ def _main():
         elif op == "capture":
             rt.rec_capture(a["status"], 0)
             rc = 0
+        elif op == "sync_error":                          # what waiting for a stream returns
+            rt.rec_sync_error(a["error"])
+            rc = 0
         elif op == "steps":
             n = C.c_int64()
             rc = lib.spkv_cache_safe_steps(who, None, C.byref(n))
@@ -311,6 +314,15 @@ def test_launches_of_a_tree_over_long_lists():
         assert rc == 0 and [g[0].split("<")[0] for g in got][1:] == ["spkv_tree_merge"]
         assert got[0][0] == f"spkv_tree_{kernel}, 0>" and got[0][2] == threads
         assert 200 <= got[0][1] <= 256 * rounds + 24
+
+
+def test_a_first_tree_after_a_prompt_is_not_captured():
+    """It waits for the lengths, which a capture refuses; once they are known it may be."""
+    prompt, tree = ["append", dict(counts=[9000, 50, 0])], ["tree", dict(counts=[4, 4, 4])]
+    refused = [["capture", dict(status=1)], ["sync_error", dict(error=900)]]
+    assert _run([{}], [prompt] + refused + [tree])[-1] == (-4, [])
+    rc, launches = _run([{}], [prompt, ["lengths", dict(kept=[2000] * 8 + [0] * 16)]] + refused + [tree])[-1]
+    assert rc == 0 and launches
 
 
 def test_trees_that_are_empty():

@@ -452,6 +452,35 @@ def test_many_rows_through_short_windows(window, keep):
         x.check()
 
 
+def test_chosen_rows_in_a_graph():
+    """One token for every sequence, by the rows and the contents of the buffers at every replay; the host's counts by advance."""
+    x = Both(3, window=40, seed=13, context=900, keep=0.5)
+    x.append([300, 0, 39])
+    x.check(attend=False)
+    steps, rng = x.cache.safe_steps(), np.random.default_rng(0)
+    k, v, f = x.rows(9)
+    rows = torch.tensor([0, 3, 6], dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):                     # records the launch; counts one step
+        x.cache.append_rows(k, v, f, rows, [0, 1, 2, 3])
+    for turn in range(80):
+        for to, new in zip((k, v, f), x.rows(9)):
+            to.copy_(new)
+        chosen = [int(r) for r in rng.integers(0, 9, 3)]
+        rows.copy_(torch.tensor(chosen, dtype=torch.int32))
+        if turn > 0:
+            x.cache.advance(1)
+        graph.replay()
+        x.oracle.append(to_numpy_f32(k)[chosen], to_numpy_f32(v)[chosen], to_numpy_f32(f)[chosen], [0, 1, 2, 3])
+        if turn % 20 == 7:
+            x.check()
+    x.check()
+    assert x.cache.safe_steps() == steps - 80
+    x.append_rows(9, [8, 0, 1, 1], [2, 0, 2])
+    x.check()
+
+
 def test_rows_that_are_not_there_are_flagged():
     x = Both(2, window=20, seed=11)
     x.append([30, 30])
