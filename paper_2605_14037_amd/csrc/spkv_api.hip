@@ -2280,9 +2280,6 @@ int spkv_cache_fork(spkv_cache_t* c, spkv_cache_t* other, const int32_t* source,
 
     const SpkvForkSource src = fork_source(from->view);
     int64_t most = 0, all = 0, fresh = 0, back = 0;
-    for (int b = 0; b < B; ++b)
-        for (int h = 0; source[b] != SPKV_FORK_KEEP && h < Hkv; ++h)
-            back = std::max(back, pages_for(c->L_ub[b * Hkv + h]) - pages_for(length_after(b, h)));
     for (int i = 0; i < plan.n_copies; ++i) {
         const int b = plan.copies.dst[i];
         for (int h = 0; h < Hkv; ++h) {
@@ -2296,8 +2293,12 @@ int spkv_cache_fork(spkv_cache_t* c, spkv_cache_t* other, const int32_t* source,
     // The one launch gives pages back when the copies have theirs: the pool has to hold what goes beside what comes.  (Of each sequence
     // the larger of both, by bounds from above of either; the two launches need no more than the result.)
     const bool both_fit = c->pages_ub + fresh <= c->carve.n_pages;
+    const bool few = apart && both_fit && most > 0 && (int64_t)plan.moves.n * Hkv <= kForkFewPairs;
+    for (int b = 0; few && b < B; ++b)
+        for (int h = 0; source[b] != SPKV_FORK_KEEP && h < Hkv; ++h)
+            back = std::max(back, pages_for(c->L_ub[b * Hkv + h]) - pages_for(length_after(b, h)));
     hipError_t e = hipSuccess;
-    if (!(apart && both_fit && most > 0 && spkv_launch_fork_few(c->view, src, plan.moves, most, back, s, &e))) {
+    if (!(few && spkv_launch_fork_few(c->view, src, plan.moves, most, back, s, &e))) {
         e = spkv_launch_fork_move(c->view, src, plan.moves, s);
         if (e == hipSuccess && most > 0) e = spkv_launch_fork_pages(c->view, src, plan.copies, plan.n_copies, most, all, fresh, s);
     }

@@ -307,8 +307,8 @@ bool spkv_launch_fork_few(const SpkvView& v, const SpkvForkSource& from, const S
                           hipStream_t s, hipError_t* e) {
     if (most_back > kForkFewBack) return false;
     const int64_t pairs = (int64_t)mv.n * v.Hkv, bytes = (most_pages + v.n_ring_pages) * spkv_page_elems(v.D) * 2;
-    if (pairs > 64) return false;
-    const int64_t wide = std::min<int64_t>(64 / pairs, std::max<int64_t>(most_pages, (bytes + 16383) / 16384));
+    if (pairs > kForkFewPairs) return false;
+    const int64_t wide = std::min<int64_t>(kForkFewPairs / pairs, std::max<int64_t>(most_pages, (bytes + 16383) / 16384));
     if (bytes > wide * (128 << 10)) return false;
     const dim3 grid((unsigned)wide, v.Hkv, mv.n);
     const int chunk = (int)std::max<int64_t>(1, std::min<int64_t>(kForkChunk, (most_pages + wide - 1) / wide));

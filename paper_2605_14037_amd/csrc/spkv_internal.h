@@ -357,6 +357,7 @@ struct SpkvForkCopies {                          // dst's pages become copies of
 // most_pages, all_pages: of a head of these sequences, of all of them, fresh_pages: of them not at hand, by the host's bound.
 hipError_t spkv_launch_fork_pages(const SpkvView& v, const SpkvForkSource& from, const SpkvForkCopies& copies, int n, int64_t most_pages,
                                   int64_t all_pages, int64_t fresh_pages, hipStream_t s);
+constexpr int kForkFewPairs = 64;
 // Both launches in one, where they are small and every move is a copy or empties; false if it is not for that.  Pages go back when the copies
 // have theirs: the pool has to hold both at once.
 // most_back: most pages that a head gives back.
